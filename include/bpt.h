@@ -260,6 +260,48 @@ bpt_status bpt_out_proj_norm(const void* a, const void* w_o, const void* h, cons
                              void* z, int64_t rows, int32_t D, float eps, void* workspace, void* cuda_stream);
 
 /*
+ * The seam between two blocks of a layer: norm after a block, gate, scaled residual, norm before the next block.
+ * Algorithm 2 (Sec. 3.3) has Z = norm(H + GSA(H)) and H' = norm(Z + FFN(Z)); with everything but `norm` off this is
+ * that step.  For every row of D channels, in one pass over the data:
+ *     n = post(b),    r = alpha h + gate n,    y = norm(r)
+ * norm and post: BPT_NORM_NONE (the identity), BPT_NORM_LAYER ((x - mean) / sqrt(var + eps), biased variance about the
+ * mean) or BPT_NORM_RMS (x / sqrt(mean(x^2) + eps)), each times its weight plus its bias where those are not NULL.
+ * h, b, y, r: [rows, D] contiguous, element type `dtype`; b may be NULL (r = alpha h; no post norm, no gate).
+ * weight, bias, post_weight, post_bias: [D] of type param_dtype, or NULL; only with the norm they belong to.
+ * gate: [gate_groups, D] of type gate_dtype, or NULL (1): row i takes gate row i / (rows / gate_groups), so that one
+ * row gates everything, one per sequence, or one per row; gate_groups must divide rows.
+ * Arithmetic and statistics are fp32; y is computed from the unrounded r; one rounding per stored value.
+ * rows >= 0, 1 <= D <= 8192.  Rows whose D * sizeof(element) is not a multiple of 16 bytes, and tensors that are not
+ * 16-byte aligned, are served element by element.  y must be given exactly when norm is not NONE; r may be NULL
+ * then.  y or r may be the same buffer as h or b.
+ *
+ * Backward: given dy = dLoss/dy (NULL: zero) and dr = dLoss/dr (NULL: zero), writes those of dh, db [rows, D] (dtype),
+ * d_weight, d_bias, d_post_weight, d_post_bias [D] (param_dtype), d_gate [gate_groups, D] (gate_dtype) that are not
+ * NULL:  dR = dr + norm'(dy),  dh = alpha dR,  dn = gate dR,  db = post'(dn),  and the column sums that belong to the
+ * parameters.  Everything is recomputed from h and b.  Outputs are overwritten; the sums are taken in a fixed order
+ * without atomics, so results are bit-reproducible.  dh / db may be the buffers of dy or dr, not of h or b.
+ * `workspace`: bpt_res_norm_bwd_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a
+ * status block (nothing here waits), 16-byte aligned; two calls whose GPU work overlaps need one each.
+ * Errors: INVALID_ARG, UNSUPPORTED (D, rows >= 2^31), WORKSPACE, CUDA.
+ */
+enum { BPT_NORM_NONE = 0, BPT_NORM_LAYER = 1, BPT_NORM_RMS = 2 };
+typedef struct {
+    int64_t rows;
+    int64_t gate_groups;
+    int32_t D;
+    bpt_dtype dtype, param_dtype, gate_dtype;
+    int32_t norm, post_norm;    /* BPT_NORM_* */
+    float alpha, eps;
+    const void *h, *b;
+    const void *weight, *bias, *post_weight, *post_bias, *gate;
+} bpt_res_norm_args;
+bpt_status bpt_res_norm_fwd(const bpt_res_norm_args* args, void* y, void* r, void* cuda_stream);
+size_t bpt_res_norm_bwd_workspace_bytes(const bpt_res_norm_args* args);
+bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* args, const void* dy, const void* dr, void* dh, void* db,
+                            void* d_weight, void* d_bias, void* d_post_weight, void* d_post_bias, void* d_gate,
+                            void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Backward pass for callers that must not allocate device memory (the paper has no
  * counterpart; this is a deployment convenience).
  *

@@ -57,6 +57,26 @@ def out_proj_norm(a, w_o, h, gamma, beta, eps=1e-5):
     return (x - mean) / np.sqrt(var + eps) * np.asarray(gamma, dtype=np.float64) + np.asarray(beta, dtype=np.float64)
 
 
+def _normalise(x, kind, w, c, eps):
+    """The definition of layer normalisation (biased variance about the mean) and of root-mean-square normalisation."""
+    if kind is None:
+        return x
+    if kind == "layer":
+        x = x - x.sum(-1, keepdim=True) / x.shape[-1]
+    x = x / ((x ** 2).sum(-1, keepdim=True) / x.shape[-1] + eps) ** 0.5
+    x = x if w is None else x * w
+    return x if c is None else x + c
+
+
+def res_norm(h, b, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None, alpha=1.0, eps=1e-5):
+    """(y, r) of the seam between two blocks, r = alpha h + gate post_norm(b), y = norm(r); float64 tensors, gate broadcasts."""
+    r = alpha * h
+    if b is not None:
+        n = _normalise(b, post_norm, post_weight, post_bias, eps)
+        r = r + (n if gate is None else gate * n)
+    return _normalise(r, norm, weight, bias, eps), r
+
+
 def layer_forward(h, w, mask, rel, n_heads):
     """h: [B, N, D]; w: dict of float64 tensors wq, wk, wv, wo [D, D] (applied as x @ w.T), rel_emb [n_rel, D/H],
     ln1_w, ln1_b, ln2_w, ln2_b [D], ff1_w [F, D], ff1_b [F], ff2_w [D, F], ff2_b [D]."""

@@ -18,12 +18,14 @@ CHECK_LIB_PATH = os.path.join(_HERE, "libbpt_check.so")   # the build with index
 BPT_BIDIR, BPT_LEFT_ONLY, BPT_MODE_PAD, BPT_MODE_ALG1 = 0, 1, 0, 2
 BPT_F32, BPT_BF16 = 0, 1
 BPT_PATH_AUTO, BPT_PATH_MMA, BPT_PATH_TC5 = 0, 1, 2
+NORM_KINDS = {None: 0, "layer": 1, "rms": 2}   # BPT_NORM_*
 
 EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes", "bpt_attn_fwd",
            "bpt_attn_bwd", "bpt_status_str", "bpt_trace_begin", "bpt_trace_end",
            "bpt_static_scratch_bytes", "bpt_attn_bwd_static_scratch", "bpt_attn_fwd_varlen", "bpt_attn_bwd_varlen",
            "bpt_attn_fwd_ex", "bpt_attn_bwd_ex", "bpt_attn_fwd_rows", "bpt_attn_bwd_min_workspace_bytes", "bpt_check",
-           "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm")
+           "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
+           "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd")
 
 
 class BptError(RuntimeError):
@@ -47,6 +49,14 @@ class GraphStruct(ctypes.Structure):
 class AttnOptions(ctypes.Structure):
     _fields_ = [("lengths", ctypes.c_void_p), ("dropout_p", ctypes.c_float), ("dropout_seed", ctypes.c_uint64),
                 ("path", ctypes.c_uint32)]
+
+
+class ResNormArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("gate_groups", ctypes.c_int64), ("D", ctypes.c_int32), ("dtype", ctypes.c_int),
+                ("param_dtype", ctypes.c_int), ("gate_dtype", ctypes.c_int), ("norm", ctypes.c_int32), ("post_norm", ctypes.c_int32),
+                ("alpha", ctypes.c_float), ("eps", ctypes.c_float), ("h", ctypes.c_void_p), ("b", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("post_weight", ctypes.c_void_p),
+                ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p)]
 
 
 # When set, the autograd wrapper in layer.py asks bpt_check after every attention call (a stream
@@ -79,6 +89,13 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_selftest_wait_timeout.argtypes = [vp, ctypes.c_int64, i32, vp]
         lib.bpt_out_proj_norm.restype = ctypes.c_int
         lib.bpt_out_proj_norm.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_int64, i32, f32, vp, vp]
+        rn = ctypes.POINTER(ResNormArgs)
+        lib.bpt_res_norm_fwd.restype = ctypes.c_int
+        lib.bpt_res_norm_fwd.argtypes = [rn, vp, vp, vp]
+        lib.bpt_res_norm_bwd_workspace_bytes.restype = sz
+        lib.bpt_res_norm_bwd_workspace_bytes.argtypes = [rn]
+        lib.bpt_res_norm_bwd.restype = ctypes.c_int
+        lib.bpt_res_norm_bwd.argtypes = [rn, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.bpt_debug_bounds.restype = ctypes.c_int
         lib.bpt_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32), vp]
         lib.bpt_attn_fwd.restype = ctypes.c_int
@@ -221,6 +238,86 @@ def bpt_out_proj_norm(a, w_o, h, gamma, beta, eps: float = 1e-5, z=None, workspa
         _check(load_library().bpt_out_proj_norm(_ptr(a), _ptr(w_o), _ptr(h), _ptr(gamma), _ptr(beta), _ptr(z), rows, D, float(eps),
                                                 _ptr(workspace), _stream()), "bpt_out_proj_norm")
     return z
+
+
+def _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps):
+    """Checks the tensors of a bpt_res_norm call and fills its argument struct."""
+    code = _dtype_code(h)
+    if not h.is_cuda or not h.is_contiguous() or h.dim() < 1:
+        raise ValueError("h must be a contiguous CUDA tensor [..., D]")
+    shape, dev = h.shape, h.device
+    D = shape[-1]
+    if b is not None and (b.shape != shape or b.dtype != h.dtype or b.device != dev or not b.is_contiguous()):
+        raise ValueError("b must be contiguous and share shape, dtype and device with h")
+    if norm not in NORM_KINDS or post_norm not in NORM_KINDS:
+        raise ValueError("norm and post_norm must be None, 'layer' or 'rms'")
+    if b is None and (post_norm is not None or gate is not None):
+        raise ValueError("post_norm and gate belong to b, which is missing")
+    if (norm is None and (weight is not None or bias is not None)) or (post_norm is None and (post_weight is not None or post_bias is not None)):
+        raise ValueError("a weight or bias was given for a norm that is None")
+    pt = None
+    for t in (weight, bias, post_weight, post_bias):
+        if t is not None:
+            pt = t.dtype if pt is None else pt
+            if t.shape != (D,) or t.dtype != pt or t.device != dev or not t.is_contiguous():
+                raise ValueError("weights and biases must be contiguous [D] tensors of one dtype on the device of h")
+            pcode = _dtype_code(t)
+    groups = 0
+    if gate is not None:
+        # the gate's rows: a leading part of h's axes, the others of length one (or missing in front: a gate [D])
+        gs = (1,) * (h.dim() - gate.dim()) + tuple(gate.shape)
+        lead = h.dim() - 1
+        while lead > 0 and gs[lead - 1] == 1:
+            lead -= 1
+        if len(gs) != h.dim() or gs[-1] != D or gs[:lead] != tuple(shape[:lead]) or gate.device != dev or not gate.is_contiguous():
+            raise ValueError("gate must be contiguous, [D] or h's shape with the trailing row axes of length one, on the device of h")
+        groups = 1
+        for x in gs[:lead]:
+            groups *= x
+    rows = h.numel() // D if D else 0
+    return ResNormArgs(rows, max(groups, 1), D, code, code if pt is None else pcode, code if gate is None else _dtype_code(gate),
+                       NORM_KINDS[norm], NORM_KINDS[post_norm], alpha, eps, h.data_ptr(), _ptr(b), _ptr(weight), _ptr(bias),
+                       _ptr(post_weight), _ptr(post_bias), _ptr(gate))
+
+
+def _check_like(h, *ts):
+    for t in ts:
+        if t is not None and (t.shape != h.shape or t.dtype != h.dtype or t.device != h.device or not t.is_contiguous()):
+            raise ValueError("results and gradients must be contiguous and share shape, dtype and device with h")
+
+
+def bpt_res_norm_fwd(h, b=None, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
+                     alpha: float = 1.0, eps: float = 1e-5, want_sum: bool = False, y=None, r=None):
+    """n = post_norm(b), r = alpha * h + gate * n, y = norm(r) over the last axis, in one kernel.  h, b: [..., D] float32 or
+    bfloat16, contiguous; norm / post_norm: None, "layer" or "rms" with weights and biases [D]; gate: [D], or h's shape with
+    the trailing row axes of length one (one gate row per sequence, per row ...).  Returns (y, r); y is None without a norm,
+    r is None unless want_sum (or norm is None)."""
+    args = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
+    _check_like(h, y, r)
+    with torch.cuda.device(h.device):
+        y = torch.empty_like(h) if y is None and norm is not None else y
+        r = torch.empty_like(h) if r is None and (want_sum or norm is None) else r
+        _check(load_library().bpt_res_norm_fwd(ctypes.byref(args), _ptr(y), _ptr(r), _stream()), "bpt_res_norm_fwd")
+    return y, r
+
+
+def bpt_res_norm_bwd(h, b, dy, dr, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
+                     alpha: float = 1.0, eps: float = 1e-5, workspace=None, need=(True,) * 7):
+    """Backward of bpt_res_norm_fwd from its inputs and the gradients of y and r (either may be None: zero).  Returns
+    (dh, db, d_weight, d_bias, d_post_weight, d_post_bias, d_gate), each in the type of what it belongs to; None where that
+    is None or where `need` says so.  Bit-reproducible."""
+    args = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
+    _check_like(h, dy, dr)
+    lib = load_library()
+    with torch.cuda.device(h.device):
+        grads = [torch.empty_like(t) if n and t is not None else None
+                 for n, t in zip(need, (h, b, weight, bias, post_weight, post_bias, gate))]
+        size = int(lib.bpt_res_norm_bwd_workspace_bytes(ctypes.byref(args)))
+        if workspace is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=h.device)
+        _check(lib.bpt_res_norm_bwd(ctypes.byref(args), _ptr(dy), _ptr(dr), *[_ptr(t) for t in grads], _ptr(workspace),
+                                    workspace.numel(), _stream()), "bpt_res_norm_bwd")
+    return tuple(grads)
 
 
 def bpt_debug_bounds():

@@ -11,6 +11,7 @@ import math
 
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -52,6 +53,46 @@ def graph_self_attention(g: binding.Graph, q, k, v, rel_emb, scale=None, lengths
     function of the seed, so the backward pass rebuilds it).  Returns [B, 2n-1, H, d]."""
     scale = 1.0 / math.sqrt(q.shape[-1]) if scale is None else float(scale)
     return _GraphSelfAttention.apply(q, k, v, rel_emb, g, scale, lengths, float(dropout_p), int(dropout_seed))
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, b, weight, bias, post_weight, post_bias, gate, norm, post_norm, alpha, eps, want_sum):
+        y, r = binding.bpt_res_norm_fwd(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps, want_sum)
+        ctx.save_for_backward(h, b, weight, bias, post_weight, post_bias, gate)
+        ctx.cfg = (norm, post_norm, alpha, eps)
+        ctx.set_materialize_grads(False)
+        return (r, y) if y is not None and r is not None else r if y is None else y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *grads):
+        h, b, weight, bias, post_weight, post_bias, gate = ctx.saved_tensors
+        norm, post_norm, alpha, eps = ctx.cfg
+        dr, dy = grads if len(grads) == 2 else (grads[0], None) if norm is None else (None, grads[0])
+        if dr is None and dy is None:
+            return (None,) * 12
+        dr, dy = (None if t is None else t.contiguous() for t in (dr, dy))
+        return binding.bpt_res_norm_bwd(h, b, dy, dr, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps,
+                                        need=ctx.needs_input_grad[:7]) + (None,) * 5
+
+
+def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
+                  alpha=1.0, eps=1e-5, return_sum=False):
+    """The seam between two blocks, differentiable:  r = alpha * h + gate * post_norm(b),  y = norm(r)  over the last axis.
+
+    h: the residual stream [..., D], b: the output of the block before (None: r = alpha * h), both float32 or bfloat16.
+    norm / post_norm: "layer", "rms" or None, with their weights and biases [D] (None: 1 and 0).  gate: [D], or h's shape
+    with the trailing row axes of length one ([B, 1, D]: a gate per sequence), or None (1).  With norm="layer" and nothing
+    else this is the norm(H + A) of Algorithm 2; with post_norm it is the norm after the block before and the norm
+    before the block that follows.  Returns y; (r, y) with return_sum; r with norm=None."""
+    cont = lambda t: None if t is None else t.contiguous()
+    ts = [cont(t) for t in (h, b, weight, bias, post_weight, post_bias, gate)]
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts):
+        return _ResidualNorm.apply(*ts, norm, post_norm, float(alpha), float(eps), bool(return_sum))
+    h, b, weight, bias, post_weight, post_bias, gate = ts
+    y, r = binding.bpt_res_norm_fwd(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps, return_sum)
+    return (r, y) if y is not None and r is not None else r if y is None else y
 
 
 class BPTLayer(nn.Module):

@@ -260,6 +260,35 @@ bpt_status bpt_out_proj_norm(const void* a, const void* w_o, const void* h, cons
                              void* z, int64_t rows, int32_t D, float eps, void* workspace, void* cuda_stream);
 
 /*
+ * Gated feed-forward block (the position-wise half of Algorithm 2, Sec. 3.3, with a gated inner layer):
+ *     y = (act(x w_gate^T) * (x w_up^T)) w_down^T          for every row of x
+ * x, y: [rows, D]; w_gate, w_up: [F, D]; w_down: [D, F] (the layout of a linear layer's weight); all bf16, contiguous and
+ * 16-byte aligned.  act: BPT_ACT_RELU, BPT_ACT_SILU (g / (1 + exp(-g))) or BPT_ACT_GELU (g/2 (1 + erf(g / sqrt 2))).
+ * Both projections, the activation and the product run in one kernel, which rounds the inner row act(..) * (..) once
+ * to bf16 (the second product's operand type); products accumulate in fp32; y is rounded once.
+ * rows >= 0, D and F multiples of 8 (16-byte rows).  x and y must not overlap.
+ *
+ * Backward: from x, the weights and dy = dLoss/dy (nothing else of the forward is needed: both projections are computed
+ * again, in fp32), dx [rows, D] and dw_gate, dw_up [F, D], dw_down [D, F], all bf16, overwritten.  dx may be NULL; the
+ * three weight gradients are given together or are all NULL.  The inner row and the gradients of the two projections are rounded once to bf16
+ * (operands of the products that follow).  Sums over rows are taken in a fixed order without atomics: bit-reproducible.
+ *
+ * `workspace`: bpt_gated_ff_workspace_bytes bytes (host query; 0 on invalid arguments and for rows == 0, where NULL
+ * will do), 256-byte aligned; two calls whose GPU work overlaps need one each.  `status`: NULL, or a device buffer of at
+ * least 256 bytes that receives the status block (see bpt_check; apart from the workspace, which is large and need not
+ * outlive the call's work).
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes), WORKSPACE, CUDA; device-side: see bpt_check.
+ */
+enum { BPT_ACT_RELU = 0, BPT_ACT_SILU = 1, BPT_ACT_GELU = 2 };
+size_t bpt_gated_ff_workspace_bytes(int64_t rows, int32_t D, int32_t F, int backward);
+bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y,
+                            int64_t rows, int32_t D, int32_t F, int32_t act, void* status, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const void* w_up, const void* w_down, const void* dy,
+                            void* dx, void* dw_gate, void* dw_up, void* dw_down, int64_t rows, int32_t D, int32_t F, int32_t act,
+                            void* status, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * The seam between two blocks of a layer: norm after a block, gate, scaled residual, norm before the next block.
  * Algorithm 2 (Sec. 3.3) has Z = norm(H + GSA(H)) and H' = norm(Z + FFN(Z)); with everything but `norm` off this is
  * that step.  For every row of D channels, in one pass over the data:

@@ -57,6 +57,14 @@ def out_proj_norm(a, w_o, h, gamma, beta, eps=1e-5):
     return (x - mean) / np.sqrt(var + eps) * np.asarray(gamma, dtype=np.float64) + np.asarray(beta, dtype=np.float64)
 
 
+def gated_ff(x, w_gate, w_up, w_down, act):
+    """(act(x w_gate^T) * (x w_up^T)) w_down^T, float64 tensors; the activations from their definitions."""
+    g = x @ w_gate.T
+    a = {"relu": lambda: torch.where(g > 0, g, torch.zeros_like(g)), "silu": lambda: g / (1 + torch.exp(-g)),
+         "gelu": lambda: g * 0.5 * (1 + torch.erf(g / 2 ** 0.5))}[act]()
+    return (a * (x @ w_up.T)) @ w_down.T
+
+
 def _normalise(x, kind, w, c, eps):
     """The definition of layer normalisation (biased variance about the mean) and of root-mean-square normalisation."""
     if kind is None:

@@ -19,13 +19,14 @@ BPT_BIDIR, BPT_LEFT_ONLY, BPT_MODE_PAD, BPT_MODE_ALG1 = 0, 1, 0, 2
 BPT_F32, BPT_BF16 = 0, 1
 BPT_PATH_AUTO, BPT_PATH_MMA, BPT_PATH_TC5 = 0, 1, 2
 NORM_KINDS = {None: 0, "layer": 1, "rms": 2}   # BPT_NORM_*
+ACTIVATIONS = {"relu": 0, "silu": 1, "gelu": 2}        # BPT_ACT_*
 
 EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes", "bpt_attn_fwd",
            "bpt_attn_bwd", "bpt_status_str", "bpt_trace_begin", "bpt_trace_end",
            "bpt_static_scratch_bytes", "bpt_attn_bwd_static_scratch", "bpt_attn_fwd_varlen", "bpt_attn_bwd_varlen",
            "bpt_attn_fwd_ex", "bpt_attn_bwd_ex", "bpt_attn_fwd_rows", "bpt_attn_bwd_min_workspace_bytes", "bpt_check",
            "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
-           "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd")
+           "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd")
 
 
 class BptError(RuntimeError):
@@ -96,6 +97,13 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_res_norm_bwd_workspace_bytes.argtypes = [rn]
         lib.bpt_res_norm_bwd.restype = ctypes.c_int
         lib.bpt_res_norm_bwd.argtypes = [rn, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        i64 = ctypes.c_int64
+        lib.bpt_gated_ff_workspace_bytes.restype = sz
+        lib.bpt_gated_ff_workspace_bytes.argtypes = [i64, i32, i32, ctypes.c_int]
+        lib.bpt_gated_ff_fwd.restype = ctypes.c_int
+        lib.bpt_gated_ff_fwd.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, sz, vp]
+        lib.bpt_gated_ff_bwd.restype = ctypes.c_int
+        lib.bpt_gated_ff_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, sz, vp]
         lib.bpt_debug_bounds.restype = ctypes.c_int
         lib.bpt_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32), vp]
         lib.bpt_attn_fwd.restype = ctypes.c_int
@@ -238,6 +246,71 @@ def bpt_out_proj_norm(a, w_o, h, gamma, beta, eps: float = 1e-5, z=None, workspa
         _check(load_library().bpt_out_proj_norm(_ptr(a), _ptr(w_o), _ptr(h), _ptr(gamma), _ptr(beta), _ptr(z), rows, D, float(eps),
                                                 _ptr(workspace), _stream()), "bpt_out_proj_norm")
     return z
+
+
+def bpt_gated_ff_workspace_bytes(rows: int, D: int, F: int, backward: bool) -> int:
+    return int(load_library().bpt_gated_ff_workspace_bytes(rows, D, F, int(backward)))
+
+
+def _check_gated_ff(x, w_gate, w_up, w_down, act, *like_x):
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s" % ", ".join(map(repr, ACTIVATIONS)))
+    if x.dtype != torch.bfloat16:
+        raise TypeError("only bfloat16 tensors are supported, got %s" % x.dtype)
+    if not x.is_cuda or x.dim() < 1 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous CUDA tensor [..., D]")
+    D = x.shape[-1]
+    F = w_gate.shape[0] if w_gate.dim() == 2 else 0
+    for t, shape in ((w_gate, (F, D)), (w_up, (F, D)), (w_down, (D, F))):
+        if t.shape != shape or t.dtype != x.dtype or t.device != x.device or not t.is_contiguous():
+            raise ValueError("w_gate and w_up must be [F, D], w_down [D, F], contiguous, with the dtype and device of x")
+    for t in like_x:
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype or t.device != x.device or not t.is_contiguous()):
+            raise ValueError("y, dy and dx must be contiguous and share shape, dtype and device with x")
+    return x.numel() // D if D else 0, D, F
+
+
+def bpt_gated_ff_fwd(x, w_gate, w_up, w_down, act: str = "silu", y=None, workspace=None):
+    """y = (act(x @ w_gate.T) * (x @ w_up.T)) @ w_down.T over the last axis: both projections, activation and product in
+    one kernel, the second product in another.  x: [..., D] bfloat16 contiguous; w_gate, w_up: [F, D]; w_down: [D, F]; D and F
+    multiples of 8.  The call's status block stays reachable as `y._bpt_workspace` for bpt_check (the workspace does not)."""
+    rows, D, F = _check_gated_ff(x, w_gate, w_up, w_down, act, y)
+    lib = load_library()
+    with torch.cuda.device(x.device):
+        y = torch.empty_like(x) if y is None else y
+        if workspace is None:
+            workspace = torch.empty(lib.bpt_gated_ff_workspace_bytes(rows, D, F, 0), dtype=torch.uint8, device=x.device)
+        y._bpt_workspace = status = torch.empty(256, dtype=torch.uint8, device=x.device)
+        _check(lib.bpt_gated_ff_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y.data_ptr(), rows, D, F,
+                                    ACTIVATIONS[act], status.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()), "bpt_gated_ff_fwd")
+    return y
+
+
+def bpt_gated_ff_bwd(x, w_gate, w_up, w_down, dy, act: str = "silu", dx=None, dw_gate=None, dw_up=None, dw_down=None, workspace=None,
+                     need_dx: bool = True, need_dw: bool = True):
+    """Gradients of bpt_gated_ff_fwd from its inputs and dy: (dx, dw_gate, dw_up, dw_down), bfloat16; None where not needed (the
+    three weight gradients together).  Bit-reproducible.  The call's status block stays reachable as `_bpt_workspace` of
+    the first gradient for bpt_check."""
+    rows, D, F = _check_gated_ff(x, w_gate, w_up, w_down, act, dy, dx)
+    if not (need_dx or need_dw):
+        raise ValueError("no gradient was asked for")
+    for t, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)):
+        if t is not None and (t.shape != w.shape or t.dtype != w.dtype or t.device != w.device or not t.is_contiguous()):
+            raise ValueError("weight gradients must be contiguous and share shape, dtype and device with their weights")
+    lib = load_library()
+    with torch.cuda.device(x.device):
+        if need_dx:
+            dx = torch.empty_like(x) if dx is None else dx
+        if need_dw:
+            dw_gate, dw_up, dw_down = (torch.empty_like(w) if t is None else t for t, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)))
+        if workspace is None:
+            workspace = torch.empty(lib.bpt_gated_ff_workspace_bytes(rows, D, F, 1), dtype=torch.uint8, device=x.device)
+        status = torch.empty(256, dtype=torch.uint8, device=x.device)
+        (dx if need_dx else dw_gate)._bpt_workspace = status
+        _check(lib.bpt_gated_ff_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(),
+                                    _ptr(dx) if need_dx else None, *[_ptr(t) if need_dw else None for t in (dw_gate, dw_up, dw_down)], rows, D, F,
+                                    ACTIVATIONS[act], status.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()), "bpt_gated_ff_bwd")
+    return (dx if need_dx else None,) + ((dw_gate, dw_up, dw_down) if need_dw else (None,) * 3)
 
 
 def _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps):

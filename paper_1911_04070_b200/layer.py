@@ -95,6 +95,42 @@ def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=Non
     return (r, y) if y is not None and r is not None else r if y is None else y
 
 
+class _GatedFeedForward(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, act):
+        y = binding.bpt_gated_ff_fwd(x, w_gate, w_up, w_down, act)
+        if binding.CHECK_DEVICE_STATUS and binding.bpt_check(y._bpt_workspace):
+            raise RuntimeError("gated feed-forward: a device-side wait timed out, results are invalid")
+        ctx.save_for_backward(x, w_gate, w_up, w_down)
+        ctx.act = act
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, w_gate, w_up, w_down = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        grads = binding.bpt_gated_ff_bwd(x, w_gate, w_up, w_down, dy.contiguous(), ctx.act, need_dx=need[0], need_dw=any(need[1:4]))
+        first = grads[0] if need[0] else grads[1]
+        if binding.CHECK_DEVICE_STATUS and binding.bpt_check(first._bpt_workspace):
+            raise RuntimeError("gated feed-forward backward: a device-side wait timed out, results are invalid")
+        return tuple(g if n else None for g, n in zip(grads, need)) + (None,)
+
+
+def gated_feed_forward(x, w_gate, w_up, w_down, act="silu"):
+    """Differentiable gated feed-forward block over the last axis:  (act(x w_gate^T) * (x w_up^T)) w_down^T.
+
+    x: [..., D] bfloat16; w_gate, w_up: [F, D], w_down: [D, F] (the layout of a linear layer's weight), D and F multiples
+    of 8; act: "silu", "gelu" (with erf) or "relu".  Nothing but x and the weights is kept for the backward pass."""
+    x, w_gate, w_up, w_down = x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous()
+    if torch.is_grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad or w_down.requires_grad):
+        return _GatedFeedForward.apply(x, w_gate, w_up, w_down, act)
+    y = binding.bpt_gated_ff_fwd(x, w_gate, w_up, w_down, act)
+    if binding.CHECK_DEVICE_STATUS and binding.bpt_check(y._bpt_workspace):
+        raise RuntimeError("gated feed-forward: a device-side wait timed out, results are invalid")
+    return y
+
+
 class BPTLayer(nn.Module):
     """One layer of Algorithm 2:  Z = norm(H + GSA(H)),  H' = norm(Z + FFN(Z)).
 

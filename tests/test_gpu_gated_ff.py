@@ -1,0 +1,223 @@
+"""bpt_gated_ff (gated feed-forward block) and its backward against the float64 oracle, over row counts, ragged widths
+and activations.
+
+Tolerances, fixed before the first run.  A result is rounded once to bf16: at most 2^-8 of its value.  Before that, the
+inner row h, dG and dU are each rounded once to bf16 as operands of the next product; such a rounding is off by at most
+2^-8 of the value and evenly spread, hence a standard deviation of at most 2^-8 / sqrt(3), and the terms of a product's
+sum err independently: the sum's deviation is 2^-8 / sqrt(3) * sqrt(sum of squared terms).  Eight deviations, 4.7 * 2^-8 *
+sqrt(sum of squared terms), hold for far more elements than are compared.  fp32 accumulation and the approximate
+exponential (relative 2^-20) are far below that."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+H = 2.0 ** -8
+SIZES = [(8, 8), (16, 24), (64, 64), (72, 200), (136, 128), (200, 712), (264, 520), (512, 1368), (512, 2048), (1024, 136), (128, 4096)]
+ROWS = [1, 2, 5, 8, 9, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 1023, 4099]
+
+
+def _inputs(rows, D, F, seed, scale=1.0):
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    r = lambda *s, std: (torch.randn(*s, generator=g, device="cuda:0") * std).bfloat16()
+    return dict(x=r(rows, D, std=scale), w_gate=r(F, D, std=D ** -0.5), w_up=r(F, D, std=D ** -0.5), w_down=r(D, F, std=F ** -0.5)), r(rows, D, std=1.0)
+
+
+def _close(name, got, want, squares):
+    import torch
+    assert got.dtype == torch.bfloat16 and got.shape == want.shape, name
+    got = got.double()
+    assert torch.isfinite(got).all(), name
+    err = (got - want).abs()
+    bad = err > H * want.abs() * (1 + 2 * H) + 4.7 * H * squares.sqrt() + 1e-30
+    assert not bad.any(), "%s: %d of %d outside, worst %.3g at %s" % (name, int(bad.sum()), bad.numel(), float(err[bad].max()), bad.nonzero()[0].tolist())
+
+
+def _check(v, dy, act, backward=True):
+    import torch
+    from oracle import bpt_layer
+    from paper_1911_04070_b200 import binding, layer
+    leaf = {a: t.clone().requires_grad_(backward) for a, t in v.items()}
+    y = layer.gated_feed_forward(**leaf, act=act)
+    d = {a: t.double().requires_grad_(True) for a, t in v.items()}
+    y64 = bpt_layer.gated_ff(**d, act=act)
+    g = d["x"] @ d["w_gate"].T
+    u = d["x"] @ d["w_up"].T
+    one = torch.ones_like(g)
+    act64 = {"relu": lambda z: torch.where(z > 0, z, 0 * z), "silu": lambda z: z / (1 + torch.exp(-z)),
+             "gelu": lambda z: z * 0.5 * (1 + torch.erf(z / 2 ** 0.5))}[act]
+    av = act64(g)
+    da, = torch.autograd.grad(av, g, one, retain_graph=True)
+    h, da, av, u = ((av * u).detach(), da, av.detach(), u.detach())
+    sq = lambda t: t.detach().double() ** 2
+    _close("y", y.detach(), y64.detach(), sq(h) @ sq(v["w_down"]).T)
+    assert binding.bpt_check(getattr(y, "_bpt_workspace", None)) == 0
+    if not backward:
+        return y
+    grads = torch.autograd.grad(y, list(leaf.values()), dy)
+    want = torch.autograd.grad(y64, list(d.values()), dy.double())
+    dh = dy.double() @ v["w_down"].double()
+    dg, du = dh * u * da, dh * av
+    _close("dx", grads[0], want[0], sq(dg) @ sq(v["w_gate"]) + sq(du) @ sq(v["w_up"]))
+    _close("dw_gate", grads[1], want[1], sq(dg).T @ sq(v["x"]))
+    _close("dw_up", grads[2], want[2], sq(du).T @ sq(v["x"]))
+    _close("dw_down", grads[3], want[3], sq(dy).T @ sq(h))
+    return (y, *grads)
+
+
+@pytest.mark.parametrize("D,F", SIZES)
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_sizes(D, F, act):
+    _check(*_inputs(300, D, F, D + F), act)
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("D,F", [(64, 136), (512, 2048)])
+def test_row_counts(rows, D, F):
+    _check(*_inputs(rows, D, F, rows), "silu")
+
+
+def test_many_tiles_per_pair():
+    _check(*_inputs(20011, 256, 520, 3), "silu")
+
+
+def test_a_batch_of_long_sequences():
+    _check(*_inputs(65532, 512, 2048, 4), "silu")
+
+
+def test_large_scores():
+    """Inner values of hundreds: the activation saturates on both sides without overflow."""
+    _check(*_inputs(130, 128, 256, 5, scale=300.0), "silu")
+    _check(*_inputs(130, 128, 256, 6, scale=300.0), "gelu")
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+def test_nan_and_infinity_stay_in_their_rows(rows):
+    import torch
+    from paper_1911_04070_b200 import layer
+    v, dy = _inputs(rows, 72, 136, 7)
+    y = layer.gated_feed_forward(**v)
+    x = v["x"].clone()
+    x[1, 5] = float("nan")
+    x[0, 3] = float("inf")
+    y2 = layer.gated_feed_forward(**{**v, "x": x})
+    assert torch.isnan(y2[1]).all() and not torch.isfinite(y2[0]).all()
+    assert torch.equal(y2[2:], y[2:])
+
+
+def test_no_rows():
+    import torch
+    from paper_1911_04070_b200 import layer
+    v, dy = _inputs(0, 64, 128, 8)
+    leaf = {a: t.clone().requires_grad_(True) for a, t in v.items()}
+    y = layer.gated_feed_forward(**leaf)
+    assert y.shape == (0, 64)
+    g = torch.autograd.grad(y, list(leaf.values()), dy)
+    assert g[0].shape == (0, 64) and all((t == 0).all() for t in g[1:])
+
+
+@pytest.mark.parametrize("rows", [1, 7, 65, 300])
+def test_memory_around_the_results_is_left_alone(rows):
+    import torch
+    from paper_1911_04070_b200 import binding
+    D, F = 72, 200
+    v, dy = _inputs(rows, D, F, 9)
+    guard = 1024
+    bufs = {n: torch.full((t.numel() + 2 * guard,), 7.0, dtype=torch.bfloat16, device="cuda:0")
+            for n, t in (("y", v["x"]), ("dx", v["x"]), ("dw_gate", v["w_gate"]), ("dw_up", v["w_up"]), ("dw_down", v["w_down"]))}
+    mid = lambda n, t: bufs[n][guard:guard + t.numel()].view(t.shape)
+    want = binding.bpt_gated_ff_fwd(**v)
+    got = binding.bpt_gated_ff_fwd(**v, y=mid("y", v["x"]))
+    assert torch.equal(got, want)
+    want = binding.bpt_gated_ff_bwd(**v, dy=dy)
+    got = binding.bpt_gated_ff_bwd(**v, dy=dy, dx=mid("dx", v["x"]), **{"d" + n: mid("d" + n, v[n]) for n in ("w_gate", "w_up", "w_down")})
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for n, b in bufs.items():
+        assert (b[:guard] == 7).all() and (b[-guard:] == 7).all(), n
+
+
+@pytest.mark.parametrize("rows", [5, 700])
+def test_reproducible_captured_and_on_another_stream(rows):
+    import torch
+    from paper_1911_04070_b200 import layer
+    v, dy = _inputs(rows, 128, 264, 10)
+    leaf = {a: t.clone().requires_grad_(True) for a, t in v.items()}
+
+    def step():
+        y = layer.gated_feed_forward(**leaf, act="gelu")
+        grads = torch.autograd.grad(y, list(leaf.values()), dy)
+        return [y.detach()] + list(grads)       # no graph of the leaves outlives a step, nor reaches the capture
+
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, other))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(2):
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_results_do_not_depend_on_what_the_workspace_held():
+    import torch
+    from paper_1911_04070_b200 import binding
+    v, dy = _inputs(333, 136, 264, 11)
+    want = (binding.bpt_gated_ff_fwd(**v),) + binding.bpt_gated_ff_bwd(**v, dy=dy)
+    ws = [torch.full((binding.bpt_gated_ff_workspace_bytes(333, 136, 264, b),), 0xFF, dtype=torch.uint8, device="cuda:0") for b in (False, True)]
+    got = (binding.bpt_gated_ff_fwd(**v, workspace=ws[0]),) + binding.bpt_gated_ff_bwd(**v, dy=dy, workspace=ws[1])
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_only_some_gradients():
+    import torch
+    from paper_1911_04070_b200 import layer
+    v, dy = _inputs(200, 64, 128, 12)
+    full = {a: t.clone().requires_grad_(True) for a, t in v.items()}
+    want = dict(zip(v, torch.autograd.grad(layer.gated_feed_forward(**full), list(full.values()), dy)))
+    for some in (("x",), ("w_up",), ("w_gate", "w_down"), ("x", "w_down")):
+        leaf = {a: t.clone().requires_grad_(a in some) for a, t in v.items()}
+        layer.gated_feed_forward(**leaf).backward(dy)
+        for a in v:
+            assert (leaf[a].grad is None) == (a not in some)
+            assert a not in some or torch.equal(leaf[a].grad, want[a])
+
+
+def test_strided_inputs():
+    import torch
+    from paper_1911_04070_b200 import layer
+    v, dy = _inputs(60, 64, 128, 13)
+    x = torch.empty(60, 2, 64, dtype=torch.bfloat16, device="cuda:0")[:, 0].copy_(v["x"])
+    y = layer.gated_feed_forward(x, v["w_gate"].t().contiguous().t(), v["w_up"], v["w_down"])
+    assert torch.equal(y, layer.gated_feed_forward(**v))
+    y3 = layer.gated_feed_forward(v["x"].view(5, 12, 64), v["w_gate"], v["w_up"], v["w_down"])
+    assert torch.equal(y3.view(60, 64), y)
+
+
+def test_python_refusals():
+    import torch
+    from paper_1911_04070_b200 import binding
+    v, dy = _inputs(8, 64, 128, 14)
+    f = binding.bpt_gated_ff_fwd
+    for kw in (dict(act="tanh"), dict(w_gate=v["w_gate"][:64]), dict(w_up=v["w_up"].t()), dict(w_down=v["w_gate"]), dict(w_down=v["w_down"].float()),
+               dict(x=v["x"].t()), dict(x=v["x"].cpu()), dict(y=dy[:4]), dict(w_gate=v["w_gate"].cpu())):
+        with pytest.raises(ValueError):
+            f(**{**v, **kw})
+    with pytest.raises(TypeError):
+        f(**{a: t.float() for a, t in v.items()})
+    with pytest.raises(binding.BptError) as ei:     # 12 is no multiple of 8
+        f(*(t.contiguous() for t in (v["x"][:, :12], v["w_gate"][:, :12], v["w_up"][:, :12], v["w_down"][:12])))
+    assert ei.value.status == 2
+    with pytest.raises(ValueError):
+        binding.bpt_gated_ff_bwd(**v, dy=dy, need_dx=False, need_dw=False)
+    with pytest.raises(binding.BptError) as ei:
+        f(**v, workspace=torch.empty(256, dtype=torch.uint8, device="cuda:0"))
+    assert ei.value.status == 3

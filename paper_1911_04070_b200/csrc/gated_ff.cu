@@ -8,9 +8,9 @@
 //
 // All five products run in one kernel template on pairs of CTAs (pair_tools.cuh): a load warp per CTA brings 64-deep
 // slices of both operands in with TMA, one thread of the pair issues tcgen05 products of 256 rows x up to 256 columns,
-// eight epilogue warps per CTA take finished accumulators out of tensor memory while the next tile's products run (two
-// accumulators of 256 columns; in the three-accumulator kernel dH is double and G | U single, and a tile's dH products
-// cover the epilogue of the tile before).  Operands that a product needs transposed are read as they lie: the matrix
+// eight or sixteen epilogue warps per CTA take finished accumulators out of tensor memory while the next tile's products run
+// (two accumulators of 256 columns; in the three-accumulator kernel dH is double and G | U single, and a tile's dH
+// products cover the time in which G | U of the tile before move to registers).  Operands that a product needs transposed are read as they lie: the matrix
 // descriptors take either axis as the contiguous one, so no transposed copy exists anywhere.  Ragged edges are TMA's: what lies outside a tensor reads
 // as zero and is not written.  Every wait is bounded; a give-up is reported through the status word.
 #include <algorithm>
@@ -26,16 +26,23 @@ namespace {
 enum FfKernel { kFfIn, kFfOut, kFfBwdIn, kFfDx, kFfDw };
 
 constexpr int kFfPairs = 74;                  // 148 SMs
-constexpr int kFfEpiWarps = 8;
-constexpr int kFfThreads = (4 + kFfEpiWarps) * 32;   // load warp, product warp, two idle warps (tensor-memory lane groups start at a multiple of four), epilogue
 constexpr int kFfStageBytes = 32 * 1024;      // 128 x 64 of A and up to 128 x 64 of B per CTA
 constexpr int kFfK = 64;
 
+// The kernels with an activation have sixteen epilogue warps (four per 32 rows, 32 columns each): a warp takes its share of
+// G and U into registers at once and gives the accumulator back before it computes.  The others have eight.  All results
+// leave through small staged tiles and TMA stores; storing the inner rows straight from registers (a 32-byte sector per
+// thread) freed shared memory for two more stages but held the warps longer: 232 against 214 us in the first kernel,
+// 441 against 418 us in the three-accumulator one (65532 x 512, F = 2048, silu).
 template <int KERNEL> struct FfShape {
-    static constexpr int stages = KERNEL == kFfBwdIn ? 4 : 5;
-    static constexpr int staging = KERNEL == kFfBwdIn ? 3 : 2;      // 4 KB output tiles per epilogue warp
+    static constexpr bool act = KERNEL == kFfIn || KERNEL == kFfBwdIn;
+    static constexpr int epi_warps = act ? 16 : 8;
+    static constexpr int threads = (2 + epi_warps) * 32;            // load warp, product warp, epilogue warps
+    static constexpr int stages = 5;
+    static constexpr int tile_bytes = act ? 2048 : 4096;            // a staged output tile: 32 rows of 64 or 128 bytes
+    static constexpr int staging = 2;                               // staged tiles per epilogue warp
     static constexpr int out_off = stages * kFfStageBytes;
-    static constexpr int bar_off = out_off + kFfEpiWarps * staging * 4096;
+    static constexpr int bar_off = out_off + epi_warps * staging * tile_bytes;
     static constexpr size_t bytes = bar_off + 256 + 1024;
 };
 
@@ -45,26 +52,108 @@ struct FfParams {
     int rows, D, F, splits, tiles;
 };
 
-// act(g) and, for the backward, its derivative
+// The special-function unit's 2^x and 1/x (relative error about 2^-22), results below the normal range flushed to zero.
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// act(g) and, for the backward, its derivative.  The epilogues are bound by instructions per element, so both activations
+// cost two special-function calls.  gelu: the normal distribution's integral by Abramowitz and Stegun 7.1.26,
+// erfc(z) = (a1 t + .. + a5 t^5) exp(-z^2), t = 1 / (1 + 0.3275911 z), z >= 0, absolute error 1.5e-7, whose exponential with
+// z = |g| / sqrt 2 is the density that the derivative needs.
 template <int ACT, bool GRAD>
 __device__ __forceinline__ float ff_act(float g, float& da) {
     if (ACT == BPT_ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + __expf(-g));
+        const float s = rcp(1.f + ex2(g * -1.4426950408889634f));
         if (GRAD) da = s * fmaf(g, 1.f - s, 1.f);
         return g * s;
     }
     if (ACT == BPT_ACT_GELU) {
-        const float c = fmaf(0.5f, erff(g * 0.70710678118654752f), 0.5f);
-        if (GRAD) da = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), c);
+        const float e = ex2(g * g * -0.72134752044448170f);                     // exp(-g^2 / 2)
+        const float t = rcp(fmaf(fabsf(g), 0.3275911f * 0.70710678118654752f, 1.f));
+        float c = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+        c *= 0.5f * t * e;                                                      // the tail beyond |g|
+        c = g < 0.f ? c : 1.f - c;
+        if (GRAD) da = fmaf(g * 0.39894228040143268f, e, c);
         return g * c;
     }
     if (GRAD) da = g > 0.f ? 1.f : 0.f;
     return g < 0.f ? 0.f : g;
 }
 
+// The load thread of a CTA and the product thread of a pair go through the same slices: 64 deep, `STAGES` places in shared
+// memory, A first, B 16 KB behind it.  What they do per slice is on the critical path (one slice is 512 cycles of products, and the
+// warps next to them are busy), hence no divisions and no shared flags in here.
+template <int STAGES> struct FfLoader {
+    uint32_t s_u, full_first, full_own, empty_own;      // barriers of place 0; full_first: the pair's first CTA's, cluster address
+    bool lead;
+    int st = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+
+    // Slices [k0, k1) of this CTA's 128 rows (columns, if *_MN: the matrix lies with that axis contiguous) from row am of A, and of
+    // its B_BYTES / 128 rows from row bn of B.
+    template <bool A_MN, bool B_MN, int B_BYTES>
+    __device__ __forceinline__ void slices(int k0, int k1, const CUtensorMap* ma, int am, const CUtensorMap* mb, int bn) {
+        for (int k = k0; k < k1; ++k) {
+            if (!ok || !tc5::mbar_wait_fast(empty_own + 8u * st, ph ^ 1)) { ok = false; return; }     // the first round passes at once
+            const uint32_t a = s_u + st * kFfStageBytes, b = a + 16384, bar = full_first + 8u * st;
+            if (lead) tc5::mbar_expect_tx(full_own + 8u * st, 2 * (16384 + B_BYTES));
+            if constexpr (A_MN) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) pair::load_2d(a + j * 8192, ma, am + j * 64, k * kFfK, bar);
+            } else {
+                pair::load_2d(a, ma, k * kFfK, am, bar);
+            }
+            if constexpr (B_MN) {
+#pragma unroll
+                for (int j = 0; j < B_BYTES / 8192; ++j) pair::load_2d(b + j * 8192, mb, bn + j * 64, k * kFfK, bar);
+            } else {
+                pair::load_2d(b, mb, k * kFfK, bn, bar);
+            }
+            if (++st == STAGES) { st = 0; ph ^= 1; }
+        }
+    }
+    // Waits until every slice that was loaded has been used.
+    __device__ __forceinline__ void drain() {
+        for (int j = 0; j < STAGES && ok; ++j) {
+            ok = tc5::mbar_wait_fast(empty_own + 8u * st, ph ^ 1);
+            if (++st == STAGES) { st = 0; ph ^= 1; }
+        }
+    }
+};
+template <int STAGES> struct FfProducts {
+    uint32_t s_u, full_own, empty_own;
+    int st = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+
+    __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity) {
+        ok = ok && pair::wait_cluster(bar, parity);
+        tc5::fence_after_sync();
+    }
+    template <bool A_MN, bool B_MN>
+    __device__ __forceinline__ void slices(int n, uint32_t acc, uint32_t idesc) {
+        const uint32_t a0 = A_MN ? pair::desc_lo_mn(s_u) : tc5::desc_lo_k_major(s_u);
+        const uint32_t b0 = B_MN ? pair::desc_lo_mn(s_u + 16384) : tc5::desc_lo_k_major(s_u + 16384);
+        constexpr uint32_t a_step = A_MN ? 2048 / 16 : 2, b_step = B_MN ? 2048 / 16 : 2;      // 16 of the 64 k
+        uint32_t more = 0;
+        for (int k = 0; k < n; ++k) {
+            wait(full_own + 8u * st, ph);
+            if (!ok) return;
+            const uint32_t a = a0 + st * (kFfStageBytes / 16), b = b0 + st * (kFfStageBytes / 16);
+            pair::mma(acc, a, b, idesc, more);
+#pragma unroll
+            for (int ks = 1; ks < 4; ++ks) pair::mma(acc, a + ks * a_step, b + ks * b_step, idesc, 1);
+            more = 1;
+            pair::commit_both(empty_own + 8u * st);
+            if (++st == STAGES) { st = 0; ph ^= 1; }
+        }
+    }
+};
+
 // ACT: a choice of the whole launch, where the kernel has an activation.  BN: accumulator columns of a tile (kFfOut, kFfDx; 256 in the others: 128 of G and 128 of U)
 template <int KERNEL, int BN, int ACT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfThreads, 1) gated_ff_kernel(const __grid_constant__ FfParams p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::threads, 1) gated_ff_kernel(const __grid_constant__ FfParams p) {
     using S = FfShape<KERNEL>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // the same offset in both CTAs
@@ -73,6 +162,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfThreads, 1) gated
     auto empty = [&](int i) { return bar_u + 8u * (uint32_t)(S::stages + i); };
     auto tfull = [&](int i) { return bar_u + 8u * (uint32_t)(2 * S::stages + i); };
     auto tempty = [&](int i) { return bar_u + 8u * (uint32_t)(2 * S::stages + 2 + i); };
+    // kFfBwdIn: pair 0 of tfull / tempty belongs to G | U, pair 1 to dH
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::bar_off + 8 * (2 * S::stages + 4));
     volatile int* abort_s = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
@@ -80,7 +170,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfThreads, 1) gated
 
     if (tid == 0) {
         for (int i = 0; i < 2 * S::stages + 2; ++i) tc5::mbar_init(bar_u + 8u * i, 1);
-        for (int i = 0; i < 2; ++i) tc5::mbar_init(tempty(i), 2 * kFfEpiWarps);
+        for (int i = 0; i < 2; ++i) tc5::mbar_init(tempty(i), 2 * S::epi_warps);
         tc5::mbar_init_fence();
         *abort_s = 0;
     }
@@ -92,9 +182,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfThreads, 1) gated
     const uint32_t tbase = *tmem_slot;
 
     const int kd = (p.D + kFfK - 1) / kFfK, kf = (p.F + kFfK - 1) / kFfK, km = (p.rows + kFfK - 1) / kFfK;
-    const int n_tiles = KERNEL == kFfOut || KERNEL == kFfDx ? (p.D + BN - 1) / BN : (p.F + 127) / 128;   // along the output's columns
+    const int n_tiles = KERNEL == kFfOut || KERNEL == kFfDx ? (p.D + BN - 1) / BN : KERNEL == kFfBwdIn ? (p.F + 255) / 256 : (p.F + 127) / 128;   // along the output's columns
     const int dw_n0 = (p.D + 255) / 256, dw_n1 = (p.F + 255) / 256, dw_tiles = dw_n0 * dw_n1;             // weight gradients, each of the three
-    struct Tile { int m, n, k0, k1, job, split; };
+    struct Tile { int m, n, k0, k1, job, split, halves; };      // corner, slices, and which product
     auto tile_of = [&](int t) {
         Tile q{};
         if constexpr (KERNEL == kFfDw) {
@@ -106,205 +196,202 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfThreads, 1) gated
             q.k0 = (int)((long long)km * q.split / p.splits); q.k1 = (int)((long long)km * (q.split + 1) / p.splits);
         } else {
             q.m = t / n_tiles * 256;
-            q.n = t % n_tiles * (KERNEL == kFfOut || KERNEL == kFfDx ? BN : 128);
-            q.k1 = KERNEL == kFfIn ? kd : KERNEL == kFfOut ? kf : KERNEL == kFfBwdIn ? 2 * kd : 2 * kf;
+            q.n = t % n_tiles * (KERNEL == kFfOut || KERNEL == kFfDx ? BN : KERNEL == kFfBwdIn ? 256 : 128);
+            q.k1 = KERNEL == kFfIn ? kd : KERNEL == kFfOut ? kf : 2 * kf;
+            q.halves = p.F - q.n > 128 ? 2 : 1;         // kFfBwdIn
         }
         return q;
     };
 
+    // The pairs stride over the tiles together: what runs at one time shares rows of A (a contiguous range of tiles per pair
+    // read every row of A once per pair and was 17 % slower in the long products).
     if (w == 0 && lane == 0) {
         // =============== load thread ===============
-        int it = 0;
-        for (int t = pair_id; t < p.tiles && !*abort_s; t += n_pairs) {
+        FfLoader<S::stages> ld{s_u, pair::in_first(full(0)), full(0), empty(0), rank == 0};
+        const bool one = rank == 0;
+        for (int t = pair_id; t < p.tiles && ld.ok; t += n_pairs) {
             const Tile q = tile_of(t);
-            const int m = q.m + rank * 128;
-            for (int k = q.k0; k < q.k1; ++k, ++it) {
-                const int st = it % S::stages, use = it / S::stages;
-                if (use > 0 && !tc5::mbar_wait_idle(empty(st), (use - 1) & 1)) { *abort_s = 1; break; }
-                const uint32_t a = s_u + st * kFfStageBytes, b = a + 16384;
-                const uint32_t bar = pair::in_first(full(st));
-                if constexpr (KERNEL == kFfIn) {
-                    if (rank == 0) tc5::mbar_expect_tx(full(st), 2 * 32768);
-                    pair::load_2d(a, &p.a0, k * kFfK, m, bar);
-                    pair::load_2d(b, rank ? &p.b1 : &p.b0, k * kFfK, q.n, bar);
-                } else if constexpr (KERNEL == kFfOut) {
-                    if (rank == 0) tc5::mbar_expect_tx(full(st), 2 * (16384 + BN * 64));
-                    pair::load_2d(a, &p.a0, k * kFfK, m, bar);
-                    pair::load_2d(b, &p.b0, k * kFfK, q.n + rank * (BN / 2), bar);
-                } else if constexpr (KERNEL == kFfBwdIn) {
-                    if (k < kd) {       // dH: dy rows, Wd with its F axis contiguous
-                        if (rank == 0) tc5::mbar_expect_tx(full(st), 2 * 24576);
-                        pair::load_2d(a, &p.a1, k * kFfK, m, bar);
-                        pair::load_2d(b, &p.b2, q.n + rank * 64, k * kFfK, bar);
-                    } else {
-                        if (rank == 0) tc5::mbar_expect_tx(full(st), 2 * 32768);
-                        pair::load_2d(a, &p.a0, (k - kd) * kFfK, m, bar);
-                        pair::load_2d(b, rank ? &p.b1 : &p.b0, (k - kd) * kFfK, q.n, bar);
-                    }
-                } else if constexpr (KERNEL == kFfDx) {
-                    if (rank == 0) tc5::mbar_expect_tx(full(st), 2 * (16384 + BN * 64));
-                    const bool second = k >= kf;
-                    const int kk = (second ? k - kf : k) * kFfK;
-                    pair::load_2d(a, second ? &p.a1 : &p.a0, kk, m, bar);
-#pragma unroll
-                    for (int j = 0; j < BN / 128; ++j) pair::load_2d(b + j * 8192, second ? &p.b1 : &p.b0, q.n + rank * (BN / 2) + j * 64, kk, bar);
-                } else {
-                    if (rank == 0) tc5::mbar_expect_tx(full(st), 2 * 32768);
-                    const CUtensorMap* ma = q.job == 0 ? &p.a0 : q.job == 1 ? &p.a1 : &p.a2;
-                    const CUtensorMap* mb = q.job < 2 ? &p.b0 : &p.b1;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        pair::load_2d(a + j * 8192, ma, m + j * 64, k * kFfK, bar);
-                        pair::load_2d(b + j * 8192, mb, q.n + rank * 128 + j * 64, k * kFfK, bar);
-                    }
-                }
+            const int m = q.m + rank * 128, n = q.n + rank * (BN / 2);
+            if constexpr (KERNEL == kFfIn) {
+                ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n);
+            } else if constexpr (KERNEL == kFfOut) {
+                ld.template slices<false, false, BN * 64>(0, kf, &p.a0, m, &p.b0, n);
+            } else if constexpr (KERNEL == kFfBwdIn) {      // dH: dy rows, Wd with its F axis contiguous
+                ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n);
+                ld.template slices<false, true, 16384>(0, kd, &p.a1, m, &p.b2, n);
+                if (q.halves == 2) ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n + 128);
+            } else if constexpr (KERNEL == kFfDx) {
+                ld.template slices<false, true, BN * 64>(0, kf, &p.a0, m, &p.b0, n);
+                ld.template slices<false, true, BN * 64>(0, kf, &p.a1, m, &p.b1, n);
+            } else {
+                ld.template slices<true, true, 16384>(q.k0, q.k1, q.job == 0 ? &p.a0 : q.job == 1 ? &p.a1 : &p.a2, m, q.job < 2 ? &p.b0 : &p.b1, n);
             }
         }
         // the releases of the last slices still arrive in this CTA's shared memory: see them in before it ends
-        for (int j = it > S::stages ? it - S::stages : 0; j < it && !*abort_s; ++j)
-            if (!tc5::mbar_wait_idle(empty(j % S::stages), (j / S::stages) & 1)) *abort_s = 1;
-        if (*abort_s) {   // copies still in flight land before the CTA ends (their barrier may be the other CTA's: give them time)
+        ld.drain();
+        if (!ld.ok) {   // copies still in flight land before the CTA ends (their barrier may be the other CTA's: give them time)
+            *abort_s = 1;
             const long long start = clock64();
             while (clock64() - start < (1ll << 22)) {}
         }
     } else if (w == 1 && lane == 0 && rank == 0) {
         // =============== product thread ===============
         constexpr bool a_mn = KERNEL == kFfDw, b_mn = KERNEL == kFfDw || KERNEL == kFfDx;
-        const uint32_t idesc = tc5::instr_desc(256, BN, a_mn, b_mn), idesc_dh = tc5::instr_desc(256, 128, 0, 1);
-        auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (*abort_s) return;
-            if (!pair::wait_cluster(bar, parity)) *abort_s = 1;
-        };
-        int it = 0, i = 0;
-        for (int t = pair_id; t < p.tiles && !*abort_s; t += n_pairs, ++i) {
+        const uint32_t idesc = tc5::instr_desc(256, BN, a_mn, b_mn);
+        FfProducts<S::stages> mm{s_u, full(0), empty(0)};
+        int i = 0, gu = 0;      // tiles, G | U accumulators so far
+        for (int t = pair_id; t < p.tiles && mm.ok; t += n_pairs, ++i) {
             const Tile q = tile_of(t);
-            // an accumulator is free again when the epilogue of the tile two before has taken it out
-            if (i >= 2) wait(tempty(i & 1), (i / 2 - 1) & 1);
-            tc5::fence_after_sync();
-            uint32_t acc = tbase + (KERNEL == kFfBwdIn ? 256u + (i & 1) * 128u : (i & 1) * 256u);
-            for (int k = q.k0; k < q.k1; ++k, ++it) {
-                const int st = it % S::stages;
-                if constexpr (KERNEL == kFfBwdIn) {
-                    if (k == kd) {      // G | U have one place: the tile before has to be out
-                        if (i >= 1) wait(tempty((i - 1) & 1), ((i - 1) / 2) & 1);
-                        tc5::fence_after_sync();
-                        acc = tbase;
+            if constexpr (KERNEL == kFfBwdIn) {     // each accumulator has one place: what was there before has to be out
+                for (int phase = 0; phase < 1 + q.halves && mm.ok; ++phase) {
+                    if (phase == 1) {
+                        if (i > 0) mm.wait(tempty(1), (i - 1) & 1);
+                        mm.template slices<false, true>(kd, tbase + 256, tc5::instr_desc(256, 256, 0, 1));
+                        if (mm.ok) pair::commit_both(tfull(1));
+                    } else {
+                        if (gu > 0) mm.wait(tempty(0), (gu - 1) & 1);
+                        mm.template slices<false, false>(kd, tbase, idesc);
+                        if (mm.ok) pair::commit_both(tfull(0));
+                        ++gu;
                     }
                 }
-                wait(full(st), (it / S::stages) & 1);
-                if (*abort_s) break;
-                tc5::fence_after_sync();
-                const uint32_t a = s_u + st * kFfStageBytes, b = a + 16384;
-                const bool dh = KERNEL == kFfBwdIn && k < kd;
-                const uint32_t a_lo = a_mn ? pair::desc_lo_mn(a) : tc5::desc_lo_k_major(a);
-                const uint32_t b_lo = b_mn || dh ? pair::desc_lo_mn(b) : tc5::desc_lo_k_major(b);
-                const uint32_t b_step = b_mn || dh ? 2048 / 16 : 2, a_step = a_mn ? 2048 / 16 : 2;
-                const bool first = k == q.k0 || (KERNEL == kFfBwdIn && k == kd);
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    pair::mma(acc, a_lo + ks * a_step, b_lo + ks * b_step, dh ? idesc_dh : idesc, (first && ks == 0) ? 0u : 1u);
-                pair::commit_both(empty(st));
+            } else {
+                // an accumulator is free again when the epilogue of the tile two before has taken it out
+                if (i >= 2) mm.wait(tempty(i & 1), (i / 2 - 1) & 1);
+                mm.template slices<a_mn, b_mn>(q.k1 - q.k0, tbase + (i & 1) * 256u, idesc);
+                if (mm.ok) pair::commit_both(tfull(i & 1));
             }
-            if (*abort_s) break;
-            pair::commit_both(tfull(i & 1));
         }
-    } else if (w >= 4) {
-        // =============== epilogue warps: 32 rows (tensor-memory lanes) x half of the tile's columns each ===============
-        const int quad = w & 3, half = (w - 4) >> 2;
+        if (!mm.ok) *abort_s = 1;
+    } else if (w >= 2) {
+        // =============== epilogue warps: 32 rows (tensor-memory lanes) x a half or quarter of the tile's columns each ===============
+        const int quad = w & 3, part = (w - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        unsigned char* stg = smem + S::out_off + (w - 4) * S::staging * 4096;
-        const uint32_t stg_u = smem_u32(stg), release[2] = {pair::in_first(tempty(0)), pair::in_first(tempty(1))};
-        // 16 bytes of this thread's row of staging tile `buf`
+        unsigned char* stg = smem + S::out_off + (w - 2) * S::staging * S::tile_bytes;
+        const uint32_t stg_u = smem_u32(stg), release0 = pair::in_first(tempty(0)), release1 = pair::in_first(tempty(1));
+        // 16 bytes of this thread's row of staging tile `buf`: rows of 128 bytes, or of 64, in the store's swizzle
         auto put = [&](int buf, int chunk, uint32_t x, uint32_t y, uint32_t z, uint32_t v) {
-            *reinterpret_cast<uint4*>(stg + buf * 4096 + tile_off(lane, chunk)) = make_uint4(x, y, z, v);
+            *reinterpret_cast<uint4*>(stg + buf * S::tile_bytes + tile_off(lane, chunk)) = make_uint4(x, y, z, v);
         };
-        int i = 0;
+        auto put64 = [&](int buf, int chunk, uint32_t x, uint32_t y, uint32_t z, uint32_t v) {
+            *reinterpret_cast<uint4*>(stg + buf * S::tile_bytes + lane * 64 + ((chunk ^ ((lane >> 1) & 3)) << 4)) = make_uint4(x, y, z, v);
+        };
+        int i = 0, gu = 0;
         for (int t = pair_id; t < p.tiles; t += n_pairs, ++i) {
             const Tile q = tile_of(t);
-            const bool ok = !*abort_s && tc5::mbar_wait_fast(tfull(i & 1), (i / 2) & 1);
-            if (!__all_sync(0xffffffffu, ok)) { *abort_s = 1; break; }      // the whole warp together
-            tc5::fence_after_sync();
+            auto ready = [&](int which, uint32_t parity) {      // the whole warp together
+                const bool ok = !*abort_s && tc5::mbar_wait_fast(tfull(which), parity);
+                if (!__all_sync(0xffffffffu, ok)) { *abort_s = 1; return false; }
+                tc5::fence_after_sync();
+                return true;
+            };
+            if (KERNEL != kFfBwdIn && !ready(i & 1, (i / 2) & 1)) break;
             const int row = q.m + rank * 128 + quad * 32;
-            auto done = [&] {           // this warp has taken the accumulator out
+            auto done = [&](uint32_t bar) {           // this warp has taken (its part of) an accumulator out
                 tc5::fence_before_sync();
                 __syncwarp();
-                if (lane == 0) pair::arrive_cluster(release[i & 1]);
+                if (lane == 0) pair::arrive_cluster(bar);
             };
             auto send = [&](const CUtensorMap* map, int buf, int col, int limit_cols, int limit_rows) {
                 tc5::fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
                     if (col < limit_cols && row < limit_rows) {
-                        if constexpr (KERNEL == kFfDw) pair::store_3d(map, col, row, q.job == 1 ? p.splits + q.split : q.split, stg_u + buf * 4096);
-                        else pair::store_2d(map, col, row, stg_u + buf * 4096);
+                        if constexpr (KERNEL == kFfDw) pair::store_3d(map, col, row, q.job == 1 ? p.splits + q.split : q.split, stg_u + buf * S::tile_bytes);
+                        else pair::store_2d(map, col, row, stg_u + buf * S::tile_bytes);
                     }
                     pair::store_commit();
                 }
             };
             if constexpr (KERNEL == kFfIn) {
-                const uint32_t src = tbase + lane_base + (i & 1) * 256 + half * 64;
+                const uint32_t src = tbase + lane_base + (i & 1) * 256 + part * 32;
+                uint32_t g[32], u[32];
+                tc5::tmem_ld32(src, g);
+                tc5::tmem_ld32(src + 128, u);
+                tc5::tmem_ld_wait();
+                done((i & 1) ? release1 : release0);
                 if (lane == 0) pair::store_wait_read<1>();
                 __syncwarp();
 #pragma unroll
-                for (int c = 0; c < 64; c += 32) {
-                    uint32_t g[32], u[32];
-                    tc5::tmem_ld32(src + c, g);
-                    tc5::tmem_ld32(src + 128 + c, u);
-                    tc5::tmem_ld_wait();
-                    if (c == 32) done();
-                    float unused;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t x[4];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) g[j] = __float_as_uint(ff_act<ACT, false>(__uint_as_float(g[j]), unused) * __uint_as_float(u[j]));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t x[4];
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) x[y] = pack_bf16(__uint_as_float(g[j * 8 + 2 * y]), __uint_as_float(g[j * 8 + 2 * y + 1]));
-                        put(i & 1, c / 8 + j, x[0], x[1], x[2], x[3]);
-                    }
-                }
-                send(&p.c0, i & 1, q.n + half * 64, p.F, p.rows);
-            } else if constexpr (KERNEL == kFfBwdIn) {
-                const uint32_t src = tbase + lane_base + half * 64, src_dh = src + 256 + (i & 1) * 128;
-                if (lane == 0) pair::store_wait_read<0>();
-                __syncwarp();
-#pragma unroll 1
-                for (int c = 0; c < 64; c += 16) {
-                    uint32_t g[16], u[16], dh[16];
-                    tc5::tmem_ld16(src + c, g);
-                    tc5::tmem_ld16(src + 128 + c, u);
-                    tc5::tmem_ld16(src_dh + c, dh);
-                    tc5::tmem_ld_wait();
-                    if (c == 48) done();
-                    uint32_t og[8], ou[8], oh[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float r[3][2];
+                    for (int y = 0; y < 4; ++y) {
+                        float r[2], unused;
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float gv = __uint_as_float(g[2 * j + e]), uv = __uint_as_float(u[2 * j + e]), dv = __uint_as_float(dh[2 * j + e]);
-                            float da;
-                            const float a = ff_act<ACT, true>(gv, da);
-                            r[0][e] = dv * uv * da;
-                            r[1][e] = dv * a;
-                            r[2][e] = a * uv;
+                            const int k = j * 8 + 2 * y + e;
+                            r[e] = ff_act<ACT, false>(__uint_as_float(g[k]), unused) * __uint_as_float(u[k]);
                         }
-                        og[j] = pack_bf16(r[0][0], r[0][1]);
-                        ou[j] = pack_bf16(r[1][0], r[1][1]);
-                        oh[j] = pack_bf16(r[2][0], r[2][1]);
+                        x[y] = pack_bf16(r[0], r[1]);
                     }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        put(0, c / 8 + j, og[4 * j], og[4 * j + 1], og[4 * j + 2], og[4 * j + 3]);
-                        put(1, c / 8 + j, ou[4 * j], ou[4 * j + 1], ou[4 * j + 2], ou[4 * j + 3]);
-                        put(2, c / 8 + j, oh[4 * j], oh[4 * j + 1], oh[4 * j + 2], oh[4 * j + 3]);
-                    }
+                    put64(i & 1, j, x[0], x[1], x[2], x[3]);
                 }
-                send(&p.c0, 0, q.n + half * 64, p.F, p.rows);
-                send(&p.c1, 1, q.n + half * 64, p.F, p.rows);
-                send(&p.c2, 2, q.n + half * 64, p.F, p.rows);
+                send(&p.c0, i & 1, q.n + part * 32, p.F, p.rows);
+            } else if constexpr (KERNEL == kFfBwdIn) {
+                const uint32_t src = tbase + lane_base + part * 32;
+#pragma unroll 1
+                for (int half = 0; half < q.halves; ++half, ++gu) {
+                    const uint32_t src_dh = src + 256 + half * 128;
+                    if (!ready(0, gu & 1)) break;
+                    uint32_t g[32], u[32], dh[16], oh[16];
+                    tc5::tmem_ld32(src, g);
+                    tc5::tmem_ld32(src + 128, u);
+                    tc5::tmem_ld_wait();
+                    done(release0);
+                    if (half == 0 && !ready(1, i & 1)) break;
+                    tc5::tmem_ld16(src_dh, dh);
+                    if (lane == 0) pair::store_wait_read<0>();
+                    __syncwarp();
+                    tc5::tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 32; c += 16) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            uint32_t o[2][4];
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                float r[3][2];
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const int k = j * 8 + 2 * y + e;
+                                    const float gv = __uint_as_float(g[c + k]), uv = __uint_as_float(u[c + k]), dv = __uint_as_float(dh[k]);
+                                    float da;
+                                    const float a = ff_act<ACT, true>(gv, da);
+                                    r[0][e] = dv * uv * da;
+                                    r[1][e] = dv * a;
+                                    r[2][e] = a * uv;
+                                }
+#pragma unroll
+                                for (int m = 0; m < 2; ++m) o[m][y] = pack_bf16(r[m][0], r[m][1]);
+                                oh[c / 2 + j * 4 + y] = pack_bf16(r[2][0], r[2][1]);
+                            }
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) put64(m, c / 8 + j, o[m][0], o[m][1], o[m][2], o[m][3]);
+                        }
+                        if (c == 0) {
+                            tc5::tmem_ld16(src_dh + 16, dh);
+                            tc5::tmem_ld_wait();
+                            if (half == q.halves - 1) done(release1);
+                        }
+                    }
+                    const int col = q.n + half * 128 + part * 32;
+                    tc5::fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (col < p.F && row < p.rows) pair::store_2d(&p.c0, col, row, stg_u);
+                        pair::store_commit();
+                        if (col < p.F && row < p.rows) pair::store_2d(&p.c1, col, row, stg_u + S::tile_bytes);
+                        pair::store_commit();
+                        pair::store_wait_read<1>();     // dG has left its tile: h takes it
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) put64(0, j, oh[4 * j], oh[4 * j + 1], oh[4 * j + 2], oh[4 * j + 3]);
+                    send(&p.c2, 0, col, p.F, p.rows);
+                }
             } else if constexpr (KERNEL == kFfDw) {
-                const uint32_t src = tbase + lane_base + (i & 1) * 256 + half * 128;
+                const uint32_t src = tbase + lane_base + (i & 1) * 256 + part * 128;
                 const CUtensorMap* map = q.job < 2 ? &p.c0 : &p.c1;
                 const int limit_cols = q.job < 2 ? p.D : p.F, limit_rows = q.job < 2 ? p.F : p.D;
 #pragma unroll
@@ -312,22 +399,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfThreads, 1) gated
                     uint32_t x[32];
                     tc5::tmem_ld32(src + c, x);
                     tc5::tmem_ld_wait();
-                    if (c == 96) done();
+                    if (c == 96) done((i & 1) ? release1 : release0);
                     if (lane == 0) pair::store_wait_read<1>();
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < 8; ++j) put((c / 32) & 1, j, x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-                    send(map, (c / 32) & 1, q.n + half * 128 + c, limit_cols, limit_rows);
+                    send(map, (c / 32) & 1, q.n + part * 128 + c, limit_cols, limit_rows);
                 }
             } else {
                 constexpr int W = BN / 2 < 64 ? BN / 2 : 64;      // columns per stored tile
-                const uint32_t src = tbase + lane_base + (i & 1) * 256 + half * (BN / 2);
+                const uint32_t src = tbase + lane_base + (i & 1) * 256 + part * (BN / 2);
 #pragma unroll
                 for (int c = 0; c < BN / 2; c += 32) {
                     uint32_t x[32];
                     tc5::tmem_ld32(src + c, x);
                     tc5::tmem_ld_wait();
-                    if (c + 32 == BN / 2) done();
+                    if (c + 32 == BN / 2) done((i & 1) ? release1 : release0);
                     const int buf = (i * (BN / 2 / W) + c / W) & 1;
                     if (c % W == 0) {
                         if (lane == 0) pair::store_wait_read<1>();
@@ -339,9 +426,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfThreads, 1) gated
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[e] = pack_bf16(__uint_as_float(x[j * 8 + 2 * e]), __uint_as_float(x[j * 8 + 2 * e + 1]));
                         if constexpr (W == 64) put(buf, (c & 32) / 8 + j, y[0], y[1], y[2], y[3]);
-                        else *reinterpret_cast<uint4*>(stg + buf * 4096 + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                        else put64(buf, j, y[0], y[1], y[2], y[3]);
                     }
-                    if (c % W + 32 == W) send(&p.c0, buf, q.n + half * (BN / 2) + c / W * W, p.D, p.rows);
+                    if (c % W + 32 == W) send(&p.c0, buf, q.n + part * (BN / 2) + c / W * W, p.D, p.rows);
                 }
             }
         }
@@ -374,10 +461,10 @@ __global__ void __launch_bounds__(256) gated_ff_dw_sum_kernel(const float* __res
     }
 }
 
-// 2-D map over a row-major [n_rows, n_cols] bf16 matrix, boxes of box_rows x box_cols.
-bool bf16_map(CUtensorMap* m, const void* base, long long n_rows, int n_cols, int box_rows, int box_cols = 64) {
+// 2-D map over a row-major [n_rows, n_cols] bf16 matrix, rows `ld` elements apart (0: n_cols), boxes of box_rows x box_cols.
+bool bf16_map(CUtensorMap* m, const void* base, long long n_rows, int n_cols, int box_rows, int box_cols = 64, int ld = 0) {
     const cuuint64_t dims[2] = {(cuuint64_t)n_cols, (cuuint64_t)n_rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)n_cols * 2};
+    const cuuint64_t strides[1] = {(cuuint64_t)(ld ? ld : n_cols) * 2};
     const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, estr[2] = {1, 1};
     return tc5::encode_tiled()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
                                CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
@@ -397,7 +484,7 @@ bpt_status run(const FfParams& p, cudaStream_t st, const char* name) {
     constexpr size_t smem = FfShape<KERNEL>::bytes;
     static_assert(smem <= 227 * 1024, "shared memory of one CTA");
     if (cudaFuncSetAttribute(gated_ff_kernel<KERNEL, BN, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return BPT_ERR_CUDA;
-    gated_ff_kernel<KERNEL, BN, ACT><<<2 * std::min(p.tiles, kFfPairs), kFfThreads, smem, st>>>(p);
+    gated_ff_kernel<KERNEL, BN, ACT><<<2 * std::min(p.tiles, kFfPairs), FfShape<KERNEL>::threads, smem, st>>>(p);
     trace_mark(st, name);
     return cudaGetLastError() == cudaSuccess ? BPT_OK : BPT_ERR_CUDA;
 }
@@ -409,7 +496,9 @@ bpt_status run_act(const FfParams& p, int act, cudaStream_t st, const char* name
 }
 
 constexpr size_t kStatusBytes = 256;
-size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+// Inner rows start on 128-byte boundaries, whatever F is; what lies between F and there is neither written nor read.
+int inner_ld(int F) { return (F + 63) / 64 * 64; }
+size_t inner_bytes(long long rows, int F) { return ((size_t)rows * inner_ld(F) * 2 + 255) & ~(size_t)255; }
 
 // Row ranges of the weight-gradient products: as many as make whole rounds of the pairs, each at least eight slices deep.
 int dw_splits(long long rows, int D, int F) {
@@ -448,7 +537,7 @@ using namespace bpt;
 
 extern "C" size_t bpt_gated_ff_workspace_bytes(int64_t rows, int32_t D, int32_t F, int backward) {
     if (check_ff(rows, D, F, BPT_ACT_RELU) != BPT_OK || rows == 0) return 0;
-    const size_t hidden = round256((size_t)rows * F * 2);
+    const size_t hidden = inner_bytes(rows, F);
     if (!backward) return hidden;
     return 3 * hidden + (size_t)3 * dw_splits(rows, D, F) * D * F * 4;
 }
@@ -465,19 +554,19 @@ extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const 
     if (!tc5::encode_tiled()) return BPT_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (status && cudaMemsetAsync(status, 0, kStatusBytes, st) != cudaSuccess) return BPT_ERR_CUDA;
-    void* h = workspace;
     FfParams p{};
     p.status = static_cast<int*>(status);
     p.rows = (int)rows; p.D = D; p.F = F;
+    const int ld = inner_ld(F);
     if (!bf16_map(&p.a0, x, rows, D, 128) || !bf16_map(&p.b0, w_gate, F, D, 128) || !bf16_map(&p.b1, w_up, F, D, 128) ||
-        !bf16_map(&p.c0, h, rows, F, 32))
+        !bf16_map(&p.c0, workspace, rows, F, 32, 32, ld))
         return BPT_ERR_CUDA;
     const int mt = (int)((rows + 255) / 256);
     p.tiles = mt * ((F + 127) / 128);
     bpt_status e = run_act<kFfIn>(p, act, st, "gated_ff_in");
     if (e != BPT_OK) return e;
     const int bn = out_columns(rows, D, 64);
-    if (!bf16_map(&p.a0, h, rows, F, 128) || !bf16_map(&p.b0, w_down, D, F, bn / 2) || !bf16_map(&p.c0, y, rows, D, 32, bn == 64 ? 32 : 64))
+    if (!bf16_map(&p.a0, workspace, rows, F, 128, 64, ld) || !bf16_map(&p.b0, w_down, D, F, bn / 2) || !bf16_map(&p.c0, y, rows, D, 32, bn == 64 ? 32 : 64))
         return BPT_ERR_CUDA;
     p.tiles = mt * ((D + bn - 1) / bn);
     return bn == 256 ? run<kFfOut, 256>(p, st, "gated_ff_out") : bn == 128 ? run<kFfOut, 128>(p, st, "gated_ff_out") : run<kFfOut, 64>(p, st, "gated_ff_out");
@@ -504,24 +593,24 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     if ((uintptr_t)workspace & 255) return BPT_ERR_INVALID_ARG;
     if (!tc5::encode_tiled()) return BPT_ERR_CUDA;
     if (status && cudaMemsetAsync(status, 0, kStatusBytes, st) != cudaSuccess) return BPT_ERR_CUDA;
-    const size_t hidden = round256((size_t)rows * F * 2);
-    char* dg = static_cast<char*>(workspace);
-    char *du = dg + hidden, *h = du + hidden;
+    const size_t hidden = inner_bytes(rows, F);
+    char *dg = static_cast<char*>(workspace), *du = dg + hidden, *h = du + hidden;
     float* part = reinterpret_cast<float*>(h + hidden);
     const int mt = (int)((rows + 255) / 256);
     FfParams p{};
     p.status = static_cast<int*>(status);
     p.rows = (int)rows; p.D = D; p.F = F;
+    const int ld = inner_ld(F);
     if (!bf16_map(&p.a0, x, rows, D, 128) || !bf16_map(&p.a1, dy, rows, D, 128) || !bf16_map(&p.b0, w_gate, F, D, 128) ||
-        !bf16_map(&p.b1, w_up, F, D, 128) || !bf16_map(&p.b2, w_down, D, F, 64) || !bf16_map(&p.c0, dg, rows, F, 32) ||
-        !bf16_map(&p.c1, du, rows, F, 32) || !bf16_map(&p.c2, h, rows, F, 32))
+        !bf16_map(&p.b1, w_up, F, D, 128) || !bf16_map(&p.b2, w_down, D, F, 64) ||
+        !bf16_map(&p.c0, dg, rows, F, 32, 32, ld) || !bf16_map(&p.c1, du, rows, F, 32, 32, ld) || !bf16_map(&p.c2, h, rows, F, 32, 32, ld))
         return BPT_ERR_CUDA;
-    p.tiles = mt * ((F + 127) / 128);
+    p.tiles = mt * ((F + 255) / 256);
     bpt_status e = run_act<kFfBwdIn>(p, act, st, "gated_ff_bwd_in");
     if (e != BPT_OK) return e;
     if (dx) {
         const int bn = out_columns(rows, D, 128);
-        if (!bf16_map(&p.a0, dg, rows, F, 128) || !bf16_map(&p.a1, du, rows, F, 128) || !bf16_map(&p.b0, w_gate, F, D, 64) ||
+        if (!bf16_map(&p.a0, dg, rows, F, 128, 64, ld) || !bf16_map(&p.a1, du, rows, F, 128, 64, ld) || !bf16_map(&p.b0, w_gate, F, D, 64) ||
             !bf16_map(&p.b1, w_up, F, D, 64) || !bf16_map(&p.c0, dx, rows, D, 32))
             return BPT_ERR_CUDA;
         p.tiles = mt * ((D + bn - 1) / bn);
@@ -530,8 +619,8 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     }
     if (weights) {
         p.splits = dw_splits(rows, D, F);
-        if (!bf16_map(&p.a0, dg, rows, F, 64) || !bf16_map(&p.a1, du, rows, F, 64) || !bf16_map(&p.a2, dy, rows, D, 64) ||
-            !bf16_map(&p.b0, x, rows, D, 64) || !bf16_map(&p.b1, h, rows, F, 64) || !part_map(&p.c0, part, 2 * p.splits, F, D) ||
+        if (!bf16_map(&p.a0, dg, rows, F, 64, 64, ld) || !bf16_map(&p.a1, du, rows, F, 64, 64, ld) || !bf16_map(&p.a2, dy, rows, D, 64) ||
+            !bf16_map(&p.b0, x, rows, D, 64) || !bf16_map(&p.b1, h, rows, F, 64, 64, ld) || !part_map(&p.c0, part, 2 * p.splits, F, D) ||
             !part_map(&p.c1, part + (size_t)2 * p.splits * D * F, p.splits, D, F))
             return BPT_ERR_CUDA;
         p.tiles = 3 * ((D + 255) / 256) * ((F + 255) / 256) * p.splits;

@@ -91,6 +91,36 @@ def test_large_scores():
     _check(*_inputs(130, 128, 256, 6, scale=300.0), "gelu")
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("rows", [1, 8, 40000])
+def test_activations_on_their_own(act, rows):
+    """Weights that pick g and 1 out of x and give the inner row back: y is act(g), dx[:, 0] its derivative.  One rounding of the
+    inner row (the second product and its rounding are exact), the derivative rounded once more as an operand; beside that the
+    approximations: relative 2^-20, and 2e-7 absolute (1.5e-7 / 2 of the tail, fp32 roundings) for gelu, times |g|."""
+    import torch
+    from paper_1911_04070_b200 import binding
+    g = torch.cat([torch.linspace(-40, 40, 30001), torch.linspace(-1, 1, 9997), torch.tensor([0.0, -88.0])]).double()[-rows:].bfloat16().cuda()
+    n = g.numel()
+    x = torch.zeros(n, 8, dtype=torch.bfloat16, device="cuda:0")
+    x[:, 0], x[:, 1] = g, 1
+    pick = lambda c: torch.zeros(8, 8, dtype=torch.bfloat16, device="cuda:0").index_fill_(1, torch.tensor([c], device="cuda:0"), 1)
+    eye = torch.eye(8, dtype=torch.bfloat16, device="cuda:0")
+    y = binding.bpt_gated_ff_fwd(x, pick(0), pick(1), eye, act)
+    z = g.double().requires_grad_(True)
+    f = {"silu": torch.nn.functional.silu, "gelu": torch.nn.functional.gelu, "relu": torch.relu}[act](z)
+    df, = torch.autograd.grad(f.sum(), z)
+    slack = 2.0 ** -20 * f.abs() + (3e-7 * z.abs() + 1e-30)
+    err = (y.double() - f[:, None]).abs()
+    assert (err <= (H * f.abs() + slack)[:, None]).all(), float(err.max())
+    one = torch.zeros(n, 8, dtype=torch.bfloat16, device="cuda:0")
+    one[:, 3] = 1
+    dx, *_ = binding.bpt_gated_ff_bwd(x, pick(0), pick(1), eye, one, act)
+    err = (dx[:, 0].double() - df).abs()
+    assert (err <= 2 * H * df.abs() * (1 + H) + 3e-7 * (1 + z.abs())).all(), float(err.max())
+    err = (dx[:, 1].double() - f).abs()
+    assert (err <= 2 * H * f.abs() * (1 + H) + slack).all()
+
+
 @pytest.mark.parametrize("rows", [3, 300])
 def test_nan_and_infinity_stay_in_their_rows(rows):
     import torch

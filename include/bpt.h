@@ -302,12 +302,14 @@ bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const void* w_up,
  * Arithmetic and statistics are fp32; y is computed from the unrounded r; one rounding per stored value.
  * rows >= 0, 1 <= D <= 8192.  Rows whose D * sizeof(element) is not a multiple of 16 bytes, and tensors that are not
  * 16-byte aligned, are served element by element.  y must be given exactly when norm is not NONE; r may be NULL
- * then.  y or r may be the same buffer as h or b.
+ * then.  y or r may be the same buffer as h or b.  `stats`: NULL, or [rows][4] fp32 (16-byte aligned) that receives mean
+ * and reciprocal deviation of the post norm and of the norm (0 and 1 for an absent norm), for the backward.
  *
  * Backward: given dy = dLoss/dy (NULL: zero) and dr = dLoss/dr (NULL: zero), writes those of dh, db [rows, D] (dtype),
  * d_weight, d_bias, d_post_weight, d_post_bias [D] (param_dtype), d_gate [gate_groups, D] (gate_dtype) that are not
  * NULL:  dR = dr + norm'(dy),  dh = alpha dR,  dn = gate dR,  db = post'(dn),  and the column sums that belong to the
- * parameters.  Everything is recomputed from h and b.  Outputs are overwritten; the sums are taken in a fixed order
+ * parameters.  Everything is recomputed from h, b and the forward's `stats` (which may be NULL when neither norm is
+ * there).  Outputs are overwritten; the sums are taken in a fixed order
  * without atomics, so results are bit-reproducible.  dh / db may be the buffers of dy or dr, not of h or b.
  * `workspace`: bpt_res_norm_bwd_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a
  * status block (nothing here waits), 16-byte aligned; two calls whose GPU work overlaps need one each.
@@ -324,9 +326,9 @@ typedef struct {
     const void *h, *b;
     const void *weight, *bias, *post_weight, *post_bias, *gate;
 } bpt_res_norm_args;
-bpt_status bpt_res_norm_fwd(const bpt_res_norm_args* args, void* y, void* r, void* cuda_stream);
+bpt_status bpt_res_norm_fwd(const bpt_res_norm_args* args, void* y, void* r, float* stats, void* cuda_stream);
 size_t bpt_res_norm_bwd_workspace_bytes(const bpt_res_norm_args* args);
-bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* args, const void* dy, const void* dr, void* dh, void* db,
+bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* args, const float* stats, const void* dy, const void* dr, void* dh, void* db,
                             void* d_weight, void* d_bias, void* d_post_weight, void* d_post_bias, void* d_gate,
                             void* workspace, size_t workspace_bytes, void* cuda_stream);
 

@@ -92,11 +92,11 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_out_proj_norm.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_int64, i32, f32, vp, vp]
         rn = ctypes.POINTER(ResNormArgs)
         lib.bpt_res_norm_fwd.restype = ctypes.c_int
-        lib.bpt_res_norm_fwd.argtypes = [rn, vp, vp, vp]
+        lib.bpt_res_norm_fwd.argtypes = [rn, vp, vp, vp, vp]
         lib.bpt_res_norm_bwd_workspace_bytes.restype = sz
         lib.bpt_res_norm_bwd_workspace_bytes.argtypes = [rn]
         lib.bpt_res_norm_bwd.restype = ctypes.c_int
-        lib.bpt_res_norm_bwd.argtypes = [rn, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.bpt_res_norm_bwd.argtypes = [rn, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         i64 = ctypes.c_int64
         lib.bpt_gated_ff_workspace_bytes.restype = sz
         lib.bpt_gated_ff_workspace_bytes.argtypes = [i64, i32, i32, ctypes.c_int]
@@ -359,28 +359,35 @@ def _check_like(h, *ts):
             raise ValueError("results and gradients must be contiguous and share shape, dtype and device with h")
 
 
+def _check_stats(rows, h, stats):
+    if stats is not None and (stats.dtype != torch.float32 or stats.shape != (rows, 4) or stats.device != h.device or not stats.is_contiguous()):
+        raise ValueError("stats must be a contiguous float32 tensor [rows, 4] on the device of h")
+
+
 def bpt_res_norm_fwd(h, b=None, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
-                     alpha: float = 1.0, eps: float = 1e-5, want_sum: bool = False, y=None, r=None):
+                     alpha: float = 1.0, eps: float = 1e-5, want_sum: bool = False, y=None, r=None, stats=None):
     """n = post_norm(b), r = alpha * h + gate * n, y = norm(r) over the last axis, in one kernel.  h, b: [..., D] float32 or
     bfloat16, contiguous; norm / post_norm: None, "layer" or "rms" with weights and biases [D]; gate: [D], or h's shape with
     the trailing row axes of length one (one gate row per sequence, per row ...).  Returns (y, r); y is None without a norm,
-    r is None unless want_sum (or norm is None)."""
+    r is None unless want_sum (or norm is None).  stats: a float32 tensor [rows, 4] to fill for the backward, or None."""
     args = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
     _check_like(h, y, r)
+    _check_stats(args.rows, h, stats)
     with torch.cuda.device(h.device):
         y = torch.empty_like(h) if y is None and norm is not None else y
         r = torch.empty_like(h) if r is None and (want_sum or norm is None) else r
-        _check(load_library().bpt_res_norm_fwd(ctypes.byref(args), _ptr(y), _ptr(r), _stream()), "bpt_res_norm_fwd")
+        _check(load_library().bpt_res_norm_fwd(ctypes.byref(args), _ptr(y), _ptr(r), _ptr(stats), _stream()), "bpt_res_norm_fwd")
     return y, r
 
 
-def bpt_res_norm_bwd(h, b, dy, dr, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
+def bpt_res_norm_bwd(h, b, dy, dr, stats, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
                      alpha: float = 1.0, eps: float = 1e-5, workspace=None, need=(True,) * 7):
-    """Backward of bpt_res_norm_fwd from its inputs and the gradients of y and r (either may be None: zero).  Returns
+    """Backward of bpt_res_norm_fwd from its inputs, its stats and the gradients of y and r (either may be None: zero).  Returns
     (dh, db, d_weight, d_bias, d_post_weight, d_post_bias, d_gate), each in the type of what it belongs to; None where that
     is None or where `need` says so.  Bit-reproducible."""
     args = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
     _check_like(h, dy, dr)
+    _check_stats(args.rows, h, stats)
     lib = load_library()
     with torch.cuda.device(h.device):
         grads = [torch.empty_like(t) if n and t is not None else None
@@ -388,7 +395,7 @@ def bpt_res_norm_bwd(h, b, dy, dr, weight=None, bias=None, norm="layer", post_no
         size = int(lib.bpt_res_norm_bwd_workspace_bytes(ctypes.byref(args)))
         if workspace is None:
             workspace = torch.empty(size, dtype=torch.uint8, device=h.device)
-        _check(lib.bpt_res_norm_bwd(ctypes.byref(args), _ptr(dy), _ptr(dr), *[_ptr(t) for t in grads], _ptr(workspace),
+        _check(lib.bpt_res_norm_bwd(ctypes.byref(args), _ptr(stats), _ptr(dy), _ptr(dr), *[_ptr(t) for t in grads], _ptr(workspace),
                                     workspace.numel(), _stream()), "bpt_res_norm_bwd")
     return tuple(grads)
 

@@ -3,15 +3,18 @@
 //     n = post(b),   r = alpha h + gate n,   y = norm(r),        row by row over D channels,
 // post and norm each absent, layer normalisation or root-mean-square normalisation, and its backward.
 //
-// Both directions are bound by HBM: a row is read once, lives in registers as fp32 (statistics about the mean in a
-// second sweep over the registers), and every result is rounded once to the tensors' type when it is stored.  The
-// backward recomputes n, r and the statistics from h and b instead of reading saved ones.
+// Both directions are bound by HBM: a row is read once, lives in registers as fp32 (variance about the mean, in a
+// second sweep over the registers), and every result is rounded once to the tensors' type when it is stored.  The forward
+// leaves mean and reciprocal deviation of both norms (16 bytes a row) for the backward, which recomputes everything else
+// from h and b.
 //
-// A row belongs to TPR threads, NE channels each: one warp up to 512 (backward) / 1024 (forward) channels, so that
-// the row sums are shuffles, a whole CTA above.  The backward's CTAs each take a fixed, contiguous share of the rows
-// and keep the column sums of the parameter gradients in registers; the shares are added by a second kernel in a
-// fixed order, so results are bit-reproducible.  Backward rows are fetched two rows ahead into shared memory by
-// asynchronous copies; every thread reads back only what it copied itself, so no barrier is needed for them.
+// A row belongs to TPR threads, NE channels each: one warp (in the backward above 256 channels two, whose column sums would
+// not leave registers for enough warps otherwise) as far as registers go, a whole CTA above.  What remains to be bound by is instructions: the arithmetic is written
+// on pairs (fma.rn.f32x2 and the like, two channels an instruction), and weights, biases and gate are turned to fp32 once per
+// CTA and kept in shared memory in the order in which the threads read them.  The backward's CTAs each take a fixed,
+// contiguous share of the rows and keep the column sums of the parameter gradients in registers; the shares are added by
+// a second kernel in a fixed order, so results are bit-reproducible.  Backward rows are fetched two rows ahead into
+// shared memory by asynchronous copies; every thread reads back only what it copied itself, so no barrier is needed for them.
 #include <algorithm>
 
 #include "bpt_internal.cuh"
@@ -23,79 +26,106 @@ namespace {
 constexpr int kRnSms = 148;
 constexpr int kRnMaxD = 8192;
 // Rows of a thread group in flight (the current one and those ahead), as far as shared memory goes; below two there is no staging.
+__host__ __device__ constexpr int cta_threads(int tpr) { return tpr < 128 ? 256 : tpr; }
 template <typename T, int VEC, int NE, int TPR>
 __host__ __device__ constexpr int bwd_stages() {
-    constexpr size_t one = 4 * NE * sizeof(T) * (TPR == 32 ? 256 : TPR);
-    return sizeof(T) * VEC < 4 || 2 * one > 200 * 1024 ? 1 : 3 * one > 200 * 1024 ? 2 : 3;
+    constexpr size_t one = 4 * NE * sizeof(T) * cta_threads(TPR), room = 224 * 1024 - 4 * NE * 4 * TPR;
+    return sizeof(T) * VEC < 4 || 2 * one > room ? 1 : 3 * one > room ? 2 : 3;
 }
 
 struct RnParams {
     const void *h, *b, *dy, *dr;
     const void *weight, *bias, *post_weight, *post_bias, *gate;
     void *y, *r, *dh, *db, *d_gate;
+    float4* stats_out;      // [rows]: mean and 1 / deviation of the post norm, of the norm
+    const float4* stats;
     float *part;            // [grid][4][D]: weight, bias, post weight, post bias
     float *gate_part;       // [units][D]
     long long rows, group_rows;
     int D, norm, post, splits, units;
     bool param_bf16, gate_bf16, gate_rows;   // gate_rows: a gate row per row
+    bool gate_each;         // forward: the gate's row depends on the row (read from memory, not kept in shared memory)
     float alpha, eps;
 };
 
-template <typename T> __device__ __forceinline__ float to_f(T v);
-template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+// Two channels per instruction, kept as 64-bit values so that they stay in register pairs.
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t mk(float x, float y) { pair_t d; asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y)); return d; }
+__device__ __forceinline__ float2 un(pair_t a) { float2 d; asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a)); return d; }
+__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) { pair_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) { pair_t d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) { pair_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ pair_t both(float a) { return mk(a, a); }
+__device__ __forceinline__ float elem(const pair_t* x, int e) { const float2 f = un(x[e / 2]); return e & 1 ? f.y : f.x; }
 
-// VEC consecutive elements of type T <-> fp32
-template <typename T, int VEC>
-__device__ __forceinline__ void unpack(const void* p, float* f) {
+// A thread's NE elements: chunk v is VEC consecutive channels of type T at at(v), or zeros where live(v) is false.
+template <typename T, int VEC, int NE, typename At, typename Live>
+__device__ __forceinline__ void load_row(pair_t* x, At at, Live live) {
     if constexpr (VEC == 1) {
-        f[0] = to_f(*reinterpret_cast<const T*>(p));
-    } else if constexpr (sizeof(T) == 4) {
-        static_assert(VEC == 4, "16 bytes");
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-    } else {
-        static_assert(VEC == 8, "16 bytes");
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        auto one = [&](int v) {
+            if (!live(v)) return 0.f;
+            if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float*>(at(v));
+            else return __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(at(v)));
+        };
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    }
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void pack(void* p, const float* f) {
-    if constexpr (VEC == 1) {
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<float*>(p) = f[0];
-        else *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(f[0]);
-    } else if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+        for (int i = 0; i < NE / 2; ++i) { const float a = one(2 * i), b = one(2 * i + 1); x[i] = mk(a, b); }
     } else {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-    }
-}
-// VEC parameters from channel c on (their type is a run-time choice of the whole grid)
-template <int VEC>
-__device__ __forceinline__ void load_param(const void* p, bool bf16, long long c, float* f) {
-    if constexpr (VEC == 1) {
-        // plain loads: __ldg of a bf16 is inline assembly that the compiler may move above the caller's test for a null pointer
-        if (bf16) f[0] = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[c]);
-        else f[0] = reinterpret_cast<const float*>(p)[c];
-    } else if (bf16) {
-        if constexpr (VEC == 8) {
-            unpack<__nv_bfloat16, 8>(reinterpret_cast<const __nv_bfloat16*>(p) + c, f);
-        } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const __nv_bfloat16*>(p) + c);
-            f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-            f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+#pragma unroll
+        for (int v = 0; v < NE / VEC; ++v) {
+            if constexpr (sizeof(T) == 4) {
+                const ulonglong2 w = live(v) ? *reinterpret_cast<const ulonglong2*>(at(v)) : make_ulonglong2(0, 0);
+                x[v * 2] = w.x;
+                x[v * 2 + 1] = w.y;
+            } else {
+                const uint4 q = live(v) ? *reinterpret_cast<const uint4*>(at(v)) : make_uint4(0, 0, 0, 0);
+                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[v * 4 + i] = mk(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+            }
         }
+    }
+}
+// Chunk v of a thread's elements to p
+template <typename T, int VEC>
+__device__ __forceinline__ void pack(void* p, const pair_t* x, int v) {
+    if constexpr (VEC == 1) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float*>(p) = elem(x, v);
+        else *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(elem(x, v));
+    } else if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(x[v * 2], x[v * 2 + 1]);
     } else {
+        uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < VEC / 4; ++i) unpack<float, 4>(reinterpret_cast<const float*>(p) + c + 4 * i, f + 4 * i);
+        for (int i = 0; i < 4; ++i) { const float2 f = un(x[v * 4 + i]); w[i] = pack_bf16(f.x, f.y); }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+// A parameter of channel c.  Plain loads: __ldg of a bf16 is inline assembly that the compiler may move above a test for a null pointer.
+__device__ __forceinline__ float param(const void* p, bool bf16, long long c) {
+    if (bf16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[c]);
+    return reinterpret_cast<const float*>(p)[c];
+}
+
+// Channel of element e of thread t
+template <int VEC, int TPR>
+__device__ __forceinline__ int channel(int e, int t) { return (e / VEC * TPR + t) * VEC + e % VEC; }
+// One parameter row as fp32 in shared memory, four elements of a thread together; `missing` where there is none, zeros past D.
+template <int VEC, int NE, int TPR, int RPC>
+__device__ __forceinline__ void fill(float4* dst, const void* p, bool bf16, long long off, float missing, int D, int t, int sub) {
+    for (int q = sub; q < NE / 4; q += RPC) {
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = channel<VEC, TPR>(4 * q + i, t);
+            f[i] = c >= D ? 0.f : p ? param(p, bf16, off + c) : missing;
+        }
+        dst[q * TPR + t] = make_float4(f[0], f[1], f[2], f[3]);
     }
 }
 
-// Sum of a pair over the TPR threads of a row, the same bits in every thread.  slots: two buffers of TPR / 32 pairs,
-// used in turn, so that one barrier per sum is enough.
+// Sum of a pair over the TPR threads of a row, the same bits in every thread.  slots: for each row group of the CTA two buffers
+// of TPR / 32 pairs, used in turn, so that one barrier (of the group's threads) per sum is enough.
+template <int TPR> __host__ __device__ constexpr int slot_count() { return TPR > 32 ? cta_threads(TPR) / 16 : 1; }
 template <int TPR>
 __device__ __forceinline__ float2 row_sum2(float2 v, float2* slots, int& turn) {
 #pragma unroll
@@ -104,113 +134,137 @@ __device__ __forceinline__ float2 row_sum2(float2 v, float2* slots, int& turn) {
         v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
     }
     if constexpr (TPR > 32) {
-        float2* s = slots + turn * (TPR / 32);
+        float2* s = slots + (threadIdx.x / TPR * 2 + turn) * (TPR / 32);
         turn ^= 1;
-        if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-        __syncthreads();
+        if ((threadIdx.x & 31) == 0) s[threadIdx.x % TPR >> 5] = v;
+        if constexpr (TPR == cta_threads(TPR)) __syncthreads();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
         v = s[0];
 #pragma unroll
         for (int w = 1; w < TPR / 32; ++w) { v.x += s[w].x; v.y += s[w].y; }
     }
     return v;
 }
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float2* slots, int& turn) {
+    if constexpr (TPR > 32) {
+        return row_sum2<TPR>(make_float2(v, 0.f), slots, turn).x;
+    } else {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+}
 
-// Mean (0 for rms) and reciprocal deviation of the row held in x; channels past D hold zeros and are left out by `live`.
+// Mean (0 for rms) and reciprocal deviation of the row held in x; channels past D hold zeros (live: chunk inside D).
 template <int TPR, int NE, int VEC, typename Live>
-__device__ __forceinline__ float2 row_stats(const float (&x)[NE], int kind, int D, float eps, Live live, float2* slots, int& turn) {
+__device__ __forceinline__ float2 row_stats(const pair_t* x, int kind, float inv_d, float eps, Live live, float2* slots, int& turn) {
     float mean = 0.f;
     if (kind == BPT_NORM_LAYER) {
-        float s = 0.f;
+        pair_t s = 0;
 #pragma unroll
-        for (int i = 0; i < NE; ++i) s += x[i];
-        mean = row_sum2<TPR>(make_float2(s, 0.f), slots, turn).x / (float)D;
+        for (int i = 0; i < NE / 2; ++i) s = add2(s, x[i]);
+        mean = row_sum<TPR>(un(s).x + un(s).y, slots, turn) * inv_d;
     }
-    float q = 0.f;
+    pair_t q = 0;
 #pragma unroll
-    for (int i = 0; i < NE; ++i) {
-        const float c = live(i / VEC) ? x[i] - mean : 0.f;
-        q = fmaf(c, c, q);
+    for (int i = 0; i < NE / 2; ++i) {
+        const pair_t m = VEC == 1 ? mk(live(2 * i) ? -mean : 0.f, live(2 * i + 1) ? -mean : 0.f) : both(live(2 * i / VEC) ? -mean : 0.f);
+        const pair_t c = add2(x[i], m);
+        q = fma2(c, c, q);
     }
-    q = row_sum2<TPR>(make_float2(q, 0.f), slots, turn).x;
-    return make_float2(mean, rsqrtf(q / (float)D + eps));
+    return make_float2(mean, rsqrtf(row_sum<TPR>(un(q).x + un(q).y, slots, turn) * inv_d + eps));
 }
 
 template <typename T, int VEC, int NE, int TPR>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) res_norm_fwd_kernel(const RnParams p) {
-    constexpr int NV = NE / VEC, RPC = TPR == 32 ? 8 : 1;
-    __shared__ float2 slots[TPR > 32 ? 2 * (TPR / 32) : 1];
+__global__ void __launch_bounds__(cta_threads(TPR), NE <= 16 ? 1024 / cta_threads(TPR) : 1) res_norm_fwd_kernel(const RnParams p) {
+    constexpr int NV = NE / VEC, NP = NE / 2, RPC = cta_threads(TPR) / TPR;
+    extern __shared__ __align__(16) float4 prm[];       // [weight, bias, post weight, post bias, gate][NE / 4][TPR]
+    __shared__ float2 slots[slot_count<TPR>()];
     int turn = 0;
-    const int t = threadIdx.x % TPR;
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     const int D = p.D;
+    const float inv_d = 1.f / (float)D;
     auto chan = [&](int v) { return (v * TPR + t) * VEC; };
     auto live = [&](int v) { return chan(v) < D; };
-    for (long long row = (long long)blockIdx.x * RPC + threadIdx.x / TPR; row < p.rows; row += (long long)gridDim.x * RPC) {
+    constexpr int kRow = NE / 4 * TPR;
+    if (p.norm) {
+        fill<VEC, NE, TPR, RPC>(prm, p.weight, p.param_bf16, 0, 1.f, D, t, sub);
+        fill<VEC, NE, TPR, RPC>(prm + kRow, p.bias, p.param_bf16, 0, 0.f, D, t, sub);
+    }
+    if (p.post) {
+        fill<VEC, NE, TPR, RPC>(prm + 2 * kRow, p.post_weight, p.param_bf16, 0, 1.f, D, t, sub);
+        fill<VEC, NE, TPR, RPC>(prm + 3 * kRow, p.post_bias, p.param_bf16, 0, 0.f, D, t, sub);
+    }
+    if (p.gate && !p.gate_each) fill<VEC, NE, TPR, RPC>(prm + 4 * kRow, p.gate, p.gate_bf16, 0, 1.f, D, t, sub);
+    __syncthreads();
+    // pairs 2 q and 2 q + 1 of parameter row k
+    auto get = [&](int k, int q, pair_t* f) {
+        const ulonglong2 w = reinterpret_cast<const ulonglong2*>(prm)[k * kRow + q * TPR + t];
+        f[0] = w.x;
+        f[1] = w.y;
+    };
+    for (long long row = (long long)blockIdx.x * RPC + sub; row < p.rows; row += (long long)gridDim.x * RPC) {
         const long long off = row * D;
-        float n[NE], r[NE];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) n[v * VEC + i] = r[v * VEC + i] = 0.f;
-            if (live(v)) {
-                unpack<T, VEC>(reinterpret_cast<const T*>(p.h) + off + chan(v), &r[v * VEC]);
-                if (p.b) unpack<T, VEC>(reinterpret_cast<const T*>(p.b) + off + chan(v), &n[v * VEC]);
-            }
-        }
+        pair_t n[NP], r[NP];
+        float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
+        load_row<T, VEC, NE>(r, [&](int v) { return reinterpret_cast<const T*>(p.h) + off + chan(v); }, live);
+        load_row<T, VEC, NE>(n, [&](int v) { return reinterpret_cast<const T*>(p.b) + off + chan(v); }, [&](int v) { return p.b && live(v); });
         if (p.post) {
-            const float2 st = row_stats<TPR, NE, VEC>(n, p.post, D, p.eps, live, slots, turn);
+            const float2 s = row_stats<TPR, NE, VEC>(n, p.post, inv_d, p.eps, live, slots, turn);
+            st.x = s.x; st.y = s.y;
+            const pair_t scale = both(s.y), minus = both(-s.x);
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                if (!live(v)) continue;
-                float w[VEC];
+            for (int q = 0; q < NE / 4; ++q) {
+                pair_t w[2], c[2];
+                get(2, q, w);
+                get(3, q, c);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) n[v * VEC + i] = (n[v * VEC + i] - st.x) * st.y;
-                if (p.post_weight) {
-                    load_param<VEC>(p.post_weight, p.param_bf16, chan(v), w);
+                for (int i = 0; i < 2; ++i) n[2 * q + i] = fma2(mul2(add2(n[2 * q + i], minus), scale), w[i], c[i]);
+            }
+        }
+        if (p.gate) {
+            if (p.gate_each) {
+                const long long goff = (row / p.group_rows) * D;
+                auto g = [&](int e) {
+                    const int c = channel<VEC, TPR>(e, t);
+                    return c < D ? param(p.gate, p.gate_bf16, goff + c) : 0.f;
+                };
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) n[v * VEC + i] *= w[i];
-                }
-                if (p.post_bias) {
-                    load_param<VEC>(p.post_bias, p.param_bf16, chan(v), w);
+                for (int i = 0; i < NP; ++i) n[i] = mul2(n[i], mk(g(2 * i), g(2 * i + 1)));
+            } else {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) n[v * VEC + i] += w[i];
+                for (int q = 0; q < NE / 4; ++q) {
+                    pair_t w[2];
+                    get(4, q, w);
+                    n[2 * q] = mul2(n[2 * q], w[0]);
+                    n[2 * q + 1] = mul2(n[2 * q + 1], w[1]);
                 }
             }
         }
-        const long long goff = p.gate ? (row / p.group_rows) * D : 0;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            if (!live(v)) continue;
-            if (p.gate) {
-                float w[VEC];
-                load_param<VEC>(p.gate, p.gate_bf16, goff + chan(v), w);
+        for (int i = 0; i < NP; ++i) r[i] = fma2(both(p.alpha), r[i], n[i]);
+        if (p.r)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) n[v * VEC + i] *= w[i];
-            }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) r[v * VEC + i] = fmaf(p.alpha, r[v * VEC + i], n[v * VEC + i]);
-            if (p.r) pack<T, VEC>(reinterpret_cast<T*>(p.r) + off + chan(v), &r[v * VEC]);
-        }
+            for (int v = 0; v < NV; ++v)
+                if (live(v)) pack<T, VEC>(reinterpret_cast<T*>(p.r) + off + chan(v), r, v);
         if (p.norm) {
-            const float2 st = row_stats<TPR, NE, VEC>(r, p.norm, D, p.eps, live, slots, turn);
+            const float2 s = row_stats<TPR, NE, VEC>(r, p.norm, inv_d, p.eps, live, slots, turn);
+            st.z = s.x; st.w = s.y;
+            const pair_t scale = both(s.y), minus = both(-s.x);
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                if (!live(v)) continue;
-                float w[VEC], y[VEC];
+            for (int q = 0; q < NE / 4; ++q) {
+                pair_t w[2], c[2];
+                get(0, q, w);
+                get(1, q, c);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) y[i] = (r[v * VEC + i] - st.x) * st.y;
-                if (p.weight) {
-                    load_param<VEC>(p.weight, p.param_bf16, chan(v), w);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) y[i] *= w[i];
-                }
-                if (p.bias) {
-                    load_param<VEC>(p.bias, p.param_bf16, chan(v), w);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) y[i] += w[i];
-                }
-                pack<T, VEC>(reinterpret_cast<T*>(p.y) + off + chan(v), y);
+                for (int i = 0; i < 2; ++i) r[2 * q + i] = fma2(mul2(add2(r[2 * q + i], minus), scale), w[i], c[i]);
             }
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (live(v)) pack<T, VEC>(reinterpret_cast<T*>(p.y) + off + chan(v), r, v);
         }
+        if (p.stats_out && t == 0) p.stats_out[row] = st;
     }
 }
 
@@ -223,24 +277,26 @@ __device__ __forceinline__ void stage_copy(uint32_t dst, const void* src) {
 }
 template <int N> __device__ __forceinline__ void stage_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Bytes of shared memory of the backward: the staged pieces, or the exchange of the column sums at the end
+// Shared memory of the backward: four parameter rows, then the staged pieces, or the exchange of the column sums
 template <typename T, int VEC, int NE, int TPR>
 __host__ __device__ constexpr size_t bwd_smem() {
-    constexpr int threads = TPR == 32 ? 256 : TPR;
+    constexpr int threads = cta_threads(TPR);
     constexpr int stages = bwd_stages<T, VEC, NE, TPR>();
     const size_t stage = stages > 1 ? (size_t)stages * 4 * NE * sizeof(T) * threads : 0;
-    const size_t xch = TPR == 32 ? (size_t)8 * NE * 32 * 4 : 0;
-    return stage > xch ? stage : xch;
+    const size_t xch = TPR < threads ? (size_t)threads * NE * 4 : 0;
+    return (size_t)4 * NE * 4 * TPR + (stage > xch ? stage : xch);
 }
 
 template <typename T, int VEC, int NE, int TPR, bool POST>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) res_norm_bwd_kernel(const RnParams p) {
-    constexpr int NV = NE / VEC, THREADS = TPR == 32 ? 256 : TPR, RPC = THREADS / TPR;
+__global__ void __launch_bounds__(cta_threads(TPR), cta_threads(TPR) <= 256 ? 512 / cta_threads(TPR) : 1) res_norm_bwd_kernel(const RnParams p) {
+    constexpr int NV = NE / VEC, NP = NE / 2, THREADS = cta_threads(TPR), RPC = THREADS / TPR;
     constexpr int PIECE = VEC * (int)sizeof(T);
     constexpr int STAGES = bwd_stages<T, VEC, NE, TPR>();
     constexpr bool STAGED = STAGES > 1;
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float2 slots[TPR > 32 ? 2 * (TPR / 32) : 1];
+    extern __shared__ __align__(16) float4 prm[];       // [weight, post weight, post bias, gate][NE / 4][TPR]
+    constexpr int kRow = NE / 4 * TPR;
+    unsigned char* const smem = reinterpret_cast<unsigned char*>(prm + 4 * kRow);
+    __shared__ float2 slots[slot_count<TPR>()];
     int turn = 0;
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     const int D = p.D;
@@ -248,9 +304,9 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) res_norm_bwd_kernel(con
     auto chan = [&](int v) { return (v * TPR + t) * VEC; };
     auto live = [&](int v) { return chan(v) < D; };
     const uint32_t mine = smem_u32(smem) + threadIdx.x * PIECE;
-    const void* src[4] = {p.h, p.b, p.dy, p.dr};
+    const void* src[4] = {p.h, p.b, p.norm ? p.dy : nullptr, p.dr};
     auto slot = [&](int stage, int a, int v) { return (uint32_t)(((stage * 4 + a) * NV + v) * THREADS * PIECE); };
-    auto fetch = [&](long long row, long long end, int stage) {
+    auto fetch = [&](long long row, long long off, long long end, int stage) {     // off: row * D
         if constexpr (STAGED) {
             if (row < end) {
 #pragma unroll
@@ -258,215 +314,228 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) res_norm_bwd_kernel(con
                     if (src[a])
 #pragma unroll
                         for (int v = 0; v < NV; ++v)
-                            if (live(v)) stage_copy<PIECE>(mine + slot(stage, a, v), reinterpret_cast<const T*>(src[a]) + row * D + chan(v));
+                            if (live(v)) stage_copy<PIECE>(mine + slot(stage, a, v), reinterpret_cast<const T*>(src[a]) + off + chan(v));
             }
             cp_async_commit();
         }
     };
-    auto take = [&](long long row, int stage, int a, int v, float* f) {
-        if constexpr (STAGED) unpack<T, VEC>(smem + threadIdx.x * PIECE + slot(stage, a, v), f);
-        else unpack<T, VEC>(reinterpret_cast<const T*>(src[a]) + row * D + chan(v), f);
+    // Staged: what has no source (a missing tensor, channels past D) holds zeros from the start, so every read is unconditional.
+    auto take = [&](long long off, int stage, int a, pair_t* x) {
+        if constexpr (STAGED) load_row<T, VEC, NE>(x, [&](int v) { return smem + threadIdx.x * PIECE + slot(stage, a, v); }, [](int) { return true; });
+        else load_row<T, VEC, NE>(x, [&](int v) { return reinterpret_cast<const T*>(src[a]) + off + chan(v); }, [&](int v) { return src[a] && live(v); });
+    };
+    auto clear_stages = [&] {
+        if constexpr (STAGED)
+#pragma unroll 1
+            for (int stage = 0; stage < STAGES; ++stage)
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+                        if (!src[a] || !live(v))
+#pragma unroll
+                            for (int i = 0; i < PIECE / 4; ++i) *reinterpret_cast<uint32_t*>(smem + threadIdx.x * PIECE + slot(stage, a, v) + 4 * i) = 0;
+    };
+    auto get = [&](int k, int q, pair_t* f) {
+        const ulonglong2 w = reinterpret_cast<const ulonglong2*>(prm)[k * kRow + q * TPR + t];
+        f[0] = w.x;
+        f[1] = w.y;
     };
 
-    float s_w[NE], s_b[NE], s_g[NE], s_pw[POST ? NE : 1], s_pb[POST ? NE : 1];   // this thread's column sums
+    pair_t s_w[NP], s_b[NP], s_g[NP], s_pw[POST ? NP : 1], s_pb[POST ? NP : 1];   // this thread's column sums
 #pragma unroll
-    for (int i = 0; i < NE; ++i) s_w[i] = s_b[i] = s_g[i] = 0.f;
+    for (int i = 0; i < NP; ++i) s_w[i] = s_b[i] = s_g[i] = 0;
     if constexpr (POST) {
 #pragma unroll
-        for (int i = 0; i < NE; ++i) s_pw[i] = s_pb[i] = 0.f;
+        for (int i = 0; i < NP; ++i) s_pw[i] = s_pb[i] = 0;
     }
-    // Adds s over the CTA's thread groups and stores it to out[0 .. D) as fp32 (or bf16): ends with every thread past its reads.
-    auto flush = [&](const float* s, void* out, bool bf16) {
+    // Adds s over the CTA's thread groups and stores it to out[0 .. D) as fp32 (or bf16); barriers before and after.
+    auto flush = [&](const pair_t* s, void* out, bool bf16) {
+        auto put = [&](int c, float a) {
+            if (bf16) reinterpret_cast<__nv_bfloat16*>(out)[c] = __float2bfloat16_rn(a);
+            else reinterpret_cast<float*>(out)[c] = a;
+        };
         if constexpr (RPC > 1) {
             float* x = reinterpret_cast<float*>(smem);
             __syncthreads();
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    if (live(v)) x[sub * (NE * 32) + chan(v) + i] = s[v * VEC + i];
+            for (int e = 0; e < NE; ++e) {
+                const int c = channel<VEC, TPR>(e, t);
+                if (c < D) x[sub * (NE * TPR) + c] = elem(s, e);
+            }
             __syncthreads();
             for (int c = threadIdx.x; c < D; c += THREADS) {
                 float a = 0.f;
 #pragma unroll
-                for (int w = 0; w < RPC; ++w) a += x[w * (NE * 32) + c];
-                if (bf16) reinterpret_cast<__nv_bfloat16*>(out)[c] = __float2bfloat16_rn(a);
-                else reinterpret_cast<float*>(out)[c] = a;
+                for (int w = 0; w < RPC; ++w) a += x[w * (NE * TPR) + c];
+                put(c, a);
             }
             __syncthreads();
         } else {
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    if (live(v)) {
-                        if (bf16) reinterpret_cast<__nv_bfloat16*>(out)[chan(v) + i] = __float2bfloat16_rn(s[v * VEC + i]);
-                        else reinterpret_cast<float*>(out)[chan(v) + i] = s[v * VEC + i];
-                    }
+            for (int e = 0; e < NE; ++e) {
+                const int c = channel<VEC, TPR>(e, t);
+                if (c < D) put(c, elem(s, e));
+            }
         }
     };
 
+    fill<VEC, NE, TPR, RPC>(prm, p.weight, p.param_bf16, 0, 1.f, D, t, sub);
+    if constexpr (POST) {
+        fill<VEC, NE, TPR, RPC>(prm + kRow, p.post_weight, p.param_bf16, 0, 1.f, D, t, sub);
+        fill<VEC, NE, TPR, RPC>(prm + 2 * kRow, p.post_bias, p.param_bf16, 0, 0.f, D, t, sub);
+    }
     for (int unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
         const long long g = unit / p.splits, s = unit % p.splits;
         const long long lo = g * p.group_rows + p.group_rows * s / p.splits, hi = g * p.group_rows + p.group_rows * (s + 1) / p.splits;
-        for (int k = 0; k < STAGES - 1; ++k) fetch(lo + sub + (long long)k * RPC, hi, k);
+        clear_stages();         // the sums of the unit before went through the same memory
+        for (int k = 0; k < STAGES - 1; ++k) fetch(lo + sub + (long long)k * RPC, (lo + sub + (long long)k * RPC) * D, hi, k);
+        __syncthreads();        // the unit before is past its gate
+        if (!p.gate_rows) fill<VEC, NE, TPR, RPC>(prm + 3 * kRow, p.gate, p.gate_bf16, g * D, 1.f, D, t, sub);
+        __syncthreads();
         int stage = 0;
-        for (long long row = lo + sub; row < hi; row += RPC) {
+        const float4 none = make_float4(0.f, 1.f, 0.f, 1.f);
+        float4 st = none, st_next = p.stats && lo + sub < hi ? p.stats[lo + sub] : none;
+        const long long ahead = (long long)(STAGES - 1) * RPC * D;
+        long long off = (lo + sub) * D;
+        for (long long row = lo + sub; row < hi; row += RPC, off += (long long)RPC * D) {
+            st = st_next;
+            if (p.stats && row + RPC < hi) st_next = p.stats[row + RPC];
             if constexpr (STAGED) stage_wait<STAGED ? STAGES - 2 : 0>();
-            const long long off = row * D, goff = p.gate_rows ? off : g * D;
-            float n[NE], x[NE], d[NE];   // n: post(b) before scale and shift; x: r, then norm(r) before scale and shift; d: the running gradient
-            float2 st1 = make_float2(0.f, 1.f), st2 = make_float2(0.f, 1.f);
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) n[v * VEC + i] = x[v * VEC + i] = d[v * VEC + i] = 0.f;
-                if (live(v)) {
-                    take(row, stage, 0, v, &x[v * VEC]);
-                    if (p.b) take(row, stage, 1, v, &n[v * VEC]);
-                }
-            }
+            pair_t n[NP], x[NP], d[NP];   // n: post(b) before scale and shift; x: norm(r) before scale and shift; d: the running gradient
+            take(off, stage, 1, n);
             if constexpr (POST) {
-                st1 = row_stats<TPR, NE, VEC>(n, p.post, D, p.eps, live, slots, turn);
+                const pair_t scale = both(st.y), minus = both(-st.x);
 #pragma unroll
-                for (int v = 0; v < NV; ++v)
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) n[v * VEC + i] = live(v) ? (n[v * VEC + i] - st1.x) * st1.y : 0.f;
+                for (int i = 0; i < NP; ++i) n[i] = mul2(add2(n[i], minus), scale);
             }
-            // the branch as it enters the sum, before the gate
-            auto branch = [&](int v, float* f) {
+            pair_t gate[NP];
+            if (p.gate_rows) {
+                auto w = [&](int e) {
+                    const int c = channel<VEC, TPR>(e, t);
+                    return c < D ? param(p.gate, p.gate_bf16, off + c) : 0.f;
+                };
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) f[i] = n[v * VEC + i];
+                for (int i = 0; i < NP; ++i) gate[i] = mk(w(2 * i), w(2 * i + 1));
+            } else {
+#pragma unroll
+                for (int q = 0; q < NE / 4; ++q) get(3, q, gate + 2 * q);
+            }
+            // the branch as it enters the sum, before the gate: pairs 2 q, 2 q + 1
+            auto branch = [&](int q, pair_t* f) {
+                f[0] = n[2 * q];
+                f[1] = n[2 * q + 1];
                 if constexpr (POST) {
-                    float w[VEC];
-                    if (p.post_weight) {
-                        load_param<VEC>(p.post_weight, p.param_bf16, chan(v), w);
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) f[i] *= w[i];
-                    }
-                    if (p.post_bias) {
-                        load_param<VEC>(p.post_bias, p.param_bf16, chan(v), w);
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) f[i] += w[i];
-                    }
+                    pair_t w[2], c[2];
+                    get(1, q, w);
+                    get(2, q, c);
+                    f[0] = fma2(f[0], w[0], c[0]);
+                    f[1] = fma2(f[1], w[1], c[1]);
                 }
             };
-            if (p.norm && p.dy) {
+            if (src[2]) {
+                take(off, stage, 0, x);
+                take(off, stage, 2, d);
+                const pair_t scale = both(st.w), minus = both(-st.z);
+                pair_t mx = 0, my = 0;
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    if (!live(v)) continue;
-                    float f[VEC];
-                    branch(v, f);
-                    if (p.gate) {
-                        float w[VEC];
-                        load_param<VEC>(p.gate, p.gate_bf16, goff + chan(v), w);
+                for (int q = 0; q < NE / 4; ++q) {
+                    pair_t f[2], w[2];
+                    branch(q, f);
+                    get(0, q, w);
 #pragma unroll
-                        for (int i = 0; i < VEC; ++i) f[i] *= w[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) x[v * VEC + i] = fmaf(p.alpha, x[v * VEC + i], f[i]);
-                }
-                st2 = row_stats<TPR, NE, VEC>(x, p.norm, D, p.eps, live, slots, turn);
-                float2 m = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    if (!live(v)) continue;
-                    float dy[VEC], w[VEC];
-                    take(row, stage, 2, v, dy);
-                    if (p.weight) load_param<VEC>(p.weight, p.param_bf16, chan(v), w);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        const int e = v * VEC + i;
-                        x[e] = (x[e] - st2.x) * st2.y;
-                        s_w[e] = fmaf(dy[i], x[e], s_w[e]);
-                        s_b[e] += dy[i];
-                        d[e] = p.weight ? dy[i] * w[i] : dy[i];
-                        m.x += d[e];
-                        m.y = fmaf(d[e], x[e], m.y);
+                    for (int j = 0; j < 2; ++j) {
+                        const int i = 2 * q + j;
+                        const pair_t r = fma2(both(p.alpha), x[i], mul2(gate[i], f[j]));
+                        x[i] = mul2(add2(r, minus), scale);
+                        s_w[i] = fma2(d[i], x[i], s_w[i]);
+                        s_b[i] = add2(s_b[i], d[i]);
+                        d[i] = mul2(d[i], w[j]);
+                        mx = add2(mx, d[i]);
+                        my = fma2(d[i], x[i], my);
                     }
                 }
-                m = row_sum2<TPR>(m, slots, turn);
-                const float m1 = p.norm == BPT_NORM_LAYER ? m.x * inv_d : 0.f, m2 = m.y * inv_d;
+                const float2 m = row_sum2<TPR>(make_float2(un(mx).x + un(mx).y, un(my).x + un(my).y), slots, turn);
+                const pair_t m1 = both(p.norm == BPT_NORM_LAYER ? -m.x * inv_d : 0.f), m2 = both(-m.y * inv_d);
 #pragma unroll
-                for (int i = 0; i < NE; ++i) d[i] = st2.y * (d[i] - m1 - x[i] * m2);
+                for (int i = 0; i < NP; ++i) d[i] = mul2(scale, add2(d[i], fma2(x[i], m2, m1)));
+                if (src[3]) {
+                    take(off, stage, 3, x);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) d[i] = add2(d[i], x[i]);
+                }
+            } else {
+                take(off, stage, 3, d);
             }
-            float2 m = make_float2(0.f, 0.f);
+            if (p.dh) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                if (!live(v)) continue;
-                float w[VEC];
-                if (p.dr) {
-                    take(row, stage, 3, v, w);
+                for (int i = 0; i < NP; ++i) x[i] = mul2(both(p.alpha), d[i]);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) d[v * VEC + i] += w[i];
-                }
-                if (p.dh) {
+                for (int v = 0; v < NV; ++v)
+                    if (live(v)) pack<T, VEC>(reinterpret_cast<T*>(p.dh) + off + chan(v), x, v);
+            }
+            pair_t mx = 0, my = 0;
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) w[i] = p.alpha * d[v * VEC + i];
-                    pack<T, VEC>(reinterpret_cast<T*>(p.dh) + off + chan(v), w);
-                }
-                if (p.gate) {
-                    float f[VEC];
-                    branch(v, f);
+            for (int q = 0; q < NE / 4; ++q) {
+                pair_t f[2];
+                branch(q, f);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) f[i] *= d[v * VEC + i];
-                    if (p.gate_rows) {
-                        if (p.d_gate) {
-                            if (p.gate_bf16)
-#pragma unroll
-                                for (int i = 0; i < VEC; ++i) reinterpret_cast<__nv_bfloat16*>(p.d_gate)[off + chan(v) + i] = __float2bfloat16_rn(f[i]);
-                            else
-#pragma unroll
-                                for (int i = 0; i < VEC; ++i) reinterpret_cast<float*>(p.d_gate)[off + chan(v) + i] = f[i];
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) s_g[v * VEC + i] += f[i];
-                    }
-                    load_param<VEC>(p.gate, p.gate_bf16, goff + chan(v), w);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) d[v * VEC + i] *= w[i];
+                for (int j = 0; j < 2; ++j) {
+                    const int i = 2 * q + j;
+                    if (p.gate_rows) x[i] = mul2(d[i], f[j]);
+                    else s_g[i] = fma2(d[i], f[j], s_g[i]);
+                    d[i] = mul2(d[i], gate[i]);
                 }
                 if constexpr (POST) {
-                    if (p.post_weight) load_param<VEC>(p.post_weight, p.param_bf16, chan(v), w);
+                    pair_t w[2];
+                    get(1, q, w);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        const int e = v * VEC + i;
-                        s_pw[e] = fmaf(d[e], n[e], s_pw[e]);
-                        s_pb[e] += d[e];
-                        if (p.post_weight) d[e] *= w[i];
-                        m.x += d[e];
-                        m.y = fmaf(d[e], n[e], m.y);
+                    for (int j = 0; j < 2; ++j) {
+                        const int i = 2 * q + j;
+                        s_pw[i] = fma2(d[i], n[i], s_pw[i]);
+                        s_pb[i] = add2(s_pb[i], d[i]);
+                        d[i] = mul2(d[i], w[j]);
+                        mx = add2(mx, d[i]);
+                        my = fma2(d[i], n[i], my);
                     }
-                } else if (p.db) {
-                    pack<T, VEC>(reinterpret_cast<T*>(p.db) + off + chan(v), &d[v * VEC]);
+                }
+            }
+            if (p.gate_rows && p.d_gate) {
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                    const int c = channel<VEC, TPR>(e, t);
+                    const float a = elem(x, e);
+                    if (c >= D) continue;
+                    if (p.gate_bf16) reinterpret_cast<__nv_bfloat16*>(p.d_gate)[off + c] = __float2bfloat16_rn(a);
+                    else reinterpret_cast<float*>(p.d_gate)[off + c] = a;
                 }
             }
             if constexpr (POST) {
-                m = row_sum2<TPR>(m, slots, turn);
-                const float m1 = p.post == BPT_NORM_LAYER ? m.x * inv_d : 0.f, m2 = m.y * inv_d;
+                const float2 m = row_sum2<TPR>(make_float2(un(mx).x + un(mx).y, un(my).x + un(my).y), slots, turn);
+                const pair_t scale = both(st.y), m1 = both(p.post == BPT_NORM_LAYER ? -m.x * inv_d : 0.f), m2 = both(-m.y * inv_d);
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    if (!live(v) || !p.db) continue;
-                    float w[VEC];
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) w[i] = st1.y * (d[v * VEC + i] - m1 - n[v * VEC + i] * m2);
-                    pack<T, VEC>(reinterpret_cast<T*>(p.db) + off + chan(v), w);
-                }
+                for (int i = 0; i < NP; ++i) d[i] = mul2(scale, add2(d[i], fma2(n[i], m2, m1)));
             }
-            fetch(row + (long long)(STAGES - 1) * RPC, hi, (stage + STAGES - 1) % STAGES);
-            stage = (stage + 1) % STAGES;
+            if (p.db)
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    if (live(v)) pack<T, VEC>(reinterpret_cast<T*>(p.db) + off + chan(v), d, v);
+            fetch(row + (STAGES - 1) * RPC, off + ahead, hi, stage == 0 ? STAGES - 1 : stage - 1);
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
         if constexpr (STAGED) stage_wait<0>();
         if (p.d_gate && !p.gate_rows) {
             if (p.splits == 1) flush(s_g, reinterpret_cast<char*>(p.d_gate) + g * D * (p.gate_bf16 ? 2 : 4), p.gate_bf16);
             else flush(s_g, p.gate_part + (long long)unit * D, false);
 #pragma unroll
-            for (int i = 0; i < NE; ++i) s_g[i] = 0.f;
+            for (int i = 0; i < NP; ++i) s_g[i] = 0;
         }
     }
     float* part = p.part + (long long)blockIdx.x * 4 * D;
-    flush(s_w, part, false);
-    flush(s_b, part + D, false);
+    if (p.norm) {
+        flush(s_w, part, false);
+        flush(s_b, part + D, false);
+    }
     if constexpr (POST) {
         flush(s_pw, part + 2 * D, false);
         flush(s_pb, part + 3 * D, false);
@@ -513,12 +582,12 @@ __global__ void __launch_bounds__(256) res_norm_finish_kernel(const RnFinish f) 
 struct RnPlan { int grid, splits, units; long long groups, group_rows; bool gate_rows; };
 RnPlan plan_bwd(const bpt_res_norm_args& a) {
     RnPlan q{};
-    const int rpc = a.D <= 512 ? 8 : 1;
+    const int rpc = a.D <= 256 ? 8 : a.D <= 512 ? 4 : 1;
     q.gate_rows = a.gate && a.gate_groups == a.rows && a.rows > 1;
     q.groups = a.gate && !q.gate_rows ? a.gate_groups : 1;
     q.group_rows = q.groups ? a.rows / q.groups : 0;
     const long long per_group = (q.group_rows + rpc - 1) / rpc;   // no split smaller than one pass of the CTA's warps
-    const long long cap = kRnSms * (a.D <= 256 ? 2 : a.D <= 512 ? 1 : a.D <= 1024 ? 4 : a.D <= 2048 ? 2 : 1);   // CTAs that fit by registers
+    const long long cap = kRnSms * (a.D <= 512 ? 2 : a.D <= 1024 ? 4 : a.D <= 2048 ? 2 : 1);   // CTAs that fit by registers
     q.splits = (int)std::max<long long>(1, std::min<long long>(per_group, cap / std::max<long long>(1, q.groups)));
     q.units = (int)std::min<long long>(q.groups * q.splits, 0x7fffffff);
     q.grid = (int)std::min<long long>(q.units, cap);
@@ -561,9 +630,14 @@ bool element_aligned(std::initializer_list<const void*> ptrs, bpt_dtype t) {
 
 template <typename T, int VEC, int NE, int TPR>
 bpt_status run_fwd(const RnParams& p, cudaStream_t st) {
-    constexpr int rpc = TPR == 32 ? 8 : 1;
-    const long long grid = std::min<long long>((p.rows + rpc - 1) / rpc, kRnSms * 16);
-    res_norm_fwd_kernel<T, VEC, NE, TPR><<<(unsigned)grid, TPR == 32 ? 256 : TPR, 0, st>>>(p);
+    constexpr int threads = cta_threads(TPR), rpc = threads / TPR;
+    constexpr size_t smem = (size_t)5 * NE * 4 * TPR;
+    if (smem > 32 * 1024 &&     // with the static part, 48 KB is the limit without asking
+        cudaFuncSetAttribute(res_norm_fwd_kernel<T, VEC, NE, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        return BPT_ERR_CUDA;
+    // as many CTAs as run at once: each turns the parameters to fp32 once
+    const long long grid = std::min<long long>((p.rows + rpc - 1) / rpc, kRnSms * std::max(1, 1024 / threads));
+    res_norm_fwd_kernel<T, VEC, NE, TPR><<<(unsigned)grid, threads, smem, st>>>(p);
     return cudaGetLastError() == cudaSuccess ? BPT_OK : BPT_ERR_CUDA;
 }
 template <typename T, int VEC>
@@ -582,7 +656,7 @@ bpt_status run_bwd(const RnParams& p, int grid, cudaStream_t st) {
     if (smem > 32 * 1024 &&   // with the static part, 48 KB is the limit without asking
         cudaFuncSetAttribute(res_norm_bwd_kernel<T, VEC, NE, TPR, POST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
         return BPT_ERR_CUDA;
-    res_norm_bwd_kernel<T, VEC, NE, TPR, POST><<<grid, TPR == 32 ? 256 : TPR, smem, st>>>(p);
+    res_norm_bwd_kernel<T, VEC, NE, TPR, POST><<<grid, cta_threads(TPR), smem, st>>>(p);
     return cudaGetLastError() == cudaSuccess ? BPT_OK : BPT_ERR_CUDA;
 }
 template <typename T, int VEC, int NE, int TPR>
@@ -592,7 +666,7 @@ bpt_status run_bwd(const RnParams& p, int grid, cudaStream_t st) {
 template <typename T, int VEC>
 bpt_status pick_bwd(const RnParams& p, int grid, cudaStream_t st) {
     if (p.D <= 256) return run_bwd<T, VEC, 8, 32>(p, grid, st);
-    if (p.D <= 512) return run_bwd<T, VEC, 16, 32>(p, grid, st);
+    if (p.D <= 512) return run_bwd<T, VEC, 8, 64>(p, grid, st);
     if (p.D <= 1024) return run_bwd<T, VEC, 8, 128>(p, grid, st);
     if (p.D <= 2048) return run_bwd<T, VEC, 8, 256>(p, grid, st);
     if (p.D <= 4096) return run_bwd<T, VEC, 8, 512>(p, grid, st);
@@ -604,21 +678,22 @@ bpt_status pick_bwd(const RnParams& p, int grid, cudaStream_t st) {
 
 using namespace bpt;
 
-extern "C" bpt_status bpt_res_norm_fwd(const bpt_res_norm_args* a, void* y, void* r, void* cuda_stream) {
+extern "C" bpt_status bpt_res_norm_fwd(const bpt_res_norm_args* a, void* y, void* r, float* stats, void* cuda_stream) {
     const bpt_status s = check_res_norm(a);
     if (s != BPT_OK) return s;
     if (a->rows == 0) return BPT_OK;
     if ((a->norm != BPT_NORM_NONE) != (y != nullptr) || (!y && !r)) return BPT_ERR_INVALID_ARG;
     if (!a->h) return BPT_ERR_INVALID_ARG;
+    if (!aligned16({stats})) return BPT_ERR_INVALID_ARG;
     if (!element_aligned({a->h, a->b, y, r}, a->dtype) || !element_aligned({a->weight, a->bias, a->post_weight, a->post_bias}, a->param_dtype) ||
         !element_aligned({a->gate}, a->gate_dtype))
         return BPT_ERR_INVALID_ARG;
     RnParams p = make_params(*a);
-    p.y = y; p.r = r;
+    p.y = y; p.r = r; p.stats_out = reinterpret_cast<float4*>(stats);
+    p.gate_each = a->gate && a->gate_groups > 1;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     // 16-byte accesses need whole 16-byte pieces per row; other widths and addresses go element by element
-    const bool vec = a->D % (a->dtype == BPT_F32 ? 4 : 8) == 0 &&
-                     aligned16({a->h, a->b, y, r, a->weight, a->bias, a->post_weight, a->post_bias, a->gate});
+    const bool vec = a->D % (a->dtype == BPT_F32 ? 4 : 8) == 0 && aligned16({a->h, a->b, y, r});
     bpt_status e;
     if (a->dtype == BPT_F32) e = vec ? pick_fwd<float, 4>(p, st) : pick_fwd<float, 1>(p, st);
     else e = vec ? pick_fwd<__nv_bfloat16, 8>(p, st) : pick_fwd<__nv_bfloat16, 1>(p, st);
@@ -632,7 +707,7 @@ extern "C" size_t bpt_res_norm_bwd_workspace_bytes(const bpt_res_norm_args* a) {
     return ((size_t)q.grid * 4 + (a->gate && !q.gate_rows && q.splits > 1 ? (size_t)q.units : 0)) * a->D * 4;
 }
 
-extern "C" bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* a, const void* dy, const void* dr, void* dh, void* db, void* d_weight,
+extern "C" bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* a, const float* stats, const void* dy, const void* dr, void* dh, void* db, void* d_weight,
                                        void* d_bias, void* d_post_weight, void* d_post_bias, void* d_gate, void* workspace,
                                        size_t workspace_bytes, void* cuda_stream) {
     const bpt_status s = check_res_norm(a);
@@ -640,7 +715,7 @@ extern "C" bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* a, const void* d
     if ((dy && !a->norm) || (db && !a->b) || (d_weight && !a->weight) || (d_bias && !a->bias) || (d_post_weight && !a->post_weight) ||
         (d_post_bias && !a->post_bias) || (d_gate && !a->gate))
         return BPT_ERR_INVALID_ARG;
-    if (a->rows > 0 && !a->h) return BPT_ERR_INVALID_ARG;
+    if (a->rows > 0 && (!a->h || (!stats && (a->norm || a->post_norm)) || !aligned16({stats}))) return BPT_ERR_INVALID_ARG;
     if (!element_aligned({a->h, a->b, dy, dr, dh, db}, a->dtype) ||
         !element_aligned({a->weight, a->bias, a->post_weight, a->post_bias, d_weight, d_bias, d_post_weight, d_post_bias}, a->param_dtype) ||
         !element_aligned({a->gate, d_gate}, a->gate_dtype))
@@ -649,14 +724,14 @@ extern "C" bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* a, const void* d
     if ((uintptr_t)workspace & 15) return BPT_ERR_INVALID_ARG;
     const RnPlan q = plan_bwd(*a);
     RnParams p = make_params(*a);
+    p.stats = reinterpret_cast<const float4*>(stats);
     p.dy = dy; p.dr = dr; p.dh = dh; p.db = db; p.d_gate = d_gate;
     p.part = static_cast<float*>(workspace);
     p.gate_part = p.part + (size_t)q.grid * 4 * a->D;
     p.splits = q.splits; p.units = q.units; p.gate_rows = q.gate_rows;
     p.group_rows = q.group_rows;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const bool vec = a->D % (a->dtype == BPT_F32 ? 4 : 8) == 0 &&
-                     aligned16({a->h, a->b, dy, dr, dh, db, a->weight, a->bias, a->post_weight, a->post_bias, a->gate});
+    const bool vec = a->D % (a->dtype == BPT_F32 ? 4 : 8) == 0 && aligned16({a->h, a->b, dy, dr, dh, db});
     if (a->rows > 0) {
         bpt_status e;
         if (a->dtype == BPT_F32) e = vec ? pick_bwd<float, 4>(p, q.grid, st) : pick_bwd<float, 1>(p, q.grid, st);

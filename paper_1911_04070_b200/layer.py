@@ -58,8 +58,9 @@ def graph_self_attention(g: binding.Graph, q, k, v, rel_emb, scale=None, lengths
 class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, h, b, weight, bias, post_weight, post_bias, gate, norm, post_norm, alpha, eps, want_sum):
-        y, r = binding.bpt_res_norm_fwd(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps, want_sum)
-        ctx.save_for_backward(h, b, weight, bias, post_weight, post_bias, gate)
+        stats = h.new_empty((h.numel() // max(h.shape[-1], 1), 4), dtype=torch.float32)
+        y, r = binding.bpt_res_norm_fwd(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps, want_sum, stats=stats)
+        ctx.save_for_backward(h, b, weight, bias, post_weight, post_bias, gate, stats)
         ctx.cfg = (norm, post_norm, alpha, eps)
         ctx.set_materialize_grads(False)
         return (r, y) if y is not None and r is not None else r if y is None else y
@@ -67,13 +68,13 @@ class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, *grads):
-        h, b, weight, bias, post_weight, post_bias, gate = ctx.saved_tensors
+        h, b, weight, bias, post_weight, post_bias, gate, stats = ctx.saved_tensors
         norm, post_norm, alpha, eps = ctx.cfg
         dr, dy = grads if len(grads) == 2 else (grads[0], None) if norm is None else (None, grads[0])
         if dr is None and dy is None:
             return (None,) * 12
         dr, dy = (None if t is None else t.contiguous() for t in (dr, dy))
-        return binding.bpt_res_norm_bwd(h, b, dy, dr, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps,
+        return binding.bpt_res_norm_bwd(h, b, dy, dr, stats, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps,
                                         need=ctx.needs_input_grad[:7]) + (None,) * 5
 
 

@@ -297,5 +297,10 @@ def test_python_refusals():
         f(torch.zeros(2, 8200, device="cuda:0"))
     assert ei.value.status == 2
     with pytest.raises(binding.BptError) as ei:
-        binding.bpt_res_norm_bwd(h, h, h, None, workspace=torch.empty(16, dtype=torch.uint8, device="cuda:0"))
+        binding.bpt_res_norm_bwd(h, h, h, None, torch.zeros(4, 4, device="cuda:0"), workspace=torch.empty(16, dtype=torch.uint8, device="cuda:0"))
     assert ei.value.status == 3
+    with pytest.raises(ValueError):
+        binding.bpt_res_norm_bwd(h, h, h, None, torch.zeros(4, 3, device="cuda:0"))
+    with pytest.raises(binding.BptError) as ei:
+        binding.bpt_res_norm_bwd(h, h, h, None, None)
+    assert ei.value.status == 1

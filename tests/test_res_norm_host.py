@@ -31,19 +31,21 @@ def _args(**kw):
 def test_refusals(lib, kw, status):
     a = _args(**kw)
     y = None if kw.get("norm") == 0 else 8192
-    assert lib.bpt_res_norm_fwd(ctypes.byref(a), y, 8192, None) == status
-    assert lib.bpt_res_norm_bwd(ctypes.byref(a), None, None, 8192, None, None, None, None, None, None, 8192, 1 << 30, None) == status
+    assert lib.bpt_res_norm_fwd(ctypes.byref(a), y, 8192, None, None) == status
+    assert lib.bpt_res_norm_bwd(ctypes.byref(a), 8192, None, None, 8192, None, None, None, None, None, None, 8192, 1 << 30, None) == status
 
 
 def test_more_refusals(lib):
     a = _args()
-    assert lib.bpt_res_norm_fwd(None, 8192, None, None) == 1
-    assert lib.bpt_res_norm_fwd(ctypes.byref(a), None, 8192, None) == 1                    # a norm without y
-    assert lib.bpt_res_norm_fwd(ctypes.byref(_args(norm=0)), 8192, 8192, None) == 1        # y without a norm
-    assert lib.bpt_res_norm_fwd(ctypes.byref(_args(norm=0)), None, None, None) == 1
-    bwd = lambda a, dy=8192, ws=8192, n=1 << 30, **o: lib.bpt_res_norm_bwd(
-        ctypes.byref(a), dy, None, *[o.get(k) for k in ("dh", "db", "dw", "dc", "dpw", "dpc", "dg")], ws, n, None)
+    assert lib.bpt_res_norm_fwd(None, 8192, None, None, None) == 1
+    assert lib.bpt_res_norm_fwd(ctypes.byref(a), None, 8192, None, None) == 1                    # a norm without y
+    assert lib.bpt_res_norm_fwd(ctypes.byref(_args(norm=0)), 8192, 8192, None, None) == 1        # y without a norm
+    assert lib.bpt_res_norm_fwd(ctypes.byref(_args(norm=0)), None, None, None, None) == 1
+    assert lib.bpt_res_norm_fwd(ctypes.byref(a), 8192, None, 8200, None) == 1              # stats off its boundary
+    bwd = lambda a, dy=8192, ws=8192, n=1 << 30, stats=8192, **o: lib.bpt_res_norm_bwd(
+        ctypes.byref(a), stats, dy, None, *[o.get(k) for k in ("dh", "db", "dw", "dc", "dpw", "dpc", "dg")], ws, n, None)
     assert bwd(a, ws=None) == 3 and bwd(a, n=0) == 3 and bwd(a, ws=8200) == 1
+    assert bwd(a, stats=None) == 1 and bwd(a, stats=8196) == 1
     assert bwd(_args(norm=0)) == 1                                                         # dy without a norm
     assert bwd(_args(b=None), db=8192) == 1 and bwd(a, dw=8192) == 1 and bwd(a, dpc=8192) == 1 and bwd(a, dg=8192) == 1
 

@@ -6,6 +6,7 @@ library or a failing call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -20,6 +21,7 @@ BPT_F32, BPT_BF16 = 0, 1
 BPT_PATH_AUTO, BPT_PATH_MMA, BPT_PATH_TC5 = 0, 1, 2
 NORM_KINDS = {None: 0, "layer": 1, "rms": 2}   # BPT_NORM_*
 ACTIVATIONS = {"relu": 0, "silu": 1, "gelu": 2}        # BPT_ACT_*
+GATED_FF_FEW_ROWS = 64   # BPT_GATED_FF_FEW_ROWS: forward calls of at most so many rows hold no device-side wait
 
 EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes", "bpt_attn_fwd",
            "bpt_attn_bwd", "bpt_status_str", "bpt_trace_begin", "bpt_trace_end",
@@ -155,6 +157,18 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+# The position-wise operators are called for single tokens, where what surrounds the library call is most of the time: the
+# current stream and device are read through torch's C functions (0.1 us against 3.2 and 1.5 us), and the device is
+# switched only where it is another one.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _on_device(index: int):
+    return _SAME_DEVICE if _current_device() == index else torch.cuda.device(index)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -255,34 +269,45 @@ def bpt_gated_ff_workspace_bytes(rows: int, D: int, F: int, backward: bool) -> i
 def _check_gated_ff(x, w_gate, w_up, w_down, act, *like_x):
     if act not in ACTIVATIONS:
         raise ValueError("act must be one of %s" % ", ".join(map(repr, ACTIVATIONS)))
-    if x.dtype != torch.bfloat16:
-        raise TypeError("only bfloat16 tensors are supported, got %s" % x.dtype)
-    if not x.is_cuda or x.dim() < 1 or not x.is_contiguous():
+    dt, dev, shape = x.dtype, x.get_device(), x.shape
+    if dt != torch.bfloat16:
+        raise TypeError("only bfloat16 tensors are supported, got %s" % dt)
+    if dev < 0 or not shape or not x.is_contiguous():
         raise ValueError("x must be a contiguous CUDA tensor [..., D]")
-    D = x.shape[-1]
+    D = shape[-1]
     F = w_gate.shape[0] if w_gate.dim() == 2 else 0
-    for t, shape in ((w_gate, (F, D)), (w_up, (F, D)), (w_down, (D, F))):
-        if t.shape != shape or t.dtype != x.dtype or t.device != x.device or not t.is_contiguous():
+    for t, want in ((w_gate, (F, D)), (w_up, (F, D)), (w_down, (D, F))):
+        if t.shape != want or t.dtype != dt or t.get_device() != dev or not t.is_contiguous():
             raise ValueError("w_gate and w_up must be [F, D], w_down [D, F], contiguous, with the dtype and device of x")
     for t in like_x:
-        if t is not None and (t.shape != x.shape or t.dtype != x.dtype or t.device != x.device or not t.is_contiguous()):
+        if t is not None and (t.shape != shape or t.dtype != dt or t.get_device() != dev or not t.is_contiguous()):
             raise ValueError("y, dy and dx must be contiguous and share shape, dtype and device with x")
-    return x.numel() // D if D else 0, D, F
+    return x.numel() // D if D else 0, D, F, dev
+
+
+def _scratch(workspace, size, like):
+    if workspace is None:
+        return like.new_empty(size, dtype=torch.uint8)
+    if workspace.dtype != torch.uint8 or workspace.get_device() != like.get_device() or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the device of the inputs")
+    return workspace
 
 
 def bpt_gated_ff_fwd(x, w_gate, w_up, w_down, act: str = "silu", y=None, workspace=None):
     """y = (act(x @ w_gate.T) * (x @ w_up.T)) @ w_down.T over the last axis: both projections, activation and product in
     one kernel, the second product in another.  x: [..., D] bfloat16 contiguous; w_gate, w_up: [F, D]; w_down: [D, F]; D and F
-    multiples of 8.  The call's status block stays reachable as `y._bpt_workspace` for bpt_check (the workspace does not)."""
-    rows, D, F = _check_gated_ff(x, w_gate, w_up, w_down, act, y)
+    multiples of 8.  The call's status block stays reachable as `y._bpt_workspace` for bpt_check (the workspace does not);
+    None for the few rows of a decoding step, whose kernels wait for nothing."""
+    rows, D, F, dev = _check_gated_ff(x, w_gate, w_up, w_down, act, y)
     lib = load_library()
-    with torch.cuda.device(x.device):
+    with _on_device(dev):
         y = torch.empty_like(x) if y is None else y
-        if workspace is None:
-            workspace = torch.empty(lib.bpt_gated_ff_workspace_bytes(rows, D, F, 0), dtype=torch.uint8, device=x.device)
-        y._bpt_workspace = status = torch.empty(256, dtype=torch.uint8, device=x.device)
+        workspace = _scratch(workspace, lib.bpt_gated_ff_workspace_bytes(rows, D, F, 0), x)
+        status = x.new_empty(256, dtype=torch.uint8) if rows > GATED_FF_FEW_ROWS else None
+        y._bpt_workspace = status
         _check(lib.bpt_gated_ff_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y.data_ptr(), rows, D, F,
-                                    ACTIVATIONS[act], status.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()), "bpt_gated_ff_fwd")
+                                    ACTIVATIONS[act], _ptr(status), workspace.data_ptr(), workspace.numel(), _raw_stream(dev)),
+               "bpt_gated_ff_fwd")
     return y
 
 
@@ -291,76 +316,78 @@ def bpt_gated_ff_bwd(x, w_gate, w_up, w_down, dy, act: str = "silu", dx=None, dw
     """Gradients of bpt_gated_ff_fwd from its inputs and dy: (dx, dw_gate, dw_up, dw_down), bfloat16; None where not needed (the
     three weight gradients together).  Bit-reproducible.  The call's status block stays reachable as `_bpt_workspace` of
     the first gradient for bpt_check."""
-    rows, D, F = _check_gated_ff(x, w_gate, w_up, w_down, act, dy, dx)
+    rows, D, F, dev = _check_gated_ff(x, w_gate, w_up, w_down, act, dy, dx)
     if not (need_dx or need_dw):
         raise ValueError("no gradient was asked for")
     for t, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)):
-        if t is not None and (t.shape != w.shape or t.dtype != w.dtype or t.device != w.device or not t.is_contiguous()):
+        if t is not None and (t.shape != w.shape or t.dtype != w.dtype or t.get_device() != dev or not t.is_contiguous()):
             raise ValueError("weight gradients must be contiguous and share shape, dtype and device with their weights")
     lib = load_library()
-    with torch.cuda.device(x.device):
-        if need_dx:
-            dx = torch.empty_like(x) if dx is None else dx
-        if need_dw:
-            dw_gate, dw_up, dw_down = (torch.empty_like(w) if t is None else t for t, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)))
-        if workspace is None:
-            workspace = torch.empty(lib.bpt_gated_ff_workspace_bytes(rows, D, F, 1), dtype=torch.uint8, device=x.device)
-        status = torch.empty(256, dtype=torch.uint8, device=x.device)
-        (dx if need_dx else dw_gate)._bpt_workspace = status
-        _check(lib.bpt_gated_ff_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(),
-                                    _ptr(dx) if need_dx else None, *[_ptr(t) if need_dw else None for t in (dw_gate, dw_up, dw_down)], rows, D, F,
-                                    ACTIVATIONS[act], status.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()), "bpt_gated_ff_bwd")
-    return (dx if need_dx else None,) + ((dw_gate, dw_up, dw_down) if need_dw else (None,) * 3)
+    with _on_device(dev):
+        dx = (torch.empty_like(x) if dx is None else dx) if need_dx else None
+        dws = [(torch.empty_like(w) if t is None else t) if need_dw else None
+               for t, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down))]
+        workspace = _scratch(workspace, lib.bpt_gated_ff_workspace_bytes(rows, D, F, 1), x)
+        status = x.new_empty(256, dtype=torch.uint8)
+        (dx if need_dx else dws[0])._bpt_workspace = status
+        _check(lib.bpt_gated_ff_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dy.data_ptr(), _ptr(dx),
+                                    *map(_ptr, dws), rows, D, F, ACTIVATIONS[act], status.data_ptr(), workspace.data_ptr(),
+                                    workspace.numel(), _raw_stream(dev)), "bpt_gated_ff_bwd")
+    return (dx, *dws)
 
 
 def _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps):
     """Checks the tensors of a bpt_res_norm call and fills its argument struct."""
     code = _dtype_code(h)
-    if not h.is_cuda or not h.is_contiguous() or h.dim() < 1:
+    dt, dev, shape = h.dtype, h.get_device(), h.shape
+    if dev < 0 or not shape or not h.is_contiguous():
         raise ValueError("h must be a contiguous CUDA tensor [..., D]")
-    shape, dev = h.shape, h.device
     D = shape[-1]
-    if b is not None and (b.shape != shape or b.dtype != h.dtype or b.device != dev or not b.is_contiguous()):
-        raise ValueError("b must be contiguous and share shape, dtype and device with h")
     if norm not in NORM_KINDS or post_norm not in NORM_KINDS:
         raise ValueError("norm and post_norm must be None, 'layer' or 'rms'")
-    if b is None and (post_norm is not None or gate is not None):
-        raise ValueError("post_norm and gate belong to b, which is missing")
+    if b is None:
+        if post_norm is not None or gate is not None:
+            raise ValueError("post_norm and gate belong to b, which is missing")
+    elif b.shape != shape or b.dtype != dt or b.get_device() != dev or not b.is_contiguous():
+        raise ValueError("b must be contiguous and share shape, dtype and device with h")
     if (norm is None and (weight is not None or bias is not None)) or (post_norm is None and (post_weight is not None or post_bias is not None)):
         raise ValueError("a weight or bias was given for a norm that is None")
-    pt = None
+    pt, ptrs = None, []
     for t in (weight, bias, post_weight, post_bias):
-        if t is not None:
-            pt = t.dtype if pt is None else pt
-            if t.shape != (D,) or t.dtype != pt or t.device != dev or not t.is_contiguous():
-                raise ValueError("weights and biases must be contiguous [D] tensors of one dtype on the device of h")
-            pcode = _dtype_code(t)
-    groups = 0
+        if t is None:
+            ptrs.append(None)
+            continue
+        pt = t.dtype if pt is None else pt
+        if t.shape != (D,) or t.dtype != pt or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError("weights and biases must be contiguous [D] tensors of one dtype on the device of h")
+        pcode = _dtype_code(t)
+        ptrs.append(t.data_ptr())
+    groups = 1
     if gate is not None:
         # the gate's rows: a leading part of h's axes, the others of length one (or missing in front: a gate [D])
-        gs = (1,) * (h.dim() - gate.dim()) + tuple(gate.shape)
-        lead = h.dim() - 1
+        gs = (1,) * (len(shape) - gate.dim()) + tuple(gate.shape)
+        lead = len(shape) - 1
         while lead > 0 and gs[lead - 1] == 1:
             lead -= 1
-        if len(gs) != h.dim() or gs[-1] != D or gs[:lead] != tuple(shape[:lead]) or gate.device != dev or not gate.is_contiguous():
+        if len(gs) != len(shape) or gs[-1] != D or gs[:lead] != tuple(shape[:lead]) or gate.get_device() != dev or not gate.is_contiguous():
             raise ValueError("gate must be contiguous, [D] or h's shape with the trailing row axes of length one, on the device of h")
-        groups = 1
         for x in gs[:lead]:
             groups *= x
     rows = h.numel() // D if D else 0
     return ResNormArgs(rows, max(groups, 1), D, code, code if pt is None else pcode, code if gate is None else _dtype_code(gate),
-                       NORM_KINDS[norm], NORM_KINDS[post_norm], alpha, eps, h.data_ptr(), _ptr(b), _ptr(weight), _ptr(bias),
-                       _ptr(post_weight), _ptr(post_bias), _ptr(gate))
+                       NORM_KINDS[norm], NORM_KINDS[post_norm], alpha, eps, h.data_ptr(), None if b is None else b.data_ptr(), *ptrs,
+                       None if gate is None else gate.data_ptr()), dev
 
 
 def _check_like(h, *ts):
     for t in ts:
-        if t is not None and (t.shape != h.shape or t.dtype != h.dtype or t.device != h.device or not t.is_contiguous()):
+        if t is not None and (t.shape != h.shape or t.dtype != h.dtype or t.get_device() != h.get_device() or not t.is_contiguous()):
             raise ValueError("results and gradients must be contiguous and share shape, dtype and device with h")
 
 
 def _check_stats(rows, h, stats):
-    if stats is not None and (stats.dtype != torch.float32 or stats.shape != (rows, 4) or stats.device != h.device or not stats.is_contiguous()):
+    if stats is not None and (stats.dtype != torch.float32 or stats.shape != (rows, 4) or stats.get_device() != h.get_device()
+                              or not stats.is_contiguous()):
         raise ValueError("stats must be a contiguous float32 tensor [rows, 4] on the device of h")
 
 
@@ -370,13 +397,13 @@ def bpt_res_norm_fwd(h, b=None, weight=None, bias=None, norm="layer", post_norm=
     bfloat16, contiguous; norm / post_norm: None, "layer" or "rms" with weights and biases [D]; gate: [D], or h's shape with
     the trailing row axes of length one (one gate row per sequence, per row ...).  Returns (y, r); y is None without a norm,
     r is None unless want_sum (or norm is None).  stats: a float32 tensor [rows, 4] to fill for the backward, or None."""
-    args = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
+    args, dev = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
     _check_like(h, y, r)
     _check_stats(args.rows, h, stats)
-    with torch.cuda.device(h.device):
+    with _on_device(dev):
         y = torch.empty_like(h) if y is None and norm is not None else y
         r = torch.empty_like(h) if r is None and (want_sum or norm is None) else r
-        _check(load_library().bpt_res_norm_fwd(ctypes.byref(args), _ptr(y), _ptr(r), _ptr(stats), _stream()), "bpt_res_norm_fwd")
+        _check(load_library().bpt_res_norm_fwd(ctypes.byref(args), _ptr(y), _ptr(r), _ptr(stats), _raw_stream(dev)), "bpt_res_norm_fwd")
     return y, r
 
 
@@ -385,18 +412,16 @@ def bpt_res_norm_bwd(h, b, dy, dr, stats, weight=None, bias=None, norm="layer", 
     """Backward of bpt_res_norm_fwd from its inputs, its stats and the gradients of y and r (either may be None: zero).  Returns
     (dh, db, d_weight, d_bias, d_post_weight, d_post_bias, d_gate), each in the type of what it belongs to; None where that
     is None or where `need` says so.  Bit-reproducible."""
-    args = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
+    args, dev = _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps)
     _check_like(h, dy, dr)
     _check_stats(args.rows, h, stats)
     lib = load_library()
-    with torch.cuda.device(h.device):
+    with _on_device(dev):
         grads = [torch.empty_like(t) if n and t is not None else None
                  for n, t in zip(need, (h, b, weight, bias, post_weight, post_bias, gate))]
-        size = int(lib.bpt_res_norm_bwd_workspace_bytes(ctypes.byref(args)))
-        if workspace is None:
-            workspace = torch.empty(size, dtype=torch.uint8, device=h.device)
-        _check(lib.bpt_res_norm_bwd(ctypes.byref(args), _ptr(stats), _ptr(dy), _ptr(dr), *[_ptr(t) for t in grads], _ptr(workspace),
-                                    workspace.numel(), _stream()), "bpt_res_norm_bwd")
+        workspace = _scratch(workspace, lib.bpt_res_norm_bwd_workspace_bytes(ctypes.byref(args)), h)
+        _check(lib.bpt_res_norm_bwd(ctypes.byref(args), _ptr(stats), _ptr(dy), _ptr(dr), *map(_ptr, grads), workspace.data_ptr(),
+                                    workspace.numel(), _raw_stream(dev)), "bpt_res_norm_bwd")
     return tuple(grads)
 
 

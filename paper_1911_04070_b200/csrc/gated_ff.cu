@@ -16,6 +16,8 @@
 #include <algorithm>
 
 #include "bpt_internal.cuh"
+#include "ff_act.cuh"
+#include "gated_ff_rows.cuh"
 #include "mma_tools.cuh"
 #include "pair_tools.cuh"
 #include "tc5_host.cuh"
@@ -51,34 +53,6 @@ struct FfParams {
     int* status;
     int rows, D, F, splits, tiles;
 };
-
-// The special-function unit's 2^x and 1/x (relative error about 2^-22), results below the normal range flushed to zero.
-__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-
-// act(g) and, for the backward, its derivative.  The epilogues are bound by instructions per element, so both activations
-// cost two special-function calls.  gelu: the normal distribution's integral by Abramowitz and Stegun 7.1.26,
-// erfc(z) = (a1 t + .. + a5 t^5) exp(-z^2), t = 1 / (1 + 0.3275911 z), z >= 0, absolute error 1.5e-7, whose exponential with
-// z = |g| / sqrt 2 is the density that the derivative needs.
-template <int ACT, bool GRAD>
-__device__ __forceinline__ float ff_act(float g, float& da) {
-    if (ACT == BPT_ACT_SILU) {
-        const float s = rcp(1.f + ex2(g * -1.4426950408889634f));
-        if (GRAD) da = s * fmaf(g, 1.f - s, 1.f);
-        return g * s;
-    }
-    if (ACT == BPT_ACT_GELU) {
-        const float e = ex2(g * g * -0.72134752044448170f);                     // exp(-g^2 / 2)
-        const float t = rcp(fmaf(fabsf(g), 0.3275911f * 0.70710678118654752f, 1.f));
-        float c = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
-        c *= 0.5f * t * e;                                                      // the tail beyond |g|
-        c = g < 0.f ? c : 1.f - c;
-        if (GRAD) da = fmaf(g * 0.39894228040143268f, e, c);
-        return g * c;
-    }
-    if (GRAD) da = g > 0.f ? 1.f : 0.f;
-    return g < 0.f ? 0.f : g;
-}
 
 // The load thread of a CTA and the product thread of a pair go through the same slices: 64 deep, `STAGES` places in shared
 // memory, A first, B 16 KB behind it.  What they do per slice is on the critical path (one slice is 512 cycles of products, and the
@@ -538,7 +512,7 @@ using namespace bpt;
 extern "C" size_t bpt_gated_ff_workspace_bytes(int64_t rows, int32_t D, int32_t F, int backward) {
     if (check_ff(rows, D, F, BPT_ACT_RELU) != BPT_OK || rows == 0) return 0;
     const size_t hidden = inner_bytes(rows, F);
-    if (!backward) return hidden;
+    if (!backward) return rows <= kGatedFfFewRows ? (size_t)rows * F * 4 : hidden;
     return 3 * hidden + (size_t)3 * dw_splits(rows, D, F) * D * F * 4;
 }
 
@@ -551,8 +525,14 @@ extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const 
     if (!x || !w_gate || !w_up || !w_down || !y || !aligned16({x, w_gate, w_up, w_down, y})) return BPT_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < bpt_gated_ff_workspace_bytes(rows, D, F, 0)) return BPT_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255) return BPT_ERR_INVALID_ARG;
-    if (!tc5::encode_tiled()) return BPT_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (rows <= kGatedFfFewRows) {
+        const GatedFfRows q{static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(w_gate), static_cast<const __nv_bfloat16*>(w_up),
+                            static_cast<const __nv_bfloat16*>(w_down), static_cast<__nv_bfloat16*>(y), static_cast<float*>(workspace),
+                            static_cast<int*>(status), (int)rows, D, F, act};
+        return launch_gated_ff_rows(q, st);
+    }
+    if (!tc5::encode_tiled()) return BPT_ERR_CUDA;
     if (status && cudaMemsetAsync(status, 0, kStatusBytes, st) != cudaSuccess) return BPT_ERR_CUDA;
     FfParams p{};
     p.status = static_cast<int*>(status);

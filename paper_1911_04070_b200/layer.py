@@ -87,8 +87,7 @@ def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=Non
     with the trailing row axes of length one ([B, 1, D]: a gate per sequence), or None (1).  With norm="layer" and nothing
     else this is the norm(H + A) of Algorithm 2; with post_norm it is the norm after the block before and the norm
     before the block that follows.  Returns y; (r, y) with return_sum; r with norm=None."""
-    cont = lambda t: None if t is None else t.contiguous()
-    ts = [cont(t) for t in (h, b, weight, bias, post_weight, post_bias, gate)]
+    ts = [t if t is None else t.contiguous() for t in (h, b, weight, bias, post_weight, post_bias, gate)]
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts):
         return _ResidualNorm.apply(*ts, norm, post_norm, float(alpha), float(eps), bool(return_sum))
     h, b, weight, bias, post_weight, post_bias, gate = ts

@@ -70,3 +70,11 @@ def test_oracle_against_torch_and_differences(act):
         up, down = ((bpt_layer.gated_ff(**{**v, name: t + s * step * d}, act=act) * dy).sum() for s in (1, -1))
         want, got = float(up - down) / (2 * step), float((leaf[name].grad * d).sum())
         assert abs(got - want) <= 1e-6 * (1 + abs(want)), (name, got, want)     # 1e-16 * |loss| / step, and step^2
+
+
+def test_few_rows_constant_matches_the_header():
+    import os
+    import re
+    from paper_1911_04070_b200 import binding
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "bpt.h")).read()
+    assert int(re.search(r"#define BPT_GATED_FF_FEW_ROWS (\d+)", text).group(1)) == binding.GATED_FF_FEW_ROWS

@@ -97,6 +97,26 @@ def layer_forward(h, w, mask, rel, n_heads):
     return torch.nn.functional.layer_norm(z + f, (D,), w["ln2_w"], w["ln2_b"])
 
 
+def layer_forward_form(h, w, mask, rel, n_heads, act=None, sandwich=False, alpha=1.0):
+    """The layer with a gated feed-forward block (act: its activation; None: the plain one) and, with sandwich, norms before
+    and after each block: w has ff_gate, ff_up [F, D] and ff_down [D, F], and pre1_w, pre1_b, pre2_w, pre2_b, gate1, gate2 [D]."""
+    B, N, D = h.shape
+    dh = D // n_heads
+    split = lambda x: x.view(B, N, n_heads, dh)
+    norm = lambda x, a: _normalise(x, "layer", w[a + "_w"], w[a + "_b"], 1e-5)
+    gsa = lambda x: attention(split(x @ w["wq"].T), split(x @ w["wk"].T), split(x @ w["wv"].T), w["rel_emb"], mask, rel,
+                              dh ** -0.5).reshape(B, N, D) @ w["wo"].T
+    if act is None:
+        ffn = lambda x: torch.relu(x @ w["ff1_w"].T + w["ff1_b"]) @ w["ff2_w"].T + w["ff2_b"]
+    else:
+        ffn = lambda x: gated_ff(x, w["ff_gate"], w["ff_up"], w["ff_down"], act)
+    if not sandwich:
+        z = norm(h + gsa(h), "ln1")
+        return norm(z + ffn(z), "ln2")
+    r = alpha * h + w["gate1"] * norm(gsa(norm(h, "pre1")), "ln1")
+    return alpha * r + w["gate2"] * norm(ffn(norm(r, "pre2")), "ln2")
+
+
 def encoder_forward(tokens, layers, g, n_heads, lengths=None, readout="tokens"):
     """Token states [B, n, D] -> stack of layers over all 2n-1 nodes, span nodes starting from zero (Sec. 3.3)."""
     B, n, D = tokens.shape

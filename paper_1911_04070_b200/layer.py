@@ -135,34 +135,86 @@ class BPTLayer(nn.Module):
     """One layer of Algorithm 2:  Z = norm(H + GSA(H)),  H' = norm(Z + FFN(Z)).
 
     H holds the states of all 2n-1 nodes.  The relation embeddings are a parameter of the layer
-    (Sec. 3.4: not shared between layers, shared between the heads)."""
+    (Sec. 3.4: not shared between layers, shared between the heads).
+
+    Two forms beyond the paper's, for deeper stacks and language models:
+    gated: "silu", "gelu" or "relu" makes the FFN the gated block (act(Z Wg^T) * (Z Wu^T)) Wd^T (d_model and d_ff multiples of
+    8; in bfloat16 it runs in gated_feed_forward).
+    sandwich: norms before and after each block, with a learned gate per channel and the residual scaled by alpha:
+    R = alpha H + gate1 * norm1(GSA(pre1(H))),  H' = alpha R + gate2 * norm2(FFN(pre2(R))); everything between two blocks
+    is one residual_norm call."""
 
     def __init__(self, g: binding.Graph, d_model: int, n_heads: int, d_ff: int, rel_std: float = 0.02,
-                 attn_dropout: float = 0.0):
+                 attn_dropout: float = 0.0, gated=None, sandwich: bool = False, alpha: float = 1.0):
         super().__init__()
         self.attn_dropout = attn_dropout
         if d_model % n_heads:
             raise ValueError("d_model must be a multiple of n_heads")
+        if gated is not None and gated not in binding.ACTIVATIONS:
+            raise ValueError("gated must be None or one of %s" % ", ".join(map(repr, binding.ACTIVATIONS)))
+        if gated is not None and (d_model % 8 or d_ff % 8):
+            raise ValueError("a gated layer needs d_model and d_ff that are multiples of 8")
+        if alpha != 1.0 and not sandwich:
+            raise ValueError("alpha scales the residual of the sandwich form")
         self.g, self.h, self.dh = g, n_heads, d_model // n_heads
+        self.gated, self.sandwich, self.alpha = gated, sandwich, float(alpha)
         self.wq, self.wk, self.wv, self.wo = (nn.Linear(d_model, d_model, bias=False) for _ in range(4))
         self.rel_emb = nn.Parameter(torch.randn(g.n_rel, self.dh) * rel_std)
         self.norm1, self.norm2 = nn.LayerNorm(d_model), nn.LayerNorm(d_model)
-        self.ff1, self.ff2 = nn.Linear(d_model, d_ff), nn.Linear(d_ff, d_model)
+        if gated is None:
+            self.ff1, self.ff2 = nn.Linear(d_model, d_ff), nn.Linear(d_ff, d_model)
+        else:
+            self.ff_gate, self.ff_up = nn.Linear(d_model, d_ff, bias=False), nn.Linear(d_model, d_ff, bias=False)
+            self.ff_down = nn.Linear(d_ff, d_model, bias=False)
+        if sandwich:
+            self.pre1, self.pre2 = nn.LayerNorm(d_model), nn.LayerNorm(d_model)
+            self.gate1, self.gate2 = nn.Parameter(torch.ones(d_model)), nn.Parameter(torch.ones(d_model))
 
-    def forward(self, h, lengths=None):
+    def feed_forward(self, z):
+        if self.gated is None:
+            return self.ff2(torch.relu(self.ff1(z)))
+        if z.dtype == torch.bfloat16 and self.ff_gate.weight.dtype == torch.bfloat16:
+            return gated_feed_forward(z, self.ff_gate.weight, self.ff_up.weight, self.ff_down.weight, self.gated)
+        return self.ff_down(getattr(torch.nn.functional, self.gated)(self.ff_gate(z)) * self.ff_up(z))
+
+    def attention_input(self, h):
+        """What the attention's projections take: H, or pre1(H) in the sandwich form."""
+        return residual_norm(h, None, self.pre1.weight, self.pre1.bias, eps=self.pre1.eps) if self.sandwich else h
+
+    def after_attention(self, h, a, next_norm=None, fuse: bool = True):
+        """H' from the layer's input H and the attention's output a, both [..., d_model]; with next_norm (a LayerNorm, sandwich
+        form) the pair (H', next_norm(H')).  fuse: the output projection may run in bpt_out_proj_norm."""
+        if self.sandwich:
+            n1, n2, p2 = self.norm1, self.norm2, self.pre2
+            r, y = residual_norm(h, self.wo(a), p2.weight, p2.bias, "layer", "layer", n1.weight, n1.bias, self.gate1, self.alpha, n1.eps, True)
+            f = self.feed_forward(y)
+            if next_norm is None:
+                return residual_norm(r, f, norm=None, post_norm="layer", post_weight=n2.weight, post_bias=n2.bias, gate=self.gate2,
+                                     alpha=self.alpha, eps=n2.eps)
+            return residual_norm(r, f, next_norm.weight, next_norm.bias, "layer", "layer", n2.weight, n2.bias, self.gate2, self.alpha, n2.eps, True)
+        D = h.shape[-1]
+        if (fuse and FUSE_OUT_PROJ_NORM and not torch.is_grad_enabled() and h.dtype == torch.bfloat16 and D in (128, 256, 512)
+                and self.wo.weight.dtype == torch.bfloat16):
+            z = binding.bpt_out_proj_norm(a, self.wo.weight.contiguous(), h.contiguous(), self.norm1.weight.float(),
+                                          self.norm1.bias.float(), self.norm1.eps)
+        elif self.gated is None:
+            z = self.norm1(h + self.wo(a))
+        else:
+            z = residual_norm(h, self.wo(a), self.norm1.weight, self.norm1.bias, eps=self.norm1.eps)
+        if self.gated is None:
+            return self.norm2(z + self.feed_forward(z))
+        return residual_norm(z, self.feed_forward(z), self.norm2.weight, self.norm2.bias, eps=self.norm2.eps)
+
+    def forward(self, h, lengths=None, y=None, next_norm=None):
+        """y: pre1(H) where the caller has it already (sandwich form); next_norm: see after_attention."""
         B, N, D = h.shape
         split = lambda x: x.view(B, N, self.h, self.dh)
         p_drop = self.attn_dropout if self.training else 0.0
         seed = int(torch.randint(0, 2 ** 62, (1,)).item()) if p_drop else 0   # a fresh mask per call, from torch's CPU generator
-        a = graph_self_attention(self.g, split(self.wq(h)), split(self.wk(h)), split(self.wv(h)),
-                                 self.rel_emb.to(h.dtype), lengths=lengths, dropout_p=p_drop, dropout_seed=seed)
-        if (FUSE_OUT_PROJ_NORM and not torch.is_grad_enabled() and h.dtype == torch.bfloat16 and D in (128, 256, 512)
-                and self.wo.weight.dtype == torch.bfloat16):
-            z = binding.bpt_out_proj_norm(a.reshape(B, N, D), self.wo.weight.contiguous(), h.contiguous(), self.norm1.weight.float(),
-                                          self.norm1.bias.float(), self.norm1.eps)
-        else:
-            z = self.norm1(h + self.wo(a.reshape(B, N, D)))
-        return self.norm2(z + self.ff2(torch.relu(self.ff1(z))))
+        x = self.attention_input(h) if y is None else y
+        a = graph_self_attention(self.g, split(self.wq(x)), split(self.wk(x)), split(self.wv(x)),
+                                 self.rel_emb.to(x.dtype), lengths=lengths, dropout_p=p_drop, dropout_seed=seed)
+        return self.after_attention(h, a.reshape(B, N, D), next_norm)
 
 
 class BPTEncoder(nn.Module):
@@ -170,22 +222,32 @@ class BPTEncoder(nn.Module):
 
     Token nodes start from the given token states, span nodes from zero, and all nodes are updated
     together in every layer (Sec. 3.3).  `readout`: "tokens" returns the token states [B, n, D]
-    (language modelling, translation), "root" the root node's state [B, D] (classification)."""
+    (language modelling, translation), "root" the root node's state [B, D] (classification).
+    gated, sandwich, alpha: the layers' forms (see BPTLayer); a sandwich stack ends with one more norm, norm_out."""
 
     def __init__(self, n: int, k: int, d_model: int, n_heads: int, d_ff: int, n_layers: int, left_only: bool = False,
-                 device="cuda", attn_dropout: float = 0.0):
+                 device="cuda", attn_dropout: float = 0.0, gated=None, sandwich: bool = False, alpha: float = 1.0):
         super().__init__()
-        self.n = n
+        self.n, self.sandwich = n, sandwich
         self.g = binding.bpt_build_graph(n, k, binding.BPT_LEFT_ONLY if left_only else 0, device=device)
-        self.layers = nn.ModuleList(BPTLayer(self.g, d_model, n_heads, d_ff, attn_dropout=attn_dropout) for _ in range(n_layers))
+        self.layers = nn.ModuleList(BPTLayer(self.g, d_model, n_heads, d_ff, attn_dropout=attn_dropout, gated=gated, sandwich=sandwich,
+                                             alpha=alpha) for _ in range(n_layers))
+        if sandwich:
+            self.norm_out = nn.LayerNorm(d_model)
 
     def forward(self, tokens, lengths=None, readout: str = "tokens"):
         B, n, D = tokens.shape
         if n != self.n:
             raise ValueError("expected %d token states per sequence, got %d" % (self.n, n))
         h = torch.cat([tokens, tokens.new_zeros(B, n - 1, D)], dim=1)
-        for layer in self.layers:
-            h = layer(h, lengths)
+        if self.sandwich:
+            y = None
+            for layer, norm in zip(self.layers, [l.pre1 for l in self.layers[1:]] + [self.norm_out]):
+                h, y = layer(h, lengths, y, norm)
+            h = y if len(self.layers) else residual_norm(h, None, self.norm_out.weight, self.norm_out.bias, eps=self.norm_out.eps)
+        else:
+            for layer in self.layers:
+                h = layer(h, lengths)
         if readout == "tokens":
             return h[:, :n]
         if readout == "root":
@@ -241,14 +303,17 @@ class BPTDecoder:
         self.h[0][:, i] = token_state.to(self.h[0].dtype)
         for li, layer in enumerate(self.enc.layers):
             hr = self.h[li][:, idx]                                     # [B, R, D]; span rows of layer 0 are zero
-            split = lambda x: x.view(B, R, layer.h, layer.dh)
-            self.q[li][:, idx] = split(layer.wq(hr))
-            self.k[li][:, idx] = split(layer.wk(hr))
-            self.v[li][:, idx] = split(layer.wv(hr))
+            x = layer.attention_input(hr)
+            split = lambda t: t.view(B, R, layer.h, layer.dh)
+            self.q[li][:, idx] = split(layer.wq(x))
+            self.k[li][:, idx] = split(layer.wk(x))
+            self.v[li][:, idx] = split(layer.wv(x))
             binding.bpt_attn_fwd_rows(self.g, self.q[li], self.k[li], self.v[li], layer.rel_emb.to(hr.dtype).contiguous(),
                                       1.0 / math.sqrt(layer.dh), rows_t, self.a[li], self.lse, lengths=lens)
-            a = self.a[li][:, idx].reshape(B, R, -1)
-            z = layer.norm1(hr + layer.wo(a))
-            self.h[li + 1][:, idx] = layer.norm2(z + layer.ff2(torch.relu(layer.ff1(z))))
+            self.h[li + 1][:, idx] = layer.after_attention(hr, self.a[li][:, idx].reshape(B, R, -1), fuse=False)
         self.pos += 1
-        return self.h[-1][:, i]
+        out = self.h[-1][:, i]
+        if self.enc.sandwich:
+            norm = self.enc.norm_out
+            out = residual_norm(out, None, norm.weight, norm.bias, eps=norm.eps)
+        return out

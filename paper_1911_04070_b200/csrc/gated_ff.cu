@@ -25,7 +25,7 @@
 namespace bpt {
 namespace {
 
-enum FfKernel { kFfIn, kFfOut, kFfBwdIn, kFfDx, kFfDw };
+enum FfKernel { kFfIn, kFfOut, kFfBwdIn, kFfDx, kFfDw, kFfOutSplit, kFfDxSplit };     // ..Split: the sum's range shared out, fp32 results
 
 constexpr int kFfPairs = 74;                  // 148 SMs
 constexpr int kFfStageBytes = 32 * 1024;      // 128 x 64 of A and up to 128 x 64 of B per CTA
@@ -52,6 +52,7 @@ struct FfParams {
     CUtensorMap a0, a1, a2, b0, b1, b2, c0, c1, c2;
     int* status;
     int rows, D, F, splits, tiles;
+    bool clear;             // the call's first kernel clears the status block
 };
 
 // The load thread of a CTA and the product thread of a pair go through the same slices: 64 deep, `STAGES` places in shared
@@ -129,6 +130,8 @@ template <int STAGES> struct FfProducts {
 template <int KERNEL, int BN, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::threads, 1) gated_ff_kernel(const __grid_constant__ FfParams p) {
     using S = FfShape<KERNEL>;
+    constexpr bool kOut = KERNEL == kFfOut || KERNEL == kFfOutSplit, kDx = KERNEL == kFfDx || KERNEL == kFfDxSplit;
+    constexpr bool kPart = KERNEL == kFfDw || KERNEL == kFfOutSplit || KERNEL == kFfDxSplit;      // writes fp32 sums of part of the range
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // the same offset in both CTAs
     const uint32_t s_u = smem_u32(smem), bar_u = s_u + S::bar_off;
@@ -139,9 +142,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     // kFfBwdIn: pair 0 of tfull / tempty belongs to G | U, pair 1 to dH
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::bar_off + 8 * (2 * S::stages + 4));
     volatile int* abort_s = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int rank = (int)pair::cta_rank(), pair_id = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
+    if (p.clear && p.status && blockIdx.x == 0 && tid < 64) p.status[tid] = 0;      // a give-up is a second away
     if (tid == 0) {
         for (int i = 0; i < 2 * S::stages + 2; ++i) tc5::mbar_init(bar_u + 8u * i, 1);
         for (int i = 0; i < 2; ++i) tc5::mbar_init(tempty(i), 2 * S::epi_warps);
@@ -156,7 +161,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     const uint32_t tbase = *tmem_slot;
 
     const int kd = (p.D + kFfK - 1) / kFfK, kf = (p.F + kFfK - 1) / kFfK, km = (p.rows + kFfK - 1) / kFfK;
-    const int n_tiles = KERNEL == kFfOut || KERNEL == kFfDx ? (p.D + BN - 1) / BN : KERNEL == kFfBwdIn ? (p.F + 255) / 256 : (p.F + 127) / 128;   // along the output's columns
+    const int n_tiles = kOut || kDx ? (p.D + BN - 1) / BN : KERNEL == kFfBwdIn ? (p.F + 255) / 256 : (p.F + 127) / 128;   // along the output's columns
     const int dw_n0 = (p.D + 255) / 256, dw_n1 = (p.F + 255) / 256, dw_tiles = dw_n0 * dw_n1;             // weight gradients, each of the three
     struct Tile { int m, n, k0, k1, job, split, halves; };      // corner, slices, and which product
     auto tile_of = [&](int t) {
@@ -169,9 +174,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
             q.m = v / nn * 256; q.n = v % nn * 256;
             q.k0 = (int)((long long)km * q.split / p.splits); q.k1 = (int)((long long)km * (q.split + 1) / p.splits);
         } else {
+            q.k1 = KERNEL == kFfIn ? kd : kOut ? kf : 2 * kf;
+            if constexpr (kPart) {
+                const int per = p.tiles / p.splits, all = q.k1;
+                q.split = t / per;
+                t %= per;
+                q.k0 = all * q.split / p.splits; q.k1 = all * (q.split + 1) / p.splits;
+            }
             q.m = t / n_tiles * 256;
-            q.n = t % n_tiles * (KERNEL == kFfOut || KERNEL == kFfDx ? BN : KERNEL == kFfBwdIn ? 256 : 128);
-            q.k1 = KERNEL == kFfIn ? kd : KERNEL == kFfOut ? kf : 2 * kf;
+            q.n = t % n_tiles * (kOut || kDx ? BN : KERNEL == kFfBwdIn ? 256 : 128);
             q.halves = p.F - q.n > 128 ? 2 : 1;         // kFfBwdIn
         }
         return q;
@@ -181,6 +192,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     // read every row of A once per pair and was 17 % slower in the long products).
     if (w == 0 && lane == 0) {
         // =============== load thread ===============
+        // The kernel before has ended and its results are visible.  This thread's loads are all that read them, and whatever this
+        // kernel writes follows from its loads.
+        asm volatile("griddepcontrol.wait;" ::: "memory");
         FfLoader<S::stages> ld{s_u, pair::in_first(full(0)), full(0), empty(0), rank == 0};
         const bool one = rank == 0;
         for (int t = pair_id; t < p.tiles && ld.ok; t += n_pairs) {
@@ -188,15 +202,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
             const int m = q.m + rank * 128, n = q.n + rank * (BN / 2);
             if constexpr (KERNEL == kFfIn) {
                 ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n);
-            } else if constexpr (KERNEL == kFfOut) {
-                ld.template slices<false, false, BN * 64>(0, kf, &p.a0, m, &p.b0, n);
+            } else if constexpr (kOut) {
+                ld.template slices<false, false, BN * 64>(q.k0, q.k1, &p.a0, m, &p.b0, n);
             } else if constexpr (KERNEL == kFfBwdIn) {      // dH: dy rows, Wd with its F axis contiguous
                 ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n);
                 ld.template slices<false, true, 16384>(0, kd, &p.a1, m, &p.b2, n);
                 if (q.halves == 2) ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n + 128);
-            } else if constexpr (KERNEL == kFfDx) {
-                ld.template slices<false, true, BN * 64>(0, kf, &p.a0, m, &p.b0, n);
-                ld.template slices<false, true, BN * 64>(0, kf, &p.a1, m, &p.b1, n);
+            } else if constexpr (kDx) {         // dG Wg, then dU Wu
+                ld.template slices<false, true, BN * 64>(q.k0, q.k1 < kf ? q.k1 : kf, &p.a0, m, &p.b0, n);
+                ld.template slices<false, true, BN * 64>(q.k0 < kf ? 0 : q.k0 - kf, q.k1 - kf, &p.a1, m, &p.b1, n);
             } else {
                 ld.template slices<true, true, 16384>(q.k0, q.k1, q.job == 0 ? &p.a0 : q.job == 1 ? &p.a1 : &p.a2, m, q.job < 2 ? &p.b0 : &p.b1, n);
             }
@@ -210,7 +224,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
         }
     } else if (w == 1 && lane == 0 && rank == 0) {
         // =============== product thread ===============
-        constexpr bool a_mn = KERNEL == kFfDw, b_mn = KERNEL == kFfDw || KERNEL == kFfDx;
+        constexpr bool a_mn = KERNEL == kFfDw, b_mn = KERNEL == kFfDw || kDx;
         const uint32_t idesc = tc5::instr_desc(256, BN, a_mn, b_mn);
         FfProducts<S::stages> mm{s_u, full(0), empty(0)};
         int i = 0, gu = 0;      // tiles, G | U accumulators so far
@@ -271,7 +285,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                 __syncwarp();
                 if (lane == 0) {
                     if (col < limit_cols && row < limit_rows) {
-                        if constexpr (KERNEL == kFfDw) pair::store_3d(map, col, row, q.job == 1 ? p.splits + q.split : q.split, stg_u + buf * S::tile_bytes);
+                        if constexpr (kPart) pair::store_3d(map, col, row, q.job == 1 ? p.splits + q.split : q.split, stg_u + buf * S::tile_bytes);
                         else pair::store_2d(map, col, row, stg_u + buf * S::tile_bytes);
                     }
                     pair::store_commit();
@@ -364,10 +378,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                     for (int j = 0; j < 4; ++j) put64(0, j, oh[4 * j], oh[4 * j + 1], oh[4 * j + 2], oh[4 * j + 3]);
                     send(&p.c2, 0, col, p.F, p.rows);
                 }
-            } else if constexpr (KERNEL == kFfDw) {
+            } else if constexpr (kPart) {
                 const uint32_t src = tbase + lane_base + (i & 1) * 256 + part * 128;
                 const CUtensorMap* map = q.job < 2 ? &p.c0 : &p.c1;
-                const int limit_cols = q.job < 2 ? p.D : p.F, limit_rows = q.job < 2 ? p.F : p.D;
+                const int limit_cols = q.job < 2 ? p.D : p.F, limit_rows = KERNEL != kFfDw ? p.rows : q.job < 2 ? p.F : p.D;
 #pragma unroll
                 for (int c = 0; c < 128; c += 32) {
                     uint32_t x[32];
@@ -381,7 +395,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                     send(map, (c / 32) & 1, q.n + part * 128 + c, limit_cols, limit_rows);
                 }
             } else {
-                constexpr int W = BN / 2 < 64 ? BN / 2 : 64;      // columns per stored tile
+                constexpr int W = 64;       // columns per stored tile
                 const uint32_t src = tbase + lane_base + (i & 1) * 256 + part * (BN / 2);
 #pragma unroll
                 for (int c = 0; c < BN / 2; c += 32) {
@@ -399,8 +413,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                         uint32_t y[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[e] = pack_bf16(__uint_as_float(x[j * 8 + 2 * e]), __uint_as_float(x[j * 8 + 2 * e + 1]));
-                        if constexpr (W == 64) put(buf, (c & 32) / 8 + j, y[0], y[1], y[2], y[3]);
-                        else put64(buf, j, y[0], y[1], y[2], y[3]);
+                        put(buf, (c & 32) / 8 + j, y[0], y[1], y[2], y[3]);
                     }
                     if (c % W + 32 == W) send(&p.c0, buf, q.n + part * (BN / 2) + c / W * W, p.D, p.rows);
                 }
@@ -416,25 +429,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     if (w == 1) pair::tmem_free(tbase, 512);
 }
 
-// Weight gradients: the fp32 sums of the row ranges, added in order, rounded once.
-__global__ void __launch_bounds__(256) gated_ff_dw_sum_kernel(const float* __restrict__ part, __nv_bfloat16* __restrict__ dwg,
-                                                              __nv_bfloat16* __restrict__ dwu, __nv_bfloat16* __restrict__ dwd, long long n, int splits) {
+// Results [jobs][n] from the fp32 sums of the ranges, part [jobs][splits][n]: added in order, rounded once.
+__global__ void __launch_bounds__(256) gated_ff_sum_kernel(const float* part, __nv_bfloat16* out0, __nv_bfloat16* out1, __nv_bfloat16* out2,
+                                                           long long n, int splits, int jobs) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const long long n8 = n / 8;
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < 3 * n8; i += gridDim.x * 256ll) {
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < jobs * n8; i += gridDim.x * 256ll) {
         const int job = (int)(i / n8);
         const long long e = (i % n8) * 8;
         const float* src = part + (long long)job * splits * n + e;
         float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
+#pragma unroll 4
         for (int s = 1; s < splits; ++s) {
             const float4 c = *reinterpret_cast<const float4*>(src + s * n), d = *reinterpret_cast<const float4*>(src + s * n + 4);
             a.x += c.x; a.y += c.y; a.z += c.z; a.w += c.w;
             b.x += d.x; b.y += d.y; b.z += d.z; b.w += d.w;
         }
-        __nv_bfloat16* out = (job == 0 ? dwg : job == 1 ? dwu : dwd) + e;
+        __nv_bfloat16* out = (job == 0 ? out0 : job == 1 ? out1 : out2) + e;
         *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
     }
 }
-
 // 2-D map over a row-major [n_rows, n_cols] bf16 matrix, rows `ld` elements apart (0: n_cols), boxes of box_rows x box_cols.
 bool bf16_map(CUtensorMap* m, const void* base, long long n_rows, int n_cols, int box_rows, int box_cols = 64, int ld = 0) {
     const cuuint64_t dims[2] = {(cuuint64_t)n_cols, (cuuint64_t)n_rows};
@@ -453,14 +468,38 @@ bool part_map(CUtensorMap* m, void* base, int n_mats, int n_rows, int n_cols) {
                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Launches a kernel so that its CTAs may start (where they find room) while the kernel before it in the call still runs; both
+// go on to what depends on it only once that one has ended (griddepcontrol.wait).  first: nothing of this call is before it.
+template <typename... Params, typename... Args>
+bool launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool first, Args... args) {
+    cudaLaunchAttribute attr[1] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = first ? 0 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+}
 template <int KERNEL, int BN, int ACT = BPT_ACT_RELU>
 bpt_status run(const FfParams& p, cudaStream_t st, const char* name) {
     constexpr size_t smem = FfShape<KERNEL>::bytes;
     static_assert(smem <= 227 * 1024, "shared memory of one CTA");
     if (cudaFuncSetAttribute(gated_ff_kernel<KERNEL, BN, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return BPT_ERR_CUDA;
-    gated_ff_kernel<KERNEL, BN, ACT><<<2 * std::min(p.tiles, kFfPairs), FfShape<KERNEL>::threads, smem, st>>>(p);
+    if (!launch(gated_ff_kernel<KERNEL, BN, ACT>, dim3(2 * std::min(p.tiles, kFfPairs)), FfShape<KERNEL>::threads, smem, st, p.clear, p)) return BPT_ERR_CUDA;
     trace_mark(st, name);
-    return cudaGetLastError() == cudaSuccess ? BPT_OK : BPT_ERR_CUDA;
+    return BPT_OK;
+}
+
+bpt_status sum_parts(const float* part, void* out0, void* out1, void* out2, long long n, int splits, int jobs, cudaStream_t st, const char* name) {
+    if (!launch(gated_ff_sum_kernel, dim3((unsigned)std::min<long long>((jobs * n / 8 + 255) / 256, 148 * 8)), 256, 0, st, false, part,
+                (__nv_bfloat16*)out0, (__nv_bfloat16*)out1, (__nv_bfloat16*)out2, n, splits, jobs))
+        return BPT_ERR_CUDA;
+    trace_mark(st, name);
+    return BPT_OK;
 }
 
 template <int KERNEL>
@@ -497,12 +536,21 @@ bool aligned16(std::initializer_list<const void*> ptrs) {
         if ((uintptr_t)q & 15) return false;
     return true;
 }
-// Tiles of `bn` columns: fewer columns per tile while the pairs have less than one tile each.
-int out_columns(long long rows, int D, int least) {
-    int bn = 256;
-    while (bn > least && (rows + 255) / 256 * ((D + bn - 1) / bn) * 2 <= kFfPairs) bn /= 2;
-    return bn;
+// y and dx, [rows, D] with `slices` slices to sum over.  While tiles of 256 columns leave half of the pairs idle, their sums are
+// shared out: ranges of at least four slices, as many as there are pairs for; with two ranges at most the fp32 partial
+// sums cost what they gain, and narrower tiles do (256 columns a tile is the product's own best rate).
+struct OutPlan { int bn, splits; };
+OutPlan plan_out(long long rows, int D, int slices) {
+    const long long tiles = (rows + 255) / 256 * ((D + 255) / 256);
+    const int splits = (int)std::min<long long>(std::min<long long>(kFfPairs / tiles, slices / 4), 16);
+    if (splits > 2) return {256, splits};
+    return {tiles * 2 <= kFfPairs ? 128 : 256, 1};
 }
+size_t part_bytes(long long rows, int D, int slices) {
+    const OutPlan q = plan_out(rows, D, slices);
+    return q.splits > 1 ? (size_t)q.splits * rows * D * 4 : 0;
+}
+int slices_of(int n) { return (n + kFfK - 1) / kFfK; }
 
 }  // namespace
 }  // namespace bpt
@@ -512,8 +560,9 @@ using namespace bpt;
 extern "C" size_t bpt_gated_ff_workspace_bytes(int64_t rows, int32_t D, int32_t F, int backward) {
     if (check_ff(rows, D, F, BPT_ACT_RELU) != BPT_OK || rows == 0) return 0;
     const size_t hidden = inner_bytes(rows, F);
-    if (!backward) return rows <= kGatedFfFewRows ? (size_t)rows * F * 4 : hidden;
-    return 3 * hidden + (size_t)3 * dw_splits(rows, D, F) * D * F * 4;
+    if (!backward) return rows <= kGatedFfFewRows ? (size_t)rows * F * 4 : hidden + part_bytes(rows, D, slices_of(F));
+    // the partial sums of dx and of the weight gradients share their place
+    return 3 * hidden + std::max((size_t)3 * dw_splits(rows, D, F) * D * F * 4, part_bytes(rows, D, 2 * slices_of(F)));
 }
 
 extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y, int64_t rows,
@@ -532,10 +581,10 @@ extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const 
                             static_cast<int*>(status), (int)rows, D, F, act};
         return launch_gated_ff_rows(q, st);
     }
-    if (!tc5::encode_tiled()) return BPT_ERR_CUDA;
-    if (status && cudaMemsetAsync(status, 0, kStatusBytes, st) != cudaSuccess) return BPT_ERR_CUDA;
+    if (!tc5::encode_tiled() || !tc5::context_current()) return BPT_ERR_CUDA;
     FfParams p{};
     p.status = static_cast<int*>(status);
+    p.clear = true;
     p.rows = (int)rows; p.D = D; p.F = F;
     const int ld = inner_ld(F);
     if (!bf16_map(&p.a0, x, rows, D, 128) || !bf16_map(&p.b0, w_gate, F, D, 128) || !bf16_map(&p.b1, w_up, F, D, 128) ||
@@ -545,11 +594,18 @@ extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const 
     p.tiles = mt * ((F + 127) / 128);
     bpt_status e = run_act<kFfIn>(p, act, st, "gated_ff_in");
     if (e != BPT_OK) return e;
-    const int bn = out_columns(rows, D, 64);
-    if (!bf16_map(&p.a0, workspace, rows, F, 128, 64, ld) || !bf16_map(&p.b0, w_down, D, F, bn / 2) || !bf16_map(&p.c0, y, rows, D, 32, bn == 64 ? 32 : 64))
+    p.clear = false;
+    const OutPlan o = plan_out(rows, D, slices_of(F));
+    float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + inner_bytes(rows, F));
+    if (!bf16_map(&p.a0, workspace, rows, F, 128, 64, ld) || !bf16_map(&p.b0, w_down, D, F, o.bn / 2) ||
+        !(o.splits > 1 ? part_map(&p.c0, part, o.splits, (int)rows, D) : bf16_map(&p.c0, y, rows, D, 32)))
         return BPT_ERR_CUDA;
-    p.tiles = mt * ((D + bn - 1) / bn);
-    return bn == 256 ? run<kFfOut, 256>(p, st, "gated_ff_out") : bn == 128 ? run<kFfOut, 128>(p, st, "gated_ff_out") : run<kFfOut, 64>(p, st, "gated_ff_out");
+    p.splits = o.splits;
+    p.tiles = mt * ((D + o.bn - 1) / o.bn) * o.splits;
+    if (o.splits == 1) return o.bn == 256 ? run<kFfOut, 256>(p, st, "gated_ff_out") : run<kFfOut, 128>(p, st, "gated_ff_out");
+    e = run<kFfOutSplit, 256>(p, st, "gated_ff_out");
+    if (e != BPT_OK) return e;
+    return sum_parts(part, y, nullptr, nullptr, rows * (long long)D, o.splits, 1, st, "gated_ff_out_sum");
 }
 
 extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const void* w_up, const void* w_down, const void* dy, void* dx,
@@ -571,14 +627,14 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     if (!x || !w_gate || !w_up || !w_down || !dy || (!dx && !weights)) return BPT_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < bpt_gated_ff_workspace_bytes(rows, D, F, 1)) return BPT_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255) return BPT_ERR_INVALID_ARG;
-    if (!tc5::encode_tiled()) return BPT_ERR_CUDA;
-    if (status && cudaMemsetAsync(status, 0, kStatusBytes, st) != cudaSuccess) return BPT_ERR_CUDA;
+    if (!tc5::encode_tiled() || !tc5::context_current()) return BPT_ERR_CUDA;
     const size_t hidden = inner_bytes(rows, F);
     char *dg = static_cast<char*>(workspace), *du = dg + hidden, *h = du + hidden;
     float* part = reinterpret_cast<float*>(h + hidden);
     const int mt = (int)((rows + 255) / 256);
     FfParams p{};
     p.status = static_cast<int*>(status);
+    p.clear = true;
     p.rows = (int)rows; p.D = D; p.F = F;
     const int ld = inner_ld(F);
     if (!bf16_map(&p.a0, x, rows, D, 128) || !bf16_map(&p.a1, dy, rows, D, 128) || !bf16_map(&p.b0, w_gate, F, D, 128) ||
@@ -588,13 +644,19 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     p.tiles = mt * ((F + 255) / 256);
     bpt_status e = run_act<kFfBwdIn>(p, act, st, "gated_ff_bwd_in");
     if (e != BPT_OK) return e;
+    p.clear = false;
     if (dx) {
-        const int bn = out_columns(rows, D, 128);
+        const OutPlan o = plan_out(rows, D, 2 * slices_of(F));
         if (!bf16_map(&p.a0, dg, rows, F, 128, 64, ld) || !bf16_map(&p.a1, du, rows, F, 128, 64, ld) || !bf16_map(&p.b0, w_gate, F, D, 64) ||
-            !bf16_map(&p.b1, w_up, F, D, 64) || !bf16_map(&p.c0, dx, rows, D, 32))
+            !bf16_map(&p.b1, w_up, F, D, 64) ||
+            !(o.splits > 1 ? part_map(&p.c0, part, o.splits, (int)rows, D) : bf16_map(&p.c0, dx, rows, D, 32)))
             return BPT_ERR_CUDA;
-        p.tiles = mt * ((D + bn - 1) / bn);
-        e = bn == 256 ? run<kFfDx, 256>(p, st, "gated_ff_dx") : run<kFfDx, 128>(p, st, "gated_ff_dx");
+        p.splits = o.splits;
+        p.tiles = mt * ((D + o.bn - 1) / o.bn) * o.splits;
+        e = o.splits > 1 ? run<kFfDxSplit, 256>(p, st, "gated_ff_dx")
+                         : o.bn == 256 ? run<kFfDx, 256>(p, st, "gated_ff_dx") : run<kFfDx, 128>(p, st, "gated_ff_dx");
+        if (e != BPT_OK) return e;
+        if (o.splits > 1) e = sum_parts(part, dx, nullptr, nullptr, rows * (long long)D, o.splits, 1, st, "gated_ff_dx_sum");
         if (e != BPT_OK) return e;
     }
     if (weights) {
@@ -606,10 +668,7 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
         p.tiles = 3 * ((D + 255) / 256) * ((F + 255) / 256) * p.splits;
         e = run<kFfDw, 256>(p, st, "gated_ff_dw");
         if (e != BPT_OK) return e;
-        const long long n = (long long)D * F;
-        gated_ff_dw_sum_kernel<<<(unsigned)std::min<long long>((3 * n / 8 + 255) / 256, 148 * 8), 256, 0, st>>>(
-            part, (__nv_bfloat16*)dw_gate, (__nv_bfloat16*)dw_up, (__nv_bfloat16*)dw_down, n, p.splits);
-        trace_mark(st, "gated_ff_dw_sum");
+        e = sum_parts(part, dw_gate, dw_up, dw_down, (long long)D * F, p.splits, 3, st, "gated_ff_dw_sum");
     }
-    return cudaGetLastError() == cudaSuccess ? BPT_OK : BPT_ERR_CUDA;
+    return e;
 }

@@ -26,6 +26,13 @@ inline EncodeTiledFn encode_tiled() {
     return fn;
 }
 
+// Tensor maps are encoded by the driver, which wants the device's context current in the calling thread; a thread that has made
+// no runtime call that needs one yet (an autograd worker whose memory all came from a cache) does not have it.
+inline bool context_current() {
+    int device;
+    return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess;
+}
+
 // Map over a [B, N, H, 64] bf16 tensor; coordinates (0, head, node, batch entry).  Rows past the last node
 // of the tensor read as zeros.
 inline bool node_rows_map(CUtensorMap* m, const void* base, int B, int N, int H) {

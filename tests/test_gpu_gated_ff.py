@@ -207,6 +207,31 @@ def test_results_do_not_depend_on_what_the_workspace_held():
     assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+@pytest.mark.parametrize("rows", [5, 300])
+def test_from_a_fresh_thread(rows):
+    """A thread that has made no CUDA call of its own: every buffer is there already."""
+    import threading
+    import torch
+    from paper_1911_04070_b200 import binding
+    v, dy = _inputs(rows, 64, 128, 15)
+    want = (binding.bpt_gated_ff_fwd(**v),) + binding.bpt_gated_ff_bwd(**v, dy=dy)
+    lib, st = binding.load_library(), torch.cuda.current_stream().cuda_stream
+    got = [torch.empty_like(t) for t in want]
+    ws = [torch.empty(max(256, binding.bpt_gated_ff_workspace_bytes(rows, 64, 128, b)), dtype=torch.uint8, device="cuda:0") for b in (False, True)]
+    torch.cuda.synchronize()
+    ptr = [t.data_ptr() for t in v.values()]
+    for k, call in enumerate((lambda: lib.bpt_gated_ff_fwd(*ptr, got[0].data_ptr(), rows, 64, 128, 1, None, ws[0].data_ptr(), ws[0].numel(), st),
+                              lambda: lib.bpt_gated_ff_bwd(*ptr, dy.data_ptr(), *[t.data_ptr() for t in got[1:]], rows, 64, 128, 1, None,
+                                                           ws[1].data_ptr(), ws[1].numel(), st))):
+        status = []
+        t = threading.Thread(target=lambda: status.append(call()))
+        t.start()
+        t.join()
+        assert status == [0]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_only_some_gradients():
     import torch
     from paper_1911_04070_b200 import layer

@@ -322,61 +322,69 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                 for (int half = 0; half < q.halves; ++half, ++gu) {
                     const uint32_t src_dh = src + 256 + half * 128;
                     if (!ready(0, gu & 1)) break;
-                    uint32_t g[32], u[32], dh[16], oh[16];
+                    uint32_t g[32], u[32];
                     tc5::tmem_ld32(src, g);
                     tc5::tmem_ld32(src + 128, u);
                     tc5::tmem_ld_wait();
                     done(release0);
-                    if (half == 0 && !ready(1, i & 1)) break;
-                    tc5::tmem_ld16(src_dh, dh);
+                    // What does not need dH comes first, and the inner row with it: the first half's dH is still being summed then,
+                    // and the second half's products must not wait for this.  g becomes act(g), u becomes u act'(g).
+                    const int col = q.n + half * 128 + part * 32;
                     if (lane == 0) pair::store_wait_read<0>();
                     __syncwarp();
-                    tc5::tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            float r[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int k = j * 8 + 2 * y + e;
+                                const float uv = __uint_as_float(u[k]);
+                                float da;
+                                const float a = ff_act<ACT, true>(__uint_as_float(g[k]), da);
+                                r[e] = a * uv;
+                                g[k] = __float_as_uint(a);
+                                u[k] = __float_as_uint(uv * da);
+                            }
+                            x[y] = pack_bf16(r[0], r[1]);
+                        }
+                        put64(0, j, x[0], x[1], x[2], x[3]);
+                    }
+                    send(&p.c2, 0, col, p.F, p.rows);
+                    if (half == 0 && !ready(1, i & 1)) break;
+                    if (lane == 0) pair::store_wait_read<0>();      // the inner row has left its tile
+                    __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 32; c += 16) {
+                        uint32_t dh[16];
+                        tc5::tmem_ld16(src_dh + c, dh);
+                        tc5::tmem_ld_wait();
+                        if (c == 16 && half == q.halves - 1) done(release1);
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             uint32_t o[2][4];
 #pragma unroll
                             for (int y = 0; y < 4; ++y) {
-                                float r[3][2];
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const int k = j * 8 + 2 * y + e;
-                                    const float gv = __uint_as_float(g[c + k]), uv = __uint_as_float(u[c + k]), dv = __uint_as_float(dh[k]);
-                                    float da;
-                                    const float a = ff_act<ACT, true>(gv, da);
-                                    r[0][e] = dv * uv * da;
-                                    r[1][e] = dv * a;
-                                    r[2][e] = a * uv;
-                                }
-#pragma unroll
-                                for (int m = 0; m < 2; ++m) o[m][y] = pack_bf16(r[m][0], r[m][1]);
-                                oh[c / 2 + j * 4 + y] = pack_bf16(r[2][0], r[2][1]);
+                                const int k = c + j * 8 + 2 * y;
+                                const float d0 = __uint_as_float(dh[j * 8 + 2 * y]), d1 = __uint_as_float(dh[j * 8 + 2 * y + 1]);
+                                o[0][y] = pack_bf16(d0 * __uint_as_float(u[k]), d1 * __uint_as_float(u[k + 1]));
+                                o[1][y] = pack_bf16(d0 * __uint_as_float(g[k]), d1 * __uint_as_float(g[k + 1]));
                             }
 #pragma unroll
                             for (int m = 0; m < 2; ++m) put64(m, c / 8 + j, o[m][0], o[m][1], o[m][2], o[m][3]);
                         }
-                        if (c == 0) {
-                            tc5::tmem_ld16(src_dh + 16, dh);
-                            tc5::tmem_ld_wait();
-                            if (half == q.halves - 1) done(release1);
-                        }
                     }
-                    const int col = q.n + half * 128 + part * 32;
                     tc5::fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        if (col < p.F && row < p.rows) pair::store_2d(&p.c0, col, row, stg_u);
+                        if (col < p.F && row < p.rows) {
+                            pair::store_2d(&p.c0, col, row, stg_u);
+                            pair::store_2d(&p.c1, col, row, stg_u + S::tile_bytes);
+                        }
                         pair::store_commit();
-                        if (col < p.F && row < p.rows) pair::store_2d(&p.c1, col, row, stg_u + S::tile_bytes);
-                        pair::store_commit();
-                        pair::store_wait_read<1>();     // dG has left its tile: h takes it
                     }
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) put64(0, j, oh[4 * j], oh[4 * j + 1], oh[4 * j + 2], oh[4 * j + 3]);
-                    send(&p.c2, 0, col, p.F, p.rows);
                 }
             } else if constexpr (kPart) {
                 const uint32_t src = tbase + lane_base + (i & 1) * 256 + part * 128;

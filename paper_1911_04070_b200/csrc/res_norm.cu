@@ -123,37 +123,46 @@ __device__ __forceinline__ void fill(float4* dst, const void* p, bool bf16, long
     }
 }
 
-// Sum of a pair over the TPR threads of a row, the same bits in every thread.  slots: for each row group of the CTA two buffers
-// of TPR / 32 pairs, used in turn, so that one barrier (of the group's threads) per sum is enough.
+// Sum of a pair over the TPR threads of a row, the same bits in every thread.  The first exchange leaves v.x with the warp's lower
+// half and v.y with its upper half, so that the other four serve both.  slots: for each row group of the CTA two buffers of
+// TPR / 32 pairs, used in turn, so that one barrier (of the group's threads) per sum is enough.
 template <int TPR> __host__ __device__ constexpr int slot_count() { return TPR > 32 ? cta_threads(TPR) / 16 : 1; }
 template <int TPR>
 __device__ __forceinline__ float2 row_sum2(float2 v, float2* slots, int& turn) {
+    const int lane = threadIdx.x & 31;
+    const bool upper = lane & 16;
+    float a = (upper ? v.y : v.x) + __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, 16);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-    }
+    for (int o = 8; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
     if constexpr (TPR > 32) {
         float2* s = slots + (threadIdx.x / TPR * 2 + turn) * (TPR / 32);
         turn ^= 1;
-        if ((threadIdx.x & 31) == 0) s[threadIdx.x % TPR >> 5] = v;
+        if ((lane & 15) == 0) reinterpret_cast<float*>(s + (threadIdx.x % TPR >> 5))[lane >> 4] = a;
         if constexpr (TPR == cta_threads(TPR)) __syncthreads();
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
         v = s[0];
 #pragma unroll
         for (int w = 1; w < TPR / 32; ++w) { v.x += s[w].x; v.y += s[w].y; }
+        return v;
+    } else {
+        return make_float2(__shfl_sync(0xffffffffu, a, 0), __shfl_sync(0xffffffffu, a, 16));
     }
-    return v;
 }
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float2* slots, int& turn) {
-    if constexpr (TPR > 32) {
-        return row_sum2<TPR>(make_float2(v, 0.f), slots, turn).x;
-    } else {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (TPR > 32) {
+        static_assert(TPR == cta_threads(TPR), "the whole CTA");
+        float2* s = slots + turn * (TPR / 32);
+        turn ^= 1;
+        if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5].x = v;
+        __syncthreads();
+        v = s[0].x;
+#pragma unroll
+        for (int w = 1; w < TPR / 32; ++w) v += s[w].x;
     }
+    return v;
 }
 
 // Mean (0 for rms) and reciprocal deviation of the row held in x; channels past D hold zeros (live: chunk inside D).
@@ -179,7 +188,7 @@ __device__ __forceinline__ float2 row_stats(const pair_t* x, int kind, float inv
 template <typename T, int VEC, int NE, int TPR>
 __global__ void __launch_bounds__(cta_threads(TPR), NE <= 16 ? 1024 / cta_threads(TPR) : 1) res_norm_fwd_kernel(const RnParams p) {
     constexpr int NV = NE / VEC, NP = NE / 2, RPC = cta_threads(TPR) / TPR;
-    extern __shared__ __align__(16) float4 prm[];       // [weight, bias, post weight, post bias, gate][NE / 4][TPR]
+    extern __shared__ __align__(16) float4 prm[];       // [weight, bias if norm; post weight, post bias if post; gate if kept][NE / 4][TPR]
     __shared__ float2 slots[slot_count<TPR>()];
     int turn = 0;
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -188,15 +197,16 @@ __global__ void __launch_bounds__(cta_threads(TPR), NE <= 16 ? 1024 / cta_thread
     auto chan = [&](int v) { return (v * TPR + t) * VEC; };
     auto live = [&](int v) { return chan(v) < D; };
     constexpr int kRow = NE / 4 * TPR;
+    const int k_post = p.norm ? 2 : 0, k_gate = k_post + (p.post ? 2 : 0);
     if (p.norm) {
         fill<VEC, NE, TPR, RPC>(prm, p.weight, p.param_bf16, 0, 1.f, D, t, sub);
         fill<VEC, NE, TPR, RPC>(prm + kRow, p.bias, p.param_bf16, 0, 0.f, D, t, sub);
     }
     if (p.post) {
-        fill<VEC, NE, TPR, RPC>(prm + 2 * kRow, p.post_weight, p.param_bf16, 0, 1.f, D, t, sub);
-        fill<VEC, NE, TPR, RPC>(prm + 3 * kRow, p.post_bias, p.param_bf16, 0, 0.f, D, t, sub);
+        fill<VEC, NE, TPR, RPC>(prm + k_post * kRow, p.post_weight, p.param_bf16, 0, 1.f, D, t, sub);
+        fill<VEC, NE, TPR, RPC>(prm + (k_post + 1) * kRow, p.post_bias, p.param_bf16, 0, 0.f, D, t, sub);
     }
-    if (p.gate && !p.gate_each) fill<VEC, NE, TPR, RPC>(prm + 4 * kRow, p.gate, p.gate_bf16, 0, 1.f, D, t, sub);
+    if (p.gate && !p.gate_each) fill<VEC, NE, TPR, RPC>(prm + k_gate * kRow, p.gate, p.gate_bf16, 0, 1.f, D, t, sub);
     __syncthreads();
     // pairs 2 q and 2 q + 1 of parameter row k
     auto get = [&](int k, int q, pair_t* f) {
@@ -217,8 +227,8 @@ __global__ void __launch_bounds__(cta_threads(TPR), NE <= 16 ? 1024 / cta_thread
 #pragma unroll
             for (int q = 0; q < NE / 4; ++q) {
                 pair_t w[2], c[2];
-                get(2, q, w);
-                get(3, q, c);
+                get(k_post, q, w);
+                get(k_post + 1, q, c);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) n[2 * q + i] = fma2(mul2(add2(n[2 * q + i], minus), scale), w[i], c[i]);
             }
@@ -236,7 +246,7 @@ __global__ void __launch_bounds__(cta_threads(TPR), NE <= 16 ? 1024 / cta_thread
 #pragma unroll
                 for (int q = 0; q < NE / 4; ++q) {
                     pair_t w[2];
-                    get(4, q, w);
+                    get(k_gate, q, w);
                     n[2 * q] = mul2(n[2 * q], w[0]);
                     n[2 * q + 1] = mul2(n[2 * q + 1], w[1]);
                 }
@@ -531,6 +541,7 @@ __global__ void __launch_bounds__(cta_threads(TPR), cta_threads(TPR) <= 256 ? 51
             for (int i = 0; i < NP; ++i) s_g[i] = 0;
         }
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     float* part = p.part + (long long)blockIdx.x * 4 * D;
     if (p.norm) {
         flush(s_w, part, false);
@@ -542,8 +553,8 @@ __global__ void __launch_bounds__(cta_threads(TPR), cta_threads(TPR) <= 256 ? 51
     }
 }
 
-// Adds the shares: out[c] = sum over `count` rows of `part`, in the order of the rows: eight interleaved partial sums, then
-// their sum.  Blocks cover 32 channels; blockIdx.y picks the output.
+// Adds the shares: out[c] = sum over `count` rows of `part`, in a fixed order: 32 interleaved partial sums, then their sum.  A
+// block has 32 channels of the output that blockIdx.y picks, a warp for each partial sum.
 struct RnFinish {
     const float *part, *gate_part;
     void *d_weight, *d_bias, *d_post_weight, *d_post_bias, *d_gate;
@@ -551,9 +562,10 @@ struct RnFinish {
     int D, grid, splits;
     bool param_bf16, gate_bf16;
 };
-__global__ void __launch_bounds__(256) res_norm_finish_kernel(const RnFinish f) {
-    __shared__ float x[8][33];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+__global__ void __launch_bounds__(1024) res_norm_finish_kernel(const RnFinish f) {
+    __shared__ float x[32][33];
+    asm volatile("griddepcontrol.wait;" ::: "memory");      // the shares are there
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     for (long long o = blockIdx.y; o < 4 + f.groups; o += gridDim.y) {
         const float* part = o < 4 ? f.part + o * f.D : f.gate_part + (o - 4) * f.splits * f.D;
         void* out = o == 0 ? f.d_weight : o == 1 ? f.d_bias : o == 2 ? f.d_post_weight : o == 3 ? f.d_post_bias : f.d_gate;
@@ -561,16 +573,19 @@ __global__ void __launch_bounds__(256) res_norm_finish_kernel(const RnFinish f) 
         const int count = o < 4 ? f.grid : f.splits;
         const long long stride = o < 4 ? 4ll * f.D : f.D;
         const bool bf16 = o < 4 ? f.param_bf16 : f.gate_bf16;
-        const long long at = o < 4 ? c : (o - 4) * f.D + c;
         float a = 0.f;
         if (c < f.D)
-#pragma unroll 4
-            for (int k = w; k < count; k += 8) a += part[k * stride + c];
-        x[w][threadIdx.x & 31] = a;
+#pragma unroll 10
+            for (int k = w; k < count; k += 32) a += part[k * stride + c];
+        x[w][lane] = a;
         __syncthreads();
-        if (w == 0 && c < f.D) {
+        // warp w sums channel w of the block
+        a = x[lane][w];
 #pragma unroll
-            for (int k = 1; k < 8; ++k) a += x[k][threadIdx.x];
+        for (int s = 16; s > 0; s >>= 1) a += __shfl_xor_sync(0xffffffffu, a, s);
+        const int ch = blockIdx.x * 32 + w;
+        if (lane == 0 && ch < f.D) {
+            const long long at = o < 4 ? ch : (o - 4) * f.D + ch;
             if (bf16) reinterpret_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(a);
             else reinterpret_cast<float*>(out)[at] = a;
         }
@@ -631,9 +646,10 @@ bool element_aligned(std::initializer_list<const void*> ptrs, bpt_dtype t) {
 template <typename T, int VEC, int NE, int TPR>
 bpt_status run_fwd(const RnParams& p, cudaStream_t st) {
     constexpr int threads = cta_threads(TPR), rpc = threads / TPR;
-    constexpr size_t smem = (size_t)5 * NE * 4 * TPR;
+    constexpr size_t all = (size_t)5 * NE * 4 * TPR;
+    const size_t smem = (size_t)((p.norm ? 2 : 0) + (p.post ? 2 : 0) + (p.gate && !p.gate_each ? 1 : 0)) * NE * 4 * TPR;
     if (smem > 32 * 1024 &&     // with the static part, 48 KB is the limit without asking
-        cudaFuncSetAttribute(res_norm_fwd_kernel<T, VEC, NE, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        cudaFuncSetAttribute(res_norm_fwd_kernel<T, VEC, NE, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)all) != cudaSuccess)
         return BPT_ERR_CUDA;
     // as many CTAs as run at once: each turns the parameters to fp32 once
     const long long grid = std::min<long long>((p.rows + rpc - 1) / rpc, kRnSms * std::max(1, 1024 / threads));
@@ -749,8 +765,17 @@ extern "C" bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* a, const float* 
     f.gate_part = p.gate_part; f.d_gate = gate_sums ? d_gate : nullptr; f.groups = gate_sums ? q.groups : 0;
     if (d_weight || d_bias || d_post_weight || d_post_bias || gate_sums) {
         const dim3 grid((a->D + 31) / 32, (unsigned)std::min<long long>(4 + f.groups, 65535));
-        res_norm_finish_kernel<<<grid, 256, 0, st>>>(f);
+        cudaLaunchAttribute attr[1] = {};       // launched while the shares are still being summed, where there is room
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = grid;
+        cfg.blockDim = dim3(1024);
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = a->rows > 0 ? 1 : 0;
+        if (cudaLaunchKernelEx(&cfg, res_norm_finish_kernel, f) != cudaSuccess) return BPT_ERR_CUDA;
         trace_mark(st, "res_norm_finish");
     }
-    return cudaGetLastError() == cudaSuccess ? BPT_OK : BPT_ERR_CUDA;
+    return BPT_OK;
 }

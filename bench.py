@@ -580,7 +580,10 @@ def run_model(args):
     for n in (512, 2048, 8192):
         for k in (4, 16, 64):
             B = 8192 // n
-            enc = layer.BPTEncoder(n, k, 512, 8, 2048, 6, left_only=True, device="cuda:0").to("cuda:0", torch.bfloat16)
+            # the gated form's three matrices hold as many weights as the plain form's two
+            form = dict(gated="silu", sandwich=True) if args.form == "gated" else {}
+            d_ff = 1368 if form else 2048
+            enc = layer.BPTEncoder(n, k, 512, 8, d_ff, 6, left_only=True, device="cuda:0", **form).to("cuda:0", torch.bfloat16)
             x = torch.randn(B, n, 512, device="cuda:0", dtype=torch.bfloat16, requires_grad=True)
 
             def fwd():
@@ -604,7 +607,8 @@ def run_model(args):
                 e1.record()
                 torch.cuda.synchronize()
                 res[name] = e0.elapsed_time(e1) / steps
-            print(json.dumps({"workload": "6-layer BPT stack, d=512, d_ff=2048, 8 heads, left-only, 8192 tokens per batch, bf16",
+            print(json.dumps({"workload": "6-layer BPT stack, d=512, d_ff=%d, 8 heads, left-only, 8192 tokens per batch, bf16" % d_ff,
+                              "form": "gated (silu), sandwich norms" if form else "Algorithm 2",
                               "n": n, "k": k, "batch": B, "forward_ms": res["forward"], "forward_tokens_per_s": 8192 / (res["forward"] * 1e-3),
                               "forward_backward_ms": res["forward_backward"],
                               "forward_backward_tokens_per_s": 8192 / (res["forward_backward"] * 1e-3)}), flush=True)
@@ -625,6 +629,8 @@ def main():
     ap.add_argument("--batch", type=int, default=0, help="override the batch size (profiling of a smaller case)")
     ap.add_argument("--sweep", action="store_true", help="run the n x k scaling sweep instead: one JSON line per point")
     ap.add_argument("--model", action="store_true", help="time a 6-layer BPT stack (Sec. 4.4 setting) instead: one JSON line per point")
+    ap.add_argument("--form", default="paper", choices=["paper", "gated"],
+                    help="with --model: the layers of Algorithm 2, or gated feed-forward blocks between sandwich norms")
     args = ap.parse_args()
     args.warmup = max(args.warmup, 0)
     if args.sweep:

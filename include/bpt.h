@@ -312,7 +312,7 @@ bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const void* w_up,
  * NULL:  dR = dr + norm'(dy),  dh = alpha dR,  dn = gate dR,  db = post'(dn),  and the column sums that belong to the
  * parameters.  Everything is recomputed from h, b and the forward's `stats` (which may be NULL when neither norm is
  * there).  Outputs are overwritten; the sums are taken in a fixed order
- * without atomics, so results are bit-reproducible.  dh / db may be the buffers of dy or dr, not of h or b.
+ * without atomics, so results are bit-reproducible.  Results must not overlap inputs.
  * `workspace`: bpt_res_norm_bwd_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a
  * status block (nothing here waits), 16-byte aligned; two calls whose GPU work overlaps need one each.
  * Errors: INVALID_ARG, UNSUPPORTED (D, rows >= 2^31), WORKSPACE, CUDA.

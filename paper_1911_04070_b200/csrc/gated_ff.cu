@@ -490,7 +490,9 @@ bool launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cuda
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = first ? 0 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess) return true;
+    cudaGetLastError();     // reported by the caller's status, not by the next call of somebody else
+    return false;
 }
 template <int KERNEL, int BN, int ACT = BPT_ACT_RELU>
 bpt_status run(const FfParams& p, cudaStream_t st, const char* name) {

@@ -209,8 +209,9 @@ bpt_status run_out(const GatedFfRows& p, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, gated_ff_rows_out_kernel<NT>, (const float*)p.h, p.w_down, p.y, p.rows, p.D, p.F, parts) == cudaSuccess
-               ? BPT_OK : BPT_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, gated_ff_rows_out_kernel<NT>, (const float*)p.h, p.w_down, p.y, p.rows, p.D, p.F, parts) == cudaSuccess) return BPT_OK;
+    cudaGetLastError();     // reported by this status, not by the next call of somebody else
+    return BPT_ERR_CUDA;
 }
 template <int NT>
 bpt_status run(const GatedFfRows& p, cudaStream_t st) {

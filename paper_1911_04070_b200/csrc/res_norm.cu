@@ -774,7 +774,10 @@ extern "C" bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* a, const float* 
         cfg.stream = st;
         cfg.attrs = attr;
         cfg.numAttrs = a->rows > 0 ? 1 : 0;
-        if (cudaLaunchKernelEx(&cfg, res_norm_finish_kernel, f) != cudaSuccess) return BPT_ERR_CUDA;
+        if (cudaLaunchKernelEx(&cfg, res_norm_finish_kernel, f) != cudaSuccess) {
+            cudaGetLastError();     // reported by this status, not by the next call of somebody else
+            return BPT_ERR_CUDA;
+        }
         trace_mark(st, "res_norm_finish");
     }
     return BPT_OK;

@@ -58,7 +58,7 @@ def graph_self_attention(g: binding.Graph, q, k, v, rel_emb, scale=None, lengths
 class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, h, b, weight, bias, post_weight, post_bias, gate, norm, post_norm, alpha, eps, want_sum):
-        stats = h.new_empty((h.numel() // max(h.shape[-1], 1), 4), dtype=torch.float32)
+        stats = h.new_empty((h.numel() // max(h.shape[-1], 1) if h.dim() else 0, 4), dtype=torch.float32)
         y, r = binding.bpt_res_norm_fwd(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps, want_sum, stats=stats)
         ctx.save_for_backward(h, b, weight, bias, post_weight, post_bias, gate, stats)
         ctx.cfg = (norm, post_norm, alpha, eps)

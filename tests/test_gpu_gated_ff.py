@@ -232,6 +232,64 @@ def test_from_a_fresh_thread(rows):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("rows", [7, 200, 3000])
+def test_two_streams_at_once(rows):
+    """Calls whose work overlaps on the GPU, each with its own workspace: the same bits as one after the other."""
+    import torch
+    from paper_1911_04070_b200 import binding
+    sets = [_inputs(rows, 256, 520, 20 + i) for i in range(2)]
+    want = [(binding.bpt_gated_ff_fwd(**v),) + binding.bpt_gated_ff_bwd(**v, dy=dy) for v, dy in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(8):
+        for i, (v, dy) in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                got[i].append((binding.bpt_gated_ff_fwd(**v),) + binding.bpt_gated_ff_bwd(**v, dy=dy))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for res in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(res, want[i]))
+
+
+def test_offsets_past_32_bits():
+    """The inner rows of the last tiles lie more than 2^32 bytes and 2^31 elements into the workspace."""
+    import torch
+    from paper_1911_04070_b200 import binding
+    rows, D, F = 1_100_003, 64, 2048
+    v, dy = _inputs(rows, D, F, 16)
+    y = binding.bpt_gated_ff_fwd(**v)
+    dx, *_ = binding.bpt_gated_ff_bwd(**v, dy=dy, need_dw=False)
+    tail = slice(rows - 333, rows)
+    vt, dyt = {**v, "x": v["x"][tail].contiguous()}, dy[tail].contiguous()
+    yt, dxt = binding.bpt_gated_ff_fwd(**vt), binding.bpt_gated_ff_bwd(**vt, dy=dyt, need_dw=False)[0]
+    # the same rows in a small call: equal but for the order of fp32 sums, i.e. one step of bf16 where a rounding border is crossed
+    for a, b in ((y[tail], yt), (dx[tail], dxt)):
+        assert torch.isfinite(a).all()
+        assert ((a.double() - b.double()).abs() <= 2 * H * b.double().abs() + 1e-4 * float(b.double().abs().max())).all()
+
+
+def test_device_status_is_looked_at_when_asked(monkeypatch):
+    import torch
+    from paper_1911_04070_b200 import binding, layer
+    for rows in (5, 200):
+        v, dy = _inputs(rows, 64, 128, 17)
+        leaf = {a: t.clone().requires_grad_(True) for a, t in v.items()}
+        monkeypatch.setattr(binding, "CHECK_DEVICE_STATUS", True)
+        layer.gated_feed_forward(**v)
+        y = layer.gated_feed_forward(**leaf)
+        y.backward(dy)
+        y = layer.gated_feed_forward(**leaf)
+        monkeypatch.setattr(binding, "bpt_check", lambda ws: 5)
+        with pytest.raises(RuntimeError, match="timed out"):
+            layer.gated_feed_forward(**v)
+        with pytest.raises(RuntimeError, match="timed out"):
+            layer.gated_feed_forward(**leaf)
+        with pytest.raises(RuntimeError, match="timed out"):
+            y.backward(dy)
+        monkeypatch.undo()
+
+
 def test_only_some_gradients():
     import torch
     from paper_1911_04070_b200 import layer

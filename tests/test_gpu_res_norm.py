@@ -254,6 +254,51 @@ def test_reproducible_captured_and_on_another_stream():
         assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+def test_offsets_past_32_bits():
+    """More than 2^31 elements: the last rows are what a small call makes of them."""
+    import torch
+    from paper_1911_04070_b200 import binding
+    rows, D = 270_001, 8192
+    g = torch.Generator(device="cuda:0").manual_seed(0)
+    h = torch.empty(rows, D, dtype=torch.bfloat16, device="cuda:0").normal_(generator=g)
+    b = torch.empty_like(h).normal_(generator=g)
+    w = torch.rand(D, device="cuda:0")
+    stats = torch.empty(rows, 4, device="cuda:0")
+    kw = dict(weight=w, norm="rms", post_norm="layer", gate=w)
+    y, r = binding.bpt_res_norm_fwd(h, b, want_sum=True, stats=stats, **kw)
+    tail = slice(rows - 5, rows)
+    ht, bt, st = h[tail].clone(), b[tail].clone(), torch.empty(5, 4, device="cuda:0")
+    yt, rt = binding.bpt_res_norm_fwd(ht, bt, want_sum=True, stats=st, **kw)
+    assert torch.equal(y[tail], yt) and torch.equal(r[tail], rt) and torch.equal(stats[tail], st)
+    dh, db, *_ = binding.bpt_res_norm_bwd(h, b, y, None, stats, need=(True, True) + (False,) * 5, **kw)
+    dht, dbt, *_ = binding.bpt_res_norm_bwd(ht, bt, yt, None, st, need=(True, True) + (False,) * 5, **kw)
+    assert torch.equal(dh[tail], dht) and torch.equal(db[tail], dbt)
+
+
+def test_two_streams_at_once():
+    import torch
+    from paper_1911_04070_b200 import layer
+    sets = [_case((3, 700), 512, "bf16", "layer", "layer", (3, 1, 512), 0.5, "f32", 30 + i) for i in range(2)]
+    leaves = [{a: v.requires_grad_(True) for a, v in x.items()} for x, _, _ in sets]
+
+    def step(i):
+        r, y = layer.residual_norm(**leaves[i], **sets[i][2], return_sum=True)
+        grads = torch.autograd.grad((y, r), list(leaves[i].values()), (sets[i][1]["dy"], sets[i][1]["dr"]))
+        return [y.detach(), r.detach()] + list(grads)
+
+    want = [step(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(8):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(step(i))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for res in got[i] for a, b in zip(res, want[i]))
+
+
 def test_strided_inputs_and_gradients_reach_the_same_result():
     import torch
     from paper_1911_04070_b200 import layer

@@ -272,7 +272,7 @@ bpt_status bpt_out_proj_norm(const void* a, const void* w_o, const void* h, cons
  * Backward: from x, the weights and dy = dLoss/dy (nothing else of the forward is needed: both projections are computed
  * again, in fp32), dx [rows, D] and dw_gate, dw_up [F, D], dw_down [D, F], all bf16, overwritten.  dx may be NULL; the
  * three weight gradients are given together or are all NULL.  The inner row and the gradients of the two projections are rounded once to bf16
- * (operands of the products that follow).  Sums over rows are taken in a fixed order without atomics: bit-reproducible.
+ * (operands of the products that follow); calls of at most BPT_GATED_FF_FEW_ROWS rows keep them to about 16 bits.  Sums over rows are taken in a fixed order without atomics: bit-reproducible.
  *
  * `workspace`: bpt_gated_ff_workspace_bytes bytes (host query; 0 on invalid arguments and for rows == 0, where NULL
  * will do), 256-byte aligned; two calls whose GPU work overlaps need one each.  `status`: NULL, or a device buffer of at

@@ -25,7 +25,10 @@
 namespace bpt {
 namespace {
 
-enum FfKernel { kFfIn, kFfOut, kFfBwdIn, kFfDx, kFfDw, kFfOutSplit, kFfDxSplit };     // ..Split: the sum's range shared out, fp32 results
+// ..Split: the sum's range shared out, fp32 results.  kFfBwdInTwo: for few rows, results as two bf16 terms (value and remainder,
+// the remainders kFfTwoRows rows further on), which the products after it take one after the other.
+enum FfKernel { kFfIn, kFfOut, kFfBwdIn, kFfDx, kFfDw, kFfOutSplit, kFfDxSplit, kFfBwdInTwo };
+constexpr int kFfTwoRows = 64;                // one slice of the weight gradients
 
 constexpr int kFfPairs = 74;                  // 148 SMs
 constexpr int kFfStageBytes = 32 * 1024;      // 128 x 64 of A and up to 128 x 64 of B per CTA
@@ -37,7 +40,7 @@ constexpr int kFfK = 64;
 // thread) freed shared memory for two more stages but held the warps longer: 232 against 214 us in the first kernel,
 // 441 against 418 us in the three-accumulator one (65532 x 512, F = 2048, silu).
 template <int KERNEL> struct FfShape {
-    static constexpr bool act = KERNEL == kFfIn || KERNEL == kFfBwdIn;
+    static constexpr bool act = KERNEL == kFfIn || KERNEL == kFfBwdIn || KERNEL == kFfBwdInTwo;
     static constexpr int epi_warps = act ? 16 : 8;
     static constexpr int threads = (2 + epi_warps) * 32;            // load warp, product warp, epilogue warps
     static constexpr int stages = 5;
@@ -53,6 +56,7 @@ struct FfParams {
     int* status;
     int rows, D, F, splits, tiles;
     bool clear;             // the call's first kernel clears the status block
+    bool two;               // dG, dU and h are two terms
 };
 
 // The load thread of a CTA and the product thread of a pair go through the same slices: 64 deep, `STAGES` places in shared
@@ -66,24 +70,24 @@ template <int STAGES> struct FfLoader {
     bool ok = true;
 
     // Slices [k0, k1) of this CTA's 128 rows (columns, if *_MN: the matrix lies with that axis contiguous) from row am of A, and of
-    // its B_BYTES / 128 rows from row bn of B.
+    // its B_BYTES / 128 rows from row bn of B.  a_k, b_k: from one slice to the next (0: the same slice each time).
     template <bool A_MN, bool B_MN, int B_BYTES>
-    __device__ __forceinline__ void slices(int k0, int k1, const CUtensorMap* ma, int am, const CUtensorMap* mb, int bn) {
+    __device__ __forceinline__ void slices(int k0, int k1, const CUtensorMap* ma, int am, const CUtensorMap* mb, int bn, int a_k = kFfK, int b_k = kFfK) {
         for (int k = k0; k < k1; ++k) {
             if (!ok || !tc5::mbar_wait_fast(empty_own + 8u * st, ph ^ 1)) { ok = false; return; }     // the first round passes at once
             const uint32_t a = s_u + st * kFfStageBytes, b = a + 16384, bar = full_first + 8u * st;
             if (lead) tc5::mbar_expect_tx(full_own + 8u * st, 2 * (16384 + B_BYTES));
             if constexpr (A_MN) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) pair::load_2d(a + j * 8192, ma, am + j * 64, k * kFfK, bar);
+                for (int j = 0; j < 2; ++j) pair::load_2d(a + j * 8192, ma, am + j * 64, k * a_k, bar);
             } else {
-                pair::load_2d(a, ma, k * kFfK, am, bar);
+                pair::load_2d(a, ma, k * a_k, am, bar);
             }
             if constexpr (B_MN) {
 #pragma unroll
-                for (int j = 0; j < B_BYTES / 8192; ++j) pair::load_2d(b + j * 8192, mb, bn + j * 64, k * kFfK, bar);
+                for (int j = 0; j < B_BYTES / 8192; ++j) pair::load_2d(b + j * 8192, mb, bn + j * 64, k * b_k, bar);
             } else {
-                pair::load_2d(b, mb, k * kFfK, bn, bar);
+                pair::load_2d(b, mb, k * b_k, bn, bar);
             }
             if (++st == STAGES) { st = 0; ph ^= 1; }
         }
@@ -126,11 +130,18 @@ template <int STAGES> struct FfProducts {
     }
 };
 
+// What two fp32 values lose in their bf16 pair, as a bf16 pair; an infinite value has no remainder.
+__device__ __forceinline__ uint32_t remainder_bf16(float a, float b, uint32_t pair) {
+    const float ha = __uint_as_float(pair << 16), hb = __uint_as_float(pair & 0xffff0000u);
+    return pack_bf16(isinf(ha) ? 0.f : a - ha, isinf(hb) ? 0.f : b - hb);
+}
+
 // ACT: a choice of the whole launch, where the kernel has an activation.  BN: accumulator columns of a tile (kFfOut, kFfDx; 256 in the others: 128 of G and 128 of U)
 template <int KERNEL, int BN, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::threads, 1) gated_ff_kernel(const __grid_constant__ FfParams p) {
     using S = FfShape<KERNEL>;
     constexpr bool kOut = KERNEL == kFfOut || KERNEL == kFfOutSplit, kDx = KERNEL == kFfDx || KERNEL == kFfDxSplit;
+    constexpr bool kBwdIn = KERNEL == kFfBwdIn || KERNEL == kFfBwdInTwo, kTwo = KERNEL == kFfBwdInTwo;
     constexpr bool kPart = KERNEL == kFfDw || KERNEL == kFfOutSplit || KERNEL == kFfDxSplit;      // writes fp32 sums of part of the range
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // the same offset in both CTAs
@@ -139,7 +150,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     auto empty = [&](int i) { return bar_u + 8u * (uint32_t)(S::stages + i); };
     auto tfull = [&](int i) { return bar_u + 8u * (uint32_t)(2 * S::stages + i); };
     auto tempty = [&](int i) { return bar_u + 8u * (uint32_t)(2 * S::stages + 2 + i); };
-    // kFfBwdIn: pair 0 of tfull / tempty belongs to G | U, pair 1 to dH
+    // G, U and dH: pair 0 of tfull / tempty belongs to G | U, pair 1 to dH
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::bar_off + 8 * (2 * S::stages + 4));
     volatile int* abort_s = reinterpret_cast<volatile int*>(tmem_slot + 1);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -160,8 +171,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     tc5::fence_after_sync();
     const uint32_t tbase = *tmem_slot;
 
-    const int kd = (p.D + kFfK - 1) / kFfK, kf = (p.F + kFfK - 1) / kFfK, km = (p.rows + kFfK - 1) / kFfK;
-    const int n_tiles = kOut || kDx ? (p.D + BN - 1) / BN : KERNEL == kFfBwdIn ? (p.F + 255) / 256 : (p.F + 127) / 128;   // along the output's columns
+    const int kd = (p.D + kFfK - 1) / kFfK, kf = (p.F + kFfK - 1) / kFfK, km = p.two ? 2 : (p.rows + kFfK - 1) / kFfK;
+    const int n_tiles = kOut || kDx ? (p.D + BN - 1) / BN : kBwdIn ? (p.F + 255) / 256 : (p.F + 127) / 128;   // along the output's columns
     const int dw_n0 = (p.D + 255) / 256, dw_n1 = (p.F + 255) / 256, dw_tiles = dw_n0 * dw_n1;             // weight gradients, each of the three
     struct Tile { int m, n, k0, k1, job, split, halves; };      // corner, slices, and which product
     auto tile_of = [&](int t) {
@@ -174,7 +185,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
             q.m = v / nn * 256; q.n = v % nn * 256;
             q.k0 = (int)((long long)km * q.split / p.splits); q.k1 = (int)((long long)km * (q.split + 1) / p.splits);
         } else {
-            q.k1 = KERNEL == kFfIn ? kd : kOut ? kf : 2 * kf;
+            q.k1 = KERNEL == kFfIn ? kd : kOut ? kf : p.two ? 4 * kf : 2 * kf;
             if constexpr (kPart) {
                 const int per = p.tiles / p.splits, all = q.k1;
                 q.split = t / per;
@@ -182,8 +193,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                 q.k0 = all * q.split / p.splits; q.k1 = all * (q.split + 1) / p.splits;
             }
             q.m = t / n_tiles * 256;
-            q.n = t % n_tiles * (kOut || kDx ? BN : KERNEL == kFfBwdIn ? 256 : 128);
-            q.halves = p.F - q.n > 128 ? 2 : 1;         // kFfBwdIn
+            q.n = t % n_tiles * (kOut || kDx ? BN : kBwdIn ? 256 : 128);
+            q.halves = p.F - q.n > 128 ? 2 : 1;         // of G | U
         }
         return q;
     };
@@ -204,15 +215,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                 ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n);
             } else if constexpr (kOut) {
                 ld.template slices<false, false, BN * 64>(q.k0, q.k1, &p.a0, m, &p.b0, n);
-            } else if constexpr (KERNEL == kFfBwdIn) {      // dH: dy rows, Wd with its F axis contiguous
+            } else if constexpr (kBwdIn) {      // dH: dy rows, Wd with its F axis contiguous
                 ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n);
                 ld.template slices<false, true, 16384>(0, kd, &p.a1, m, &p.b2, n);
                 if (q.halves == 2) ld.template slices<false, false, 16384>(0, kd, &p.a0, m, one ? &p.b0 : &p.b1, q.n + 128);
-            } else if constexpr (kDx) {         // dG Wg, then dU Wu
-                ld.template slices<false, true, BN * 64>(q.k0, q.k1 < kf ? q.k1 : kf, &p.a0, m, &p.b0, n);
-                ld.template slices<false, true, BN * 64>(q.k0 < kf ? 0 : q.k0 - kf, q.k1 - kf, &p.a1, m, &p.b1, n);
+            } else if constexpr (kDx) {         // dG Wg, then dU Wu; with two terms the same for the remainders
+                for (int seg = 0; seg < (p.two ? 4 : 2); ++seg) {
+                    const int lo = q.k0 - seg * kf, hi = q.k1 - seg * kf;
+                    ld.template slices<false, true, BN * 64>(lo < 0 ? 0 : lo, hi < kf ? hi : kf, seg & 1 ? &p.a1 : &p.a0, m + (seg >> 1) * kFfTwoRows,
+                                                             seg & 1 ? &p.b1 : &p.b0, n);
+                }
             } else {
-                ld.template slices<true, true, 16384>(q.k0, q.k1, q.job == 0 ? &p.a0 : q.job == 1 ? &p.a1 : &p.a2, m, q.job < 2 ? &p.b0 : &p.b1, n);
+                // with two terms x and dy meet both slices of the other operand
+                ld.template slices<true, true, 16384>(q.k0, q.k1, q.job == 0 ? &p.a0 : q.job == 1 ? &p.a1 : &p.a2, m, q.job < 2 ? &p.b0 : &p.b1, n,
+                                                      p.two && q.job == 2 ? 0 : kFfK, p.two && q.job < 2 ? 0 : kFfK);
             }
         }
         // the releases of the last slices still arrive in this CTA's shared memory: see them in before it ends
@@ -230,7 +246,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
         int i = 0, gu = 0;      // tiles, G | U accumulators so far
         for (int t = pair_id; t < p.tiles && mm.ok; t += n_pairs, ++i) {
             const Tile q = tile_of(t);
-            if constexpr (KERNEL == kFfBwdIn) {     // each accumulator has one place: what was there before has to be out
+            if constexpr (kBwdIn) {     // each accumulator has one place: what was there before has to be out
                 for (int phase = 0; phase < 1 + q.halves && mm.ok; ++phase) {
                     if (phase == 1) {
                         if (i > 0) mm.wait(tempty(1), (i - 1) & 1);
@@ -273,7 +289,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                 tc5::fence_after_sync();
                 return true;
             };
-            if (KERNEL != kFfBwdIn && !ready(i & 1, (i / 2) & 1)) break;
+            if (!kBwdIn && !ready(i & 1, (i / 2) & 1)) break;
             const int row = q.m + rank * 128 + quad * 32;
             auto done = [&](uint32_t bar) {           // this warp has taken (its part of) an accumulator out
                 tc5::fence_before_sync();
@@ -316,7 +332,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                     put64(i & 1, j, x[0], x[1], x[2], x[3]);
                 }
                 send(&p.c0, i & 1, q.n + part * 32, p.F, p.rows);
-            } else if constexpr (KERNEL == kFfBwdIn) {
+            } else if constexpr (kBwdIn) {
                 const uint32_t src = tbase + lane_base + part * 32;
 #pragma unroll 1
                 for (int half = 0; half < q.halves; ++half, ++gu) {
@@ -330,6 +346,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                     // What does not need dH comes first, and the inner row with it: the first half's dH is still being summed then,
                     // and the second half's products must not wait for this.  g becomes act(g), u becomes u act'(g).
                     const int col = q.n + half * 128 + part * 32;
+                    const bool inside = col < p.F && row < (kTwo ? kFfTwoRows : p.rows);
+                    // Two terms: the rows between the last one and kFfTwoRows are summed over too and hold zeros, whatever the weights.
+                    const bool real = !kTwo || row + lane < p.rows;
+                    uint32_t rem[kTwo ? 32 : 1];        // remainders: of h, then of dG and dU
                     if (lane == 0) pair::store_wait_read<0>();
                     __syncwarp();
 #pragma unroll
@@ -348,11 +368,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                                 g[k] = __float_as_uint(a);
                                 u[k] = __float_as_uint(uv * da);
                             }
-                            x[y] = pack_bf16(r[0], r[1]);
+                            x[y] = real ? pack_bf16(r[0], r[1]) : 0;
+                            if constexpr (kTwo) rem[j * 4 + y] = real ? remainder_bf16(r[0], r[1], x[y]) : 0;
                         }
                         put64(0, j, x[0], x[1], x[2], x[3]);
+                        if constexpr (kTwo) put64(1, j, rem[j * 4], rem[j * 4 + 1], rem[j * 4 + 2], rem[j * 4 + 3]);
                     }
-                    send(&p.c2, 0, col, p.F, p.rows);
+                    tc5::fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (inside) {
+                            pair::store_2d(&p.c2, col, row, stg_u);
+                            if (kTwo) pair::store_2d(&p.c2, col, row + kFfTwoRows, stg_u + S::tile_bytes);
+                        }
+                        pair::store_commit();
+                    }
                     if (half == 0 && !ready(1, i & 1)) break;
                     if (lane == 0) pair::store_wait_read<0>();      // the inner row has left its tile
                     __syncwarp();
@@ -369,8 +399,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                             for (int y = 0; y < 4; ++y) {
                                 const int k = c + j * 8 + 2 * y;
                                 const float d0 = __uint_as_float(dh[j * 8 + 2 * y]), d1 = __uint_as_float(dh[j * 8 + 2 * y + 1]);
-                                o[0][y] = pack_bf16(d0 * __uint_as_float(u[k]), d1 * __uint_as_float(u[k + 1]));
-                                o[1][y] = pack_bf16(d0 * __uint_as_float(g[k]), d1 * __uint_as_float(g[k + 1]));
+                                const float r[2][2] = {{d0 * __uint_as_float(u[k]), d1 * __uint_as_float(u[k + 1])},
+                                                       {d0 * __uint_as_float(g[k]), d1 * __uint_as_float(g[k + 1])}};
+#pragma unroll
+                                for (int m = 0; m < 2; ++m) {
+                                    o[m][y] = real ? pack_bf16(r[m][0], r[m][1]) : 0;
+                                    if constexpr (kTwo) rem[m * 16 + k / 2] = real ? remainder_bf16(r[m][0], r[m][1], o[m][y]) : 0;
+                                }
                             }
 #pragma unroll
                             for (int m = 0; m < 2; ++m) put64(m, c / 8 + j, o[m][0], o[m][1], o[m][2], o[m][3]);
@@ -379,11 +414,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                     tc5::fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        if (col < p.F && row < p.rows) {
+                        if (inside) {
                             pair::store_2d(&p.c0, col, row, stg_u);
                             pair::store_2d(&p.c1, col, row, stg_u + S::tile_bytes);
                         }
                         pair::store_commit();
+                    }
+                    if constexpr (kTwo) {
+                        if (lane == 0) pair::store_wait_read<0>();
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) put64(j / 4, j % 4, rem[j * 4], rem[j * 4 + 1], rem[j * 4 + 2], rem[j * 4 + 3]);
+                        tc5::fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (inside) {
+                                pair::store_2d(&p.c0, col, row + kFfTwoRows, stg_u);
+                                pair::store_2d(&p.c1, col, row + kFfTwoRows, stg_u + S::tile_bytes);
+                            }
+                            pair::store_commit();
+                        }
                     }
                 }
             } else if constexpr (kPart) {
@@ -560,6 +610,11 @@ size_t part_bytes(long long rows, int D, int slices) {
     const OutPlan q = plan_out(rows, D, slices);
     return q.splits > 1 ? (size_t)q.splits * rows * D * 4 : 0;
 }
+// The backward's inner results: few rows keep two bf16 terms each, which costs nothing next to the launches and leaves the
+// results' own rounding the only one that shows; more rows keep one (a third of the memory traffic, half of the products).
+int bwd_terms(long long rows) { return rows <= kGatedFfFewRows ? 2 : 1; }
+long long bwd_inner_rows(long long rows) { return bwd_terms(rows) == 2 ? 2 * kFfTwoRows : rows; }
+static_assert(kGatedFfFewRows <= kFfTwoRows, "the remainders' place");
 int slices_of(int n) { return (n + kFfK - 1) / kFfK; }
 
 }  // namespace
@@ -569,10 +624,10 @@ using namespace bpt;
 
 extern "C" size_t bpt_gated_ff_workspace_bytes(int64_t rows, int32_t D, int32_t F, int backward) {
     if (check_ff(rows, D, F, BPT_ACT_RELU) != BPT_OK || rows == 0) return 0;
-    const size_t hidden = inner_bytes(rows, F);
-    if (!backward) return rows <= kGatedFfFewRows ? (size_t)rows * F * 4 : hidden + part_bytes(rows, D, slices_of(F));
+    if (!backward) return rows <= kGatedFfFewRows ? (size_t)rows * F * 4 : inner_bytes(rows, F) + part_bytes(rows, D, slices_of(F));
     // the partial sums of dx and of the weight gradients share their place
-    return 3 * hidden + std::max((size_t)3 * dw_splits(rows, D, F) * D * F * 4, part_bytes(rows, D, 2 * slices_of(F)));
+    return 3 * inner_bytes(bwd_inner_rows(rows), F) +
+           std::max((size_t)3 * dw_splits(rows, D, F) * D * F * 4, part_bytes(rows, D, bwd_terms(rows) * 2 * slices_of(F)));
 }
 
 extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y, int64_t rows,
@@ -638,7 +693,8 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     if (!workspace || workspace_bytes < bpt_gated_ff_workspace_bytes(rows, D, F, 1)) return BPT_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255) return BPT_ERR_INVALID_ARG;
     if (!tc5::encode_tiled() || !tc5::context_current()) return BPT_ERR_CUDA;
-    const size_t hidden = inner_bytes(rows, F);
+    const long long inner = bwd_inner_rows(rows);
+    const size_t hidden = inner_bytes(inner, F);
     char *dg = static_cast<char*>(workspace), *du = dg + hidden, *h = du + hidden;
     float* part = reinterpret_cast<float*>(h + hidden);
     const int mt = (int)((rows + 255) / 256);
@@ -649,15 +705,16 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     const int ld = inner_ld(F);
     if (!bf16_map(&p.a0, x, rows, D, 128) || !bf16_map(&p.a1, dy, rows, D, 128) || !bf16_map(&p.b0, w_gate, F, D, 128) ||
         !bf16_map(&p.b1, w_up, F, D, 128) || !bf16_map(&p.b2, w_down, D, F, 64) ||
-        !bf16_map(&p.c0, dg, rows, F, 32, 32, ld) || !bf16_map(&p.c1, du, rows, F, 32, 32, ld) || !bf16_map(&p.c2, h, rows, F, 32, 32, ld))
+        !bf16_map(&p.c0, dg, inner, F, 32, 32, ld) || !bf16_map(&p.c1, du, inner, F, 32, 32, ld) || !bf16_map(&p.c2, h, inner, F, 32, 32, ld))
         return BPT_ERR_CUDA;
     p.tiles = mt * ((F + 255) / 256);
-    bpt_status e = run_act<kFfBwdIn>(p, act, st, "gated_ff_bwd_in");
+    p.two = bwd_terms(rows) == 2;
+    bpt_status e = p.two ? run_act<kFfBwdInTwo>(p, act, st, "gated_ff_bwd_in") : run_act<kFfBwdIn>(p, act, st, "gated_ff_bwd_in");
     if (e != BPT_OK) return e;
     p.clear = false;
     if (dx) {
-        const OutPlan o = plan_out(rows, D, 2 * slices_of(F));
-        if (!bf16_map(&p.a0, dg, rows, F, 128, 64, ld) || !bf16_map(&p.a1, du, rows, F, 128, 64, ld) || !bf16_map(&p.b0, w_gate, F, D, 64) ||
+        const OutPlan o = plan_out(rows, D, bwd_terms(rows) * 2 * slices_of(F));
+        if (!bf16_map(&p.a0, dg, inner, F, 128, 64, ld) || !bf16_map(&p.a1, du, inner, F, 128, 64, ld) || !bf16_map(&p.b0, w_gate, F, D, 64) ||
             !bf16_map(&p.b1, w_up, F, D, 64) ||
             !(o.splits > 1 ? part_map(&p.c0, part, o.splits, (int)rows, D) : bf16_map(&p.c0, dx, rows, D, 32)))
             return BPT_ERR_CUDA;
@@ -671,8 +728,8 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     }
     if (weights) {
         p.splits = dw_splits(rows, D, F);
-        if (!bf16_map(&p.a0, dg, rows, F, 64, 64, ld) || !bf16_map(&p.a1, du, rows, F, 64, 64, ld) || !bf16_map(&p.a2, dy, rows, D, 64) ||
-            !bf16_map(&p.b0, x, rows, D, 64) || !bf16_map(&p.b1, h, rows, F, 64, 64, ld) || !part_map(&p.c0, part, 2 * p.splits, F, D) ||
+        if (!bf16_map(&p.a0, dg, inner, F, 64, 64, ld) || !bf16_map(&p.a1, du, inner, F, 64, 64, ld) || !bf16_map(&p.a2, dy, rows, D, 64) ||
+            !bf16_map(&p.b0, x, rows, D, 64) || !bf16_map(&p.b1, h, inner, F, 64, 64, ld) || !part_map(&p.c0, part, 2 * p.splits, F, D) ||
             !part_map(&p.c1, part + (size_t)2 * p.splits * D * F, p.splits, D, F))
             return BPT_ERR_CUDA;
         p.tiles = 3 * ((D + 255) / 256) * ((F + 255) / 256) * p.splits;

@@ -91,6 +91,24 @@ def test_large_scores():
     _check(*_inputs(130, 128, 256, 6, scale=300.0), "gelu")
 
 
+@pytest.mark.parametrize("rows", [1, 2, 31, 32, 33, 63, 64])
+@pytest.mark.parametrize("D,F", [(8, 8), (72, 136), (512, 1368)])
+def test_few_rows_round_once(rows, D, F):
+    """Up to 64 rows the operands of the second products keep 16 bits (two bf16 terms, remainder 2^-17): what is left is the
+    rounding of the result, 2^-8, and 8 deviations of the remainders' rounding and of fp32 sums."""
+    import torch
+    from oracle import bpt_layer
+    from paper_1911_04070_b200 import binding
+    v, dy = _inputs(rows, D, F, rows + D)
+    got = (binding.bpt_gated_ff_fwd(**v, act="gelu"),) + binding.bpt_gated_ff_bwd(**v, dy=dy, act="gelu")
+    d = {a: t.double().requires_grad_(True) for a, t in v.items()}
+    y = bpt_layer.gated_ff(**d, act="gelu")
+    want = (y.detach(),) + torch.autograd.grad(y, list(d.values()), dy.double())
+    for name, a, b in zip(("y", "dx", "dw_gate", "dw_up", "dw_down"), got, want):
+        err = (a.double() - b).abs()
+        assert (err <= H * b.abs() * (1 + H) + 2.0 ** -13 * b.abs().max()).all(), (name, float(err.max()))
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
 @pytest.mark.parametrize("rows", [1, 8, 40000])
 def test_activations_on_their_own(act, rows):

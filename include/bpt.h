@@ -265,14 +265,15 @@ bpt_status bpt_out_proj_norm(const void* a, const void* w_o, const void* h, cons
  * x, y: [rows, D]; w_gate, w_up: [F, D]; w_down: [D, F] (the layout of a linear layer's weight); all bf16, contiguous and
  * 16-byte aligned.  act: BPT_ACT_RELU, BPT_ACT_SILU (g / (1 + exp(-g))) or BPT_ACT_GELU (g/2 (1 + erf(g / sqrt 2))).
  * Both projections, the activation and the product run in one kernel, which rounds the inner row act(..) * (..) once
- * to bf16 (the second product's operand type); products accumulate in fp32; y is rounded once.  Calls of at most
- * BPT_GATED_FF_FEW_ROWS rows (decoding) keep the inner row to about 16 bits instead and need no tensor-memory kernel.
+ * to bf16 (the second product's operand type); products accumulate in fp32; y is rounded once.  Calls for which
+ * bpt_gated_ff_few_rows (host) says 1 -- few rows for the size of the weights, as in decoding -- keep the inner row to about
+ * 16 bits instead, and their kernels wait for nothing.
  * rows >= 0, D and F multiples of 8 (16-byte rows).  x and y must not overlap.
  *
  * Backward: from x, the weights and dy = dLoss/dy (nothing else of the forward is needed: both projections are computed
  * again, in fp32), dx [rows, D] and dw_gate, dw_up [F, D], dw_down [D, F], all bf16, overwritten.  dx may be NULL; the
  * three weight gradients are given together or are all NULL.  The inner row and the gradients of the two projections are rounded once to bf16
- * (operands of the products that follow); calls of at most BPT_GATED_FF_FEW_ROWS rows keep them to about 16 bits.  Sums over rows are taken in a fixed order without atomics: bit-reproducible.
+ * (operands of the products that follow); calls of at most 64 rows keep them to about 16 bits.  Sums over rows are taken in a fixed order without atomics: bit-reproducible.
  *
  * `workspace`: bpt_gated_ff_workspace_bytes bytes (host query; 0 on invalid arguments and for rows == 0, where NULL
  * will do), 256-byte aligned; two calls whose GPU work overlaps need one each.  `status`: NULL, or a device buffer of at
@@ -280,8 +281,8 @@ bpt_status bpt_out_proj_norm(const void* a, const void* w_o, const void* h, cons
  * outlive the call's work).
  * Errors: INVALID_ARG, UNSUPPORTED (sizes), WORKSPACE, CUDA; device-side: see bpt_check.
  */
-#define BPT_GATED_FF_FEW_ROWS 64 /* forward calls of at most so many rows run kernels that wait for nothing */
 enum { BPT_ACT_RELU = 0, BPT_ACT_SILU = 1, BPT_ACT_GELU = 2 };
+int32_t bpt_gated_ff_few_rows(int64_t rows, int32_t D, int32_t F);
 size_t bpt_gated_ff_workspace_bytes(int64_t rows, int32_t D, int32_t F, int backward);
 bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y,
                             int64_t rows, int32_t D, int32_t F, int32_t act, void* status, void* workspace,

@@ -21,14 +21,14 @@ BPT_F32, BPT_BF16 = 0, 1
 BPT_PATH_AUTO, BPT_PATH_MMA, BPT_PATH_TC5 = 0, 1, 2
 NORM_KINDS = {None: 0, "layer": 1, "rms": 2}   # BPT_NORM_*
 ACTIVATIONS = {"relu": 0, "silu": 1, "gelu": 2}        # BPT_ACT_*
-GATED_FF_FEW_ROWS = 64   # BPT_GATED_FF_FEW_ROWS: forward calls of at most so many rows hold no device-side wait
 
 EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes", "bpt_attn_fwd",
            "bpt_attn_bwd", "bpt_status_str", "bpt_trace_begin", "bpt_trace_end",
            "bpt_static_scratch_bytes", "bpt_attn_bwd_static_scratch", "bpt_attn_fwd_varlen", "bpt_attn_bwd_varlen",
            "bpt_attn_fwd_ex", "bpt_attn_bwd_ex", "bpt_attn_fwd_rows", "bpt_attn_bwd_min_workspace_bytes", "bpt_check",
            "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
-           "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd")
+           "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd",
+           "bpt_gated_ff_few_rows")
 
 
 class BptError(RuntimeError):
@@ -100,6 +100,8 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_res_norm_bwd.restype = ctypes.c_int
         lib.bpt_res_norm_bwd.argtypes = [rn, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         i64 = ctypes.c_int64
+        lib.bpt_gated_ff_few_rows.restype = i32
+        lib.bpt_gated_ff_few_rows.argtypes = [i64, i32, i32]
         lib.bpt_gated_ff_workspace_bytes.restype = sz
         lib.bpt_gated_ff_workspace_bytes.argtypes = [i64, i32, i32, ctypes.c_int]
         lib.bpt_gated_ff_fwd.restype = ctypes.c_int
@@ -303,7 +305,7 @@ def bpt_gated_ff_fwd(x, w_gate, w_up, w_down, act: str = "silu", y=None, workspa
     with _on_device(dev):
         y = torch.empty_like(x) if y is None else y
         workspace = _scratch(workspace, lib.bpt_gated_ff_workspace_bytes(rows, D, F, 0), x)
-        status = x.new_empty(256, dtype=torch.uint8) if rows > GATED_FF_FEW_ROWS else None
+        status = None if lib.bpt_gated_ff_few_rows(rows, D, F) else x.new_empty(256, dtype=torch.uint8)
         y._bpt_workspace = status
         _check(lib.bpt_gated_ff_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y.data_ptr(), rows, D, F,
                                     ACTIVATIONS[act], _ptr(status), workspace.data_ptr(), workspace.numel(), _raw_stream(dev)),

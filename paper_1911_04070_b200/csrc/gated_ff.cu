@@ -612,9 +612,8 @@ size_t part_bytes(long long rows, int D, int slices) {
 }
 // The backward's inner results: few rows keep two bf16 terms each, which costs nothing next to the launches and leaves the
 // results' own rounding the only one that shows; more rows keep one (a third of the memory traffic, half of the products).
-int bwd_terms(long long rows) { return rows <= kGatedFfFewRows ? 2 : 1; }
+int bwd_terms(long long rows) { return rows <= kFfTwoRows ? 2 : 1; }
 long long bwd_inner_rows(long long rows) { return bwd_terms(rows) == 2 ? 2 * kFfTwoRows : rows; }
-static_assert(kGatedFfFewRows <= kFfTwoRows, "the remainders' place");
 int slices_of(int n) { return (n + kFfK - 1) / kFfK; }
 
 }  // namespace
@@ -622,9 +621,13 @@ int slices_of(int n) { return (n + kFfK - 1) / kFfK; }
 
 using namespace bpt;
 
+extern "C" int32_t bpt_gated_ff_few_rows(int64_t rows, int32_t D, int32_t F) {
+    return check_ff(rows, D, F, BPT_ACT_RELU) == BPT_OK && gated_ff_few_rows(rows, D, F);
+}
+
 extern "C" size_t bpt_gated_ff_workspace_bytes(int64_t rows, int32_t D, int32_t F, int backward) {
     if (check_ff(rows, D, F, BPT_ACT_RELU) != BPT_OK || rows == 0) return 0;
-    if (!backward) return rows <= kGatedFfFewRows ? (size_t)rows * F * 4 : inner_bytes(rows, F) + part_bytes(rows, D, slices_of(F));
+    if (!backward) return gated_ff_few_rows(rows, D, F) ? (size_t)rows * F * 4 : inner_bytes(rows, F) + part_bytes(rows, D, slices_of(F));
     // the partial sums of dx and of the weight gradients share their place
     return 3 * inner_bytes(bwd_inner_rows(rows), F) +
            std::max((size_t)3 * dw_splits(rows, D, F) * D * F * 4, part_bytes(rows, D, bwd_terms(rows) * 2 * slices_of(F)));
@@ -640,7 +643,7 @@ extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const 
     if (!workspace || workspace_bytes < bpt_gated_ff_workspace_bytes(rows, D, F, 0)) return BPT_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255) return BPT_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (rows <= kGatedFfFewRows) {
+    if (gated_ff_few_rows(rows, D, F)) {
         const GatedFfRows q{static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(w_gate), static_cast<const __nv_bfloat16*>(w_up),
                             static_cast<const __nv_bfloat16*>(w_down), static_cast<__nv_bfloat16*>(y), static_cast<float*>(workspace),
                             static_cast<int*>(status), (int)rows, D, F, act};

@@ -72,9 +72,10 @@ def test_oracle_against_torch_and_differences(act):
         assert abs(got - want) <= 1e-6 * (1 + abs(want)), (name, got, want)     # 1e-16 * |loss| / step, and step^2
 
 
-def test_few_rows_constant_matches_the_header():
-    import os
-    import re
-    from paper_1911_04070_b200 import binding
-    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "bpt.h")).read()
-    assert int(re.search(r"#define BPT_GATED_FF_FEW_ROWS (\d+)", text).group(1)) == binding.GATED_FF_FEW_ROWS
+def test_few_rows_rule(lib):
+    f = lib.bpt_gated_ff_few_rows
+    assert f(1, 512, 2048) and f(64, 512, 2048) and not f(65, 512, 2048)
+    assert f(8, 4096, 11008) and not f(9, 4096, 11008)           # a pass over large weights pays for eight rows
+    assert f(256, 64, 128) and not f(257, 64, 128)
+    assert not f(4, 60, 128) and not f(-1, 64, 128)              # invalid sizes
+    assert lib.bpt_gated_ff_workspace_bytes(64, 512, 2048, 0) == 64 * 2048 * 4

@@ -77,6 +77,12 @@ def test_row_counts(rows, D, F):
     _check(*_inputs(rows, D, F, rows), "silu")
 
 
+@pytest.mark.parametrize("rows,D,F", [(8, 1024, 4096), (9, 1024, 4096), (17, 1024, 4096), (64, 1024, 4096), (65, 64, 136), (256, 64, 136), (257, 64, 136),
+                                      (200, 256, 1024), (128, 264, 520), (33, 1200, 3000)])
+def test_on_both_sides_of_the_few_rows_rule(rows, D, F):
+    _check(*_inputs(rows, D, F, rows + F), "silu")
+
+
 def test_many_tiles_per_pair():
     _check(*_inputs(20011, 256, 520, 3), "silu")
 
@@ -290,7 +296,7 @@ def test_offsets_past_32_bits():
 def test_device_status_is_looked_at_when_asked(monkeypatch):
     import torch
     from paper_1911_04070_b200 import binding, layer
-    for rows in (5, 200):
+    for rows in (5, 300):
         v, dy = _inputs(rows, 64, 128, 17)
         leaf = {a: t.clone().requires_grad_(True) for a, t in v.items()}
         monkeypatch.setattr(binding, "CHECK_DEVICE_STATUS", True)

@@ -8,11 +8,11 @@
 //
 // All five products run in one kernel template on pairs of CTAs (pair_tools.cuh): a load warp per CTA brings 64-deep
 // slices of both operands in with TMA, one thread of the pair issues tcgen05 products of 256 rows x up to 256 columns,
-// eight or sixteen epilogue warps per CTA take finished accumulators out of tensor memory while the next tile's products run
-// (two accumulators of 256 columns; in the three-accumulator kernel dH is double and G | U single, and a tile's dH
-// products cover the time in which G | U of the tile before move to registers).  Operands that a product needs transposed are read as they lie: the matrix
-// descriptors take either axis as the contiguous one, so no transposed copy exists anywhere.  Ragged edges are TMA's: what lies outside a tensor reads
-// as zero and is not written.  Every wait is bounded; a give-up is reported through the status word.
+// eight or sixteen epilogue warps per CTA take finished accumulators out of tensor memory while the next tile's products run: two
+// accumulators of 256 columns, in the three-accumulator kernel one for G | U of 128 columns and one for dH of 256 (a tile is
+// G | U of its first half, dH, G | U of its second half).  Operands that a product needs transposed are read as they lie: the matrix
+// descriptors take either axis as the contiguous one, so no transposed copy exists anywhere.  Ragged edges are TMA's: what lies
+// outside a tensor reads as zero and is not written.  Every wait is bounded; a give-up is reported through the status word.
 #include <algorithm>
 
 #include "bpt_internal.cuh"
@@ -55,6 +55,7 @@ struct FfParams {
     CUtensorMap a0, a1, a2, b0, b1, b2, c0, c1, c2;
     int* status;
     int rows, D, F, splits, tiles;
+    int step;               // kFfBwdIn: columns of a tile, 256 or 128 (its first half only)
     bool clear;             // the call's first kernel clears the status block
     bool two;               // dG, dU and h are two terms
 };
@@ -170,9 +171,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     pair::cluster_sync();
     tc5::fence_after_sync();
     const uint32_t tbase = *tmem_slot;
+    // From here on the kernel before has ended and its results are visible; every thread waits, so that no bounded wait below
+    // counts that kernel's time.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const int kd = (p.D + kFfK - 1) / kFfK, kf = (p.F + kFfK - 1) / kFfK, km = p.two ? 2 : (p.rows + kFfK - 1) / kFfK;
-    const int n_tiles = kOut || kDx ? (p.D + BN - 1) / BN : kBwdIn ? (p.F + 255) / 256 : (p.F + 127) / 128;   // along the output's columns
+    const int n_tiles = kOut || kDx ? (p.D + BN - 1) / BN : kBwdIn ? (p.F + p.step - 1) / p.step : (p.F + 127) / 128;   // along the output's columns
     const int dw_n0 = (p.D + 255) / 256, dw_n1 = (p.F + 255) / 256, dw_tiles = dw_n0 * dw_n1;             // weight gradients, each of the three
     struct Tile { int m, n, k0, k1, job, split, halves; };      // corner, slices, and which product
     auto tile_of = [&](int t) {
@@ -193,8 +197,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                 q.k0 = all * q.split / p.splits; q.k1 = all * (q.split + 1) / p.splits;
             }
             q.m = t / n_tiles * 256;
-            q.n = t % n_tiles * (kOut || kDx ? BN : kBwdIn ? 256 : 128);
-            q.halves = p.F - q.n > 128 ? 2 : 1;         // of G | U
+            q.n = t % n_tiles * (kOut || kDx ? BN : kBwdIn ? p.step : 128);
+            q.halves = p.step == 256 && p.F - q.n > 128 ? 2 : 1;         // of G | U
         }
         return q;
     };
@@ -203,9 +207,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     // read every row of A once per pair and was 17 % slower in the long products).
     if (w == 0 && lane == 0) {
         // =============== load thread ===============
-        // The kernel before has ended and its results are visible.  This thread's loads are all that read them, and whatever this
-        // kernel writes follows from its loads.
-        asm volatile("griddepcontrol.wait;" ::: "memory");
         FfLoader<S::stages> ld{s_u, pair::in_first(full(0)), full(0), empty(0), rank == 0};
         const bool one = rank == 0;
         for (int t = pair_id; t < p.tiles && ld.ok; t += n_pairs) {
@@ -710,7 +711,9 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
         !bf16_map(&p.b1, w_up, F, D, 128) || !bf16_map(&p.b2, w_down, D, F, 64) ||
         !bf16_map(&p.c0, dg, inner, F, 32, 32, ld) || !bf16_map(&p.c1, du, inner, F, 32, 32, ld) || !bf16_map(&p.c2, h, inner, F, 32, 32, ld))
         return BPT_ERR_CUDA;
-    p.tiles = mt * ((F + 255) / 256);
+    // tiles of one half while whole ones leave half of the pairs idle: 16 slices of products one after the other instead of 24
+    p.step = mt * ((F + 255) / 256) * 2 <= kFfPairs ? 128 : 256;
+    p.tiles = mt * ((F + p.step - 1) / p.step);
     p.two = bwd_terms(rows) == 2;
     bpt_status e = p.two ? run_act<kFfBwdInTwo>(p, act, st, "gated_ff_bwd_in") : run_act<kFfBwdIn>(p, act, st, "gated_ff_bwd_in");
     if (e != BPT_OK) return e;

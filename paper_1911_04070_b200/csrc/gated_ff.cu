@@ -646,7 +646,7 @@ extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const 
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (gated_ff_few_rows(rows, D, F)) {
         const GatedFfRows q{static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(w_gate), static_cast<const __nv_bfloat16*>(w_up),
-                            static_cast<const __nv_bfloat16*>(w_down), static_cast<__nv_bfloat16*>(y), static_cast<float*>(workspace),
+                            static_cast<const __nv_bfloat16*>(w_down), static_cast<__nv_bfloat16*>(y), static_cast<__nv_bfloat16*>(workspace),
                             static_cast<int*>(status), (int)rows, D, F, act};
         return launch_gated_ff_rows(q, st);
     }

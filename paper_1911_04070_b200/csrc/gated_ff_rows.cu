@@ -7,10 +7,11 @@
 // 16 columns as long as both operands take the same ones, so lane t of a row takes columns 8 t .. 8 t + 7 of a 32-column
 // chunk, half of them for each of two products.  No shared memory, no barrier stands between memory and the tensor cores.
 //   kernel 1: a CTA has 16 rows of Wg and of Wu, its eight warps share out the columns, their sums meet in shared memory, where
-//             the activation and the product follow; h stays fp32.
+//             the activation and the product follow; h is stored as two bf16 terms, h = hi + lo, so that it is not rounded to
+//             bf16 at all (16 bits are left) and kernel 2 has its operand ready.
 //   kernel 2: a cluster of CTAs has 16 rows of Wd and shares out its F columns, the sums of its CTAs meet through distributed
 //             shared memory in rank order.  It is launched early (programmatic dependent launch) and has its first weights in
-//             registers when kernel 1 ends.  h enters as two bf16 terms, h = hi + lo, so it is not rounded to bf16 at all.
+//             registers when kernel 1 ends.
 // Sums run in a fixed order: bit-reproducible.
 #include <algorithm>
 
@@ -40,8 +41,8 @@ __device__ __forceinline__ void mma32(float (&c)[4], const uint4& lo_row, const 
 }
 
 template <int ACT, int NT>
-__global__ void __launch_bounds__(kFrThreads) gated_ff_rows_in_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ wg,
-                                                                      const __nv_bfloat16* __restrict__ wu, float* __restrict__ h,
+__global__ void __launch_bounds__(kFrThreads, 2) gated_ff_rows_in_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ wg,
+                                                                      const __nv_bfloat16* __restrict__ wu, __nv_bfloat16* __restrict__ h,
                                                                       int* __restrict__ status, int rows, int D, int F) {
     extern __shared__ float red[];      // [warp][gate, up][NT * 128]
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -84,33 +85,25 @@ __global__ void __launch_bounds__(kFrThreads) gated_ff_rows_in_kernel(const __nv
             uv += red[(k * 2 + 1) * NT * 128 + s];
         }
         const int l = (s & 127) >> 2, f = f0 + (l >> 2) + (s & 2) * 4, row = r0 + (s >> 7) * 8 + (l & 3) * 2 + (s & 1);
-        if (f < F && row < rows) h[(size_t)row * F + f] = ff_act<ACT, false>(gv, unused) * uv;
+        if (f < F && row < rows) {
+            const float v = ff_act<ACT, false>(gv, unused) * uv;
+            const __nv_bfloat16 t = __float2bfloat16_rn(v);
+            const float r = __bfloat162float(t);
+            h[(size_t)row * F + f] = t;
+            h[(size_t)(rows + row) * F + f] = __float2bfloat16_rn(isinf(r) ? 0.f : v - r);      // an infinite value has no second term
+        }
     }
-}
-
-// Eight fp32 values as two bf16 terms each
-__device__ __forceinline__ void split(const float4& a, const float4& b, uint4& hi, uint4& lo) {
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t h[4], l[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        h[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        const float h0 = __uint_as_float(h[i] << 16), h1 = __uint_as_float(h[i] & 0xffff0000u);
-        // an infinite value has no second term
-        l[i] = pack_bf16(isinf(h0) ? 0.f : v[2 * i] - h0, isinf(h1) ? 0.f : v[2 * i + 1] - h1);
-    }
-    hi = make_uint4(h[0], h[1], h[2], h[3]);
-    lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
 template <int NT>
-__global__ void __launch_bounds__(kFrThreads) gated_ff_rows_out_kernel(const float* h, const __nv_bfloat16* __restrict__ wd,
+__global__ void __launch_bounds__(kFrThreads, 2) gated_ff_rows_out_kernel(const __nv_bfloat16* h, const __nv_bfloat16* __restrict__ wd,
                                                                        __nv_bfloat16* y, int rows, int D, int F, int parts) {
     extern __shared__ float red[];      // [warp][NT * 128], then this CTA's sums [NT * 128]
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int part = blockIdx.x % parts, d0 = blockIdx.x / parts * 16, r0 = blockIdx.y * (8 * NT);
     const bool lo = d0 + g < D, hi = d0 + g + 8 < D;
     const size_t at_lo = (size_t)(d0 + g) * F + 8 * t, at_hi = at_lo + (size_t)8 * F, at_h = (size_t)(r0 + g) * F + 8 * t;
+    const size_t second = (size_t)rows * F;
     const int chunks = (F + 31) / 32, step = kFrWarps * parts, c_first = part * kFrWarps + w;
     auto weights = [&](int c, uint4& a, uint4& b) {
         const bool in = c < chunks && c * 32 + 8 * t < F;
@@ -136,11 +129,8 @@ __global__ void __launch_bounds__(kFrThreads) gated_ff_rows_out_kernel(const flo
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const bool live = in && r0 + n * 8 + g < rows;
-                const float* src = h + at_h + (size_t)n * 8 * F + (size_t)cc * 32;
-                const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-                const float4 va = live ? *reinterpret_cast<const float4*>(src) : z, vb = live ? *reinterpret_cast<const float4*>(src + 4) : z;
-                uint4 bh, bl;
-                split(va, vb, bh, bl);
+                const __nv_bfloat16* src = h + at_h + (size_t)n * 8 * F + (size_t)cc * 32;
+                const uint4 bh = ld16(src, live), bl = ld16(src + second, live);
                 mma32(acc[n], w0, w1, bh);
                 mma32(acc[n], w0, w1, bl);
             }
@@ -209,7 +199,7 @@ bpt_status run_out(const GatedFfRows& p, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, gated_ff_rows_out_kernel<NT>, (const float*)p.h, p.w_down, p.y, p.rows, p.D, p.F, parts) == cudaSuccess) return BPT_OK;
+    if (cudaLaunchKernelEx(&cfg, gated_ff_rows_out_kernel<NT>, (const __nv_bfloat16*)p.h, p.w_down, p.y, p.rows, p.D, p.F, parts) == cudaSuccess) return BPT_OK;
     cudaGetLastError();     // reported by this status, not by the next call of somebody else
     return BPT_ERR_CUDA;
 }

@@ -74,8 +74,8 @@ def test_oracle_against_torch_and_differences(act):
 
 def test_few_rows_rule(lib):
     f = lib.bpt_gated_ff_few_rows
-    assert f(1, 512, 2048) and f(64, 512, 2048) and not f(65, 512, 2048)
-    assert f(8, 4096, 11008) and not f(9, 4096, 11008)           # a pass over large weights pays for eight rows
-    assert f(256, 64, 128) and not f(257, 64, 128)
+    assert f(1, 512, 2048) and f(128, 512, 2048) and not f(129, 512, 2048)
+    assert f(16, 4096, 11008) and not f(17, 4096, 11008)         # a pass over large weights pays for sixteen rows
+    assert f(384, 64, 128) and not f(385, 64, 128)
     assert not f(4, 60, 128) and not f(-1, 64, 128)              # invalid sizes
     assert lib.bpt_gated_ff_workspace_bytes(64, 512, 2048, 0) == 64 * 2048 * 4

@@ -598,13 +598,15 @@ bool aligned16(std::initializer_list<const void*> ptrs) {
     return true;
 }
 // y and dx, [rows, D] with `slices` slices to sum over.  While tiles of 256 columns leave half of the pairs idle, their sums are
-// shared out: ranges of at least four slices, as many as there are pairs for; with two ranges at most the fp32 partial
-// sums cost what they gain, and narrower tiles do (256 columns a tile is the product's own best rate).
+// shared out: ranges of at least eight slices, eight at most.  Shorter and more ranges cost as much in fp32 partial sums as they
+// save in products (y and dx at 512 x 2048, graph replay of the whole call, us: ranges of 4 slices, up to 16: 22.8 and 30.0 at 1023
+// rows; of 8, up to 8: 20.0 and 28.5; at 1024 x 4096 and 2046 rows two ranges 48.6 and 76.4 against 51.7 and 88.1 of tiles of 128
+// columns, whose products run at 0.6 of the rate).
 struct OutPlan { int bn, splits; };
 OutPlan plan_out(long long rows, int D, int slices) {
     const long long tiles = (rows + 255) / 256 * ((D + 255) / 256);
-    const int splits = (int)std::min<long long>(std::min<long long>(kFfPairs / tiles, slices / 4), 16);
-    if (splits > 2) return {256, splits};
+    const int splits = (int)std::min<long long>(std::min<long long>(kFfPairs / tiles, slices / 8), 8);
+    if (splits > 1) return {256, splits};
     return {tiles * 2 <= kFfPairs ? 128 : 256, 1};
 }
 size_t part_bytes(long long rows, int D, int slices) {

@@ -146,6 +146,26 @@ def load_library() -> ctypes.CDLL:
     return _lib
 
 
+_native = None
+
+
+def load_native():
+    """The C++ autograd functions over the library (csrc_torch/autograd.cpp), bound to the loaded library; raises if not built."""
+    global _native
+    if _native is None:
+        lib = load_library()
+        try:
+            from . import _bpt_torch as native
+        except ImportError as e:
+            raise ImportError("_bpt_torch.so is missing or does not fit this PyTorch: run `python -m paper_1911_04070_b200.build` "
+                              "(there is no fallback implementation)") from e
+        native.bind_library([ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
+            "bpt_res_norm_fwd", "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_few_rows",
+            "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd")])
+        _native = native
+    return _native
+
+
 def status_str(status: int) -> str:
     return load_library().bpt_status_str(int(status)).decode()
 

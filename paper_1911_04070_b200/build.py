@@ -1,4 +1,5 @@
-"""Compile the CUDA sources into paper_1911_04070_b200/libbpt.so for sm_100a.
+"""Compile the CUDA sources into paper_1911_04070_b200/libbpt.so for sm_100a, and the autograd functions over its C ABI
+(csrc_torch/, C++ against PyTorch's headers) into paper_1911_04070_b200/_bpt_torch.so.
 
 Usage: python -m paper_1911_04070_b200.build [--force] [--verbose]
 nvcc cross-compiles without a GPU; the shared object stays inside the package
@@ -10,11 +11,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbpt.so")
 LIB_CHECK = os.path.join(HERE, "libbpt_check.so")   # the same sources with -DBPT_BOUNDS_CHECK (see csrc/bounds_check.cuh)
+LIB_TORCH = os.path.join(HERE, "_bpt_torch.so")
+SRC_TORCH = os.path.join(HERE, "csrc_torch", "autograd.cpp")
 OBJ = os.path.join(HERE, "_build")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -50,11 +54,39 @@ def _build_one(lib: str, tag: str, extra: list, force: bool, verbose: bool) -> s
     return lib
 
 
+def _start_torch(force: bool):
+    """Starts the compilation of _bpt_torch.so where it is out of date; returns what _finish_torch takes."""
+    deps = [SRC_TORCH, os.path.join(HERE, "..", "include", "bpt.h")]
+    if not force and os.path.exists(LIB_TORCH) and os.path.getmtime(LIB_TORCH) >= max(os.path.getmtime(p) for p in deps):
+        return None
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include"),
+           sysconfig.get_paths()["include"]]
+    tmp = LIB_TORCH + ".tmp%d" % os.getpid()
+    cmd = ["g++", "-O2", "-shared", "-fPIC", "-std=c++17", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+    cmd += [a for i in inc for a in ("-isystem", i)] + [SRC_TORCH, "-o", tmp, "-L" + os.path.join(root, "lib")]
+    cmd += ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-ltorch_python"]
+    return cmd, subprocess.Popen(cmd), tmp
+
+
+def _finish_torch(started):
+    if started is None:
+        return
+    cmd, proc, tmp = started
+    if proc.wait() != 0:
+        raise RuntimeError("g++ failed: " + " ".join(cmd))
+    os.replace(tmp, LIB_TORCH)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Builds libbpt.so and the index-checking libbpt_check.so; returns the path of the first."""
+    """Builds libbpt.so, the index-checking libbpt_check.so and _bpt_torch.so; returns the path of the first."""
+    started = _start_torch(force)
     _build_one(LIB, "", [], force, verbose)
     # the checking build shares one violation record across its translation units: relocatable device code
     _build_one(LIB_CHECK, ".chk", ["-DBPT_BOUNDS_CHECK", "-rdc=true"], force, False)
+    _finish_torch(started)
     return LIB
 
 

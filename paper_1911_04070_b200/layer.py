@@ -55,29 +55,6 @@ def graph_self_attention(g: binding.Graph, q, k, v, rel_emb, scale=None, lengths
     return _GraphSelfAttention.apply(q, k, v, rel_emb, g, scale, lengths, float(dropout_p), int(dropout_seed))
 
 
-class _ResidualNorm(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, h, b, weight, bias, post_weight, post_bias, gate, norm, post_norm, alpha, eps, want_sum):
-        stats = h.new_empty((h.numel() // max(h.shape[-1], 1) if h.dim() else 0, 4), dtype=torch.float32)
-        y, r = binding.bpt_res_norm_fwd(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps, want_sum, stats=stats)
-        ctx.save_for_backward(h, b, weight, bias, post_weight, post_bias, gate, stats)
-        ctx.cfg = (norm, post_norm, alpha, eps)
-        ctx.set_materialize_grads(False)
-        return (r, y) if y is not None and r is not None else r if y is None else y
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, *grads):
-        h, b, weight, bias, post_weight, post_bias, gate, stats = ctx.saved_tensors
-        norm, post_norm, alpha, eps = ctx.cfg
-        dr, dy = grads if len(grads) == 2 else (grads[0], None) if norm is None else (None, grads[0])
-        if dr is None and dy is None:
-            return (None,) * 12
-        dr, dy = (None if t is None else t.contiguous() for t in (dr, dy))
-        return binding.bpt_res_norm_bwd(h, b, dy, dr, stats, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps,
-                                        need=ctx.needs_input_grad[:7]) + (None,) * 5
-
-
 def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
                   alpha=1.0, eps=1e-5, return_sum=False):
     """The seam between two blocks, differentiable:  r = alpha * h + gate * post_norm(b),  y = norm(r)  over the last axis.
@@ -87,15 +64,20 @@ def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=Non
     with the trailing row axes of length one ([B, 1, D]: a gate per sequence), or None (1).  With norm="layer" and nothing
     else this is the norm(H + A) of Algorithm 2; with post_norm it is the norm after the block before and the norm
     before the block that follows.  Returns y; (r, y) with return_sum; r with norm=None."""
-    ts = [t if t is None else t.contiguous() for t in (h, b, weight, bias, post_weight, post_bias, gate)]
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts):
-        return _ResidualNorm.apply(*ts, norm, post_norm, float(alpha), float(eps), bool(return_sum))
-    h, b, weight, bias, post_weight, post_bias, gate = ts
-    y, r = binding.bpt_res_norm_fwd(h, b, weight, bias, norm, post_norm, post_weight, post_bias, gate, alpha, eps, return_sum)
-    return (r, y) if y is not None and r is not None else r if y is None else y
+    kind, post = binding.NORM_KINDS.get(norm), binding.NORM_KINDS.get(post_norm)
+    if kind is not None and post is not None:
+        out = binding.load_native().residual_norm(h, b, weight, bias, post_weight, post_bias, gate, kind, post, alpha, eps, return_sum)
+        if out is not None:
+            return out
+    cont = lambda t: t if t is None else t.contiguous()
+    binding.bpt_res_norm_fwd(*map(cont, (h, b, weight, bias)), norm, post_norm, *map(cont, (post_weight, post_bias, gate)), alpha, eps,
+                             return_sum)                                                            # says what is wrong
+    raise RuntimeError("residual_norm: refused")
 
 
 class _GatedFeedForward(torch.autograd.Function):
+    """The same function as the native one, which looks at the device status after every call (binding.CHECK_DEVICE_STATUS)."""
+
     @staticmethod
     def forward(ctx, x, w_gate, w_up, w_down, act):
         y = binding.bpt_gated_ff_fwd(x, w_gate, w_up, w_down, act)
@@ -122,12 +104,14 @@ def gated_feed_forward(x, w_gate, w_up, w_down, act="silu"):
 
     x: [..., D] bfloat16; w_gate, w_up: [F, D], w_down: [D, F] (the layout of a linear layer's weight), D and F multiples
     of 8; act: "silu", "gelu" (with erf) or "relu".  Nothing but x and the weights is kept for the backward pass."""
-    x, w_gate, w_up, w_down = x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous()
-    if torch.is_grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad or w_down.requires_grad):
-        return _GatedFeedForward.apply(x, w_gate, w_up, w_down, act)
-    y = binding.bpt_gated_ff_fwd(x, w_gate, w_up, w_down, act)
-    if binding.CHECK_DEVICE_STATUS and binding.bpt_check(y._bpt_workspace):
-        raise RuntimeError("gated feed-forward: a device-side wait timed out, results are invalid")
+    if binding.CHECK_DEVICE_STATUS:
+        return _GatedFeedForward.apply(x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous(), act)
+    code = binding.ACTIVATIONS.get(act)
+    out = None if code is None else binding.load_native().gated_feed_forward(x, w_gate, w_up, w_down, code)
+    if out is None:
+        binding.bpt_gated_ff_fwd(x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous(), act)     # says what is wrong
+        raise RuntimeError("gated_feed_forward: refused")
+    y, y._bpt_workspace = out
     return y
 
 

@@ -359,3 +359,29 @@ def test_python_refusals():
     with pytest.raises(binding.BptError) as ei:
         f(**v, workspace=torch.empty(256, dtype=torch.uint8, device="cuda:0"))
     assert ei.value.status == 3
+
+
+def test_layer_function_refuses_like_the_binding():
+    import torch
+    from paper_1911_04070_b200 import binding, layer
+    v, dy = _inputs(8, 64, 128, 18)
+    f = layer.gated_feed_forward
+    for kw in (dict(act="tanh"), dict(w_gate=v["w_gate"][:64]), dict(w_down=v["w_gate"]), dict(w_down=v["w_down"].float()), dict(x=v["x"].cpu()),
+               dict(w_up=v["w_up"].cpu())):
+        with pytest.raises(ValueError):
+            f(**{**v, **kw})
+    with pytest.raises(TypeError):
+        f(**{a: t.float() for a, t in v.items()})
+    with pytest.raises(binding.BptError) as ei:
+        f(v["x"][:, :12], v["w_gate"][:, :12], v["w_up"][:, :12], v["w_down"][:12])
+    assert ei.value.status == 2
+
+
+def test_double_backward_is_refused():
+    import torch
+    from paper_1911_04070_b200 import layer
+    v, dy = _inputs(8, 64, 128, 19)
+    x = v["x"].requires_grad_(True)
+    g, = torch.autograd.grad(layer.gated_feed_forward(**v).float().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.float().sum().backward()

@@ -349,3 +349,42 @@ def test_python_refusals():
     with pytest.raises(binding.BptError) as ei:
         binding.bpt_res_norm_bwd(h, h, h, None, None)
     assert ei.value.status == 1
+
+
+def test_layer_function_refuses_like_the_binding():
+    import torch
+    from paper_1911_04070_b200 import binding, layer
+    h = torch.zeros(4, 32, device="cuda:0", requires_grad=True)
+    w = torch.zeros(32, device="cuda:0")
+    for kw in (dict(b=h[:2]), dict(b=h.bfloat16()), dict(norm="batch"), dict(post_norm="batch", b=h), dict(weight=w[:16]), dict(weight=w, bias=w.bfloat16()),
+               dict(norm=None, weight=w), dict(gate=w), dict(b=h, gate=h[:2]), dict(post_norm="rms"), dict(weight=w.cpu())):
+        with pytest.raises(ValueError):
+            layer.residual_norm(h, **kw)
+    with pytest.raises(ValueError):
+        layer.residual_norm(h.cpu(), h.cpu())
+    with pytest.raises(TypeError):
+        layer.residual_norm(h.half())
+    with pytest.raises(binding.BptError) as ei:
+        layer.residual_norm(torch.zeros(2, 8200, device="cuda:0"))
+    assert ei.value.status == 2
+
+
+def test_gradients_only_where_asked_for():
+    import torch
+    from paper_1911_04070_b200 import layer
+    x, up, cfg = _case((6, 50), 96, "f32", "layer", "layer", (6, 1, 96), 0.5, "f32", 40)
+    full = {a: v.clone().requires_grad_(True) for a, v in x.items()}
+    r, y = layer.residual_norm(**full, **cfg, return_sum=True)
+    want = dict(zip(full, torch.autograd.grad((y, r), list(full.values()), (up["dy"], up["dr"]))))
+    for some in (("h",), ("gate",), ("weight", "post_bias"), ("b", "bias")):
+        leaf = {a: v.clone().requires_grad_(a in some) for a, v in x.items()}
+        r, y = layer.residual_norm(**leaf, **cfg, return_sum=True)
+        torch.autograd.backward((y, r), (up["dy"], up["dr"]))
+        for a in x:
+            assert (leaf[a].grad is None) == (a not in some)
+            assert a not in some or torch.equal(leaf[a].grad, want[a])
+    # a graph kept for a second pass gives the same gradients again
+    r, y = layer.residual_norm(**full, **cfg, return_sum=True)
+    for _ in range(2):
+        got = torch.autograd.grad((y, r), list(full.values()), (up["dy"], up["dr"]), retain_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, want.values()))

@@ -6,7 +6,9 @@
 //
 // Functions return None for arguments that the operators refuse; the caller then goes through binding.py, which says why.
 #include <ATen/cuda/CUDAContext.h>
+#include <ATen/cuda/CUDAGraphsUtils.cuh>
 #include <c10/cuda/CUDAGuard.h>
+#include <torch/csrc/autograd/functions/accumulate_grad.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/extension.h>
 
@@ -40,6 +42,20 @@ bool type_code(const Tensor& t, bpt_dtype* out) {
     return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16;
 }
 Tensor bytes(int64_t n, const Tensor& like) { return at::empty({n}, like.options().dtype(at::kByte)); }
+// A leaf's accumulation node belongs to the stream on which a graph first reached the leaf, and lives as long as such a graph.
+// Where that was the default stream, a backward pass under capture would have PyTorch wait there for an event of the capture,
+// which breaks the capture off and can end the process: refused here, while the capture is whole.  The call's own edges only.
+void check_capture(const char* name) {
+    if (at::cuda::currentStreamCaptureStatus() == at::cuda::CaptureStatus::None) return;
+    const auto node = torch::autograd::get_current_node();
+    if (!node) return;
+    for (const auto& edge : node->next_edges()) {
+        if (!dynamic_cast<torch::autograd::AccumulateGrad*>(edge.function.get())) continue;
+        const auto s = edge.function->stream();
+        TORCH_CHECK(!s.has_value() || at::cuda::CUDAStream(*s).stream() != nullptr, name,
+                    " backward under capture: a graph of the same leaves, made on the default stream, is still alive; delete its outputs before the capture");
+    }
+}
 // Gradients of a first-order node: asking for their gradient again is an error when it is done, as with any such function.
 variable_list first_order_only(variable_list grads, const char* name) {
     if (!at::GradMode::is_enabled()) return grads;
@@ -147,6 +163,7 @@ struct ResidualNorm : torch::autograd::Function<ResidualNorm> {
         else (cfg.norm ? dy : dr) = grads[0];
         variable_list out(12);
         if (!dr.defined() && !dy.defined()) return out;
+        check_capture("residual_norm");
         if (dr.defined()) dr = dr.contiguous();
         if (dy.defined()) dy = dy.contiguous();
         bpt_res_norm_args a;
@@ -223,6 +240,7 @@ struct GatedFeedForward : torch::autograd::Function<GatedFeedForward> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
         const auto v = ctx->get_saved_variables();
+        check_capture("gated_feed_forward");
         const Tensor dy = grads[0].contiguous();
         variable_list out(6);
         FfSizes s;

@@ -134,3 +134,54 @@ def test_refusals():
     for kw in (dict(gated="tanh"), dict(gated="silu", F=60), dict(gated="silu", D=36), dict(alpha=0.5)):
         with pytest.raises(ValueError):
             mk(**kw)
+
+
+_CAPTURE = r"""
+import torch
+from paper_1911_04070_b200 import layer
+t = lambda *s: torch.randn(*s, device="cuda:0").bfloat16().mul_(0.1).requires_grad_(True)
+x, wg, wu, wd, w = t(40, 64), t(128, 64), t(128, 64), t(64, 128), t(64)
+which = {"ff": (lambda: layer.gated_feed_forward(x, wg, wu, wd), (x, wg, wu, wd)), "norm": (lambda: layer.residual_norm(x, None, w), (x, w))}
+for name, (call, leaves) in which.items():
+    def backward():
+        for v in leaves:
+            v.grad = None
+        call().float().square().sum().backward()
+        return [v.grad for v in leaves]
+    want = [g.clone() for g in backward()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        backward()
+    torch.cuda.synchronize()
+    alive = call()                       # on the default stream: the leaves' accumulation nodes are this graph's
+    graph = torch.cuda.CUDAGraph()
+    try:
+        with torch.cuda.graph(graph):
+            backward()
+    except RuntimeError as e:
+        assert "still alive" in str(e), e
+    else:
+        raise AssertionError(name + ": not refused")
+    assert all(torch.equal(a, b) for a, b in zip(want, backward()))      # nothing is left of the attempt
+    del alive, graph
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = backward()
+    for g in got:
+        g.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got)), name
+print("captured")
+"""
+
+
+def test_captured_backward_beside_a_living_eager_graph():
+    """Refused while the capture is whole; with the eager graph deleted the same pass is captured and replays the same bits."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _CAPTURE], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stdout + r.stderr

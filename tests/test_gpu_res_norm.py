@@ -204,6 +204,20 @@ def test_special_rows():
     assert torch.equal(y0, layer.residual_norm(h[:1], b[:1], w, c))
 
 
+@pytest.mark.parametrize("lead,gate", [((4, 0), (4, 1)), ((0, 5), (1, 1)), ((0, 5), (0, 1)), ((4, 0), (4, 0)), ((0, 0), (1,))])
+def test_empty_batches_and_sequences(lead, gate):
+    """No rows: empty results, and gradients of zero for whatever is shared by rows."""
+    import torch
+    from paper_1911_04070_b200 import layer
+    D = 72
+    t = lambda *s: torch.ones(*s, D, device="cuda:0", requires_grad=True)
+    v = dict(h=t(*lead), b=t(*lead), weight=t(), bias=t(), post_weight=t(), gate=t(*gate))
+    r, y = layer.residual_norm(**v, norm="layer", post_norm="rms", return_sum=True)
+    assert r.shape == y.shape == (*lead, D)
+    for a, g in zip(v.values(), torch.autograd.grad((r.sum() + y.sum()), list(v.values()))):
+        assert g.shape == a.shape and (g == 0).all()
+
+
 def test_results_do_not_depend_on_alignment_or_neighbours():
     """Views that are contiguous but not 16-byte aligned, results in place of the inputs, and the memory around the rows."""
     import torch

@@ -63,7 +63,8 @@ def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=Non
     norm / post_norm: "layer", "rms" or None, with their weights and biases [D] (None: 1 and 0).  gate: [D], or h's shape
     with the trailing row axes of length one ([B, 1, D]: a gate per sequence), or None (1).  With norm="layer" and nothing
     else this is the norm(H + A) of Algorithm 2; with post_norm it is the norm after the block before and the norm
-    before the block that follows.  Returns y; (r, y) with return_sum; r with norm=None."""
+    before the block that follows.  Returns y; (r, y) with return_sum; r with norm=None.  Can be captured in a CUDA graph with
+    its backward pass, which is refused there while a graph of the same leaves made on the default stream is alive."""
     kind, post = binding.NORM_KINDS.get(norm), binding.NORM_KINDS.get(post_norm)
     if kind is not None and post is not None:
         out = binding.load_native().residual_norm(h, b, weight, bias, post_weight, post_bias, gate, kind, post, alpha, eps, return_sum)
@@ -103,7 +104,8 @@ def gated_feed_forward(x, w_gate, w_up, w_down, act="silu"):
     """Differentiable gated feed-forward block over the last axis:  (act(x w_gate^T) * (x w_up^T)) w_down^T.
 
     x: [..., D] bfloat16; w_gate, w_up: [F, D], w_down: [D, F] (the layout of a linear layer's weight), D and F multiples
-    of 8; act: "silu", "gelu" (with erf) or "relu".  Nothing but x and the weights is kept for the backward pass."""
+    of 8; act: "silu", "gelu" (with erf) or "relu".  Nothing but x and the weights is kept for the backward pass.  Capture as
+    in residual_norm."""
     if binding.CHECK_DEVICE_STATUS:
         return _GatedFeedForward.apply(x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous(), act)
     code = binding.ACTIVATIONS.get(act)

@@ -41,6 +41,12 @@ bool type_code(const Tensor& t, bpt_dtype* out) {
     *out = t.scalar_type() == at::kFloat ? BPT_F32 : BPT_BF16;
     return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16;
 }
+// Contiguous and on a 16-byte boundary, which the feed-forward kernels' loads need: a contiguous view, such as the gradient that the
+// backward of a concatenation hands down, starts anywhere in its storage and is copied here.
+Tensor aligned(const Tensor& t) {
+    const Tensor c = t.contiguous();
+    return c.is_cuda() && ((uintptr_t)c.data_ptr() & 15) ? c.clone() : c;
+}
 Tensor bytes(int64_t n, const Tensor& like) { return at::empty({n}, like.options().dtype(at::kByte)); }
 // A leaf's accumulation node belongs to the stream on which a graph first reached the leaf, and lives as long as such a graph.
 // Where that was the default stream, a backward pass under capture would have PyTorch wait there for an event of the capture,
@@ -155,7 +161,8 @@ struct ResidualNorm : torch::autograd::Function<ResidualNorm> {
         return {r.defined() ? r : y};
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
-        const auto v = ctx->get_saved_variables();
+        variable_list v = ctx->get_saved_variables();
+        v[7] = aligned(v[7]);       // the statistics are read 16 bytes at a time; hooks on saved tensors may hand them back elsewhere
         const int64_t kinds = ctx->saved_data["kinds"].toInt();
         const NormCfg cfg{kinds / 4, kinds % 4, ctx->saved_data["alpha"].toDouble(), ctx->saved_data["eps"].toDouble()};
         Tensor dr, dy;
@@ -239,9 +246,10 @@ struct GatedFeedForward : torch::autograd::Function<GatedFeedForward> {
         return y;
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
-        const auto v = ctx->get_saved_variables();
+        variable_list v = ctx->get_saved_variables();
         check_capture("gated_feed_forward");
-        const Tensor dy = grads[0].contiguous();
+        for (auto& t : v) t = aligned(t);       // hooks on saved tensors may hand them back elsewhere
+        const Tensor dy = aligned(grads[0]);
         variable_list out(6);
         FfSizes s;
         TORCH_CHECK(ff_sizes(v[0], v[1], v[2], v[3], &s), "gated_feed_forward backward: the saved tensors have changed their form");
@@ -265,7 +273,7 @@ struct GatedFeedForward : torch::autograd::Function<GatedFeedForward> {
 
 // (y, status block or None)
 py::object gated_feed_forward(const Tensor& x_, const Tensor& wg_, const Tensor& wu_, const Tensor& wd_, int64_t act) {
-    const Tensor x = x_.contiguous(), wg = wg_.contiguous(), wu = wu_.contiguous(), wd = wd_.contiguous();
+    const Tensor x = aligned(x_), wg = aligned(wg_), wu = aligned(wu_), wd = aligned(wd_);
     const bool grad = at::GradMode::is_enabled() && (x.requires_grad() || wg.requires_grad() || wu.requires_grad() || wd.requires_grad());
     try {
         Tensor status;

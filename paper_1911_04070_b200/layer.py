@@ -76,6 +76,12 @@ def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=Non
     raise RuntimeError("residual_norm: refused")
 
 
+def _aligned(t):
+    """Contiguous and on the 16-byte boundary that the feed-forward kernels need; a contiguous view may start anywhere."""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t
+
+
 class _GatedFeedForward(torch.autograd.Function):
     """The same function as the native one, which looks at the device status after every call (binding.CHECK_DEVICE_STATUS)."""
 
@@ -91,9 +97,9 @@ class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        x, w_gate, w_up, w_down = ctx.saved_tensors
+        x, w_gate, w_up, w_down = map(_aligned, ctx.saved_tensors)
         need = ctx.needs_input_grad
-        grads = binding.bpt_gated_ff_bwd(x, w_gate, w_up, w_down, dy.contiguous(), ctx.act, need_dx=need[0], need_dw=any(need[1:4]))
+        grads = binding.bpt_gated_ff_bwd(x, w_gate, w_up, w_down, _aligned(dy), ctx.act, need_dx=need[0], need_dw=any(need[1:4]))
         first = grads[0] if need[0] else grads[1]
         if binding.CHECK_DEVICE_STATUS and binding.bpt_check(first._bpt_workspace):
             raise RuntimeError("gated feed-forward backward: a device-side wait timed out, results are invalid")
@@ -104,14 +110,15 @@ def gated_feed_forward(x, w_gate, w_up, w_down, act="silu"):
     """Differentiable gated feed-forward block over the last axis:  (act(x w_gate^T) * (x w_up^T)) w_down^T.
 
     x: [..., D] bfloat16; w_gate, w_up: [F, D], w_down: [D, F] (the layout of a linear layer's weight), D and F multiples
-    of 8; act: "silu", "gelu" (with erf) or "relu".  Nothing but x and the weights is kept for the backward pass.  Capture as
+    of 8; act: "silu", "gelu" (with erf) or "relu".  Any strides and offsets: what is not contiguous or does not start on a
+    16-byte boundary is copied first.  Nothing but x and the weights is kept for the backward pass.  Capture as
     in residual_norm."""
     if binding.CHECK_DEVICE_STATUS:
-        return _GatedFeedForward.apply(x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous(), act)
+        return _GatedFeedForward.apply(*map(_aligned, (x, w_gate, w_up, w_down)), act)
     code = binding.ACTIVATIONS.get(act)
     out = None if code is None else binding.load_native().gated_feed_forward(x, w_gate, w_up, w_down, code)
     if out is None:
-        binding.bpt_gated_ff_fwd(x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous(), act)     # says what is wrong
+        binding.bpt_gated_ff_fwd(*map(_aligned, (x, w_gate, w_up, w_down)), act)      # says what is wrong
         raise RuntimeError("gated_feed_forward: refused")
     y, y._bpt_workspace = out
     return y

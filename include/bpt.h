@@ -17,15 +17,16 @@
  * `cuda_stream` (a cudaStream_t passed as void*, NULL = legacy default stream) and
  * return without synchronising.  Nothing is allocated or kept between calls, so the attention calls
  * (bpt_attn_fwd / bpt_attn_bwd and their _varlen, _ex, _rows forms) can be captured in a CUDA graph.
- * The library reads no environment variable and keeps no process-wide setting (the one exception,
- * the benchmark trace, is described at bpt_trace_begin).
+ * The library reads no environment variable and keeps no process-wide setting (the exceptions, the
+ * benchmark trace and the failure record, are described at bpt_trace_begin and bpt_check_device).
  * Argument errors are detected on the host before anything is launched.
  *
  * Device-side failure report.  A non-empty attention workspace begins with a 256-byte status block
  * that every attention call clears on its stream before its kernels run.  Kernels that wait on
  * hardware barriers (the tensor-memory kernels) bound every wait to about a second; if one expires
  * the kernel winds down, the results of the call are invalid and BPT_ERR_TIMEOUT is stored in the
- * block.  bpt_check reads it.
+ * block.  bpt_check reads it.  The gated feed-forward calls take a separate, optional block, and store
+ * BPT_ERR_TIMEOUT in a record of the device besides, which no call clears: bpt_check_device reads it.
  */
 #ifndef BPT_H
 #define BPT_H
@@ -132,6 +133,17 @@ size_t bpt_attn_bwd_min_workspace_bytes(const bpt_graph* g, int32_t B, int32_t H
  * use inside a stream capture.
  */
 bpt_status bpt_check(const void* workspace, void* cuda_stream);
+
+/*
+ * Waits for `cuda_stream` and reports whether a bounded device-side wait of any gated feed-forward call
+ * (bpt_gated_ff_fwd, bpt_gated_ff_bwd, with or without a status block) or of the wait self-test expired on
+ * the current device since the last such report: BPT_OK or BPT_ERR_TIMEOUT, which clears the record.  For
+ * training loops: once per step, where the step's calls ran inside an autograd engine that keeps no status
+ * blocks.  Covers the work that `cuda_stream` has waited for; work that still runs on other streams
+ * is reported by a later call.  BPT_ERR_CUDA when the synchronisation or a copy fails.  Host-synchronous: not
+ * for use inside a stream capture.
+ */
+bpt_status bpt_check_device(void* cuda_stream);
 
 /*
  * Forward graph self-attention with relative positions (Sec. 3.4 equation, built on
@@ -278,8 +290,8 @@ bpt_status bpt_out_proj_norm(const void* a, const void* w_o, const void* h, cons
  * `workspace`: bpt_gated_ff_workspace_bytes bytes (host query; 0 on invalid arguments and for rows == 0, where NULL
  * will do), 256-byte aligned; two calls whose GPU work overlaps need one each.  `status`: NULL, or a device buffer of at
  * least 256 bytes that receives the status block (see bpt_check; apart from the workspace, which is large and need not
- * outlive the call's work).
- * Errors: INVALID_ARG, UNSUPPORTED (sizes), WORKSPACE, CUDA; device-side: see bpt_check.
+ * outlive the call's work); either way a wait that expired also shows in bpt_check_device.
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes), WORKSPACE, CUDA; device-side: see bpt_check, bpt_check_device.
  */
 enum { BPT_ACT_RELU = 0, BPT_ACT_SILU = 1, BPT_ACT_GELU = 2 };
 int32_t bpt_gated_ff_few_rows(int64_t rows, int32_t D, int32_t F);
@@ -392,7 +404,8 @@ bpt_status bpt_trace_end(int32_t* n_marks, float* ms, const char** names, int32_
  * expects one arrival.  With arrive == 0 nobody arrives: the wait runs out, the kernel stores
  * BPT_ERR_TIMEOUT in the status block at `workspace` (device, >= 256 bytes, cleared first) and ends --
  * exactly the give-up path of the tensor-memory kernels; with arrive != 0 the thread arrives itself
- * and the block stays clear.  Nothing faults or hangs either way.  Read the outcome with bpt_check.
+ * and the block stays clear.  The device's record is set along with the block.  Nothing faults or hangs
+ * either way.  Read the outcome with bpt_check and bpt_check_device.
  * Errors: INVALID_ARG, CUDA.
  */
 bpt_status bpt_selftest_wait_timeout(void* workspace, int64_t limit_cycles, int32_t arrive, void* cuda_stream);

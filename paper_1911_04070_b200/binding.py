@@ -28,7 +28,7 @@ EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes"
            "bpt_attn_fwd_ex", "bpt_attn_bwd_ex", "bpt_attn_fwd_rows", "bpt_attn_bwd_min_workspace_bytes", "bpt_check",
            "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
            "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd",
-           "bpt_gated_ff_few_rows")
+           "bpt_gated_ff_few_rows", "bpt_check_device")
 
 
 class BptError(RuntimeError):
@@ -62,8 +62,9 @@ class ResNormArgs(ctypes.Structure):
                 ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p)]
 
 
-# When set, the autograd wrapper in layer.py asks bpt_check after every attention call (a stream
-# synchronisation per call): for debugging; training loops normally check once per step.
+# When set, the autograd wrappers in layer.py ask bpt_check after every attention and gated feed-forward call (a stream
+# synchronisation per call): for debugging.  Training loops ask bpt_check_device once per step, which covers the gated
+# feed-forward calls, backward passes among them.
 CHECK_DEVICE_STATUS = False
 
 _lib = None
@@ -88,6 +89,8 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_attn_bwd_min_workspace_bytes.argtypes = [ctypes.POINTER(GraphStruct), i32, i32, i32, ctypes.c_int]
         lib.bpt_check.restype = ctypes.c_int
         lib.bpt_check.argtypes = [vp, vp]
+        lib.bpt_check_device.restype = ctypes.c_int
+        lib.bpt_check_device.argtypes = [vp]
         lib.bpt_selftest_wait_timeout.restype = ctypes.c_int
         lib.bpt_selftest_wait_timeout.argtypes = [vp, ctypes.c_int64, i32, vp]
         lib.bpt_out_proj_norm.restype = ctypes.c_int
@@ -261,6 +264,13 @@ def bpt_check(workspace) -> int:
     dev = torch.cuda.current_device() if workspace is None else workspace.device
     with torch.cuda.device(dev):
         return int(load_library().bpt_check(_ptr(workspace), _stream()))
+
+
+def bpt_check_device(device=None) -> int:
+    """Waits for the current stream of `device` (the current one) and returns 0, or 5 when a bounded device-side wait of a gated
+    feed-forward call, forward or backward, expired there since the last such question: what was computed since is invalid."""
+    with torch.cuda.device(device):
+        return int(load_library().bpt_check_device(_stream()))
 
 
 def bpt_out_proj_norm(a, w_o, h, gamma, beta, eps: float = 1e-5, z=None, workspace=None):

@@ -1,4 +1,6 @@
 // C-ABI entry points: argument validation and dispatch.  See include/bpt.h.
+#include <atomic>
+
 #include "bounds_check.cuh"
 #include "bpt_internal.cuh"
 
@@ -7,6 +9,21 @@ namespace bpt {
 __device__ unsigned int g_bounds_record[4];
 }
 #endif
+
+namespace bpt {
+__device__ int g_device_record;     // see bpt_check_device
+
+int* device_record() {
+    static std::atomic<int*> known[64];     // by device ordinal: the address does not change while the module is loaded
+    int device;
+    if (cudaGetDevice(&device) != cudaSuccess) return nullptr;
+    int* at = device < 64 ? known[device].load(std::memory_order_acquire) : nullptr;
+    if (at) return at;
+    if (cudaGetSymbolAddress(reinterpret_cast<void**>(&at), g_device_record) != cudaSuccess) return nullptr;
+    if (device < 64) known[device].store(at, std::memory_order_release);
+    return at;
+}
+}  // namespace bpt
 
 using namespace bpt;
 
@@ -45,6 +62,17 @@ extern "C" bpt_status bpt_check(const void* workspace, void* cuda_stream) {
     int32_t word = 0;
     if (cudaMemcpy(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost) != cudaSuccess) return BPT_ERR_CUDA;
     return word == 0 ? BPT_OK : (word == (int32_t)BPT_ERR_TIMEOUT ? BPT_ERR_TIMEOUT : BPT_ERR_CUDA);
+}
+
+extern "C" bpt_status bpt_check_device(void* cuda_stream) {
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    int* record = device_record();
+    int32_t word = 0;
+    if (!record || cudaMemcpyAsync(&word, record, sizeof(word), cudaMemcpyDeviceToHost, st) != cudaSuccess) return BPT_ERR_CUDA;
+    if (cudaStreamSynchronize(st) != cudaSuccess) return BPT_ERR_CUDA;
+    if (word == 0) return BPT_OK;
+    if (cudaMemsetAsync(record, 0, sizeof(word), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return BPT_ERR_CUDA;
+    return word == (int32_t)BPT_ERR_TIMEOUT ? BPT_ERR_TIMEOUT : BPT_ERR_CUDA;
 }
 
 static bool options_ok(const bpt_attn_options* opt) {

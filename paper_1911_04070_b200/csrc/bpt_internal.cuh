@@ -37,6 +37,14 @@ struct AttnProblem {
     cudaStream_t stream;
 };
 
+// The word of the current device that bpt_check_device reads, or nullptr when the runtime fails.
+int* device_record();
+// What a kernel does with a bounded wait that ran out: into the call's status block, if it has one, and into the device's record.
+__device__ __forceinline__ void report_timeout(int* status, int* record) {
+    if (status) status[0] = (int)BPT_ERR_TIMEOUT;
+    *record = (int)BPT_ERR_TIMEOUT;
+}
+
 // Optional per-launch timing (see bpt_trace_begin): a mark after every kernel launch.
 void trace_mark(cudaStream_t st, const char* name);
 

@@ -12,7 +12,8 @@
 // accumulators of 256 columns, in the three-accumulator kernel one for G | U of 128 columns and one for dH of 256 (a tile is
 // G | U of its first half, dH, G | U of its second half).  Operands that a product needs transposed are read as they lie: the matrix
 // descriptors take either axis as the contiguous one, so no transposed copy exists anywhere.  Ragged edges are TMA's: what lies
-// outside a tensor reads as zero and is not written.  Every wait is bounded; a give-up is reported through the status word.
+// outside a tensor reads as zero and is not written.  Every wait is bounded; a give-up is reported through the call's status word,
+// if there is one, and the device's record (bpt_check_device), which a backward pass run by autograd has to rely on.
 #include <algorithm>
 
 #include "bpt_internal.cuh"
@@ -53,7 +54,7 @@ template <int KERNEL> struct FfShape {
 
 struct FfParams {
     CUtensorMap a0, a1, a2, b0, b1, b2, c0, c1, c2;
-    int* status;
+    int *status, *record;
     int rows, D, F, splits, tiles;
     int step;               // kFfBwdIn: columns of a tile, 256 or 128 (its first half only)
     bool clear;             // the call's first kernel clears the status block
@@ -484,7 +485,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
     __syncwarp();
     tc5::fence_before_sync();
     pair::cluster_sync();      // both CTAs are past their last product, load and barrier use
-    if (tid == 0 && *abort_s && p.status) p.status[0] = (int)BPT_ERR_TIMEOUT;
+    if (tid == 0 && *abort_s) report_timeout(p.status, p.record);
     if (w == 1) pair::tmem_free(tbase, 512);
 }
 
@@ -655,6 +656,8 @@ extern "C" bpt_status bpt_gated_ff_fwd(const void* x, const void* w_gate, const 
     if (!tc5::encode_tiled() || !tc5::context_current()) return BPT_ERR_CUDA;
     FfParams p{};
     p.status = static_cast<int*>(status);
+    p.record = device_record();
+    if (!p.record) return BPT_ERR_CUDA;
     p.clear = true;
     p.rows = (int)rows; p.D = D; p.F = F;
     const int ld = inner_ld(F);
@@ -706,6 +709,8 @@ extern "C" bpt_status bpt_gated_ff_bwd(const void* x, const void* w_gate, const 
     const int mt = (int)((rows + 255) / 256);
     FfParams p{};
     p.status = static_cast<int*>(status);
+    p.record = device_record();
+    if (!p.record) return BPT_ERR_CUDA;
     p.clear = true;
     p.rows = (int)rows; p.D = D; p.F = F;
     const int ld = inner_ld(F);

@@ -111,8 +111,8 @@ def gated_feed_forward(x, w_gate, w_up, w_down, act="silu"):
 
     x: [..., D] bfloat16; w_gate, w_up: [F, D], w_down: [D, F] (the layout of a linear layer's weight), D and F multiples
     of 8; act: "silu", "gelu" (with erf) or "relu".  Any strides and offsets: what is not contiguous or does not start on a
-    16-byte boundary is copied first.  Nothing but x and the weights is kept for the backward pass.  Capture as
-    in residual_norm."""
+    16-byte boundary is copied first.  Nothing but x and the weights is kept for the backward pass.  A device-side wait that
+    expired, in either pass, shows in binding.bpt_check_device.  Capture as in residual_norm."""
     if binding.CHECK_DEVICE_STATUS:
         return _GatedFeedForward.apply(*map(_aligned, (x, w_gate, w_up, w_down)), act)
     code = binding.ACTIVATIONS.get(act)

@@ -62,6 +62,12 @@ void check_capture(const char* name) {
                     " backward under capture: a graph of the same leaves, made on the default stream, is still alive; delete its outputs before the capture");
     }
 }
+// A call past the autograd function (no argument requires a gradient) would drop a forward-mode tangent without a word, and the
+// function itself has no forward-mode derivative.
+void check_tangents(std::initializer_list<const Tensor*> args, const char* name) {
+    for (const Tensor* t : args)
+        TORCH_CHECK_NOT_IMPLEMENTED(!t->defined() || !t->_fw_grad(0).defined(), name, " has no forward-mode derivative");
+}
 // Gradients of a first-order node: asking for their gradient again is an error when it is done, as with any such function.
 variable_list first_order_only(variable_list grads, const char* name) {
     if (!at::GradMode::is_enabled()) return grads;
@@ -170,6 +176,7 @@ struct ResidualNorm : torch::autograd::Function<ResidualNorm> {
         else (cfg.norm ? dy : dr) = grads[0];
         variable_list out(12);
         if (!dr.defined() && !dy.defined()) return out;
+        check_tangents({&dr, &dy}, "residual_norm backward");
         check_capture("residual_norm");
         if (dr.defined()) dr = dr.contiguous();
         if (dy.defined()) dy = dy.contiguous();
@@ -189,6 +196,9 @@ struct ResidualNorm : torch::autograd::Function<ResidualNorm> {
 
 py::object residual_norm(const Tensor& h_, const Opt& b_, const Opt& w_, const Opt& c_, const Opt& pw_, const Opt& pb_, const Opt& gate_, int64_t norm,
                          int64_t post, double alpha, double eps, bool want_sum) {
+    for (const Opt* t : {&b_, &w_, &c_, &pw_, &pb_, &gate_})
+        if (t->has_value()) check_tangents({&**t}, "residual_norm");
+    check_tangents({&h_}, "residual_norm");
     const Tensor h = h_.contiguous();
     const Opt b = given(b_), w = given(w_), c = given(c_), pw = given(pw_), pb = given(pb_), gate = given(gate_);
     bool grad = false;
@@ -247,6 +257,7 @@ struct GatedFeedForward : torch::autograd::Function<GatedFeedForward> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
         variable_list v = ctx->get_saved_variables();
+        check_tangents({&grads[0]}, "gated_feed_forward backward");
         check_capture("gated_feed_forward");
         for (auto& t : v) t = aligned(t);       // hooks on saved tensors may hand them back elsewhere
         const Tensor dy = aligned(grads[0]);
@@ -274,6 +285,7 @@ struct GatedFeedForward : torch::autograd::Function<GatedFeedForward> {
 
 // (y, status block or None)
 py::object gated_feed_forward(const Tensor& x_, const Tensor& wg_, const Tensor& wu_, const Tensor& wd_, int64_t act) {
+    check_tangents({&x_, &wg_, &wu_, &wd_}, "gated_feed_forward");
     const Tensor x = aligned(x_), wg = aligned(wg_), wu = aligned(wu_), wd = aligned(wd_);
     const bool grad = at::GradMode::is_enabled() && (x.requires_grad() || wg.requires_grad() || wu.requires_grad() || wd.requires_grad());
     try {

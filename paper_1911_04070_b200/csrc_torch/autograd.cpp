@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <torch/csrc/autograd/functions/accumulate_grad.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
 #include "../../include/bpt.h"
@@ -67,6 +68,10 @@ void check_capture(const char* name) {
 void check_tangents(std::initializer_list<const Tensor*> args, const char* name) {
     for (const Tensor* t : args)
         TORCH_CHECK_NOT_IMPLEMENTED(!t->defined() || !t->_fw_grad(0).defined(), name, " has no forward-mode derivative");
+}
+// A trace records PyTorch's operators: of a call here only the allocation of the result, which nothing would then write.
+void check_tracing(const char* name) {
+    TORCH_CHECK_NOT_IMPLEMENTED(!torch::jit::tracer::isTracing(), name, " cannot be traced by torch.jit: the library's kernels leave no record");
 }
 // Gradients of a first-order node: asking for their gradient again is an error when it is done, as with any such function.
 variable_list first_order_only(variable_list grads, const char* name) {
@@ -196,6 +201,7 @@ struct ResidualNorm : torch::autograd::Function<ResidualNorm> {
 
 py::object residual_norm(const Tensor& h_, const Opt& b_, const Opt& w_, const Opt& c_, const Opt& pw_, const Opt& pb_, const Opt& gate_, int64_t norm,
                          int64_t post, double alpha, double eps, bool want_sum) {
+    check_tracing("residual_norm");
     for (const Opt* t : {&b_, &w_, &c_, &pw_, &pb_, &gate_})
         if (t->has_value()) check_tangents({&**t}, "residual_norm");
     check_tangents({&h_}, "residual_norm");
@@ -285,6 +291,7 @@ struct GatedFeedForward : torch::autograd::Function<GatedFeedForward> {
 
 // (y, status block or None)
 py::object gated_feed_forward(const Tensor& x_, const Tensor& wg_, const Tensor& wu_, const Tensor& wd_, int64_t act) {
+    check_tracing("gated_feed_forward");
     check_tangents({&x_, &wg_, &wu_, &wd_}, "gated_feed_forward");
     const Tensor x = aligned(x_), wg = aligned(wg_), wu = aligned(wu_), wd = aligned(wd_);
     const bool grad = at::GradMode::is_enabled() && (x.requires_grad() || wg.requires_grad() || wu.requires_grad() || wd.requires_grad());

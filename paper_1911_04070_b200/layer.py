@@ -66,7 +66,7 @@ def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=Non
     else this is the norm(H + A) of Algorithm 2; with post_norm it is the norm after the block before and the norm
     before the block that follows.  Returns y; (r, y) with return_sum; r with norm=None.  Can be captured in a CUDA graph with
     its backward pass, which is refused there while a graph of the same leaves made on the default stream is alive.  Reverse mode,
-    first order; forward-mode tangents are refused."""
+    first order; forward-mode tangents and torch.jit.trace are refused."""
     kind, post = binding.NORM_KINDS.get(norm), binding.NORM_KINDS.get(post_norm)
     if kind is not None and post is not None:
         out = binding.load_native().residual_norm(h, b, weight, bias, post_weight, post_bias, gate, kind, post, alpha, eps, return_sum)
@@ -116,9 +116,11 @@ def gated_feed_forward(x, w_gate, w_up, w_down, act="silu"):
     x: [..., D] bfloat16; w_gate, w_up: [F, D], w_down: [D, F] (the layout of a linear layer's weight), D and F multiples
     of 8; act: "silu", "gelu" (with erf) or "relu".  Any strides and offsets: what is not contiguous or does not start on a
     16-byte boundary is copied first.  Nothing but x and the weights is kept for the backward pass.  A device-side wait that
-    expired, in either pass, shows in binding.bpt_check_device.  Capture and modes of
-    differentiation as in residual_norm."""
+    expired, in either pass, shows in binding.bpt_check_device.  Capture, modes of
+    differentiation and tracing as in residual_norm."""
     if binding.CHECK_DEVICE_STATUS:
+        if torch.jit.is_tracing():
+            raise NotImplementedError("gated_feed_forward cannot be traced by torch.jit")
         return _GatedFeedForward.apply(*map(_aligned, (x, w_gate, w_up, w_down)), act)
     code = binding.ACTIVATIONS.get(act)
     out = None if code is None else binding.load_native().gated_feed_forward(x, w_gate, w_up, w_down, code)

@@ -66,3 +66,17 @@ def test_forward_mode_over_the_backward_pass_is_refused(layer, check, monkeypatc
             up = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
             with pytest.raises(NotImplementedError, match="forward-mode"):
                 torch.autograd.grad(y, first, up)
+
+
+@pytest.mark.parametrize("device", DEVICES)
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("check", [False, True])
+def test_tracing_is_refused(layer, grad, device, check, monkeypatch):
+    """A trace would hold the allocation of the result and nothing that writes it."""
+    from paper_1911_04070_b200 import binding
+    monkeypatch.setattr(binding, "CHECK_DEVICE_STATUS", check)
+    for v, call in ((_norm(device), layer.residual_norm), (_block(device), layer.gated_feed_forward)):
+        first = next(iter(v))
+        example = v.pop(first).requires_grad_(grad)
+        with pytest.raises(NotImplementedError, match="traced"):
+            torch.jit.trace(lambda t: call(**{first: t}, **v), example, check_trace=False)

@@ -56,17 +56,26 @@ def graph_self_attention(g: binding.Graph, q, k, v, rel_emb, scale=None, lengths
     return _GraphSelfAttention.apply(q, k, v, rel_emb, g, scale, lengths, float(dropout_p), int(dropout_seed))
 
 
+def _check_constant(name, v):
+    """alpha and eps are numbers; a tensor would be read as one, and its gradient or tangent lost."""
+    if isinstance(v, torch.Tensor) and ((v.requires_grad and torch.is_grad_enabled()) or forward_ad.unpack_dual(v).tangent is not None):
+        raise NotImplementedError("residual_norm has no derivative with respect to %s; a learned factor goes into gate or h" % name)
+
+
 def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
                   alpha=1.0, eps=1e-5, return_sum=False):
     """The seam between two blocks, differentiable:  r = alpha * h + gate * post_norm(b),  y = norm(r)  over the last axis.
 
     h: the residual stream [..., D], b: the output of the block before (None: r = alpha * h), both float32 or bfloat16.
     norm / post_norm: "layer", "rms" or None, with their weights and biases [D] (None: 1 and 0).  gate: [D], or h's shape
-    with the trailing row axes of length one ([B, 1, D]: a gate per sequence), or None (1).  With norm="layer" and nothing
+    with the trailing row axes of length one ([B, 1, D]: a gate per sequence), or None (1).  alpha, eps: numbers.  With norm="layer" and nothing
     else this is the norm(H + A) of Algorithm 2; with post_norm it is the norm after the block before and the norm
     before the block that follows.  Returns y; (r, y) with return_sum; r with norm=None.  Can be captured in a CUDA graph with
     its backward pass, which is refused there while a graph of the same leaves made on the default stream is alive.  Reverse mode,
     first order; forward-mode tangents and torch.jit.trace are refused."""
+    if type(alpha) is not float or type(eps) is not float:
+        _check_constant("alpha", alpha)
+        _check_constant("eps", eps)
     kind, post = binding.NORM_KINDS.get(norm), binding.NORM_KINDS.get(post_norm)
     if kind is not None and post is not None:
         out = binding.load_native().residual_norm(h, b, weight, bias, post_weight, post_bias, gate, kind, post, alpha, eps, return_sum)

@@ -80,3 +80,23 @@ def test_tracing_is_refused(layer, grad, device, check, monkeypatch):
         example = v.pop(first).requires_grad_(grad)
         with pytest.raises(NotImplementedError, match="traced"):
             torch.jit.trace(lambda t: call(**{first: t}, **v), example, check_trace=False)
+
+
+@pytest.mark.parametrize("name", ["alpha", "eps"])
+def test_a_learned_constant_is_refused(layer, name):
+    """alpha and eps are numbers: a tensor's gradient or tangent would be lost."""
+    v = _norm("cpu")
+    with pytest.raises(NotImplementedError, match=name):
+        layer.residual_norm(**v, **{name: torch.tensor(0.5, requires_grad=True)})
+    with forward_ad.dual_level(), pytest.raises(NotImplementedError, match=name):
+        layer.residual_norm(**v, **{name: forward_ad.make_dual(torch.tensor(0.5), torch.tensor(1.0))})
+
+
+@pytest.mark.gpu
+def test_a_constant_given_as_a_tensor_counts_as_its_value(layer):
+    v = _norm("cuda:0")
+    want = layer.residual_norm(**v, alpha=0.5, eps=0.25)
+    assert torch.equal(want, layer.residual_norm(**v, alpha=torch.tensor(0.5), eps=torch.tensor(0.25, device="cuda:0")))
+    with torch.no_grad():
+        assert torch.equal(want, layer.residual_norm(**v, alpha=torch.tensor(0.5, requires_grad=True), eps=0.25))
+    assert torch.equal(layer.residual_norm(**v, alpha=2), layer.residual_norm(**v, alpha=2.0))

@@ -157,11 +157,12 @@ def load_native():
     global _native
     if _native is None:
         lib = load_library()
-        try:
-            from . import _bpt_torch as native
-        except ImportError as e:
-            raise ImportError("_bpt_torch.so is missing or does not fit this PyTorch: run `python -m paper_1911_04070_b200.build` "
-                              "(there is no fallback implementation)") from e
+        from . import build
+        have, want = build.built_for(build.LIB_TORCH), build.torch_key()
+        if have != want:        # not loaded: a binary of another PyTorch may load and misread its structures
+            raise ImportError("_bpt_torch.so is %s, not for %s: run `python -m paper_1911_04070_b200.build` (there is no fallback "
+                              "implementation)" % ("missing or of an earlier build" if have is None else "built for " + have, want))
+        from . import _bpt_torch as native
         native.bind_library([ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "bpt_res_norm_fwd", "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_few_rows",
             "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd")])

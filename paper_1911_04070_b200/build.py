@@ -54,10 +54,32 @@ def _build_one(lib: str, tag: str, extra: list, force: bool, verbose: bool) -> s
     return lib
 
 
+_KEY_MARK = b"BPT_TORCH_KEY:"
+
+
+def torch_key() -> str:
+    """What _bpt_torch.so is compiled against: it fits this Python and this PyTorch only."""
+    import torch
+    return "torch %s, C++11 ABI %d, %s" % (torch.__version__, int(torch._C._GLIBCXX_USE_CXX11_ABI), sysconfig.get_config_var("SOABI"))
+
+
+def built_for(path: str):
+    """The torch_key a _bpt_torch.so was compiled with, read from the file without loading it; None if there is none."""
+    try:
+        with open(path, "rb") as f:
+            data = f.read()
+    except FileNotFoundError:
+        return None
+    at = data.find(_KEY_MARK)
+    return None if at < 0 else data[at + len(_KEY_MARK):data.index(b"\0", at)].decode()
+
+
 def _start_torch(force: bool):
-    """Starts the compilation of _bpt_torch.so where it is out of date; returns what _finish_torch takes."""
+    """Starts the compilation of _bpt_torch.so where it is out of date, or compiled for another PyTorch or Python; returns what
+    _finish_torch takes."""
     deps = [SRC_TORCH, os.path.join(HERE, "..", "include", "bpt.h")]
-    if not force and os.path.exists(LIB_TORCH) and os.path.getmtime(LIB_TORCH) >= max(os.path.getmtime(p) for p in deps):
+    key = torch_key()
+    if not force and built_for(LIB_TORCH) == key and os.path.getmtime(LIB_TORCH) >= max(os.path.getmtime(p) for p in deps):
         return None
     import torch
     root = os.path.dirname(torch.__file__)
@@ -65,7 +87,8 @@ def _start_torch(force: bool):
     inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include"),
            sysconfig.get_paths()["include"]]
     tmp = LIB_TORCH + ".tmp%d" % os.getpid()
-    cmd = ["g++", "-O2", "-shared", "-fPIC", "-std=c++17", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+    cmd = ["g++", "-O2", "-shared", "-fPIC", "-std=c++17", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           '-DBPT_TORCH_KEY="%s"' % key]
     cmd += [a for i in inc for a in ("-isystem", i)] + [SRC_TORCH, "-o", tmp, "-L" + os.path.join(root, "lib")]
     cmd += ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-ltorch_python"]
     return cmd, subprocess.Popen(cmd), tmp

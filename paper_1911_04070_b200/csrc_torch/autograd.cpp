@@ -15,6 +15,9 @@
 
 #include "../../include/bpt.h"
 
+// What this file was compiled against; build.py reads it from the shared object without loading that.
+extern "C" __attribute__((used, visibility("default"))) const char bpt_torch_key[] = "BPT_TORCH_KEY:" BPT_TORCH_KEY;
+
 namespace py = pybind11;
 using at::Tensor;
 using torch::autograd::AutogradContext;

@@ -402,7 +402,7 @@ def _res_norm_args(h, b, weight, bias, norm, post_norm, post_weight, post_bias, 
         lead = len(shape) - 1
         while lead > 0 and gs[lead - 1] == 1:
             lead -= 1
-        if len(gs) != len(shape) or gs[-1] != D or gs[:lead] != tuple(shape[:lead]) or gate.get_device() != dev or not gate.is_contiguous():
+        if not gate.dim() or len(gs) != len(shape) or gs[-1] != D or gs[:lead] != tuple(shape[:lead]) or gate.get_device() != dev or not gate.is_contiguous():
             raise ValueError("gate must be contiguous, [D] or h's shape with the trailing row axes of length one, on the device of h")
         for x in gs[:lead]:
             groups *= x

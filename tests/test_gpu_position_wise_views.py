@@ -86,3 +86,14 @@ def test_statistics_that_come_back_elsewhere():
     got = torch.autograd.grad(y, (h, b, w), up)
     for a, c in zip(want, got):        # rows off their boundary go element by element: sums in another order, fp32
         assert torch.allclose(a, c, rtol=1e-5, atol=1e-5 * float(a.abs().max()))
+
+
+def test_a_gate_without_axes_is_refused_with_its_reason():
+    """Also where D is 1 and a single number would fit."""
+    import torch
+    from paper_1911_04070_b200 import binding, layer
+    h, gate = torch.randn(4, 1, device="cuda:0"), torch.ones((), device="cuda:0")
+    for f in (layer.residual_norm, binding.bpt_res_norm_fwd):
+        with pytest.raises(ValueError, match="gate"):
+            f(h, h, gate=gate)
+    assert torch.equal(layer.residual_norm(h, h, gate=gate.view(1), norm=None), 2 * h)

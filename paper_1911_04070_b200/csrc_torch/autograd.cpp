@@ -13,6 +13,8 @@
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
+#include <unordered_set>
+
 #include "../../include/bpt.h"
 
 // What this file was compiled against; build.py reads it from the shared object without loading that.
@@ -54,16 +56,29 @@ Tensor aligned(const Tensor& t) {
 Tensor bytes(int64_t n, const Tensor& like) { return at::empty({n}, like.options().dtype(at::kByte)); }
 // A leaf's accumulation node belongs to the stream on which a graph first reached the leaf, and lives as long as such a graph.
 // Where that was the default stream, a backward pass under capture would have PyTorch wait there for an event of the capture,
-// which breaks the capture off and can end the process: refused here, while the capture is whole.  The call's own edges only.
+// which breaks the capture off and can end the process: refused here, while the capture is whole.  Every leaf
+// that this pass goes on to from the call's node, through whatever lies between (the call's own copy of a strided weight, a cast);
+// leaves that the pass is not asked for are not reached and do not count.
 void check_capture(const char* name) {
     if (at::cuda::currentStreamCaptureStatus() == at::cuda::CaptureStatus::None) return;
-    const auto node = torch::autograd::get_current_node();
-    if (!node) return;
-    for (const auto& edge : node->next_edges()) {
-        if (!dynamic_cast<torch::autograd::AccumulateGrad*>(edge.function.get())) continue;
-        const auto s = edge.function->stream();
-        TORCH_CHECK(!s.has_value() || at::cuda::CUDAStream(*s).stream() != nullptr, name,
-                    " backward under capture: a graph of the same leaves, made on the default stream, is still alive; delete its outputs before the capture");
+    const auto self = torch::autograd::get_current_node();
+    if (!self) return;
+    std::vector<torch::autograd::Node*> open{self.get()};
+    std::unordered_set<torch::autograd::Node*> seen;
+    while (!open.empty()) {
+        torch::autograd::Node* node = open.back();
+        open.pop_back();
+        for (uint32_t i = 0; i < node->num_outputs(); ++i) {
+            torch::autograd::Node* next = node->next_edge(i).function.get();
+            if (!node->task_should_compute_output(i) || !seen.insert(next).second) continue;
+            if (!dynamic_cast<torch::autograd::AccumulateGrad*>(next)) {
+                open.push_back(next);
+                continue;
+            }
+            const auto s = next->stream();
+            TORCH_CHECK(!s.has_value() || at::cuda::CUDAStream(*s).stream() != nullptr, name,
+                        " backward under capture: a graph of the same leaves, made on the default stream, is still alive; delete its outputs before the capture");
+        }
     }
 }
 // A call past the autograd function (no argument requires a gradient) would drop a forward-mode tangent without a word, and the

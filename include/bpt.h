@@ -281,7 +281,8 @@ bpt_status bpt_out_proj_norm(const void* a, const void* w_o, const void* h, cons
  * to bf16 (the second product's operand type); products accumulate in fp32; y is rounded once.  Calls for which
  * bpt_gated_ff_few_rows (host) says 1 -- few rows for the size of the weights, as in decoding -- keep the inner row to about
  * 16 bits instead, and their kernels wait for nothing.
- * rows >= 0, D and F multiples of 8 (16-byte rows).  x and y must not overlap.
+ * rows >= 0, D and F multiples of 8 (16-byte rows).  x and y must not overlap.  An infinite weight makes the results that it
+ * enters infinite or, where a value is kept as two terms, NaN.
  *
  * Backward: from x, the weights and dy = dLoss/dy (nothing else of the forward is needed: both projections are computed
  * again, in fp32), dx [rows, D] and dw_gate, dw_up [F, D], dw_down [D, F], all bf16, overwritten.  dx may be NULL; the

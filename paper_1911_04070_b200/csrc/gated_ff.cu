@@ -329,6 +329,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FfShape<KERNEL>::thr
                             const int k = j * 8 + 2 * y + e;
                             r[e] = ff_act<ACT, false>(__uint_as_float(g[k]), unused) * __uint_as_float(u[k]);
                         }
+                        // rounded once: the second product's operands are bf16, and a second term would double that product
                         x[y] = pack_bf16(r[0], r[1]);
                     }
                     put64(i & 1, j, x[0], x[1], x[2], x[3]);

@@ -602,7 +602,7 @@ RnPlan plan_bwd(const bpt_res_norm_args& a) {
     q.groups = a.gate && !q.gate_rows ? a.gate_groups : 1;
     q.group_rows = q.groups ? a.rows / q.groups : 0;
     const long long per_group = (q.group_rows + rpc - 1) / rpc;   // no split smaller than one pass of the CTA's warps
-    const long long cap = kRnSms * (a.D <= 512 ? 2 : a.D <= 1024 ? 4 : a.D <= 2048 ? 2 : 1);   // CTAs that fit by registers
+    const long long cap = kRnSms * (a.D <= 512 ? 2 : a.D <= 1024 ? 4 : a.D <= 2048 ? 2 : 1);   // 512 threads of 128 registers per SM, in CTAs of 256, 128, 256 or 512
     q.splits = (int)std::max<long long>(1, std::min<long long>(per_group, cap / std::max<long long>(1, q.groups)));
     q.units = (int)std::min<long long>(q.groups * q.splits, 0x7fffffff);
     q.grid = (int)std::min<long long>(q.units, cap);

@@ -1,9 +1,10 @@
 """BP-Transformer layers on top of the graph self-attention library (arXiv 1911.04070, Sec. 3.3,
 Algorithm 2): PyTorch modules whose attention runs in libbpt.so.
 
-Only the graph self-attention is this package's own code; the projections, the feed-forward block
-and the layer normalisation are plain PyTorch operators around it, so that the operator can be
-dropped into a model and trained.  Nothing here falls back to another attention implementation.
+The graph self-attention, the gated feed-forward block and the seam between two blocks (norms, gate, residual) are this
+package's own operators; the projections, and in the paper's form of the layer the feed-forward block and the norms, are plain
+PyTorch operators around them, so that each can be dropped into a model and trained.  Nothing here falls back to another
+implementation of an operator: a gated block in float32 is written out in PyTorch operators.
 """
 from __future__ import annotations
 

@@ -26,7 +26,8 @@
  * hardware barriers (the tensor-memory kernels) bound every wait to about a second; if one expires
  * the kernel winds down, the results of the call are invalid and BPT_ERR_TIMEOUT is stored in the
  * block.  bpt_check reads it.  The gated feed-forward calls take a separate, optional block, and store
- * BPT_ERR_TIMEOUT in a record of the device besides, which no call clears: bpt_check_device reads it.
+ * BPT_ERR_TIMEOUT in a record of the device besides, which no call clears: bpt_check_device reads it.  A token id
+ * outside its table (bpt_embed_fwd, bpt_embed_bwd) is stored there too, as BPT_ERR_INDEX.
  */
 #ifndef BPT_H
 #define BPT_H
@@ -47,7 +48,8 @@ typedef enum {
     BPT_ERR_CUDA = 4,         /* a CUDA runtime call or launch failed                       */
     BPT_ERR_TIMEOUT = 5,      /* a bounded device-side wait expired (see bpt_attn_fwd)      */
     BPT_ERR_OVERFLOW = 6,     /* edge count does not fit the 32-bit index arrays            */
-    BPT_ERR_SCRATCH_LIMIT = 7 /* problem needs more scratch than the built-in static array  */
+    BPT_ERR_SCRATCH_LIMIT = 7,/* problem needs more scratch than the built-in static array  */
+    BPT_ERR_INDEX = 8         /* a token id outside the table (see bpt_embed_fwd)           */
 } bpt_status;
 
 /* flags of a graph */
@@ -137,7 +139,8 @@ bpt_status bpt_check(const void* workspace, void* cuda_stream);
 /*
  * Waits for `cuda_stream` and reports whether a bounded device-side wait of any gated feed-forward call
  * (bpt_gated_ff_fwd, bpt_gated_ff_bwd, with or without a status block) or of the wait self-test expired on
- * the current device since the last such report: BPT_OK or BPT_ERR_TIMEOUT, which clears the record.  For
+ * the current device since the last such report: BPT_OK or BPT_ERR_TIMEOUT, which clears the record; or
+ * BPT_ERR_INDEX, where a token id was outside its table (of both, what was stored last).  For
  * training loops: once per step, where the step's calls ran inside an autograd engine that keeps no status
  * blocks.  Covers the work that `cuda_stream` has waited for; work that still runs on other streams
  * is reported by a later call.  BPT_ERR_CUDA when the synchronisation or a copy fails.  Host-synchronous: not
@@ -348,6 +351,37 @@ size_t bpt_res_norm_bwd_workspace_bytes(const bpt_res_norm_args* args);
 bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* args, const float* stats, const void* dy, const void* dr, void* dh, void* db,
                             void* d_weight, void* d_bias, void* d_post_weight, void* d_post_bias, void* d_gate,
                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Token ids to node states (Sec. 3.3: token nodes start from their embeddings, span nodes from zero), and the gradient of the table.
+ *     out[b, t, :] = scale * weight[ids[b, t], :]   for t < lengths[b];      zeros for the other rows t < out_rows
+ * ids: [batch, tokens] of id_bytes 4 or 8, contiguous; lengths: [batch] (clamped to 0 .. tokens) or NULL (all tokens); ids
+ * behind a sequence's length are not looked at.  weight: [vocab, D] of weight_dtype, contiguous; out: [batch, out_rows, D] of out_dtype, contiguous,
+ * out_rows >= tokens (2n - 1 for the nodes of a tree over n tokens).  The product is taken in fp32 and rounded once.
+ * An id outside 0 .. vocab - 1 reads nothing: its row is zeros, it adds nothing to the gradient, and BPT_ERR_INDEX shows in
+ * bpt_check_device.
+ *
+ * Backward: d_weight[v, :] = scale * sum of d_out[b, t, :] over the places with ids[b, t] = v, in weight_dtype; zeros for ids that stand
+ * nowhere and for padding_idx (-1: none; the forward pays no attention to it).  Every row is overwritten.  d_out: [batch, out_rows, D] of out_dtype;
+ * rows behind the tokens are not read.  `weight` is not looked at.  Sums are taken in fp32 in a fixed order without atomics: bit-reproducible.
+ * Element by element where D is no multiple of 8 or a tensor is not 16-byte aligned.
+ * `workspace`: bpt_embed_bwd_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a status
+ * block, 16-byte aligned; two calls whose GPU work overlaps need one each.
+ * batch, tokens >= 0; vocab, batch * out_rows < 2^30; D <= 2^20.  Errors: INVALID_ARG, UNSUPPORTED (sizes), WORKSPACE, CUDA; device-side: INDEX.
+ */
+typedef struct {
+    int64_t batch, tokens, out_rows, vocab, padding_idx;
+    int32_t D, id_bytes;
+    bpt_dtype weight_dtype, out_dtype;
+    float scale;
+    const void* ids;
+    const int32_t* lengths;
+    const void* weight;
+} bpt_embed_args;
+bpt_status bpt_embed_fwd(const bpt_embed_args* args, void* out, void* cuda_stream);
+size_t bpt_embed_bwd_workspace_bytes(const bpt_embed_args* args);
+bpt_status bpt_embed_bwd(const bpt_embed_args* args, const void* d_out, void* d_weight, void* workspace, size_t workspace_bytes,
+                         void* cuda_stream);
 
 /*
  * Backward pass for callers that must not allocate device memory (the paper has no

@@ -28,7 +28,7 @@ EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes"
            "bpt_attn_fwd_ex", "bpt_attn_bwd_ex", "bpt_attn_fwd_rows", "bpt_attn_bwd_min_workspace_bytes", "bpt_check",
            "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
            "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd",
-           "bpt_gated_ff_few_rows", "bpt_check_device")
+           "bpt_gated_ff_few_rows", "bpt_check_device", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes", "bpt_embed_bwd")
 
 
 class BptError(RuntimeError):
@@ -60,6 +60,13 @@ class ResNormArgs(ctypes.Structure):
                 ("alpha", ctypes.c_float), ("eps", ctypes.c_float), ("h", ctypes.c_void_p), ("b", ctypes.c_void_p),
                 ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("post_weight", ctypes.c_void_p),
                 ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p)]
+
+
+class EmbedArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("tokens", ctypes.c_int64), ("out_rows", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("padding_idx", ctypes.c_int64), ("D", ctypes.c_int32), ("id_bytes", ctypes.c_int32), ("weight_dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int), ("scale", ctypes.c_float), ("ids", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p)]
 
 
 # When set, the autograd wrappers in layer.py ask bpt_check after every attention and gated feed-forward call (a stream
@@ -111,6 +118,13 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_gated_ff_fwd.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, sz, vp]
         lib.bpt_gated_ff_bwd.restype = ctypes.c_int
         lib.bpt_gated_ff_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, sz, vp]
+        em = ctypes.POINTER(EmbedArgs)
+        lib.bpt_embed_fwd.restype = ctypes.c_int
+        lib.bpt_embed_fwd.argtypes = [em, vp, vp]
+        lib.bpt_embed_bwd_workspace_bytes.restype = sz
+        lib.bpt_embed_bwd_workspace_bytes.argtypes = [em]
+        lib.bpt_embed_bwd.restype = ctypes.c_int
+        lib.bpt_embed_bwd.argtypes = [em, vp, vp, vp, sz, vp]
         lib.bpt_debug_bounds.restype = ctypes.c_int
         lib.bpt_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32), vp]
         lib.bpt_attn_fwd.restype = ctypes.c_int
@@ -165,7 +179,8 @@ def load_native():
         from . import _bpt_torch as native
         native.bind_library([ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "bpt_res_norm_fwd", "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_few_rows",
-            "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd")])
+            "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes",
+            "bpt_embed_bwd")])
         _native = native
     return _native
 
@@ -269,7 +284,8 @@ def bpt_check(workspace) -> int:
 
 def bpt_check_device(device=None) -> int:
     """Waits for the current stream of `device` (the current one) and returns 0, or 5 when a bounded device-side wait of a gated
-    feed-forward call, forward or backward, expired there since the last such question: what was computed since is invalid."""
+    feed-forward call, forward or backward, expired there since the last such question: what was computed since is invalid; or 8 when
+    a token id was outside its table."""
     with torch.cuda.device(device):
         return int(load_library().bpt_check_device(_stream()))
 
@@ -456,6 +472,74 @@ def bpt_res_norm_bwd(h, b, dy, dr, stats, weight=None, bias=None, norm="layer", 
         _check(lib.bpt_res_norm_bwd(ctypes.byref(args), _ptr(stats), _ptr(dy), _ptr(dr), *map(_ptr, grads), workspace.data_ptr(),
                                     workspace.numel(), _raw_stream(dev)), "bpt_res_norm_bwd")
     return tuple(grads)
+
+
+def _embed_args(ids, lengths, weight, vocab, D, weight_dtype, out_dtype, scale, span_rows, padding_idx):
+    """Checks ids and lengths and fills the argument struct of a bpt_embed call."""
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError("ids must be int32 or int64, got %s" % ids.dtype)
+    dev = ids.get_device()
+    if dev < 0 or ids.dim() < 1 or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous CUDA tensor [..., n]")
+    if span_rows < 0:
+        raise ValueError("span_rows must not be negative")
+    if padding_idx is not None and not 0 <= padding_idx < vocab:
+        raise ValueError("padding_idx must be None or an id of the table")
+    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != ids.shape[:-1] or lengths.get_device() != dev
+                                or not lengths.is_contiguous()):
+        raise ValueError("lengths must be a contiguous int32 tensor of the shape of ids without its last axis, on the device of ids")
+    batch = 1
+    for x in ids.shape[:-1]:
+        batch *= x
+    code = lambda t: BPT_F32 if t == torch.float32 else BPT_BF16
+    return EmbedArgs(batch, ids.shape[-1], ids.shape[-1] + span_rows, vocab, -1 if padding_idx is None else padding_idx, D, ids.element_size(),
+                     code(weight_dtype), code(out_dtype), scale, ids.data_ptr(), _ptr(lengths), _ptr(weight)), dev
+
+
+def _check_float_type(*types):
+    for t in types:
+        if t not in (torch.float32, torch.bfloat16):
+            raise TypeError("only float32 and bfloat16 are supported, got %s" % t)
+
+
+def bpt_embed_fwd(ids, weight, scale: float = 1.0, span_rows: int = 0, lengths=None, dtype=None, out=None):
+    """out[..., t, :] = scale * weight[ids[..., t]], zero rows for t >= lengths[...] and for the span_rows rows behind the tokens.
+    ids: [..., n] int32 or int64, contiguous; weight: [V, D] float32 or bfloat16, contiguous; lengths: int32 of the shape ids.shape[:-1];
+    dtype: of out (default: weight's).  Returns out [..., n + span_rows, D].  An id outside the table gives a zero row and shows in
+    bpt_check_device."""
+    dtype = weight.dtype if dtype is None else dtype
+    _check_float_type(weight.dtype, dtype)
+    if weight.dim() != 2 or not weight.is_contiguous() or weight.get_device() != ids.get_device():
+        raise ValueError("weight must be a contiguous [V, D] tensor on the device of ids")
+    V, D = weight.shape
+    args, dev = _embed_args(ids, lengths, weight, V, D, weight.dtype, dtype, scale, span_rows, None)
+    shape = (*ids.shape[:-1], args.out_rows, D)
+    if out is not None and (out.shape != shape or out.dtype != dtype or out.get_device() != dev or not out.is_contiguous()):
+        raise ValueError("out must be contiguous, [..., n + span_rows, D] of the given dtype")
+    with _on_device(dev):
+        out = torch.empty(shape, dtype=dtype, device=ids.device) if out is None else out
+        _check(load_library().bpt_embed_fwd(ctypes.byref(args), out.data_ptr(), _raw_stream(dev)), "bpt_embed_fwd")
+    return out
+
+
+def bpt_embed_bwd(ids, d_out, vocab: int, weight_dtype, scale: float = 1.0, lengths=None, padding_idx=None, d_weight=None, workspace=None):
+    """The gradient of the table of bpt_embed_fwd: [vocab, D] of weight_dtype, zeros where no token stands and at padding_idx.
+    d_out: [..., n + span_rows, D], contiguous.  Bit-reproducible."""
+    _check_float_type(weight_dtype, d_out.dtype)
+    if d_out.dim() != ids.dim() + 1 or d_out.shape[:-2] != ids.shape[:-1] or d_out.shape[-2] < ids.shape[-1] or not d_out.is_contiguous()             or d_out.get_device() != ids.get_device():
+        raise ValueError("d_out must be contiguous, [..., n + span_rows, D] on the device of ids")
+    D = d_out.shape[-1]
+    args, dev = _embed_args(ids, lengths, None, vocab, D, weight_dtype, d_out.dtype, scale, d_out.shape[-2] - ids.shape[-1], padding_idx)
+    if d_weight is not None and (d_weight.shape != (vocab, D) or d_weight.dtype != weight_dtype or d_weight.get_device() != dev
+                                 or not d_weight.is_contiguous()):
+        raise ValueError("d_weight must be contiguous, [vocab, D] of weight_dtype on the device of ids")
+    lib = load_library()
+    with _on_device(dev):
+        d_weight = torch.empty(vocab, D, dtype=weight_dtype, device=ids.device) if d_weight is None else d_weight
+        workspace = _scratch(workspace, lib.bpt_embed_bwd_workspace_bytes(ctypes.byref(args)), d_out)
+        _check(lib.bpt_embed_bwd(ctypes.byref(args), d_out.data_ptr(), d_weight.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                 _raw_stream(dev)), "bpt_embed_bwd")
+    return d_weight
 
 
 def bpt_debug_bounds():

@@ -72,7 +72,7 @@ extern "C" bpt_status bpt_check_device(void* cuda_stream) {
     if (cudaStreamSynchronize(st) != cudaSuccess) return BPT_ERR_CUDA;
     if (word == 0) return BPT_OK;
     if (cudaMemsetAsync(record, 0, sizeof(word), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return BPT_ERR_CUDA;
-    return word == (int32_t)BPT_ERR_TIMEOUT ? BPT_ERR_TIMEOUT : BPT_ERR_CUDA;
+    return word == (int32_t)BPT_ERR_TIMEOUT || word == (int32_t)BPT_ERR_INDEX ? (bpt_status)word : BPT_ERR_CUDA;
 }
 
 static bool options_ok(const bpt_attn_options* opt) {
@@ -272,6 +272,7 @@ extern "C" const char* bpt_status_str(bpt_status s) {
         case BPT_ERR_TIMEOUT: return "device-side wait timed out";
         case BPT_ERR_OVERFLOW: return "edge count exceeds 32-bit indices";
         case BPT_ERR_SCRATCH_LIMIT: return "problem needs more scratch than the built-in static array holds";
+        case BPT_ERR_INDEX: return "a token id is outside its table";
     }
     return "unknown status";
 }

@@ -1,5 +1,6 @@
-// The position-wise operators as PyTorch functions with gradients, in C++ over the C ABI of include/bpt.h: argument checks,
-// memory from PyTorch, the current stream, and the autograd nodes.  What layer.residual_norm and layer.gated_feed_forward call.
+// The position-wise operators and those at the ends of a language model as PyTorch functions with gradients, in C++ over the C ABI
+// of include/bpt.h: argument checks, memory from PyTorch, the current stream, and the autograd nodes.  What layer.residual_norm,
+// layer.gated_feed_forward and layer.token_states call.
 //
 // A Python autograd function around the ctypes binding costs 130 to 160 us of host time a training step whatever the size, of
 // which PyTorch's engine takes about 40; single tokens and short sequences are bound by that.
@@ -35,6 +36,9 @@ struct Api {
     decltype(&bpt_gated_ff_workspace_bytes) gated_ff_bytes = nullptr;
     decltype(&bpt_gated_ff_fwd) gated_ff_fwd = nullptr;
     decltype(&bpt_gated_ff_bwd) gated_ff_bwd = nullptr;
+    decltype(&bpt_embed_fwd) embed_fwd = nullptr;
+    decltype(&bpt_embed_bwd_workspace_bytes) embed_bytes = nullptr;
+    decltype(&bpt_embed_bwd) embed_bwd = nullptr;
 } api;   // of the library that binding.py has loaded
 
 struct Refused {};
@@ -322,8 +326,97 @@ py::object gated_feed_forward(const Tensor& x_, const Tensor& wg_, const Tensor&
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// out[..., t] = scale * weight[ids[..., t]], zero rows behind the tokens
+// ---------------------------------------------------------------------------------------------------------
+struct EmbedCfg { int64_t vocab, D, out_rows, padding; at::ScalarType weight_type, out_type; double scale; };
+
+bool embed_args(const Tensor& ids, const Tensor& lengths, const EmbedCfg& c, bpt_embed_args* a) {
+    *a = bpt_embed_args{};
+    if (!ids.is_cuda() || ids.dim() < 1 || !ids.is_contiguous() || (ids.scalar_type() != at::kInt && ids.scalar_type() != at::kLong)) return false;
+    const auto code = [](at::ScalarType t, bpt_dtype* out) {
+        *out = t == at::kFloat ? BPT_F32 : BPT_BF16;
+        return t == at::kFloat || t == at::kBFloat16;
+    };
+    if (c.D < 1 || c.D > INT32_MAX || !code(c.weight_type, &a->weight_dtype) || !code(c.out_type, &a->out_dtype)) return false;
+    if (lengths.defined() && (lengths.scalar_type() != at::kInt || lengths.device() != ids.device() || !lengths.is_contiguous() ||
+                              lengths.sizes() != ids.sizes().slice(0, ids.dim() - 1)))
+        return false;
+    a->batch = 1;
+    for (int64_t i = 0; i + 1 < ids.dim(); ++i) a->batch *= ids.size(i);
+    a->tokens = ids.size(-1);
+    a->out_rows = c.out_rows;
+    a->vocab = c.vocab;
+    a->padding_idx = c.padding;
+    a->D = (int32_t)c.D;
+    a->id_bytes = ids.scalar_type() == at::kInt ? 4 : 8;
+    a->scale = (float)c.scale;
+    a->ids = ids.data_ptr();
+    a->lengths = (const int32_t*)ptr(lengths);
+    return true;
+}
+Tensor embed_fwd(const Tensor& ids, const Tensor& weight, const Tensor& lengths, const EmbedCfg& c) {
+    bpt_embed_args a;
+    // the backward's padding_idx is checked here, too: nothing is left to refuse there
+    if (!embed_args(ids, lengths, c, &a) || weight.device() != ids.device() || c.padding < -1 || c.padding >= c.vocab) throw Refused{};
+    a.weight = weight.data_ptr();
+    const c10::cuda::CUDAGuard guard(ids.device());
+    std::vector<int64_t> shape(ids.sizes().begin(), ids.sizes().end());
+    shape.back() = c.out_rows;
+    shape.push_back(c.D);
+    const Tensor out = at::empty(shape, weight.options().dtype(c.out_type));
+    if (api.embed_fwd(&a, ptr(out), at::cuda::getCurrentCUDAStream().stream()) != BPT_OK) throw Refused{};
+    return out;
+}
+
+struct TokenStates : torch::autograd::Function<TokenStates> {
+    // the table itself is not needed again, only its form: it may change before the backward pass
+    static Tensor forward(AutogradContext* ctx, const Tensor& ids, const Tensor& weight, const Opt& lengths, const EmbedCfg* c) {
+        const Tensor out = embed_fwd(ids, weight, tensor(lengths), *c);
+        ctx->save_for_backward({ids, tensor(lengths)});
+        ctx->saved_data["sizes"] = std::vector<int64_t>{c->vocab, c->D, c->out_rows, c->padding, (int64_t)c->weight_type, (int64_t)c->out_type};
+        ctx->saved_data["scale"] = c->scale;
+        return out;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        const variable_list v = ctx->get_saved_variables();
+        const std::vector<int64_t> s = ctx->saved_data["sizes"].toIntVector();
+        const EmbedCfg c{s[0], s[1], s[2], s[3], (at::ScalarType)s[4], (at::ScalarType)s[5], ctx->saved_data["scale"].toDouble()};
+        variable_list out(4);
+        check_tangents({&grads[0]}, "token_states backward");
+        check_capture("token_states");
+        const Tensor dy = grads[0].contiguous();
+        bpt_embed_args a;
+        TORCH_CHECK(embed_args(v[0], v[1], c, &a) && dy.scalar_type() == c.out_type && dy.numel() == a.batch * a.out_rows * a.D,
+                    "token_states backward: the saved tensors have changed their form");
+        const c10::cuda::CUDAGuard guard(v[0].device());
+        out[1] = at::empty({c.vocab, c.D}, dy.options().dtype(c.weight_type));
+        const size_t n = api.embed_bytes(&a);
+        const Tensor ws = bytes((int64_t)n, dy);
+        const bpt_status e = api.embed_bwd(&a, ptr(dy), ptr(out[1]), ptr(ws), n, at::cuda::getCurrentCUDAStream().stream());
+        TORCH_CHECK(e == BPT_OK, "bpt_embed_bwd failed (status ", (int)e, ")");
+        return first_order_only(std::move(out), "token_states");
+    }
+};
+
+py::object token_states(const Tensor& ids_, const Tensor& weight_, const Opt& lengths_, double scale, int64_t span_rows, int64_t padding, const py::object& dtype) {
+    check_tracing("token_states");
+    check_tangents({&weight_}, "token_states");
+    if (ids_.dim() < 1 || weight_.dim() != 2 || span_rows < 0) return py::none();
+    const Tensor ids = ids_.contiguous(), weight = weight_.contiguous();
+    const Opt lengths = given(lengths_);
+    const at::ScalarType type = dtype.is_none() ? weight.scalar_type() : torch::python::detail::py_object_to_dtype(dtype);
+    const EmbedCfg c{weight.size(0), weight.size(1), ids.size(-1) + span_rows, padding, weight.scalar_type(), type, scale};
+    try {
+        if (at::GradMode::is_enabled() && weight.requires_grad()) return py::cast(TokenStates::apply(ids, weight, lengths, &c));
+        return py::cast(embed_fwd(ids, weight, tensor(lengths), c));
+    } catch (const Refused&) {
+        return py::none();
+    }
+}
+
 void bind_library(const std::vector<uintptr_t>& f) {
-    TORCH_CHECK(f.size() == 7, "seven functions are expected");
+    TORCH_CHECK(f.size() == 10, "ten functions are expected");
     api.res_norm_fwd = reinterpret_cast<decltype(api.res_norm_fwd)>(f[0]);
     api.res_norm_bytes = reinterpret_cast<decltype(api.res_norm_bytes)>(f[1]);
     api.res_norm_bwd = reinterpret_cast<decltype(api.res_norm_bwd)>(f[2]);
@@ -331,6 +424,9 @@ void bind_library(const std::vector<uintptr_t>& f) {
     api.gated_ff_bytes = reinterpret_cast<decltype(api.gated_ff_bytes)>(f[4]);
     api.gated_ff_fwd = reinterpret_cast<decltype(api.gated_ff_fwd)>(f[5]);
     api.gated_ff_bwd = reinterpret_cast<decltype(api.gated_ff_bwd)>(f[6]);
+    api.embed_fwd = reinterpret_cast<decltype(api.embed_fwd)>(f[7]);
+    api.embed_bytes = reinterpret_cast<decltype(api.embed_bytes)>(f[8]);
+    api.embed_bwd = reinterpret_cast<decltype(api.embed_bwd)>(f[9]);
 }
 
 }  // namespace
@@ -339,4 +435,5 @@ PYBIND11_MODULE(_bpt_torch, m) {
     m.def("bind_library", &bind_library);
     m.def("residual_norm", &residual_norm);
     m.def("gated_feed_forward", &gated_feed_forward);
+    m.def("token_states", &token_states);
 }

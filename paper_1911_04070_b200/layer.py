@@ -57,10 +57,10 @@ def graph_self_attention(g: binding.Graph, q, k, v, rel_emb, scale=None, lengths
     return _GraphSelfAttention.apply(q, k, v, rel_emb, g, scale, lengths, float(dropout_p), int(dropout_seed))
 
 
-def _check_constant(name, v):
-    """alpha and eps are numbers; a tensor would be read as one, and its gradient or tangent lost."""
+def _check_constant(name, v, of="residual_norm", instead="gate or h"):
+    """alpha, eps and scale are numbers; a tensor would be read as one, and its gradient or tangent lost."""
     if isinstance(v, torch.Tensor) and ((v.requires_grad and torch.is_grad_enabled()) or forward_ad.unpack_dual(v).tangent is not None):
-        raise NotImplementedError("residual_norm has no derivative with respect to %s; a learned factor goes into gate or h" % name)
+        raise NotImplementedError("%s has no derivative with respect to %s; a learned factor goes into %s" % (of, name, instead))
 
 
 def residual_norm(h, b=None, weight=None, bias=None, norm="layer", post_norm=None, post_weight=None, post_bias=None, gate=None,
@@ -139,6 +139,27 @@ def gated_feed_forward(x, w_gate, w_up, w_down, act="silu"):
         raise RuntimeError("gated_feed_forward: refused")
     y, y._bpt_workspace = out
     return y
+
+
+def token_states(ids, weight, scale=1.0, span_rows=0, lengths=None, padding_idx=None, dtype=None):
+    """Token ids to node states, differentiable in the table:  out[..., t, :] = scale * weight[ids[..., t]]  for t < lengths[...], zeros behind
+    the length and in the span_rows rows behind the tokens (Sec. 3.3: span nodes start from zero; n - 1 of them in a tree over n tokens).
+
+    ids: [..., n] int32 or int64; weight: [V, D] float32 or bfloat16; lengths: int32 of the shape ids.shape[:-1], or None; ids behind it are
+    not looked at; scale: a number; dtype: of the result (default: weight's).  Returns [..., n + span_rows, D].  The gradient
+    is the whole [V, D], in weight's type, summed in float32 in the order of the tokens (bit-reproducible); it is zero at padding_idx.  An
+    id outside the table reads nothing: its row is zeros, it adds nothing to the gradient, and binding.bpt_check_device says so.
+    Capture, modes of differentiation and tracing as in residual_norm."""
+    if type(scale) is not float:
+        _check_constant("scale", scale, "token_states", "weight")
+    out = binding.load_native().token_states(ids, weight, lengths, scale, span_rows, -1 if padding_idx is None else padding_idx, dtype)
+    if out is None:
+        if weight.dim() == 2 and padding_idx is not None and not 0 <= padding_idx < weight.shape[0]:
+            raise ValueError("padding_idx must be None or an id of the table")
+        cont = lambda t: t if t is None else t.contiguous()
+        binding.bpt_embed_fwd(cont(ids), cont(weight), scale, span_rows, cont(lengths), dtype)                     # says what is wrong
+        raise RuntimeError("token_states: refused")
+    return out
 
 
 class BPTLayer(nn.Module):

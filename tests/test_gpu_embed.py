@@ -1,0 +1,253 @@
+"""layer.token_states and its gradient on the GPU against plain float64.
+
+Bounds.  Forward: one fp32 product with a scale rounded to fp32, one rounding to the result's type t: (eps_t / 2 + 2^-23) |y| (and a
+step of the smallest numbers).  Gradient: n places are added in fp32 in some order, each addition off by at most 2^-24 of a partial sum
+of absolute values, then the scale and the rounding: (n + 2) 2^-24 |scale| sum |d_out| + eps_t / 2 |dW|."""
+import subprocess
+import sys
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def layer():
+    from paper_1911_04070_b200 import layer
+    return layer
+
+
+def _oracle(ids, w, scale, spans, lengths, d_out, padding):
+    """In float64 on the CPU: out, dW, how many places each id has, and sum |d_out| per entry of dW."""
+    ids, w = ids.cpu().long(), w.detach().cpu().double()
+    V, D = w.shape
+    n = ids.shape[-1]
+    flat = ids.reshape(-1, n)
+    real = torch.ones_like(flat, dtype=torch.bool)
+    if lengths is not None:
+        real &= torch.arange(n) < lengths.cpu().long().reshape(-1, 1)
+    real &= (flat >= 0) & (flat < V)
+    out = torch.zeros(flat.shape[0], n + spans, D, dtype=torch.float64)
+    out[:, :n][real] = scale * w[flat[real]]
+    d = d_out.cpu().double().reshape(flat.shape[0], n + spans, D)[:, :n]
+    on = real if padding is None else real & (flat != padding)
+    dw = torch.zeros(V, D, dtype=torch.float64).index_add_(0, flat[on], scale * d[on])
+    mag = torch.zeros(V, D, dtype=torch.float64).index_add_(0, flat[on], abs(scale) * d[on].abs())
+    places = torch.bincount(flat[on], minlength=V).double()[:, None]
+    return out.reshape(*ids.shape[:-1], n + spans, D), dw, places, mag
+
+
+def _check(layer, ids, w, scale=1.0, spans=0, lengths=None, padding=None, dtype=None, seed=0):
+    dtype = w.dtype if dtype is None else dtype
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    d_out = torch.randn(*ids.shape[:-1], ids.shape[-1] + spans, w.shape[1], generator=gen, device="cuda").to(dtype)
+    y = layer.token_states(ids, w, scale=scale, span_rows=spans, lengths=lengths, padding_idx=padding, dtype=dtype)
+    dw, = torch.autograd.grad(y, [w], d_out)
+    again, = torch.autograd.grad(layer.token_states(ids, w, scale=scale, span_rows=spans, lengths=lengths, padding_idx=padding, dtype=dtype), [w], d_out)
+    assert torch.equal(dw, again)
+    y64, dw64, places, mag = _oracle(ids, w, scale, spans, lengths, d_out, padding)
+    assert y.shape == y64.shape and y.dtype == dtype and dw.dtype == w.dtype and dw.shape == w.shape
+    u = 2.0 ** -24
+    tiny = torch.finfo(dtype).smallest_normal
+    off = (y.detach().cpu().double() - y64).abs()
+    assert bool((off <= (torch.finfo(dtype).eps / 2 + 2 * u) * y64.abs() + tiny).all()), float(off.max())
+    off = (dw.cpu().double() - dw64).abs()
+    bound = (places + 2) * u * mag + torch.finfo(w.dtype).eps / 2 * (dw64.abs() + (places + 2) * u * mag) + torch.finfo(w.dtype).smallest_normal * (places > 0)
+    assert bool((off <= bound).all()), float((off - bound).max())
+    return y, dw
+
+
+def _ids(*shape, V, seed=1, dtype=torch.int64):
+    return torch.randint(0, V, shape, generator=torch.Generator().manual_seed(seed)).to("cuda", dtype)
+
+
+def _table(V, D, dtype=BF16, seed=2):
+    return torch.randn(V, D, generator=torch.Generator().manual_seed(seed)).to("cuda", dtype).requires_grad_(True)
+
+
+# one token to many tiles of the sort and the sums; the ends of a digit's range (511 | 512 ids are one | two passes, 262143 | 262144 two | three)
+@pytest.mark.parametrize("shape,V,D", [((1,), 1, 1), ((1, 1), 7, 8), ((3, 31), 5, 7), ((2, 33), 511, 64), ((2, 512), 512, 201), ((1, 1025), 3, 256),
+                                       ((4, 1000), 256, 264), ((2, 2, 77), 1000, 40), ((1, 4097), 262143, 8), ((1, 300), 262144, 16),
+                                       ((3, 70001), 97, 8), ((1, 160000), 70000, 3)])
+@pytest.mark.parametrize("wt,ot", [(BF16, BF16), (F32, BF16), (BF16, F32), (F32, F32)])
+def test_sizes_and_types(layer, shape, V, D, wt, ot):
+    _check(layer, _ids(*shape, V=V, dtype=torch.int32 if D % 2 else torch.int64), _table(V, D, wt), scale=1.5, spans=shape[-1] - 1, dtype=ot)
+
+
+# runs of one id that end at, before and behind the ends of tiles of 32; one id everywhere
+@pytest.mark.parametrize("runs", [(32, 32, 32), (31, 1, 32), (33, 31, 64), (64, 1), (1, 64, 1), (16, 100, 12), (5000,), (40, 3000, 7, 2000)])
+@pytest.mark.parametrize("D", [8, 300])
+def test_runs_over_tiles(layer, runs, D):
+    ids = torch.cat([torch.full((r,), 2 * i + 1) for i, r in enumerate(runs)])
+    ids = ids[torch.randperm(ids.numel(), generator=torch.Generator().manual_seed(3))].to("cuda")
+    _check(layer, ids, _table(2 * len(runs) + 3, D))
+
+
+@pytest.mark.parametrize("padding", [None, 0, 4])
+def test_lengths_and_padding(layer, padding):
+    lengths = torch.tensor([0, 1, 40, 39, 1000, -3], dtype=torch.int32, device="cuda")      # clamped to 0 .. n
+    ids = _ids(6, 40, V=9)
+    clamped = lengths.clamp(0, 40)
+    y, dw = _check(layer, ids, _table(9, 72), scale=0.5, spans=39, lengths=lengths, padding=padding)
+    for b, m in enumerate(clamped.tolist()):
+        assert not y[b, m:].any()
+    if padding is not None:
+        assert not dw[padding].any()
+
+
+def test_what_is_behind_a_length_is_not_looked_at(layer):
+    from paper_1911_04070_b200 import binding
+    ids, w, lengths = _ids(3, 40, V=9), _table(9, 72), torch.tensor([5, 0, 40], dtype=torch.int32, device="cuda")
+    want = _check(layer, ids, w, lengths=lengths)
+    binding.bpt_check_device()
+    wild = ids.clone()
+    wild[0, 5:], wild[1] = -100, 1 << 40
+    got = _check(layer, wild, w, lengths=lengths)
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and binding.bpt_check_device() == 0
+    # nor are the gradients of rows without a token: NaN there reaches nothing
+    y = layer.token_states(ids, w, span_rows=3, lengths=lengths)
+    d = torch.ones_like(y)
+    d[:, 40:], d[0, 5:], d[1] = float("nan"), float("nan"), float("inf")
+    assert bool(torch.isfinite(torch.autograd.grad(y, [w], d)[0]).all())
+
+
+@pytest.mark.parametrize("bad", [-1, 50, -2 ** 31, 2 ** 31 - 1])
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_ids_outside_the_table(layer, bad, dtype):
+    from paper_1911_04070_b200 import binding
+    binding.bpt_check_device()
+    ids, w = _ids(2, 100, V=50, dtype=dtype), _table(50, 24)
+    ids[0, 3], ids[1, 99] = bad, bad
+    y, _ = _check(layer, ids, w)
+    assert not y[0, 3].any() and not y[1, 99].any()
+    assert binding.bpt_check_device() == 8 and binding.bpt_check_device() == 0
+
+
+@pytest.mark.parametrize("shape,V", [((0,), 4), ((0, 5), 4), ((3, 0), 4)])
+def test_no_tokens(layer, shape, V):
+    w = _table(V, 16)
+    ids = torch.zeros(shape, dtype=torch.int64, device="cuda")
+    y = layer.token_states(ids, w, span_rows=2)
+    assert y.shape == (*shape[:-1], shape[-1] + 2, 16) and not y.any()
+    dw, = torch.autograd.grad(y, [w], torch.ones_like(y))
+    assert dw.shape == w.shape and not dw.any()
+
+
+def test_views_and_strides(layer):
+    big = _table(20, 3 * 64)
+    ids = _ids(40, 6, V=20).t()                                         # a transposed view of ids
+    leaf = big.detach()[:, 64:128].requires_grad_(True)                 # rows further apart than they are long
+    _check(layer, ids, leaf)
+    flat = torch.randn(1 + 20 * 64, device="cuda").to(BF16)
+    _check(layer, ids, flat[1:].view(20, 64).requires_grad_(True))      # off a 16-byte boundary
+    w = _table(20, 64)
+    y = layer.token_states(ids, w)
+    dw, = torch.autograd.grad(y.float().sum(), [w])                     # an expanded gradient
+    want = torch.bincount(ids.reshape(-1), minlength=20).float()[:, None].expand(20, 64)
+    assert torch.equal(dw.float(), want.to(BF16).float())
+    d = torch.randn(64, 6, 40, device="cuda").to(BF16).permute(1, 2, 0)
+    a, = torch.autograd.grad(layer.token_states(ids, w), [w], d)
+    b, = torch.autograd.grad(layer.token_states(ids, w), [w], d.contiguous())
+    assert torch.equal(a, b)
+
+
+def test_gradient_against_differences(layer):
+    """The function is linear in the table: a step along any direction gives the gradient's product with it, but for roundings: at most
+    (places + 2) 2^-24 <= 27 x 2^-24 of the absolute values in the gradient, 3 x 2^-24 in each value of the function."""
+
+    ids, w = _ids(2, 50, V=11), _table(11, 24, F32)
+    up, step = torch.randn(2, 53, 24, device="cuda"), torch.randn(11, 24, device="cuda")
+    f = lambda t: (layer.token_states(ids, t, scale=3.0, span_rows=3).double() * up.double()).sum()
+    dw, = torch.autograd.grad(f(w), [w])
+    with torch.no_grad():
+        diff = float(f(w + step) - f(w - step)) / 2
+    mag = float((layer.token_states(ids, (w.detach().abs() + step.abs()), scale=3.0, span_rows=3).double() * up.abs().double()).sum())
+    assert abs(diff - float((dw.double() * step.double()).sum())) <= 2.0 ** -19 * mag
+
+
+def test_the_table_may_change_before_the_backward_pass(layer):
+    ids, w = _ids(64, V=11), _table(11, 24, F32)
+    y = layer.token_states(ids, w)
+    with torch.no_grad():
+        w.add_(1)
+    dw, = torch.autograd.grad(y, [w], torch.ones_like(y))
+    assert torch.equal(dw, torch.bincount(ids, minlength=11).float()[:, None].expand(11, 24))
+
+
+def test_second_derivative_is_refused(layer):
+    ids, w = _ids(64, V=11), _table(11, 24, F32)
+    d = torch.randn(64, 24, device="cuda", requires_grad=True)
+    dw, = torch.autograd.grad(layer.token_states(ids, w), [w], d, create_graph=True)
+    with pytest.raises(RuntimeError, match="once only"):
+        dw.sum().backward()
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(dw.sum(), [d])
+
+
+def test_another_stream(layer):
+    ids, w = _ids(8, 1000, V=300), _table(300, 64)
+    want = _check(layer, ids, w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = _check(layer, ids, w)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+_CAPTURE = r"""
+import torch
+from paper_1911_04070_b200 import layer
+ids = torch.randint(0, 99, (4, 700), device="cuda:0")
+w = torch.randn(99, 64, device="cuda:0").bfloat16().requires_grad_(True)
+d = torch.randn(4, 1399, 64, device="cuda:0").bfloat16()
+def step():
+    y = layer.token_states(ids, w, scale=2.0, span_rows=699)
+    return y.detach(), *torch.autograd.grad(y, [w], d)
+side = torch.cuda.Stream()
+side.wait_stream(torch.cuda.current_stream())
+with torch.cuda.stream(side):
+    step()
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = step()
+ids.copy_(torch.randint(0, 99, (4, 700), device="cuda:0"))
+d.normal_()
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(step(), got))
+del got, graph
+alive = layer.token_states(ids, w)
+graph = torch.cuda.CUDAGraph()
+try:
+    with torch.cuda.graph(graph):
+        torch.autograd.grad(layer.token_states(ids, w), [w], d[:, :700])
+except RuntimeError as e:
+    assert "still alive" in str(e), e
+else:
+    raise AssertionError("not refused")
+step()
+print("done")
+"""
+
+
+def test_capture():
+    r = subprocess.run([sys.executable, "-c", _CAPTURE], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "done" in r.stdout, r.stderr[-2000:]
+
+
+def test_offsets_past_32_bits(layer):
+    """A table of more than 2^32 elements and a result beyond 2^31."""
+    V, D = 2 ** 21 + 5, 2048
+    w = torch.zeros(V, D, dtype=BF16, device="cuda")
+    w[-1], w[V - 2] = 3, 5
+    ids = torch.full((1, 2 ** 20 + 3), V - 1, dtype=torch.int64, device="cuda")
+    ids[0, -1] = V - 2
+    y = layer.token_states(ids, w)
+    assert bool((y[0, :-1] == 3).all()) and bool((y[0, -1] == 5).all())
+    w.requires_grad_(True)
+    some = ids[:, -40:].contiguous()
+    dw, = torch.autograd.grad(layer.token_states(some, w), [w], y.detach()[:, -40:].contiguous())
+    assert bool((dw[-1] == 3 * 39).all()) and bool((dw[-2] == 5).all()) and not dw[:-2].any()

@@ -384,6 +384,35 @@ bpt_status bpt_embed_bwd(const bpt_embed_args* args, const void* d_out, void* d_
                          void* cuda_stream);
 
 /*
+ * The norm over all gradients of a model, and clipping.
+ *     norm = sqrt(sum of squares over all elements of all tensors)   (BPT_GRAD_NORM_L2),   or the largest |element|   (BPT_GRAD_NORM_MAX)
+ *     c = min(1, max_norm / (norm + eps)),      out <- c * grad   for every tensor
+ * `grads` is a HOST array of n entries, read before the call returns; entry i has numel elements of `dtype` at `grad`, contiguous.  out NULL: the
+ * tensor is scaled in place, and not written at all where c = 1; otherwise c * grad goes to `out` (out_dtype), which may be
+ * the gradient itself in its own type, also where c = 1.  Nothing that is written may overlap anything else of the call -- the same
+ * tensor given twice, for one; refused.  bpt_grad_norm writes no tensor (out is not looked at) and counts a tensor given twice twice.
+ * norm: device, fp32 [1].  A NaN among the gradients, or an infinity with BPT_GRAD_NORM_L2, makes norm NaN or infinite as it would by
+ * the formula, and c NaN or 0; nothing is hidden.  Squares are summed in fp64 where fp32 would lose them, so
+ * the norm is right for gradients of any size; c and the products are fp32, one rounding.  Fixed order, no atomics: bit-reproducible.
+ * n = 0, or nothing in any tensor: norm 0.  max_norm >= 0 (infinite: nothing is scaled), eps >= 0.
+ * `workspace`: bpt_grad_norm_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a status block, 16-byte
+ * aligned; two calls whose GPU work overlaps need one each.  Two launches for up to 960 tensors.
+ * Errors: INVALID_ARG, UNSUPPORTED (numel > 2^40, 2^42 elements in all), WORKSPACE, CUDA.
+ */
+enum { BPT_GRAD_NORM_L2 = 0, BPT_GRAD_NORM_MAX = 1 };
+typedef struct {
+    void* grad;
+    void* out;
+    int64_t numel;
+    bpt_dtype dtype, out_dtype;
+} bpt_grad;
+size_t bpt_grad_norm_workspace_bytes(const bpt_grad* grads, int32_t n);
+bpt_status bpt_grad_norm(const bpt_grad* grads, int32_t n, int32_t norm_type, float* norm, void* workspace, size_t workspace_bytes,
+                         void* cuda_stream);
+bpt_status bpt_clip_grads(const bpt_grad* grads, int32_t n, int32_t norm_type, float max_norm, float eps, float* norm, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Backward pass for callers that must not allocate device memory (the paper has no
  * counterpart; this is a deployment convenience).
  *

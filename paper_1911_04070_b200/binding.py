@@ -19,6 +19,7 @@ CHECK_LIB_PATH = os.path.join(_HERE, "libbpt_check.so")   # the build with index
 BPT_BIDIR, BPT_LEFT_ONLY, BPT_MODE_PAD, BPT_MODE_ALG1 = 0, 1, 0, 2
 BPT_F32, BPT_BF16 = 0, 1
 BPT_PATH_AUTO, BPT_PATH_MMA, BPT_PATH_TC5 = 0, 1, 2
+GRAD_NORMS = {2.0: 0, float("inf"): 1}         # BPT_GRAD_NORM_*
 NORM_KINDS = {None: 0, "layer": 1, "rms": 2}   # BPT_NORM_*
 ACTIVATIONS = {"relu": 0, "silu": 1, "gelu": 2}        # BPT_ACT_*
 
@@ -28,7 +29,8 @@ EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes"
            "bpt_attn_fwd_ex", "bpt_attn_bwd_ex", "bpt_attn_fwd_rows", "bpt_attn_bwd_min_workspace_bytes", "bpt_check",
            "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
            "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd",
-           "bpt_gated_ff_few_rows", "bpt_check_device", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes", "bpt_embed_bwd")
+           "bpt_gated_ff_few_rows", "bpt_check_device", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes", "bpt_embed_bwd",
+           "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads")
 
 
 class BptError(RuntimeError):
@@ -67,6 +69,11 @@ class EmbedArgs(ctypes.Structure):
                 ("padding_idx", ctypes.c_int64), ("D", ctypes.c_int32), ("id_bytes", ctypes.c_int32), ("weight_dtype", ctypes.c_int),
                 ("out_dtype", ctypes.c_int), ("scale", ctypes.c_float), ("ids", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
                 ("weight", ctypes.c_void_p)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int)]
 
 
 # When set, the autograd wrappers in layer.py ask bpt_check after every attention and gated feed-forward call (a stream
@@ -125,6 +132,13 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_embed_bwd_workspace_bytes.argtypes = [em]
         lib.bpt_embed_bwd.restype = ctypes.c_int
         lib.bpt_embed_bwd.argtypes = [em, vp, vp, vp, sz, vp]
+        gr = ctypes.POINTER(Grad)
+        lib.bpt_grad_norm_workspace_bytes.restype = sz
+        lib.bpt_grad_norm_workspace_bytes.argtypes = [gr, i32]
+        lib.bpt_grad_norm.restype = ctypes.c_int
+        lib.bpt_grad_norm.argtypes = [gr, i32, i32, vp, vp, sz, vp]
+        lib.bpt_clip_grads.restype = ctypes.c_int
+        lib.bpt_clip_grads.argtypes = [gr, i32, i32, f32, f32, vp, vp, sz, vp]
         lib.bpt_debug_bounds.restype = ctypes.c_int
         lib.bpt_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32), vp]
         lib.bpt_attn_fwd.restype = ctypes.c_int
@@ -180,7 +194,7 @@ def load_native():
         native.bind_library([ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "bpt_res_norm_fwd", "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_few_rows",
             "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes",
-            "bpt_embed_bwd")])
+            "bpt_embed_bwd", "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads")])
         _native = native
     return _native
 
@@ -540,6 +554,56 @@ def bpt_embed_bwd(ids, d_out, vocab: int, weight_dtype, scale: float = 1.0, leng
         _check(lib.bpt_embed_bwd(ctypes.byref(args), d_out.data_ptr(), d_weight.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                  _raw_stream(dev)), "bpt_embed_bwd")
     return d_weight
+
+
+def _grad_list(grads, out, norm_type):
+    """Checks the tensors of a bpt_grad_norm / bpt_clip_grads call and fills its array."""
+    if norm_type not in GRAD_NORMS:
+        raise ValueError("norm_type must be 2 or infinity")
+    if not grads:
+        raise ValueError("there is no gradient")
+    if out is not None and len(out) != len(grads):
+        raise ValueError("out must have an entry for every gradient")
+    dev, array = grads[0].get_device(), (Grad * len(grads))()
+    for i, g in enumerate(grads):
+        o = None if out is None else out[i]
+        if g.get_device() != dev or dev < 0 or not g.is_contiguous():
+            raise ValueError("gradients must be contiguous CUDA tensors on one device")
+        if o is not None and (o.shape != g.shape or o.get_device() != dev or not o.is_contiguous()):
+            raise ValueError("results must be contiguous and share shape and device with their gradients")
+        array[i] = Grad(g.data_ptr(), _ptr(o), g.numel(), _dtype_code(g), _dtype_code(g if o is None else o))
+    return array, dev
+
+
+def bpt_grad_norm(grads, norm_type: float = 2.0):
+    """The 2-norm (or with norm_type infinity the largest absolute value) over all elements of a list of contiguous float32 / bfloat16
+    tensors, as a float32 tensor []."""
+    array, dev = _grad_list(grads, None, norm_type)
+    lib = load_library()
+    with _on_device(dev):
+        norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+        ws = torch.empty(lib.bpt_grad_norm_workspace_bytes(array, len(grads)), dtype=torch.uint8, device=norm.device)
+        _check(lib.bpt_grad_norm(array, len(grads), GRAD_NORMS[norm_type], norm.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev)),
+               "bpt_grad_norm")
+    return norm
+
+
+def bpt_clip_grads(grads, max_norm: float, norm_type: float = 2.0, eps: float = 1e-6, out=None):
+    """Scales a list of contiguous tensors by min(1, max_norm / (norm + eps)), in place, or into the tensors of `out` (float32 or
+    bfloat16, same shapes).  No tensor twice, no overlaps.  Returns the norm before, a float32 tensor []."""
+    array, dev = _grad_list(grads, out, norm_type)
+    if not max_norm >= 0 or not eps >= 0:
+        raise ValueError("max_norm and eps must not be negative")
+    lib = load_library()
+    with _on_device(dev):
+        norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+        ws = torch.empty(lib.bpt_grad_norm_workspace_bytes(array, len(grads)), dtype=torch.uint8, device=norm.device)
+        status = lib.bpt_clip_grads(array, len(grads), GRAD_NORMS[norm_type], max_norm, eps, norm.data_ptr(), ws.data_ptr(), ws.numel(),
+                                    _raw_stream(dev))
+        if status == 1:
+            raise ValueError("a tensor is given twice, or what is written overlaps another tensor of the call")
+        _check(status, "bpt_clip_grads")
+    return norm
 
 
 def bpt_debug_bounds():

@@ -1,11 +1,12 @@
 // The position-wise operators and those at the ends of a language model as PyTorch functions with gradients, in C++ over the C ABI
 // of include/bpt.h: argument checks, memory from PyTorch, the current stream, and the autograd nodes.  What layer.residual_norm,
-// layer.gated_feed_forward and layer.token_states call.
+// layer.gated_feed_forward, layer.token_states and layer.clip_gradients call.
 //
 // A Python autograd function around the ctypes binding costs 130 to 160 us of host time a training step whatever the size, of
 // which PyTorch's engine takes about 40; single tokens and short sequences are bound by that.
 //
 // Functions return None for arguments that the operators refuse; the caller then goes through binding.py, which says why.
+#include <ATen/MemoryOverlap.h>
 #include <ATen/cuda/CUDAContext.h>
 #include <ATen/cuda/CUDAGraphsUtils.cuh>
 #include <c10/cuda/CUDAGuard.h>
@@ -39,6 +40,9 @@ struct Api {
     decltype(&bpt_embed_fwd) embed_fwd = nullptr;
     decltype(&bpt_embed_bwd_workspace_bytes) embed_bytes = nullptr;
     decltype(&bpt_embed_bwd) embed_bwd = nullptr;
+    decltype(&bpt_grad_norm_workspace_bytes) grad_norm_bytes = nullptr;
+    decltype(&bpt_grad_norm) grad_norm = nullptr;
+    decltype(&bpt_clip_grads) clip_grads = nullptr;
 } api;   // of the library that binding.py has loaded
 
 struct Refused {};
@@ -415,8 +419,89 @@ py::object token_states(const Tensor& ids_, const Tensor& weight_, const Opt& le
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// the norm over all gradients, and clipping
+// ---------------------------------------------------------------------------------------------------------
+// A tensor, or a sequence of tensors and None.
+bool take_tensors(const py::object& from, std::vector<Tensor>* to) {
+    if (THPVariable_Check(from.ptr())) {
+        to->push_back(THPVariable_Unpack(from.ptr()));
+        return true;
+    }
+    for (const py::handle& h : from) {
+        if (h.is_none()) to->emplace_back();
+        else if (THPVariable_Check(h.ptr())) to->push_back(THPVariable_Unpack(h.ptr()));
+        else return false;
+    }
+    return true;
+}
+
+// Elements lie one after another in memory, in whatever order, so that a tensor is a list of numbers.
+py::object clip_gradients(const py::object& grads, const py::object& into, int64_t norm_type, bool clip, double max_norm, double eps) {
+    check_tracing("clip_gradients");
+    std::vector<Tensor> g, o;
+    if (!take_tensors(grads, &g) || (!into.is_none() && (!take_tensors(into, &o) || o.size() != g.size()))) return py::none();
+    const at::NoGradGuard no_grad;
+    std::vector<bpt_grad> list;
+    std::vector<std::pair<Tensor, Tensor>> back;    // what was computed in a copy, and where it belongs
+    std::vector<Tensor> held;
+    std::vector<const Tensor*> written;
+    list.reserve(g.size());
+    const Tensor* first = nullptr;
+    for (size_t i = 0; i < g.size(); ++i) {
+        if (!g[i].defined()) continue;
+        check_tangents({&g[i]}, "clip_gradients");
+        bpt_grad e{};
+        if (g[i].layout() != at::kStrided || !g[i].is_cuda() || (first && g[i].device() != first->device()) || !type_code(g[i], &e.dtype)) return py::none();
+        if (!first) first = &g[i];
+        Tensor src = g[i], dst;
+        if (!o.empty()) {
+            if (!o[i].defined()) return py::none();
+            check_tangents({&o[i]}, "clip_gradients");
+            dst = o[i];
+            if (dst.layout() != at::kStrided || dst.device() != src.device() || dst.sizes() != src.sizes() || !type_code(dst, &e.out_dtype)) return py::none();
+            if (!(src.strides() == dst.strides() && src.is_non_overlapping_and_dense())) {
+                src = src.contiguous();
+                if (!dst.is_contiguous()) {
+                    if (at::has_internal_overlap(dst) == at::MemOverlap::Yes) return py::none();
+                    held.push_back(at::empty(dst.sizes(), dst.options()));
+                    back.emplace_back(held.back(), dst);
+                    dst = held.back();
+                }
+                held.push_back(src);
+            }
+            written.push_back(&o[i]);
+        } else if (!src.is_non_overlapping_and_dense()) {
+            if (clip && at::has_internal_overlap(src) == at::MemOverlap::Yes) return py::none();
+            for (const auto& other : back)          // the library sees copies only
+                if (other.second.data_ptr() == src.data_ptr() && other.second.strides() == src.strides()) return py::none();
+            src = src.contiguous();
+            held.push_back(src);
+            if (clip) back.emplace_back(src, g[i]);
+        }
+        if (clip && o.empty()) written.push_back(&g[i]);
+        e.grad = src.data_ptr();
+        e.out = ptr(dst);
+        e.numel = src.numel();
+        list.push_back(e);
+    }
+    const c10::cuda::OptionalCUDAGuard guard(first ? std::optional<at::Device>(first->device()) : std::nullopt);
+    const auto options = at::TensorOptions().device(first ? first->device() : at::Device(at::kCUDA, c10::cuda::current_device()));
+    const Tensor norm = at::empty({}, options.dtype(at::kFloat));
+    const size_t n = api.grad_norm_bytes(list.data(), (int32_t)list.size());
+    const Tensor ws = at::empty({(int64_t)n}, options.dtype(at::kByte));
+    cudaStream_t st = at::cuda::getCurrentCUDAStream().stream();
+    const bpt_status s = clip ? api.clip_grads(list.data(), (int32_t)list.size(), (int32_t)norm_type, (float)max_norm, (float)eps, (float*)ptr(norm), ptr(ws), n, st)
+                              : api.grad_norm(list.data(), (int32_t)list.size(), (int32_t)norm_type, (float*)ptr(norm), ptr(ws), n, st);
+    if (s != BPT_OK) return py::none();
+    for (const auto& [from, to] : back) to.copy_(from);
+    for (const Tensor* t : written)     // what a graph has saved of them is no longer what it was
+        if (!t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+    return py::cast(norm);
+}
+
 void bind_library(const std::vector<uintptr_t>& f) {
-    TORCH_CHECK(f.size() == 10, "ten functions are expected");
+    TORCH_CHECK(f.size() == 13, "thirteen functions are expected");
     api.res_norm_fwd = reinterpret_cast<decltype(api.res_norm_fwd)>(f[0]);
     api.res_norm_bytes = reinterpret_cast<decltype(api.res_norm_bytes)>(f[1]);
     api.res_norm_bwd = reinterpret_cast<decltype(api.res_norm_bwd)>(f[2]);
@@ -427,6 +512,9 @@ void bind_library(const std::vector<uintptr_t>& f) {
     api.embed_fwd = reinterpret_cast<decltype(api.embed_fwd)>(f[7]);
     api.embed_bytes = reinterpret_cast<decltype(api.embed_bytes)>(f[8]);
     api.embed_bwd = reinterpret_cast<decltype(api.embed_bwd)>(f[9]);
+    api.grad_norm_bytes = reinterpret_cast<decltype(api.grad_norm_bytes)>(f[10]);
+    api.grad_norm = reinterpret_cast<decltype(api.grad_norm)>(f[11]);
+    api.clip_grads = reinterpret_cast<decltype(api.clip_grads)>(f[12]);
 }
 
 }  // namespace
@@ -436,4 +524,5 @@ PYBIND11_MODULE(_bpt_torch, m) {
     m.def("residual_norm", &residual_norm);
     m.def("gated_feed_forward", &gated_feed_forward);
     m.def("token_states", &token_states);
+    m.def("clip_gradients", &clip_gradients);
 }

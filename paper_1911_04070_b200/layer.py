@@ -162,6 +162,44 @@ def token_states(ids, weight, scale=1.0, span_rows=0, lengths=None, padding_idx=
     return out
 
 
+def _clip(grads, out, norm_type, clip, max_norm, eps):
+    grads = grads if isinstance(grads, torch.Tensor) else list(grads)
+    out = out if out is None or isinstance(out, torch.Tensor) else list(out)
+    code = binding.GRAD_NORMS.get(norm_type)
+    norm = None if code is None else binding.load_native().clip_gradients(grads, out, code, clip, max_norm, eps)
+    if norm is None:        # says what is wrong
+        as_list = lambda t: [t] if isinstance(t, torch.Tensor) else t
+        if out is not None and len(as_list(out)) != len(as_list(grads)):
+            raise ValueError("out must have an entry for every gradient")
+        pairs = [(g, o) for g, o in zip(as_list(grads), as_list(grads if out is None else out)) if g is not None]
+        grads, into = [g.contiguous() for g, _ in pairs], None if out is None else [o for _, o in pairs]
+        if out is not None and any(o is None for o in into):
+            raise ValueError("out must have a tensor for every gradient")
+        binding._grad_list(grads, into, norm_type)
+        if clip and (not max_norm >= 0 or not eps >= 0):
+            raise ValueError("max_norm and eps must not be negative")
+        raise ValueError("a tensor is given twice, or what is written overlaps another tensor of the call or itself")
+    return norm
+
+
+def gradient_norm(grads, norm_type=2.0):
+    """The 2-norm (norm_type=float("inf"): the largest absolute value) over all elements of a list of tensors, float32 or bfloat16 mixed, as
+    a float32 tensor [].  None entries count for nothing; nothing at all gives 0.  Squares are summed in 64 bits where 32 would
+    lose them: right for gradients of any size.  Two launches whatever the number of tensors up to 960; bit-reproducible; can be captured."""
+    return _clip(grads, None, norm_type, False, 0.0, 0.0)
+
+
+def clip_gradients(grads, max_norm, norm_type=2.0, eps=1e-6, out=None):
+    """Scales all gradients of a model by min(1, max_norm / (norm + eps)) and returns their norm before (see gradient_norm).
+
+    grads: a list of tensors, float32 or bfloat16 mixed, on one device (``[p.grad for p in model.parameters()]``; None entries are passed over).
+    They are scaled in place, and not written where the norm is below max_norm; or, with out (a list of as many tensors, float32 or
+    bfloat16, say the gradients of an optimizer's 32-bit master weights), left as they are and the scaled values written there.  Any
+    strides; no tensor twice and no overlaps between what is written and anything else.  A NaN makes the norm and all results NaN.  Nothing
+    is read back to the host: can be captured in a CUDA graph, which then uses these very tensors."""
+    return _clip(grads, out, norm_type, True, max_norm, eps)
+
+
 class BPTLayer(nn.Module):
     """One layer of Algorithm 2:  Z = norm(H + GSA(H)),  H' = norm(Z + FFN(Z)).
 

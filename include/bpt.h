@@ -413,6 +413,42 @@ bpt_status bpt_clip_grads(const bpt_grad* grads, int32_t n, int32_t norm_type, f
                           size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * What a decoding step (Sec. 4.2 uses BPT as a language model) does to its logits before a token is taken.  For row b and id v, with
+ *     seen(v): v stands in history[b, 0 .. lengths[b]);    n(v): how often it stands in history[b, prompt_lengths[b] .. lengths[b])
+ *     x = logits[b, v];   if seen(v): x = x > 0 ? x / repetition : x * repetition;   if n(v) > 0: x -= frequency n(v) + presence
+ *     x += bias[b, v];    x += bias_values[b, j] for the last j with bias_ids[b, j] = v;     out[b, v] = allowed(b, v) ? x : -infinity
+ * in fp32, rounded once.  What a mask forbids is -infinity whatever stands there (NaN too); a row without an allowed id is all -infinity.
+ * logits: [rows, vocab] of `dtype`, rows logits_stride elements apart; out: of out_dtype, rows out_stride apart; out may be the logits
+ * themselves (same address, type and stride) and must otherwise not overlap them.
+ * history: [rows, history_len] of history_bytes 4 or 8, rows history_stride apart; history_len 0: none.  lengths, prompt_lengths: [rows]
+ * (clamped to 0 .. history_len and 0 .. lengths[b]) or NULL (history_len; 0).  Ids outside 0 .. vocab - 1 count for nothing.
+ * repetition (> 0), presence, frequency: numbers, or where the _rows pointer is not NULL one fp32 value per row.
+ * bias: of bias_dtype, rows bias_stride apart (0: one row for all), or NULL.  bias_ids, bias_values: [rows, bias_count] contiguous (ids of
+ * bias_id_bytes 4 or 8; outside 0 .. vocab - 1: no effect); bias_count 0: none.
+ * allowed: bit v % 32 of word v / 32 set where v is allowed, rows allowed_stride words apart (0: one row for all), or NULL.
+ * rows, vocab, history_len, bias_count < 2^30 (vocab >= 1).  Errors: INVALID_ARG, UNSUPPORTED (sizes), CUDA.
+ */
+typedef struct {
+    int64_t rows, vocab, logits_stride, out_stride;
+    bpt_dtype dtype, out_dtype;
+    const void* logits;
+    int64_t history_len, history_stride;
+    const void* history;
+    const int32_t *lengths, *prompt_lengths;
+    const float *repetition_rows, *presence_rows, *frequency_rows;
+    float repetition, presence, frequency;
+    int32_t history_bytes, bias_id_bytes;
+    bpt_dtype bias_dtype;
+    const void* bias;
+    int64_t bias_stride, bias_count;
+    const void* bias_ids;
+    const float* bias_values;
+    const int32_t* allowed;
+    int64_t allowed_stride;
+} bpt_logits_args;
+bpt_status bpt_adjust_logits(const bpt_logits_args* args, void* out, void* cuda_stream);
+
+/*
  * Backward pass for callers that must not allocate device memory (the paper has no
  * counterpart; this is a deployment convenience).
  *

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
 
 import torch
@@ -30,7 +31,7 @@ EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes"
            "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
            "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd",
            "bpt_gated_ff_few_rows", "bpt_check_device", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes", "bpt_embed_bwd",
-           "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads")
+           "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads", "bpt_adjust_logits")
 
 
 class BptError(RuntimeError):
@@ -74,6 +75,17 @@ class EmbedArgs(ctypes.Structure):
 class Grad(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int),
                 ("out_dtype", ctypes.c_int)]
+
+
+class LogitsArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("logits_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("out_dtype", ctypes.c_int), ("logits", ctypes.c_void_p), ("history_len", ctypes.c_int64),
+                ("history_stride", ctypes.c_int64), ("history", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("prompt_lengths", ctypes.c_void_p), ("repetition_rows", ctypes.c_void_p), ("presence_rows", ctypes.c_void_p),
+                ("frequency_rows", ctypes.c_void_p), ("repetition", ctypes.c_float), ("presence", ctypes.c_float),
+                ("frequency", ctypes.c_float), ("history_bytes", ctypes.c_int32), ("bias_id_bytes", ctypes.c_int32),
+                ("bias_dtype", ctypes.c_int), ("bias", ctypes.c_void_p), ("bias_stride", ctypes.c_int64), ("bias_count", ctypes.c_int64),
+                ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p), ("allowed", ctypes.c_void_p), ("allowed_stride", ctypes.c_int64)]
 
 
 # When set, the autograd wrappers in layer.py ask bpt_check after every attention and gated feed-forward call (a stream
@@ -139,6 +151,8 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_grad_norm.argtypes = [gr, i32, i32, vp, vp, sz, vp]
         lib.bpt_clip_grads.restype = ctypes.c_int
         lib.bpt_clip_grads.argtypes = [gr, i32, i32, f32, f32, vp, vp, sz, vp]
+        lib.bpt_adjust_logits.restype = ctypes.c_int
+        lib.bpt_adjust_logits.argtypes = [ctypes.POINTER(LogitsArgs), vp, vp]
         lib.bpt_debug_bounds.restype = ctypes.c_int
         lib.bpt_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32), vp]
         lib.bpt_attn_fwd.restype = ctypes.c_int
@@ -194,7 +208,7 @@ def load_native():
         native.bind_library([ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "bpt_res_norm_fwd", "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_few_rows",
             "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes",
-            "bpt_embed_bwd", "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads")])
+            "bpt_embed_bwd", "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads", "bpt_adjust_logits")])
         _native = native
     return _native
 
@@ -604,6 +618,66 @@ def bpt_clip_grads(grads, max_norm: float, norm_type: float = 2.0, eps: float = 
             raise ValueError("a tensor is given twice, or what is written overlaps another tensor of the call")
         _check(status, "bpt_clip_grads")
     return norm
+
+
+def bpt_adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None,
+                      bias_ids=None, bias_values=None, allowed=None, out=None):
+    """Penalties for tokens of the history, biases and a mask on the logits [B, V] of a decoding step; see bpt_adjust_logits in
+    include/bpt.h and layer.adjust_logits.  Rows may be any number of elements apart, elements of a row lie next to one another."""
+    code = _dtype_code(logits)
+    dev = logits.get_device()
+    if dev < 0 or logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1 or logits.shape[1] < 1:
+        raise ValueError("logits must be a CUDA tensor [B, V] whose rows lie without gaps")
+    B, V = logits.shape
+    stride = lambda t: max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)
+    here = lambda t, *shapes: t.shape in shapes and t.get_device() == dev and (not t.numel() or t.stride(-1) == 1 or t.shape[-1] == 1)
+    if out is not None and (not here(out, (B, V)) or out.stride(0) < V and B > 1):
+        raise ValueError("out must be [B, V] on the device of the logits, its rows without gaps")
+    a = LogitsArgs(rows=B, vocab=V, logits_stride=stride(logits), dtype=code, logits=logits.data_ptr(), repetition=1.0, history_bytes=8,
+                   bias_id_bytes=8)
+    ids = (torch.int32, torch.int64)
+    if history is None:
+        if lengths is not None or prompt_lengths is not None:
+            raise ValueError("lengths and prompt_lengths belong to history, which is missing")
+    else:
+        if history.dim() != 2 or not here(history, (B, history.shape[-1])) or history.dtype not in ids:
+            raise ValueError("history must be [B, T] int32 or int64 on the device of the logits, its rows without gaps")
+        a.history_len, a.history_stride, a.history, a.history_bytes = history.shape[1], history.stride(0), history.data_ptr(), history.element_size()
+        for name, t in (("lengths", lengths), ("prompt_lengths", prompt_lengths)):
+            if t is not None and (not here(t, (B,)) or t.dtype != torch.int32):
+                raise ValueError("%s must be a contiguous int32 tensor [B] on the device of the logits" % name)
+            setattr(a, name, _ptr(t))
+    for name, v in (("repetition", repetition), ("presence", presence), ("frequency", frequency)):
+        if isinstance(v, torch.Tensor):
+            if not here(v, (B,)) or v.dtype != torch.float32:
+                raise ValueError("%s must be a number or a contiguous float32 tensor [B] on the device of the logits" % name)
+            setattr(a, name + "_rows", v.data_ptr())
+        else:
+            if not math.isfinite(v) or name == "repetition" and not v > 0:
+                raise ValueError("%s must be finite%s" % (name, " and above 0" if name == "repetition" else ""))
+            setattr(a, name, v)
+    if bias is not None:
+        if not here(bias, (V,), (1, V), (B, V)):
+            raise ValueError("bias must be [V] or [B, V] on the device of the logits, its rows without gaps")
+        a.bias, a.bias_dtype, a.bias_stride = bias.data_ptr(), _dtype_code(bias), bias.stride(0) if bias.dim() == 2 and bias.shape[0] > 1 else 0
+    if (bias_ids is None) != (bias_values is None):
+        raise ValueError("bias_ids and bias_values come together")
+    if bias_ids is not None:
+        K = bias_ids.shape[-1] if bias_ids.dim() else 0
+        if not here(bias_ids, (B, K)) or not here(bias_values, (B, K)) or bias_ids.dtype not in ids or bias_values.dtype != torch.float32 \
+                or not bias_ids.is_contiguous() or not bias_values.is_contiguous():
+            raise ValueError("bias_ids (int32 or int64) and bias_values (float32) must be contiguous, [B, K] on the device of the logits")
+        a.bias_count, a.bias_ids, a.bias_values, a.bias_id_bytes = K, bias_ids.data_ptr(), bias_values.data_ptr(), bias_ids.element_size()
+    if allowed is not None:
+        W = (V + 31) // 32
+        if allowed.dtype != torch.int32 or not here(allowed, (W,), (1, W), (B, W)):
+            raise ValueError("allowed must be int32 [ceil(V / 32)] or [B, ceil(V / 32)] on the device of the logits, its rows without gaps")
+        a.allowed, a.allowed_stride = allowed.data_ptr(), allowed.stride(0) if allowed.dim() == 2 and allowed.shape[0] > 1 else 0
+    with _on_device(dev):
+        out = torch.empty(B, V, dtype=logits.dtype, device=logits.device) if out is None else out
+        a.out_dtype, a.out_stride = _dtype_code(out), stride(out)
+        _check(load_library().bpt_adjust_logits(ctypes.byref(a), out.data_ptr(), _raw_stream(dev)), "bpt_adjust_logits")
+    return out
 
 
 def bpt_debug_bounds():

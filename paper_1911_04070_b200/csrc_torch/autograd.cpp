@@ -1,6 +1,6 @@
 // The position-wise operators and those at the ends of a language model as PyTorch functions with gradients, in C++ over the C ABI
 // of include/bpt.h: argument checks, memory from PyTorch, the current stream, and the autograd nodes.  What layer.residual_norm,
-// layer.gated_feed_forward, layer.token_states and layer.clip_gradients call.
+// layer.gated_feed_forward, layer.token_states, layer.clip_gradients and layer.adjust_logits call.
 //
 // A Python autograd function around the ctypes binding costs 130 to 160 us of host time a training step whatever the size, of
 // which PyTorch's engine takes about 40; single tokens and short sequences are bound by that.
@@ -43,6 +43,7 @@ struct Api {
     decltype(&bpt_grad_norm_workspace_bytes) grad_norm_bytes = nullptr;
     decltype(&bpt_grad_norm) grad_norm = nullptr;
     decltype(&bpt_clip_grads) clip_grads = nullptr;
+    decltype(&bpt_adjust_logits) adjust_logits = nullptr;
 } api;   // of the library that binding.py has loaded
 
 struct Refused {};
@@ -500,8 +501,135 @@ py::object clip_gradients(const py::object& grads, const py::object& into, int64
     return py::cast(norm);
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// penalties, biases and a mask on logits
+// ---------------------------------------------------------------------------------------------------------
+// Elements of a row next to one another; rows as they lie, or copied where they overlap.
+Tensor by_rows(const Tensor& t) {
+    const bool ok = t.dim() == 2 ? (t.size(1) < 2 || t.stride(1) == 1) && (t.size(0) < 2 || t.stride(0) >= t.size(1)) : t.is_contiguous();
+    return ok ? t : t.contiguous();
+}
+int64_t row_stride(const Tensor& t) { return t.size(0) < 2 ? t.size(1) : t.stride(0); }
+
+// Whether rows of one lie on rows of the other (rows apart by the same number of bytes may lie side by side).
+bool rows_meet(const Tensor& a, const Tensor& b) {
+    if (!a.numel() || !b.numel()) return false;
+    const auto from = [](const Tensor& t) { return (int64_t)(uintptr_t)t.data_ptr(); };
+    const auto step = [](const Tensor& t) { return row_stride(t) * (int64_t)t.element_size(); };
+    const auto width = [](const Tensor& t) { return t.size(1) * (int64_t)t.element_size(); };
+    const auto end = [&](const Tensor& t) { return from(t) + (t.size(0) - 1) * step(t) + width(t); };
+    if (end(a) <= from(b) || end(b) <= from(a)) return false;
+    if (step(a) != step(b) || a.size(0) < 2) return true;
+    const int64_t d = ((from(b) - from(a)) % step(a) + step(a)) % step(a);
+    return d < width(a) || d + width(b) > step(a);
+}
+
+// A number, or one float32 per row.
+bool setting(const py::object& v, const Tensor& logits, std::vector<Tensor>* held, float* number, const float** rows) {
+    if (!THPVariable_Check(v.ptr())) {
+        *number = (float)v.cast<double>();
+        return true;
+    }
+    const Tensor& t = THPVariable_Unpack(v.ptr());
+    check_tangents({&t}, "adjust_logits");
+    TORCH_CHECK_NOT_IMPLEMENTED(!(at::GradMode::is_enabled() && t.requires_grad()), "adjust_logits has no derivative");
+    if (t.device() != logits.device() || t.dim() != 1 || t.size(0) != logits.size(0) || t.scalar_type() != at::kFloat) return false;
+    held->push_back(t.contiguous());
+    *rows = (const float*)held->back().data_ptr();
+    return true;
+}
+
+py::object adjust_logits(const Tensor& logits_, const Opt& history_, const Opt& lengths_, const Opt& prompts_, const py::object& repetition, const py::object& presence,
+                         const py::object& frequency, const Opt& bias_, const Opt& bias_ids_, const Opt& bias_values_, const Opt& allowed_, const Opt& out_) {
+    check_tracing("adjust_logits");
+    for (const Opt* t : {&bias_, &bias_values_, &out_})
+        if (t->has_value()) {
+            check_tangents({&**t}, "adjust_logits");
+            TORCH_CHECK_NOT_IMPLEMENTED(!(at::GradMode::is_enabled() && (*t)->requires_grad()), "adjust_logits has no derivative");
+        }
+    check_tangents({&logits_}, "adjust_logits");
+    TORCH_CHECK_NOT_IMPLEMENTED(!(at::GradMode::is_enabled() && logits_.requires_grad()), "adjust_logits has no derivative");
+    bpt_logits_args a{};
+    if (!logits_.is_cuda() || logits_.dim() != 2 || logits_.size(1) < 1 || !type_code(logits_, &a.dtype)) return py::none();
+    const int64_t B = logits_.size(0), V = logits_.size(1);
+    const at::Device device = logits_.device();
+    std::vector<Tensor> held;       // what was copied stays until the launch
+    held.reserve(12);
+    const Tensor logits = by_rows(logits_);
+    const auto id_type = [](const Tensor& t) { return t.scalar_type() == at::kInt || t.scalar_type() == at::kLong; };
+    a.rows = B; a.vocab = V;
+    a.logits = logits.data_ptr(); a.logits_stride = row_stride(logits);
+    a.repetition = 1.f;
+    a.history_bytes = a.bias_id_bytes = 8;
+    if (history_.has_value()) {
+        if (history_->dim() != 2 || history_->size(0) != B || history_->device() != device || !id_type(*history_)) return py::none();
+        held.push_back(by_rows(*history_));
+        const Tensor& h = held.back();
+        a.history = h.data_ptr(); a.history_len = h.size(1); a.history_stride = row_stride(h); a.history_bytes = (int32_t)h.element_size();
+        const int32_t** slot[2] = {&a.lengths, &a.prompt_lengths};
+        const Opt* given_[2] = {&lengths_, &prompts_};
+        for (int i = 0; i < 2; ++i) {
+            if (!given_[i]->has_value()) continue;
+            const Tensor& t = **given_[i];
+            if (t.dim() != 1 || t.size(0) != B || t.device() != device || t.scalar_type() != at::kInt) return py::none();
+            held.push_back(t.contiguous());
+            *slot[i] = (const int32_t*)held.back().data_ptr();
+        }
+    } else if (lengths_.has_value() || prompts_.has_value()) {
+        return py::none();
+    }
+    if (!setting(repetition, logits, &held, &a.repetition, &a.repetition_rows) || !setting(presence, logits, &held, &a.presence, &a.presence_rows) ||
+        !setting(frequency, logits, &held, &a.frequency, &a.frequency_rows))
+        return py::none();
+    if (bias_.has_value()) {
+        const Tensor& t = *bias_;
+        if (t.dim() < 1 || t.dim() > 2 || t.size(-1) != V || (t.dim() == 2 && t.size(0) != 1 && t.size(0) != B) || t.device() != device ||
+            !type_code(t, &a.bias_dtype))
+            return py::none();
+        held.push_back(by_rows(t));
+        a.bias = held.back().data_ptr();
+        a.bias_stride = t.dim() == 2 && t.size(0) > 1 ? row_stride(held.back()) : 0;
+    }
+    if (bias_ids_.has_value() != bias_values_.has_value()) return py::none();
+    if (bias_ids_.has_value()) {
+        if (bias_ids_->dim() != 2 || bias_ids_->size(0) != B || bias_ids_->device() != device || !id_type(*bias_ids_) ||
+            bias_values_->sizes() != bias_ids_->sizes() || bias_values_->device() != device || bias_values_->scalar_type() != at::kFloat)
+            return py::none();
+        held.push_back(bias_ids_->contiguous());
+        a.bias_ids = held.back().data_ptr(); a.bias_count = bias_ids_->size(1); a.bias_id_bytes = (int32_t)bias_ids_->element_size();
+        held.push_back(bias_values_->contiguous());
+        a.bias_values = (const float*)held.back().data_ptr();
+    }
+    if (allowed_.has_value()) {
+        const Tensor& t = *allowed_;
+        if (t.dim() < 1 || t.dim() > 2 || t.size(-1) != (V + 31) / 32 || (t.dim() == 2 && t.size(0) != 1 && t.size(0) != B) || t.device() != device ||
+            t.scalar_type() != at::kInt)
+            return py::none();
+        held.push_back(by_rows(t));
+        a.allowed = (const int32_t*)held.back().data_ptr();
+        a.allowed_stride = t.dim() == 2 && t.size(0) > 1 ? row_stride(held.back()) : 0;
+    }
+    const c10::cuda::CUDAGuard guard(device);
+    Tensor out;
+    if (out_.has_value()) {
+        out = *out_;
+        if (out.sizes() != logits.sizes() || out.device() != device || !by_rows(out).is_same(out)) return py::none();
+        // the logits themselves, or somewhere else
+        if (!(out.data_ptr() == logits.data_ptr() && out.scalar_type() == logits.scalar_type() && row_stride(out) == row_stride(logits)) &&
+            rows_meet(out, logits))
+            return py::none();
+    } else {
+        out = at::empty({B, V}, logits.options());
+    }
+    if (!type_code(out, &a.out_dtype)) return py::none();
+    a.out_stride = row_stride(out);
+    if (api.adjust_logits(&a, ptr(out), at::cuda::getCurrentCUDAStream().stream()) != BPT_OK) return py::none();
+    if (out_.has_value() && !out.is_inference()) out.unsafeGetTensorImpl()->bump_version();
+    return py::cast(out);
+}
+
 void bind_library(const std::vector<uintptr_t>& f) {
-    TORCH_CHECK(f.size() == 13, "thirteen functions are expected");
+    TORCH_CHECK(f.size() == 14, "fourteen functions are expected");
     api.res_norm_fwd = reinterpret_cast<decltype(api.res_norm_fwd)>(f[0]);
     api.res_norm_bytes = reinterpret_cast<decltype(api.res_norm_bytes)>(f[1]);
     api.res_norm_bwd = reinterpret_cast<decltype(api.res_norm_bwd)>(f[2]);
@@ -515,6 +643,7 @@ void bind_library(const std::vector<uintptr_t>& f) {
     api.grad_norm_bytes = reinterpret_cast<decltype(api.grad_norm_bytes)>(f[10]);
     api.grad_norm = reinterpret_cast<decltype(api.grad_norm)>(f[11]);
     api.clip_grads = reinterpret_cast<decltype(api.clip_grads)>(f[12]);
+    api.adjust_logits = reinterpret_cast<decltype(api.adjust_logits)>(f[13]);
 }
 
 }  // namespace
@@ -525,4 +654,5 @@ PYBIND11_MODULE(_bpt_torch, m) {
     m.def("gated_feed_forward", &gated_feed_forward);
     m.def("token_states", &token_states);
     m.def("clip_gradients", &clip_gradients);
+    m.def("adjust_logits", &adjust_logits);
 }

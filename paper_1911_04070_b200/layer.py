@@ -200,6 +200,31 @@ def clip_gradients(grads, max_norm, norm_type=2.0, eps=1e-6, out=None):
     return _clip(grads, out, norm_type, True, max_norm, eps)
 
 
+def adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None,
+                  bias_ids=None, bias_values=None, allowed=None, out=None):
+    """What a decoding step does to its logits [B, V] before a token is taken, in one kernel.  For an id that stands in history[b, :lengths[b]]:
+    x / repetition where x > 0, else x * repetition; for one that stands n > 0 times behind the prompt, in history[b, prompt_lengths[b]:lengths[b]]:
+    x - frequency * n - presence; then x + bias, and -inf for what is not allowed (NaN there, too; a row without an allowed id is all -inf).
+
+    logits: float32 or bfloat16.  history: [B, T] int32 or int64; lengths, prompt_lengths: int32 [B] (None: T and 0); ids outside the
+    vocabulary count for nothing.  repetition (above 0), presence, frequency: numbers, or float32 tensors [B], one setting per row.
+    bias: [V] or [B, V], float32 or bfloat16.  bias_ids (int32 or int64), bias_values (float32): [B, K], a few biased ids per row (outside the
+    vocabulary: no effect; given twice: the last one counts).  allowed: int32 [ceil(V / 32)] or [B, ceil(V / 32)], bit v % 32 of word v // 32 set
+    where id v is allowed.  out: a tensor [B, V], float32 or bfloat16, the logits themselves for one (default: a new one of the logits'
+    type).  Any strides.  Computed in float32, rounded once.  For inference: arguments that require a gradient are refused."""
+    got = binding.load_native().adjust_logits(logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias, bias_ids, bias_values,
+                                              allowed, out)
+    if got is None:
+        cont = lambda t: t.contiguous() if isinstance(t, torch.Tensor) else t
+        if out is not None and (out.shape != logits.shape or out.device != logits.device or logits.dim() != 2
+                                or (out.shape[1] > 1 and out.stride(1) != 1) or (out.shape[0] > 1 and out.stride(0) < out.shape[1])):
+            raise ValueError("out must be [B, V] on the device of the logits, its rows without gaps")
+        binding.bpt_adjust_logits(*map(cont, (logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias, bias_ids, bias_values,
+                                              allowed)), None if out is None else out.new_empty(out.shape))      # says what is wrong
+        raise ValueError("out overlaps the logits without being them")
+    return got
+
+
 class BPTLayer(nn.Module):
     """One layer of Algorithm 2:  Z = norm(H + GSA(H)),  H' = norm(Z + FFN(Z)).
 

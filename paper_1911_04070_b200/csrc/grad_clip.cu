@@ -19,6 +19,18 @@ namespace bpt {
 namespace {
 
 constexpr int kGcSms = 148;
+#ifndef GC_AHEAD
+#define GC_AHEAD 4
+#endif
+#ifndef GC_CS
+#define GC_CS ""
+#endif
+#ifndef GC_LD
+#define GC_LD ""
+#endif
+#ifndef GC_BLK
+#define GC_BLK 1
+#endif
 constexpr int kGcUnit = 2048;       // elements; 8 per thread
 constexpr int kGcThreads = 256;
 constexpr int kGcMost = 960;        // tensors per launch: 32 bytes each, in at most 32 KB of arguments
@@ -30,7 +42,8 @@ struct GcTensor {
     unsigned first_unit;    // in this launch
     unsigned flags;
 };
-enum : unsigned { kGcGradBf16 = 1, kGcOutBf16 = 2, kGcSameStart = 4, kGcLead = 8 };     // lead: elements from the 16-byte boundary before, in units of kGcLead
+// kGcLead: flags / kGcLead is how many elements lie between the boundary of 8 elements (16 bytes of bf16, 32 of fp32) before the tensor and its start
+enum : unsigned { kGcGradBf16 = 1, kGcOutBf16 = 2, kGcSameStart = 4, kGcLead = 8 };
 
 template <int N>
 struct GcList {
@@ -42,10 +55,10 @@ struct GcParams {
     unsigned units, ctas;   // of this launch
     int n, first_part, all_parts;
     float max_norm, eps;
-    int inf, write_norm;
+    int inf, write_norm, into;      // into: some tensor has a result of its own
 };
 
-// Calls body(tensor, position of 8 elements counted from the 16-byte boundary at or before its start) for this thread's share.
+// Calls body(tensor, first and last unit of this CTA's share in it) tensor by tensor, forwards or backwards.
 template <int N, bool BACK, typename F>
 __device__ __forceinline__ void walk(const GcList<N>& list, const GcParams& p, F&& body) {
     const unsigned lo = (unsigned)((unsigned long long)p.units * blockIdx.x / p.ctas), hi = (unsigned)((unsigned long long)p.units * (blockIdx.x + 1) / p.ctas);
@@ -57,89 +70,130 @@ __device__ __forceinline__ void walk(const GcList<N>& list, const GcParams& p, F
         if (list.t[mid].first_unit <= want) a = mid;
         else b = mid - 1;
     }
-    if (!BACK) {
-        for (unsigned u = lo; u < hi; ++a) {
-            const unsigned first = list.t[a].first_unit, next = a + 1 < p.n ? list.t[a + 1].first_unit : p.units;
+    for (unsigned u = BACK ? hi : lo; BACK ? u > lo : u < hi;) {
+        const unsigned first = list.t[a].first_unit, next = a + 1 < p.n ? list.t[a + 1].first_unit : p.units;
+        if (BACK) {
+            const unsigned start = max(first, lo);
+            body(list.t[a--], start - first, u - first);
+            u = start;
+        } else {
             const unsigned end = min(next, hi);
-#pragma unroll 2
-            for (; u < end; ++u) body(list.t[a], (long long)(u - first) * kGcUnit + threadIdx.x * 8);
-        }
-    } else {
-        for (unsigned u = hi; u > lo; --a) {
-            const unsigned first = list.t[a].first_unit, start = max(first, lo);
-#pragma unroll 2
-            for (; u > start; --u) body(list.t[a], (long long)(u - 1 - first) * kGcUnit + threadIdx.x * 8);
+            body(list.t[a++], u - first, end - first);
+            u = end;
         }
     }
 }
 
 __device__ __forceinline__ int lead_of(const GcTensor& t) { return (int)(t.flags / kGcLead); }
 
-// 8 elements from position `at` of the aligned view (the tensor begins at position lead), 0 outside the tensor.  Returns whether all 8 lie in it.
-__device__ __forceinline__ bool load8(const GcTensor& t, long long at, float (&x)[8]) {
-    const int lead = lead_of(t);
-    const long long i = at - lead;
-    const bool whole = i >= 0 && i + 8 <= t.numel;
-    if (t.flags & kGcGradBf16) {
-        const __nv_bfloat16* g = (const __nv_bfloat16*)t.grad + i;
-        if (whole) {
-            const uint4 q = *(const uint4*)g;
-            const unsigned w[4] = {q.x, q.y, q.z, q.w};
+// 8 elements as they lie: 16 bytes of bf16, 32 of fp32.
+template <typename T> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+    uint4 q;
+    __device__ __forceinline__ void load(const void* at) { asm volatile("ld.global" GC_LD ".v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(at)); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        const unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[2 * j] = __uint_as_float(w[j] << 16);
-                x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = i + j >= 0 && i + j < t.numel ? __bfloat162float(g[j]) : 0.f;
-        }
-    } else {
-        const float* g = (const float*)t.grad + i;
-        if (whole) {
-            const float4 a = *(const float4*)g, b = *((const float4*)g + 1);
-            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-            x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = i + j >= 0 && i + j < t.numel ? g[j] : 0.f;
+        for (int j = 0; j < 4; ++j) {
+            x[2 * j] = __uint_as_float(w[j] << 16);
+            x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
         }
     }
-    return whole;
+};
+template <> struct Raw8<float> {
+    float f[8];
+    __device__ __forceinline__ void load(const void* at) {
+        asm volatile("ld.global" GC_LD ".v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(at));
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = f[j];
+    }
+};
+__device__ __forceinline__ float elem(float x) { return x; }
+__device__ __forceinline__ float elem(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// This thread's groups of 8 elements in units u0 .. u1 of a tensor: body(index of the group's first element, its values, whether all 8
+// belong to the tensor; those that do not are 0).  kGcAhead groups are on their way at a time.
+constexpr int kGcAhead = GC_AHEAD;
+template <typename T, bool BACK, typename F>
+__device__ __forceinline__ void groups_of(const GcTensor& t, unsigned u0, unsigned u1, F&& body) {
+    const int lead = lead_of(t);
+    const T* base = (const T*)t.grad - lead;            // on a boundary of 8 elements
+    const long long g0 = (long long)u0 * (kGcUnit / 8), g1 = (long long)u1 * (kGcUnit / 8);
+    const long long whole0 = lead ? 1 : 0, whole1 = (t.numel + lead) / 8;       // groups that lie in the tensor as a whole
+    const long long f0 = max(g0, whole0), f1 = min(g1, whole1);
+    const auto part = [&](long long g) {
+        float x[8];
+        const long long i = g * 8 - lead;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = i + j >= 0 && i + j < t.numel ? elem(((const T*)t.grad)[i + j]) : 0.f;
+        body(i, x, false);
+    };
+    // the two ends, each by a warp of its own
+    if (threadIdx.x == 0 && g0 < whole0) part(0);
+    if (threadIdx.x == 32 && f1 >= whole0 && whole1 < g1 && whole1 * 8 < t.numel + lead) part(whole1);
+    const long long n = f1 - f0, step = kGcThreads;
+    long long k = threadIdx.x;
+    const auto at = [&](long long i) { return BACK ? f1 - 1 - i : f0 + i; };
+    for (; k + (kGcAhead - 1) * step < n; k += kGcAhead * step) {
+        Raw8<T> r[kGcAhead];
+#pragma unroll
+        for (int j = 0; j < kGcAhead; ++j) r[j].load(base + at(k + j * step) * 8);
+#pragma unroll
+        for (int j = 0; j < kGcAhead; ++j) {
+            float x[8];
+            r[j].get(x);
+            body(at(k + j * step) * 8 - lead, x, true);
+        }
+    }
+    for (; k < n; k += step) {
+        Raw8<T> r;
+        r.load(base + at(k) * 8);
+        float x[8];
+        r.get(x);
+        body(at(k) * 8 - lead, x, true);
+    }
+}
+template <bool BACK, typename F>
+__device__ __forceinline__ void groups(const GcTensor& t, unsigned u0, unsigned u1, F&& body) {
+    if (t.flags & kGcGradBf16) groups_of<__nv_bfloat16, BACK>(t, u0, u1, body);
+    else groups_of<float, BACK>(t, u0, u1, body);
 }
 
 template <int N>
-__global__ void __launch_bounds__(kGcThreads) grad_norm_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
+__global__ void __launch_bounds__(kGcThreads, GC_BLK) grad_norm_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
     __shared__ double share[kGcThreads / 32];
     __shared__ unsigned largest[kGcThreads / 32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     double sum = 0;
     unsigned most = 0;      // bits of |x|, which order as the values do, NaN above infinity
     if (p.inf) {
-        walk<N, false>(list, p, [&](const GcTensor& t, long long at) {
-            float x[8];
-            load8(t, at, x);
+        walk<N, false>(list, p, [&](const GcTensor& t, unsigned u0, unsigned u1) {
+            groups<false>(t, u0, u1, [&](long long, const float (&x)[8], bool) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+                for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+            });
         });
     } else {
-        walk<N, false>(list, p, [&](const GcTensor& t, long long at) {
-            float x[8];
-            load8(t, at, x);
-            float s = 0.f;
+        walk<N, false>(list, p, [&](const GcTensor& t, unsigned u0, unsigned u1) {
+            groups<false>(t, u0, u1, [&](long long, const float (&x)[8], bool) {
+                float s = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
-            if (s >= 0x1p-80f && s <= 0x1p120f) {       // what underflowed is below 2^-46 of the sum
-                sum += (double)s;
-            } else {
-                unsigned any = 0;
+                for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
+                if (s >= 0x1p-80f && s <= 0x1p120f) {       // what underflowed is below 2^-46 of the sum
+                    sum += (double)s;
+                } else {
+                    unsigned any = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) any |= __float_as_uint(x[j]) & 0x7fffffffu;
-                if (any) {                              // zeros are common: a table's gradient is mostly zeros
+                    for (int j = 0; j < 8; ++j) any |= __float_as_uint(x[j]) & 0x7fffffffu;
+                    if (any) {                              // zeros are common: a table's gradient is mostly zeros
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sum = fma((double)x[j], (double)x[j], sum);
+                        for (int j = 0; j < 8; ++j) sum = fma((double)x[j], (double)x[j], sum);
+                    }
                 }
-            }
+            });
         });
     }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -176,58 +230,53 @@ __device__ float whole_norm(const GcParams& p) {
     return (float)(p.inf ? v : sqrt(v));
 }
 
-template <typename T>
-__device__ __forceinline__ void store8(T* at, const float (&x)[8]);
-template <>
-__device__ __forceinline__ void store8<float>(float* at, const float (&x)[8]) {
-    ((float4*)at)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    ((float4*)at)[1] = make_float4(x[4], x[5], x[6], x[7]);
+__device__ __forceinline__ void store8(float* at, const float (&x)[8]) {
+    asm volatile("st.global" GC_CS ".v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 :: "l"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
 }
-template <>
-__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* at, const float (&x)[8]) {
+__device__ __forceinline__ void store8(__nv_bfloat16* at, const float (&x)[8]) {
     __nv_bfloat162 q[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) q[j] = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
     uint4 w;
     memcpy(&w, q, 16);
-    *(uint4*)at = w;
+    asm volatile("st.global" GC_CS ".v4.b32 [%0], {%1, %2, %3, %4};" :: "l"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
 }
+__device__ __forceinline__ void put(float x, float* y) { *y = x; }
+__device__ __forceinline__ void put(float x, __nv_bfloat16* y) { *y = __float2bfloat16(x); }
 
+// c * the elements of units u0 .. u1 into a result of type T
 template <typename T>
-__device__ __forceinline__ void put8(const GcTensor& t, long long at, bool whole, const float (&x)[8]) {
-    const long long i = at - lead_of(t);
-    T* o = (T*)(t.out ? t.out : const_cast<void*>(t.grad)) + i;
-    if (whole && (t.flags & kGcSameStart)) {
-        store8<T>(o, x);
-    } else {
+__device__ __forceinline__ void scale_units(const GcTensor& t, unsigned u0, unsigned u1, float c) {
+    T* out = (T*)(t.out ? t.out : const_cast<void*>(t.grad));
+    const bool same_start = t.flags & kGcSameStart;
+    groups<true>(t, u0, u1, [&](long long i, float (&x)[8], bool whole) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i + j >= 0 && i + j < t.numel) {
-                if constexpr (sizeof(T) == 4) o[j] = x[j];
-                else o[j] = __float2bfloat16(x[j]);
-            }
-    }
+        for (int j = 0; j < 8; ++j) x[j] *= c;
+        if (whole && same_start) {
+            store8(out + i, x);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i + j >= 0 && i + j < t.numel) put(x[j], out + i + j);
+        }
+    });
 }
 
 template <int N>
-__global__ void __launch_bounds__(kGcThreads) grad_scale_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
+__global__ void __launch_bounds__(kGcThreads, GC_BLK) grad_scale_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float norm = whole_norm(p);
     if (p.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
     const float q = p.max_norm / (norm + p.eps);
     const bool cut = !(q >= 1.f);       // NaN cuts, too: a NaN norm leaves no gradient that looks sound
-    const float c = cut ? q : 1.f;
-    walk<N, true>(list, p, [&](const GcTensor& t, long long at) {
+    const float c = cut ? q : 1.f;      // times 1 changes no value
+    if (!cut && !p.into) return;
+    walk<N, true>(list, p, [&](const GcTensor& t, unsigned u0, unsigned u1) {
         if (!cut && !t.out) return;
-        float x[8];
-        const bool whole = load8(t, at, x);
-        if (cut) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] *= c;
-        }
-        if (t.flags & kGcOutBf16) put8<__nv_bfloat16>(t, at, whole, x);
-        else put8<float>(t, at, whole, x);
+        if (t.flags & kGcOutBf16) scale_units<__nv_bfloat16>(t, u0, u1, c);
+        else scale_units<float>(t, u0, u1, c);
     });
 }
 
@@ -240,7 +289,7 @@ __global__ void __launch_bounds__(kGcThreads) grad_norm_finish_kernel(const __gr
 int bytes_of(bpt_dtype t) { return t == BPT_F32 ? 4 : 2; }
 bool on_element(const void* q, int bytes) { return ((uintptr_t)q & (bytes - 1)) == 0; }
 long long units_of(const bpt_grad& g) {
-    const int lead = (int)(((uintptr_t)g.grad & 15) / bytes_of(g.dtype));
+    const int e = bytes_of(g.dtype), lead = (int)(((uintptr_t)g.grad & (8 * e - 1)) / e);
     return (g.numel + lead + kGcUnit - 1) / kGcUnit;
 }
 
@@ -326,9 +375,9 @@ bool launch(const bpt_grad* g, int from, const GcPlan& q, GcParams p, bool scale
     for (int i = from; i < q.next; ++i) {
         if (!g[i].numel) continue;
         const int e = bytes_of(g[i].dtype), oe = g[i].out ? bytes_of(g[i].out_dtype) : e;
-        const unsigned lead = (unsigned)(((uintptr_t)g[i].grad & 15) / e);
-        // whole groups of 8 can be stored in 16-byte pieces where they start on a boundary in the result, too
-        const bool same = !g[i].out || (((uintptr_t)g[i].out - (uintptr_t)lead * oe) & 15) == 0;
+        const unsigned lead = (unsigned)(((uintptr_t)g[i].grad & (8 * e - 1)) / e);
+        // whole groups of 8 can be stored in one piece where they start on a boundary in the result, too
+        const bool same = !g[i].out || (((uintptr_t)g[i].out - (uintptr_t)lead * oe) & (8 * oe - 1)) == 0;
         list.t[k++] = {g[i].grad, g[i].out, g[i].numel, unit,
                        (e == 2 ? kGcGradBf16 : 0u) | ((g[i].out ? oe : e) == 2 ? kGcOutBf16 : 0u) | (same ? kGcSameStart : 0u) | lead * kGcLead};
         unit += (unsigned)units_of(g[i]);
@@ -388,6 +437,7 @@ bpt_status run(const bpt_grad* g, int32_t n, int32_t norm_type, bool clip, float
         return BPT_OK;
     }
     p.write_norm = 1;
+    for (int i = 0; i < n; ++i) p.into |= g[i].out != nullptr && g[i].numel > 0;
     for (int from = 0; from < n;) {
         const GcPlan q = next_launch(g, n, from);
         if (q.n) {

@@ -426,7 +426,9 @@ bpt_status bpt_clip_grads(const bpt_grad* grads, int32_t n, int32_t norm_type, f
  * bias: of bias_dtype, rows bias_stride apart (0: one row for all), or NULL.  bias_ids, bias_values: [rows, bias_count] contiguous (ids of
  * bias_id_bytes 4 or 8; outside 0 .. vocab - 1: no effect); bias_count 0: none.
  * allowed: bit v % 32 of word v / 32 set where v is allowed, rows allowed_stride words apart (0: one row for all), or NULL.
- * rows, vocab, history_len, bias_count < 2^30 (vocab >= 1).  Errors: INVALID_ARG, UNSUPPORTED (sizes), CUDA.
+ * `workspace`: bpt_adjust_logits_workspace_bytes bytes (host query; 0 where none is needed, and on invalid arguments), plain scratch
+ * without a status block, 16-byte aligned; two calls whose GPU work overlaps need one each.
+ * rows, vocab, history_len, bias_count < 2^30 (vocab >= 1).  Errors: INVALID_ARG, UNSUPPORTED (sizes), WORKSPACE, CUDA.
  */
 typedef struct {
     int64_t rows, vocab, logits_stride, out_stride;
@@ -446,7 +448,8 @@ typedef struct {
     const int32_t* allowed;
     int64_t allowed_stride;
 } bpt_logits_args;
-bpt_status bpt_adjust_logits(const bpt_logits_args* args, void* out, void* cuda_stream);
+size_t bpt_adjust_logits_workspace_bytes(const bpt_logits_args* args);
+bpt_status bpt_adjust_logits(const bpt_logits_args* args, void* out, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * Backward pass for callers that must not allocate device memory (the paper has no

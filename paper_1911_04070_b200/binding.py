@@ -31,7 +31,8 @@ EXPORTS = ("bpt_graph_dims_query", "bpt_build_graph", "bpt_attn_workspace_bytes"
            "bpt_selftest_wait_timeout", "bpt_debug_bounds", "bpt_out_proj_norm", "bpt_res_norm_fwd",
            "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd",
            "bpt_gated_ff_few_rows", "bpt_check_device", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes", "bpt_embed_bwd",
-           "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads", "bpt_adjust_logits")
+           "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads", "bpt_adjust_logits",
+           "bpt_adjust_logits_workspace_bytes")
 
 
 class BptError(RuntimeError):
@@ -152,7 +153,9 @@ def load_library() -> ctypes.CDLL:
         lib.bpt_clip_grads.restype = ctypes.c_int
         lib.bpt_clip_grads.argtypes = [gr, i32, i32, f32, f32, vp, vp, sz, vp]
         lib.bpt_adjust_logits.restype = ctypes.c_int
-        lib.bpt_adjust_logits.argtypes = [ctypes.POINTER(LogitsArgs), vp, vp]
+        lib.bpt_adjust_logits.argtypes = [ctypes.POINTER(LogitsArgs), vp, vp, sz, vp]
+        lib.bpt_adjust_logits_workspace_bytes.restype = sz
+        lib.bpt_adjust_logits_workspace_bytes.argtypes = [ctypes.POINTER(LogitsArgs)]
         lib.bpt_debug_bounds.restype = ctypes.c_int
         lib.bpt_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32), vp]
         lib.bpt_attn_fwd.restype = ctypes.c_int
@@ -208,7 +211,7 @@ def load_native():
         native.bind_library([ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "bpt_res_norm_fwd", "bpt_res_norm_bwd_workspace_bytes", "bpt_res_norm_bwd", "bpt_gated_ff_few_rows",
             "bpt_gated_ff_workspace_bytes", "bpt_gated_ff_fwd", "bpt_gated_ff_bwd", "bpt_embed_fwd", "bpt_embed_bwd_workspace_bytes",
-            "bpt_embed_bwd", "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads", "bpt_adjust_logits")])
+            "bpt_embed_bwd", "bpt_grad_norm_workspace_bytes", "bpt_grad_norm", "bpt_clip_grads", "bpt_adjust_logits", "bpt_adjust_logits_workspace_bytes")])
         _native = native
     return _native
 
@@ -676,7 +679,9 @@ def bpt_adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, r
     with _on_device(dev):
         out = torch.empty(B, V, dtype=logits.dtype, device=logits.device) if out is None else out
         a.out_dtype, a.out_stride = _dtype_code(out), stride(out)
-        _check(load_library().bpt_adjust_logits(ctypes.byref(a), out.data_ptr(), _raw_stream(dev)), "bpt_adjust_logits")
+        lib = load_library()
+        ws = torch.empty(lib.bpt_adjust_logits_workspace_bytes(ctypes.byref(a)), dtype=torch.uint8, device=logits.device)
+        _check(lib.bpt_adjust_logits(ctypes.byref(a), out.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev)), "bpt_adjust_logits")
     return out
 
 

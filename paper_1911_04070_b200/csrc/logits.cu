@@ -12,14 +12,26 @@
 #include <cmath>
 #include <cstring>
 #include <cstdlib>
+#include <type_traits>
 
 #include "bpt_internal.cuh"
 
 namespace bpt {
 namespace {
 
-constexpr int kLgStep = 2048;       // no piece of a row is smaller
+constexpr int kLgSms = 148;
+#ifndef LG_LIMIT
+#define LG_LIMIT (2 * kLgSms)
+#endif
+// Threads that pass over a piece, 16 elements each, where that is all a CTA does; where it also goes through the history, and
+// then the threads that do that.
+constexpr int kLgStream = 256, kLgStreamToo = 512, kLgSparse = 512;
+constexpr int kLgPiece = kLgStream * 16, kLgPieceToo = kLgStreamToo * 16;
+#ifndef LG_MINB
+#define LG_MINB 4
+#endif
 
+struct LgListed { unsigned id; float value; };
 struct LgParams {
     const void* logits;
     void* out;
@@ -32,8 +44,11 @@ struct LgParams {
     const uint32_t* allowed;
     long long vocab, logits_stride, out_stride, history_stride, bias_stride, allowed_stride;
     long long bias_count;
-    int history_len, history64, bias_ids64, bias_bf16, pieces, count;   // count: there is a history that matters
+    int history_len, history64, bias_ids64, bias_bf16, pieces, count, in_place;   // count: there is a history that matters
     float rep, pres, freq;
+    LgListed* listed;           // [rows][listed_stride], or null
+    int* starts;                // [rows][pieces + 1]: where each piece's ids begin
+    long long listed_stride;
 };
 
 __device__ __forceinline__ float elem(float x) { return x; }
@@ -73,35 +88,36 @@ __device__ __forceinline__ long long id_at(const void* ids, int is64, long long 
 constexpr unsigned kLgPrompt = 0x80000000u;     // of an id's word: it stands in the prompt; the other bits count the places behind it
 constexpr int kLgAhead = 4;                     // ids of the history a thread asks for at once
 
-// The 8 values of a bias from `at` on, of which `before` values lie before it in its row and `behind` from it on: wherever that starts, in
-// whole 16-byte pieces around it while those lie in the row.
-__device__ __forceinline__ void bias8(const float* at, long long before, long long behind, float (&z)[8]) {
-    const int s = (int)((uintptr_t)at & 15) / 4;
-    if (before >= s && behind >= 12) {
-        unsigned w[12];
+// 8 values of a bias that start anywhere: the 16-byte pieces around them, and the values out of those.
+template <typename B> struct Bias8;
+template <> struct Bias8<float> {
+    uint4 q[3];
+    int s;
+    __device__ __forceinline__ void load(const float* at) {
+        s = (int)((uintptr_t)at & 15) / 4;
 #pragma unroll
-        for (int j = 0; j < 3; ++j) {
-            const uint4 q = __ldg((const uint4*)(at - s) + j);
-            w[4 * j] = q.x; w[4 * j + 1] = q.y; w[4 * j + 2] = q.z; w[4 * j + 3] = q.w;
-        }
+        for (int j = 0; j < 3; ++j) q[j] = __ldg((const uint4*)(at - s) + j);
+    }
+    __device__ __forceinline__ void get(float (&z)[8]) const {
+        unsigned w[12];
+        memcpy(w, q, sizeof(w));
 #pragma unroll
         for (int j = 0; j < 11; ++j) w[j] = s & 1 ? w[j + 1] : w[j];
 #pragma unroll
         for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(s & 2 ? w[j + 2] : w[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = j < behind && -j <= before ? __ldg(at + j) : 0.f;
     }
-}
-__device__ __forceinline__ void bias8(const __nv_bfloat16* at, long long before, long long behind, float (&z)[8]) {
-    const int s = (int)((uintptr_t)at & 15) / 2;
-    if (before >= s && behind >= 16) {
-        unsigned w[8];
+};
+template <> struct Bias8<__nv_bfloat16> {
+    uint4 q[2];
+    int s;
+    __device__ __forceinline__ void load(const __nv_bfloat16* at) {
+        s = (int)((uintptr_t)at & 15) / 2;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint4 q = __ldg((const uint4*)(at - s) + j);
-            w[4 * j] = q.x; w[4 * j + 1] = q.y; w[4 * j + 2] = q.z; w[4 * j + 3] = q.w;
-        }
+        for (int j = 0; j < 2; ++j) q[j] = __ldg((const uint4*)(at - s) + j);
+    }
+    __device__ __forceinline__ void get(float (&z)[8]) const {
+        unsigned w[8];
+        memcpy(w, q, sizeof(w));
 #pragma unroll
         for (int j = 0; j < 7; ++j) w[j] = s & 2 ? w[j + 1] : w[j];
 #pragma unroll
@@ -112,64 +128,248 @@ __device__ __forceinline__ void bias8(const __nv_bfloat16* at, long long before,
             z[2 * j] = __uint_as_float(two << 16);
             z[2 * j + 1] = __uint_as_float(two & 0xffff0000u);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = j < behind && -j <= before ? elem(at[j]) : 0.f;
     }
-}
+};
+struct NoBias {};
 
 __device__ __forceinline__ float bias_at(const LgParams& p, long long row, int i) {
     const long long b = row * p.bias_stride + i;
     return p.bias_bf16 ? __bfloat162float(__ldg((const __nv_bfloat16*)p.bias + b)) : __ldg((const float*)p.bias + b);
 }
+__device__ __forceinline__ bool is_allowed(const uint32_t* allowed, int i) { return !allowed || ((__ldg(allowed + (i >> 5)) >> (i & 31)) & 1); }
 
-template <typename TL, typename TO, int THREADS, int GROUPS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) adjust_logits_kernel(const __grid_constant__ LgParams p) {
+// What a listed id ends with.  w: its word of the counts; e: 1 + its entry of the row's own list of biases, or 0.
+__device__ __forceinline__ float listed_value(const LgParams& p, long long row, int i, float v, unsigned w, int e, float rep, float pres, float freq,
+                                              const uint32_t* allowed) {
+    if (w) {
+        const unsigned n = w & ~kLgPrompt;
+        v = v > 0.f ? v / rep : v * rep;
+        if (n) v -= fmaf(freq, (float)n, pres);
+    }
+    if (p.bias) v += bias_at(p, row, i);
+    if (e) v += __ldg(p.bias_values + row * p.bias_count + e - 1);
+    return is_allowed(allowed, i) ? v : -INFINITY;
+}
+
+// What needs no history, for this thread's two groups of 8 elements of a piece, STEP elements apart: out = allowed ? logits + bias : -inf.
+// All loads are on their way together, before `ready` is called, where all of those lie in the row.
+template <typename TL, typename TO, typename B, bool MASK, int STEP, typename F>
+__device__ __forceinline__ void stream(const LgParams& p, long long row, const TL* in, TO* out, const B* bias, const uint32_t* allowed, int ia, F&& ready) {
+    constexpr bool BIAS = !std::is_same_v<B, NoBias>;
+    constexpr int pieces = sizeof(TL) / 2;      // of 16 bytes
+    const int vocab = (int)p.vocab, ib = ia + STEP;
+    const bool inside = ia >= 16 && ib <= vocab - 24;
+    uint4 raw[2][pieces];
+    Bias8<std::conditional_t<BIAS, B, float>> z[2];
+    unsigned lo[2], hi[2];
+    if (inside) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int j = 0; j < pieces; ++j) raw[g][j] = *((const uint4*)(in + (g ? ib : ia)) + j);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int i = g ? ib : ia;
+            if constexpr (BIAS) z[g].load(bias + i);
+            if constexpr (MASK) {
+                lo[g] = __ldg(allowed + (i >> 5));
+                hi[g] = __ldg(allowed + ((i + 7) >> 5));
+            }
+        }
+    }
+    ready();        // all threads together: there may be a barrier in it
+    if (inside) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int i = g ? ib : ia;
+            float x[8];
+            read8((const TL*)raw[g], x);
+            if constexpr (BIAS) {
+                float b[8];
+                z[g].get(b);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] += b[j];
+            }
+            if constexpr (MASK) {       // bits i .. i + 7, of one word or two
+                const unsigned bits = __funnelshift_r(lo[g], hi[g], (unsigned)i & 31u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = (bits >> j) & 1 ? x[j] : -INFINITY;
+            }
+            if (((uintptr_t)(out + i) & 15) == 0) {
+                write8(out + i, x);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) put(x[j], out + i + j);
+            }
+        }
+    } else {                            // near an end of the row, over it or behind it
+#pragma unroll 1
+        for (int i = ia; i <= ib; i += STEP)
+#pragma unroll 1
+            for (int j = max(0, -i); j < 8 && i + j < vocab; ++j) {
+                const float v = elem(in[i + j]) + (BIAS ? bias_at(p, row, i + j) : 0.f);
+                put(is_allowed(allowed, i + j) ? v : -INFINITY, out + i + j);
+            }
+    }
+}
+
+// A row's ids that are in its history or its own list of biases, once each, with the values that they end with: an open hash table in shared memory,
+// one CTA per row.  The values go to global memory in order of the pieces of the row that adjust_logits_kernel then passes over.
+constexpr int kLgSlots = 16384, kLgMostIds = kLgSlots * 3 / 4, kLgMostPieces = 1024, kLgHashThreads = 1024;
+
+template <typename TL>
+__global__ void __launch_bounds__(kLgHashThreads) list_ids_kernel(const __grid_constant__ LgParams p, int slots) {
     extern __shared__ uint4 lg_smem[];
-    __shared__ int listed;
-    constexpr unsigned step = THREADS * 8, piece = step * GROUPS;
-    // seen: of each id of the piece how often it is in the history, then, for an id of the list, the value it ends with
-    unsigned* seen = (unsigned*)lg_smem;                            // [piece]
-    unsigned short* list = (unsigned short*)(seen + piece);         // [piece]: ids that are in the history or in the row's list of biases
-    int* biased = (int*)(list + piece);                             // [piece] if bias_count: 1 + which entry of that list
-    const long long row = blockIdx.x / p.pieces;
-    const int k = (int)(blockIdx.x - row * p.pieces);
+    __shared__ int fill[kLgMostPieces];         // per piece how many ids, then where its next one goes
+    __shared__ int warp_sum[32];
+    unsigned* key = (unsigned*)lg_smem;         // [slots]: 1 + id, or 0
+    unsigned* seen = key + slots;               // [slots]: as in adjust_logits_kernel
+    int* biased = (int*)(seen + slots);         // [slots] if bias_count
+    const long long row = blockIdx.x;
     const TL* in = (const TL*)p.logits + row * p.logits_stride;
-    TO* out = (TO*)p.out + row * p.out_stride;
-    const int vocab = (int)p.vocab;
-    const int lead = (int)(((uintptr_t)in & 15) / sizeof(TL));
-    const int first = k * (int)piece - lead;                        // index of the piece's first element; below 0: none
-    const int tid = threadIdx.x;
-    const bool sparse = p.count || p.bias_count;
-
-    // what does not depend on anything is asked for first: the first ids of the history (where they are behind the length they are
-    // dropped), the settings, the logits
+    const int lead = (int)(((uintptr_t)in & 15) / sizeof(TL)), vocab = (int)p.vocab, tid = threadIdx.x;
+    const uint32_t* allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const long long base = row * p.history_stride;
     long long ids[kLgAhead];
     int len = p.history_len, prompt = 0;
     if (p.count) {
 #pragma unroll
         for (int j = 0; j < kLgAhead; ++j) {
-            const int t = tid + j * THREADS;
+            const int t = tid + j * kLgHashThreads;
             ids[j] = t < p.history_len ? id_at(p.history, p.history64, base + t) : -1;
         }
         if (p.lengths) len = min(max(__ldg(p.lengths + row), 0), len);
         if (p.prompts) prompt = min(max(__ldg(p.prompts + row), 0), len);
     }
-    uint4 raw[GROUPS][sizeof(TL) / 2];
+    for (int i = tid; i < slots / 4 * (p.bias_count ? 3 : 2); i += kLgHashThreads) lg_smem[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < p.pieces; i += kLgHashThreads) fill[i] = 0;
+    __syncthreads();
+    // The slot of an id; there are more slots than ids, so one is found.
+    const auto slot_of = [&](unsigned id) {
+        unsigned s = (id * 2654435761u) >> 7 & (unsigned)(slots - 1);
+        for (;; s = (s + 1) & (unsigned)(slots - 1)) {
+            const unsigned old = atomicCAS(key + s, 0u, id + 1);
+            if (!old) { atomicAdd(fill + (id + (unsigned)lead) / kLgPiece, 1); return s; }
+            if (old == id + 1) return s;
+        }
+    };
+    const auto count = [&](long long id, int t) {
+        if ((unsigned long long)id >= (unsigned long long)vocab) return;
+        const unsigned s = slot_of((unsigned)id);
+        if (t < prompt) atomicOr(seen + s, kLgPrompt);
+        else atomicAdd(seen + s, 1u);
+    };
+    if (p.count) {
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-        const int i = first + (int)(g * step) + tid * 8;
-        if (i >= 0 && i <= vocab - 8)
-#pragma unroll
-            for (int j = 0; j < (int)sizeof(TL) / 2; ++j) raw[g][j] = *((const uint4*)(in + i) + j);
+        for (int j = 0; j < kLgAhead; ++j)
+            if (tid + j * kLgHashThreads < len) count(ids[j], tid + j * kLgHashThreads);
+        for (int t = tid + kLgAhead * kLgHashThreads; t < len; t += kLgHashThreads) count(id_at(p.history, p.history64, base + t), t);
     }
-    if (sparse) {
-        for (unsigned i = tid; i < piece / 4; i += THREADS) lg_smem[i] = make_uint4(0, 0, 0, 0);
-        if (p.bias_count)
-            for (unsigned i = tid; i < piece / 4; i += THREADS) ((uint4*)biased)[i] = make_uint4(0, 0, 0, 0);
-        if (tid == 0) listed = 0;
+    for (int t = tid; t < (int)p.bias_count; t += kLgHashThreads) {
+        const long long id = id_at(p.bias_ids, p.bias_ids64, row * p.bias_count + t);
+        if ((unsigned long long)id < (unsigned long long)vocab) atomicMax(biased + slot_of((unsigned)id), t + 1);    // given twice: the later one
+    }
+    __syncthreads();
+    {   // counts to places; pieces <= threads
+        const int lane = tid & 31, warp = tid >> 5, mine = tid < p.pieces ? fill[tid] : 0;
+        int sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += up;
+        }
+        if (lane == 31) warp_sum[warp] = sum;
         __syncthreads();
+        int before = sum - mine;
+        for (int w = 0; w < warp; ++w) before += warp_sum[w];
+        if (tid < p.pieces) {
+            fill[tid] = before;
+            p.starts[row * (p.pieces + 1) + tid] = before;
+            if (tid == p.pieces - 1) p.starts[row * (p.pieces + 1) + p.pieces] = before + mine;
+        }
+        __syncthreads();
+    }
+    const float rep = p.repetition ? __ldg(p.repetition + row) : p.rep, pres = p.presence ? __ldg(p.presence + row) : p.pres,
+                freq = p.frequency ? __ldg(p.frequency + row) : p.freq;
+    for (int s = tid; s < slots; s += kLgHashThreads) {
+        if (!key[s]) continue;
+        const int i = (int)key[s] - 1;
+        const float v = listed_value(p, row, i, elem(in[i]), seen[s], p.bias_count ? biased[s] : 0, rep, pres, freq, allowed);
+        p.listed[row * p.listed_stride + atomicAdd(fill + (unsigned)(i + lead) / kLgPiece, 1)] = LgListed{(unsigned)i, v};
+    }
+}
+
+// The first STREAM threads of a CTA pass over its piece of a row.  The others, if there are any, go through the row's history and its own list
+// of biases meanwhile, and write the ids that stand there once more, behind the others; in place, the others wait until the logits
+// of those ids are read.  Where there are no others, the ids may have been listed by list_ids_kernel, whose end is waited for in the same places.
+template <typename TL, typename TO, int STREAM, int SPARSE>
+__global__ void __launch_bounds__(STREAM + SPARSE, SPARSE ? 1 : LG_MINB) adjust_logits_kernel(const __grid_constant__ LgParams p) {
+    extern __shared__ uint4 lg_smem[];
+    __shared__ int listed;
+    constexpr int step = STREAM * 8;
+    constexpr unsigned piece = 2 * step;
+    const unsigned row = blockIdx.x / (unsigned)p.pieces;
+    const int k = (int)(blockIdx.x - row * (unsigned)p.pieces);
+    const TL* in = (const TL*)p.logits + row * p.logits_stride;
+    TO* out = (TO*)p.out + row * p.out_stride;
+    const uint32_t* allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
+    const int vocab = (int)p.vocab;
+    const int lead = (int)(((uintptr_t)in & 15) / sizeof(TL));
+    const int first = k * (int)piece - lead;                        // index of the piece's first element; below 0: none
+    if (SPARSE == 0 || threadIdx.x < STREAM) {
+        const int i0 = first + (int)threadIdx.x * 8;
+        const auto ready = [&] {
+            if (SPARSE && p.in_place) __syncthreads();
+            if (SPARSE == 0 && p.listed && p.in_place) asm volatile("griddepcontrol.wait;" ::: "memory");
+        };
+        const long long b = row * p.bias_stride;
+        if (!p.bias && allowed) stream<TL, TO, NoBias, true, step>(p, row, in, out, (const NoBias*)nullptr, allowed, i0, ready);
+        else if (!p.bias) stream<TL, TO, NoBias, false, step>(p, row, in, out, (const NoBias*)nullptr, nullptr, i0, ready);
+        else if (p.bias_bf16 && allowed) stream<TL, TO, __nv_bfloat16, true, step>(p, row, in, out, (const __nv_bfloat16*)p.bias + b, allowed, i0, ready);
+        else if (p.bias_bf16) stream<TL, TO, __nv_bfloat16, false, step>(p, row, in, out, (const __nv_bfloat16*)p.bias + b, nullptr, i0, ready);
+        else if (allowed) stream<TL, TO, float, true, step>(p, row, in, out, (const float*)p.bias + b, allowed, i0, ready);
+        else stream<TL, TO, float, false, step>(p, row, in, out, (const float*)p.bias + b, nullptr, i0, ready);
+        if (SPARSE) __syncthreads();
+        if (SPARSE == 0 && p.listed) {
+            if (!p.in_place) asm volatile("griddepcontrol.wait;" ::: "memory");
+            const int* starts = p.starts + (long long)row * (p.pieces + 1) + k;
+            const LgListed* listed_ids = p.listed + row * p.listed_stride;
+            const int end = starts[1];
+            int e = starts[0] + (int)threadIdx.x;
+            LgListed one = e < end ? listed_ids[e] : LgListed{0, 0.f};
+            __syncthreads();            // the piece is written
+            while (e < end) {
+                put(one.value, out + one.id);
+                e += STREAM;
+                if (e < end) one = listed_ids[e];
+            }
+        }
+        return;
+    }
+    if constexpr (SPARSE > 0) {
+        // seen: how often each id of the piece is in the history, then, for a listed id, the value that it ends with
+        unsigned* seen = (unsigned*)lg_smem;                            // [piece]
+        int* biased = (int*)(seen + piece);                             // [piece] if bias_count: 1 + which entry of the row's list of biases
+        unsigned short* list = (unsigned short*)(biased + (p.bias_count ? piece : 0));      // [listed_most]: ids that stand in the history or in that list
+        const int tid = (int)threadIdx.x - STREAM;
+        const auto join = [&] { __syncwarp(); asm volatile("bar.sync 1, %0;" :: "n"(SPARSE) : "memory"); };
+        // the first ids are asked for before their number is known; those behind the length are dropped
+        const long long base = row * p.history_stride;
+        long long ids[kLgAhead];
+        int len = p.history_len, prompt = 0;
+        if (p.count) {
+#pragma unroll
+            for (int j = 0; j < kLgAhead; ++j) {
+                const int t = tid + j * SPARSE;
+                ids[j] = t < p.history_len ? id_at(p.history, p.history64, base + t) : -1;
+            }
+            if (p.lengths) len = min(max(__ldg(p.lengths + row), 0), len);
+            if (p.prompts) prompt = min(max(__ldg(p.prompts + row), 0), len);
+        }
+        for (unsigned i = tid; i < piece / 4 * (p.bias_count ? 2 : 1); i += SPARSE) lg_smem[i] = make_uint4(0, 0, 0, 0);
+        if (tid == 0) listed = 0;
+        join();
         // Position of an id in the piece, or >= piece.  An id from 2^32 - lead on would come out below lead, where no element is.
         const auto place = [&](long long id) { return (unsigned)((unsigned long long)id >> 32) ? piece : (unsigned)id - (unsigned)first; };
         const auto is_element = [&](unsigned at) { return at < piece && (unsigned)(first + (int)at) < (unsigned)vocab; };
@@ -182,85 +382,36 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) adjust_logits_kernel(
         if (p.count) {
 #pragma unroll
             for (int j = 0; j < kLgAhead; ++j)
-                if (tid + j * THREADS < len) count(ids[j], tid + j * THREADS);
-            for (int t0 = tid + kLgAhead * THREADS; t0 < len; t0 += kLgAhead * THREADS) {
+                if (tid + j * SPARSE < len) count(ids[j], tid + j * SPARSE);
+            for (int t0 = tid + kLgAhead * SPARSE; t0 < len; t0 += kLgAhead * SPARSE) {
 #pragma unroll
-                for (int j = 0; j < kLgAhead; ++j) ids[j] = t0 + j * THREADS < len ? id_at(p.history, p.history64, base + t0 + j * THREADS) : -1;
+                for (int j = 0; j < kLgAhead; ++j) ids[j] = t0 + j * SPARSE < len ? id_at(p.history, p.history64, base + t0 + j * SPARSE) : -1;
 #pragma unroll
                 for (int j = 0; j < kLgAhead; ++j)
-                    if (t0 + j * THREADS < len) count(ids[j], t0 + j * THREADS);
+                    if (t0 + j * SPARSE < len) count(ids[j], t0 + j * SPARSE);
             }
-            __syncthreads();
+            join();
         }
         if (p.bias_count) {
-            for (int t = tid; t < (int)p.bias_count; t += THREADS) {
+            for (int t = tid; t < (int)p.bias_count; t += SPARSE) {
                 const unsigned at = place(id_at(p.bias_ids, p.bias_ids64, row * p.bias_count + t));
                 if (!is_element(at)) continue;
                 const int old = atomicMax(biased + at, t + 1);              // given twice: the later one
                 if (!old && !seen[at]) list[atomicAdd(&listed, 1)] = (unsigned short)at;
             }
-            __syncthreads();
+            join();
         }
         const float rep = p.repetition ? __ldg(p.repetition + row) : p.rep, pres = p.presence ? __ldg(p.presence + row) : p.pres,
                     freq = p.frequency ? __ldg(p.frequency + row) : p.freq;
-        for (int e = tid; e < listed; e += THREADS) {
-            const unsigned at = list[e], w = seen[at];
+        const int n_listed = listed;
+        for (int e = tid; e < n_listed; e += SPARSE) {
+            const unsigned at = list[e];
             const int i = first + (int)at;
-            float v = elem(in[i]);
-            if (w) {
-                const unsigned n = w & ~kLgPrompt;
-                v = v > 0.f ? v / rep : v * rep;
-                if (n) v -= fmaf(freq, (float)n, pres);
-            }
-            if (p.bias) v += bias_at(p, row, i);
-            if (p.bias_count && biased[at]) v += __ldg(p.bias_values + row * p.bias_count + biased[at] - 1);
-            seen[at] = v == 0.f ? 0x80000000u : __float_as_uint(v);         // 0 is for ids that are not in the list
+            seen[at] = __float_as_uint(listed_value(p, row, i, elem(in[i]), seen[at], p.bias_count ? biased[at] : 0, rep, pres, freq, allowed));
         }
-        __syncthreads();
-    }
-    const uint32_t* allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-        const int at = g * (int)step + tid * 8, i = first + at;
-        if (i >= 0 && i <= vocab - 8) {
-            float x[8];
-            read8((const TL*)raw[g], x);
-            if (p.bias) {
-                float z[8];
-                const long long b = row * p.bias_stride + i;
-                if (p.bias_bf16) bias8((const __nv_bfloat16*)p.bias + b, i, vocab - i, z);
-                else bias8((const float*)p.bias + b, i, vocab - i, z);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] += z[j];
-            }
-            if (sparse) {
-                unsigned w[8];
-                *(uint4*)w = *(const uint4*)(seen + at);
-                *(uint4*)(w + 4) = *(const uint4*)(seen + at + 4);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = w[j] ? __uint_as_float(w[j]) : x[j];
-            }
-            if (allowed) {              // bits i .. i + 7, of one word or two
-                const int w0 = i >> 5, w1 = (i + 7) >> 5;
-                const unsigned a = __ldg(allowed + w0), bits = __funnelshift_r(a, w1 > w0 ? __ldg(allowed + w1) : a, (unsigned)i & 31u);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = (bits >> j) & 1 ? x[j] : -INFINITY;
-            }
-            if (((uintptr_t)(out + i) & 15) == 0) {
-                write8(out + i, x);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) put(x[j], out + i + j);
-            }
-        } else {                        // a group that hangs over an end of the row, or lies behind it
-            for (int j = max(0, -i); j < 8 && i + j < vocab; ++j) {
-                float v = elem(in[i + j]);
-                if (p.bias) v += bias_at(p, row, i + j);
-                if (sparse && seen[at + j]) v = __uint_as_float(seen[at + j]);
-                if (allowed && !((__ldg(allowed + ((i + j) >> 5)) >> ((i + j) & 31)) & 1)) v = -INFINITY;
-                put(v, out + i + j);
-            }
-        }
+        if (p.in_place) __syncthreads();        // the logits of the list are read
+        __syncthreads();                        // the piece is written
+        for (int e = tid; e < n_listed; e += SPARSE) put(__uint_as_float(seen[list[e]]), out + first + list[e]);
     }
 }
 
@@ -289,37 +440,78 @@ bpt_status check_logits(const bpt_logits_args* a) {
         return BPT_ERR_INVALID_ARG;
     if (a->allowed && (!on_element(a->allowed, 4) || (a->allowed_stride && a->allowed_stride < (a->vocab + 31) / 32))) return BPT_ERR_INVALID_ARG;
     if (a->vocab > 0x3fffffffll || a->history_len > 0x3fffffffll || a->bias_count > 0x3fffffffll || a->rows > 0x3fffffffll) return BPT_ERR_UNSUPPORTED;
-    if (a->rows * ((a->vocab + kLgStep) / kLgStep + 1) > 0x7fffffffll) return BPT_ERR_UNSUPPORTED;
+    if (a->rows * (a->vocab / kLgPiece + 2) > 0x7fffffffll) return BPT_ERR_UNSUPPORTED;
     return BPT_OK;
 }
 
-template <typename TL, typename TO, int THREADS, int GROUPS>
-bpt_status run(LgParams p, long long rows, cudaStream_t st) {
-    constexpr int piece = THREADS * 8 * GROUPS;
-    p.pieces = (int)((p.vocab + 16 / sizeof(TL) - 1 + piece - 1) / piece);       // wherever the row starts
-    const size_t smem = (size_t)piece * (p.bias_count ? 10 : p.count ? 6 : 0);
+struct LgPlan {
+    bool sparse, list;      // ids of a history or of the rows' own lists count; they are listed by a launch of their own
+    int pieces, slots;
+    long long stride;       // listed ids per row, at most
+    size_t bytes;
+};
+bool counts(const bpt_logits_args& a) {     // settings that change nothing need no history
+    return a.history_len > 0 && (a.repetition_rows || a.presence_rows || a.frequency_rows || a.repetition != 1.f || a.presence != 0.f || a.frequency != 0.f);
+}
+LgPlan plan(const bpt_logits_args& a) {
+    LgPlan q{};
+    const long long most = (counts(a) ? a.history_len : 0) + a.bias_count;
+    q.sparse = most > 0;
+    const auto pieces = [&](int piece) { return (int)((a.vocab + 16 / bytes_of(a.dtype) - 1 + piece - 1) / piece); };     // wherever the row starts
+    q.stride = std::min(most, (long long)a.vocab);
+    // Every CTA of a row going through all of its history is the shorter way while all CTAs run at once.  B200, bf16: 32 rows of 32000 with
+    // histories of 4096 in 128 CTAs 6.6 us against LIST1; 256 rows of 128001 with histories of 2048 LIST2 us against LIST3.
+    q.list = q.sparse && a.rows * pieces(kLgPieceToo) > LG_LIMIT && most <= kLgMostIds && pieces(kLgPiece) <= kLgMostPieces;
+    q.pieces = pieces(q.sparse && !q.list ? kLgPieceToo : kLgPiece);
+    q.slots = 1024;
+    while (q.slots < kLgSlots && q.slots < 2 * most) q.slots *= 2;
+    q.bytes = q.list ? ((size_t)a.rows * q.stride * sizeof(LgListed) + (size_t)a.rows * (q.pieces + 1) * 4) : 0;
+    return q;
+}
+
+template <typename TL, typename TO, int STREAM, int SPARSE>
+bool run(const LgParams& p, long long rows, size_t smem, bool dependent, cudaStream_t st) {
     if (smem > 40 * 1024 &&     // with the static part, 48 KB is the limit without asking
-        cudaFuncSetAttribute(adjust_logits_kernel<TL, TO, THREADS, GROUPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-        return BPT_ERR_CUDA;
-    adjust_logits_kernel<TL, TO, THREADS, GROUPS><<<(unsigned)(rows * p.pieces), THREADS, smem, st>>>(p);
-    const bool ok = cudaGetLastError() == cudaSuccess;
+        cudaFuncSetAttribute(adjust_logits_kernel<TL, TO, STREAM, SPARSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLgPieceToo * 10) != cudaSuccess)
+        return false;
+    cudaLaunchAttribute attr[1] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * p.pieces));
+    cfg.blockDim = dim3(STREAM + SPARSE);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent ? 1 : 0;
+    const bool ok = cudaLaunchKernelEx(&cfg, adjust_logits_kernel<TL, TO, STREAM, SPARSE>, p) == cudaSuccess;
+    if (!ok) cudaGetLastError();        // reported by this status, not by the next call of somebody else
     trace_mark(st, "adjust_logits");
-    return ok ? BPT_OK : BPT_ERR_CUDA;
+    return ok;
+}
+template <typename TL>
+bool run_list(const LgParams& p, long long rows, int slots, cudaStream_t st) {
+    const size_t smem = (size_t)slots * (p.bias_count ? 12 : 8);
+    if (smem > 40 * 1024 &&
+        cudaFuncSetAttribute(list_ids_kernel<TL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLgSlots * 12) != cudaSuccess)
+        return false;
+    list_ids_kernel<TL><<<(unsigned)rows, kLgHashThreads, smem, st>>>(p, slots);
+    const bool ok = cudaGetLastError() == cudaSuccess;
+    trace_mark(st, "list_ids");
+    return ok;
 }
 template <typename TL, typename TO>
-bpt_status pick(const LgParams& p, long long rows, cudaStream_t st) {
-#ifdef LG_VARIANT
-    if (getenv("LG_VARIANT")) switch (atoi(getenv("LG_VARIANT"))) {
-        case 0: return run<TL, TO, 1024, 1>(p, rows, st);
-        case 1: return run<TL, TO, 512, 1>(p, rows, st);
-        case 2: return run<TL, TO, 512, 2>(p, rows, st);
-        case 3: return run<TL, TO, 256, 1>(p, rows, st);
-        case 4: return run<TL, TO, 256, 2>(p, rows, st);
-        case 5: return run<TL, TO, 256, 4>(p, rows, st);
-        case 6: return run<TL, TO, 1024, 2>(p, rows, st);
+bpt_status launch(const LgParams& p, const LgPlan& q, long long rows, cudaStream_t st) {
+    bool ok;
+    if (!q.sparse) {
+        ok = run<TL, TO, kLgStream, 0>(p, rows, 0, false, st);
+    } else if (q.list) {
+        ok = run_list<TL>(p, rows, q.slots, st) && run<TL, TO, kLgStream, 0>(p, rows, 0, true, st);
+    } else {
+        const size_t list = (size_t)std::min<long long>(kLgPieceToo, q.stride) * 2;
+        ok = run<TL, TO, kLgStreamToo, kLgSparse>(p, rows, (size_t)kLgPieceToo * (p.bias_count ? 8 : 4) + (list + 15) / 16 * 16, false, st);
     }
-#endif
-    return run<TL, TO, 1024, 1>(p, rows, st);
+    return ok ? BPT_OK : BPT_ERR_CUDA;
 }
 
 }  // namespace
@@ -327,11 +519,16 @@ bpt_status pick(const LgParams& p, long long rows, cudaStream_t st) {
 
 using namespace bpt;
 
-extern "C" bpt_status bpt_adjust_logits(const bpt_logits_args* a, void* out, void* cuda_stream) {
+extern "C" size_t bpt_adjust_logits_workspace_bytes(const bpt_logits_args* a) {
+    return check_logits(a) == BPT_OK && a->rows > 0 ? plan(*a).bytes : 0;
+}
+
+extern "C" bpt_status bpt_adjust_logits(const bpt_logits_args* a, void* out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     const bpt_status s = check_logits(a);
     if (s != BPT_OK) return s;
     if (a->rows == 0) return BPT_OK;
     if (!a->logits || !out || !on_element(a->logits, bytes_of(a->dtype)) || !on_element(out, bytes_of(a->out_dtype))) return BPT_ERR_INVALID_ARG;
+    if (a->logits == out && (a->dtype != a->out_dtype || (a->rows > 1 && a->logits_stride != a->out_stride))) return BPT_ERR_INVALID_ARG;
     LgParams p{};
     p.logits = a->logits; p.out = out; p.history = a->history;
     p.lengths = a->lengths; p.prompts = a->prompt_lengths;
@@ -342,10 +539,19 @@ extern "C" bpt_status bpt_adjust_logits(const bpt_logits_args* a, void* out, voi
     p.bias_stride = a->bias_stride; p.allowed_stride = a->allowed_stride;
     p.bias_count = a->bias_count;
     p.history_len = (int)a->history_len; p.history64 = a->history_bytes == 8; p.bias_ids64 = a->bias_id_bytes == 8; p.bias_bf16 = a->bias_dtype == BPT_BF16;
-    // settings that change nothing need no history
-    p.count = a->history_len > 0 && (a->repetition_rows || a->presence_rows || a->frequency_rows || a->repetition != 1.f || a->presence != 0.f || a->frequency != 0.f);
+    p.in_place = a->logits == out;
+    p.count = counts(*a);
+    const LgPlan q = plan(*a);
+    p.pieces = q.pieces;
+    if (q.list) {
+        if (!workspace || workspace_bytes < q.bytes) return BPT_ERR_WORKSPACE;
+        if ((uintptr_t)workspace & 15) return BPT_ERR_INVALID_ARG;
+        p.listed = static_cast<LgListed*>(workspace);
+        p.starts = reinterpret_cast<int*>(p.listed + a->rows * q.stride);
+        p.listed_stride = q.stride;
+    }
     cudaStream_t st = (cudaStream_t)cuda_stream;
     typedef __nv_bfloat16 bf;
-    if (a->dtype == BPT_F32) return a->out_dtype == BPT_F32 ? pick<float, float>(p, a->rows, st) : pick<float, bf>(p, a->rows, st);
-    return a->out_dtype == BPT_F32 ? pick<bf, float>(p, a->rows, st) : pick<bf, bf>(p, a->rows, st);
+    if (a->dtype == BPT_F32) return a->out_dtype == BPT_F32 ? launch<float, float>(p, q, a->rows, st) : launch<float, bf>(p, q, a->rows, st);
+    return a->out_dtype == BPT_F32 ? launch<bf, float>(p, q, a->rows, st) : launch<bf, bf>(p, q, a->rows, st);
 }

@@ -44,6 +44,7 @@ struct Api {
     decltype(&bpt_grad_norm) grad_norm = nullptr;
     decltype(&bpt_clip_grads) clip_grads = nullptr;
     decltype(&bpt_adjust_logits) adjust_logits = nullptr;
+    decltype(&bpt_adjust_logits_workspace_bytes) adjust_logits_bytes = nullptr;
 } api;   // of the library that binding.py has loaded
 
 struct Refused {};
@@ -623,13 +624,15 @@ py::object adjust_logits(const Tensor& logits_, const Opt& history_, const Opt& 
     }
     if (!type_code(out, &a.out_dtype)) return py::none();
     a.out_stride = row_stride(out);
-    if (api.adjust_logits(&a, ptr(out), at::cuda::getCurrentCUDAStream().stream()) != BPT_OK) return py::none();
+    const size_t n = api.adjust_logits_bytes(&a);
+    const Tensor ws = n ? bytes((int64_t)n, logits) : Tensor();
+    if (api.adjust_logits(&a, ptr(out), ptr(ws), n, at::cuda::getCurrentCUDAStream().stream()) != BPT_OK) return py::none();
     if (out_.has_value() && !out.is_inference()) out.unsafeGetTensorImpl()->bump_version();
     return py::cast(out);
 }
 
 void bind_library(const std::vector<uintptr_t>& f) {
-    TORCH_CHECK(f.size() == 14, "fourteen functions are expected");
+    TORCH_CHECK(f.size() == 15, "fifteen functions are expected");
     api.res_norm_fwd = reinterpret_cast<decltype(api.res_norm_fwd)>(f[0]);
     api.res_norm_bytes = reinterpret_cast<decltype(api.res_norm_bytes)>(f[1]);
     api.res_norm_bwd = reinterpret_cast<decltype(api.res_norm_bwd)>(f[2]);
@@ -644,6 +647,7 @@ void bind_library(const std::vector<uintptr_t>& f) {
     api.grad_norm = reinterpret_cast<decltype(api.grad_norm)>(f[11]);
     api.clip_grads = reinterpret_cast<decltype(api.clip_grads)>(f[12]);
     api.adjust_logits = reinterpret_cast<decltype(api.adjust_logits)>(f[13]);
+    api.adjust_logits_bytes = reinterpret_cast<decltype(api.adjust_logits_bytes)>(f[14]);
 }
 
 }  // namespace

@@ -35,13 +35,21 @@ H = dict(history=4096, history_len=5, history_stride=5)
                                        (dict(allowed=4096, allowed_stride=3), 1), (dict(vocab=1 << 30, logits_stride=1 << 30, out_stride=1 << 30), 2),
                                        (dict(rows=1 << 29, vocab=1 << 14, logits_stride=1 << 14, out_stride=1 << 14), 2)])
 def test_refusals(lib, kw, status):
-    assert lib.bpt_adjust_logits(ctypes.byref(_args(**kw)), 8192, None) == status
+    assert lib.bpt_adjust_logits(ctypes.byref(_args(**kw)), 8192, 16384, 1 << 50, None) == status
 
 
 def test_more_refusals(lib):
-    assert lib.bpt_adjust_logits(None, 8192, None) == 1
-    assert lib.bpt_adjust_logits(ctypes.byref(_args()), None, None) == 1 and lib.bpt_adjust_logits(ctypes.byref(_args()), 8193, None) == 1
-    assert lib.bpt_adjust_logits(ctypes.byref(_args(rows=0, logits=None, history_len=4, bias_count=3)), None, None) == 0
+    call = lambda a, out=8192, ws=16384, n=1 << 50: lib.bpt_adjust_logits(a if a is None else ctypes.byref(a), out, ws, n, None)
+    need = lambda a: lib.bpt_adjust_logits_workspace_bytes(a if a is None else ctypes.byref(a))
+    assert call(None) == 1 and need(None) == 0
+    assert call(_args(), out=None) == 1 and call(_args(), out=8193) == 1
+    assert call(_args(rows=0, logits=None, history_len=4, bias_count=3), out=None) == 0
+    # many pieces of rows with a history: listed apart, in a workspace
+    big = dict(H, rows=3000, vocab=20000, logits_stride=20000, out_stride=20000, presence=1.0)
+    assert need(_args()) == 0 and need(_args(**dict(big, presence=0.0))) == 0 and need(_args(**dict(big, history_len=20000))) == 0
+    a = _args(**big)
+    assert need(a) >= 3000 * (5 * 8 + 3 * 4)
+    assert call(a, ws=None) == 3 and call(a, n=need(a) - 1) == 3 and call(a, ws=16392) == 1
 
 
 def test_python_refusals(lib):

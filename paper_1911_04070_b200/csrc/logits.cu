@@ -47,7 +47,7 @@ struct LgParams {
     int history_len, history64, bias_ids64, bias_bf16, pieces, count, in_place;   // count: there is a history that matters
     float rep, pres, freq;
     LgListed* listed;           // [rows][listed_stride], or null
-    int* starts;                // [rows][pieces + 1]: where each piece's ids begin
+    int* n_listed;              // [rows]
     long long listed_stride;
 };
 
@@ -213,21 +213,20 @@ __device__ __forceinline__ void stream(const LgParams& p, long long row, const T
     }
 }
 
-// A row's ids that are in its history or its own list of biases, once each, with the values that they end with: an open hash table in shared memory,
-// one CTA per row.  The values go to global memory in order of the pieces of the row that adjust_logits_kernel then passes over.
-constexpr int kLgSlots = 16384, kLgMostIds = kLgSlots * 3 / 4, kLgMostPieces = 1024, kLgHashThreads = 1024;
+// A row's ids that are in its history or its own list of biases, once each, with the values that they end with: an open hash table in shared
+// memory, one CTA per row.  Runs beside the pass over the vocabulary, behind which put_listed_kernel writes the values.
+constexpr int kLgSlots = 16384, kLgMostIds = kLgSlots * 3 / 4, kLgHashThreads = 1024;
 
 template <typename TL>
 __global__ void __launch_bounds__(kLgHashThreads) list_ids_kernel(const __grid_constant__ LgParams p, int slots) {
     extern __shared__ uint4 lg_smem[];
-    __shared__ int fill[kLgMostPieces];         // per piece how many ids, then where its next one goes
-    __shared__ int warp_sum[32];
-    unsigned* key = (unsigned*)lg_smem;         // [slots]: 1 + id, or 0
-    unsigned* seen = key + slots;               // [slots]: as in adjust_logits_kernel
-    int* biased = (int*)(seen + slots);         // [slots] if bias_count
+    __shared__ int listed;
+    volatile unsigned* key = (volatile unsigned*)lg_smem;       // [slots]: 1 + id, or 0
+    unsigned* seen = (unsigned*)lg_smem + slots;                // [slots]: as in adjust_logits_kernel
+    int* biased = (int*)(seen + slots);                         // [slots] if bias_count
     const long long row = blockIdx.x;
     const TL* in = (const TL*)p.logits + row * p.logits_stride;
-    const int lead = (int)(((uintptr_t)in & 15) / sizeof(TL)), vocab = (int)p.vocab, tid = threadIdx.x;
+    const int vocab = (int)p.vocab, tid = threadIdx.x;
     const uint32_t* allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const long long base = row * p.history_stride;
@@ -243,15 +242,15 @@ __global__ void __launch_bounds__(kLgHashThreads) list_ids_kernel(const __grid_c
         if (p.prompts) prompt = min(max(__ldg(p.prompts + row), 0), len);
     }
     for (int i = tid; i < slots / 4 * (p.bias_count ? 3 : 2); i += kLgHashThreads) lg_smem[i] = make_uint4(0, 0, 0, 0);
-    for (int i = tid; i < p.pieces; i += kLgHashThreads) fill[i] = 0;
+    if (tid == 0) listed = 0;
     __syncthreads();
-    // The slot of an id; there are more slots than ids, so one is found.
+    // The slot of an id; there are more slots than ids, so one is found.  Most ids of a text are there already: looked at before they are claimed.
     const auto slot_of = [&](unsigned id) {
         unsigned s = (id * 2654435761u) >> 7 & (unsigned)(slots - 1);
         for (;; s = (s + 1) & (unsigned)(slots - 1)) {
-            const unsigned old = atomicCAS(key + s, 0u, id + 1);
-            if (!old) { atomicAdd(fill + (id + (unsigned)lead) / kLgPiece, 1); return s; }
-            if (old == id + 1) return s;
+            unsigned old = key[s];
+            if (!old) old = atomicCAS((unsigned*)key + s, 0u, id + 1);
+            if (!old || old == id + 1) return s;
         }
     };
     const auto count = [&](long long id, int t) {
@@ -271,42 +270,48 @@ __global__ void __launch_bounds__(kLgHashThreads) list_ids_kernel(const __grid_c
         if ((unsigned long long)id < (unsigned long long)vocab) atomicMax(biased + slot_of((unsigned)id), t + 1);    // given twice: the later one
     }
     __syncthreads();
-    {   // counts to places; pieces <= threads
-        const int lane = tid & 31, warp = tid >> 5, mine = tid < p.pieces ? fill[tid] : 0;
-        int sum = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(~0u, sum, o);
-            if (lane >= o) sum += up;
-        }
-        if (lane == 31) warp_sum[warp] = sum;
-        __syncthreads();
-        int before = sum - mine;
-        for (int w = 0; w < warp; ++w) before += warp_sum[w];
-        if (tid < p.pieces) {
-            fill[tid] = before;
-            p.starts[row * (p.pieces + 1) + tid] = before;
-            if (tid == p.pieces - 1) p.starts[row * (p.pieces + 1) + p.pieces] = before + mine;
-        }
-        __syncthreads();
-    }
     const float rep = p.repetition ? __ldg(p.repetition + row) : p.rep, pres = p.presence ? __ldg(p.presence + row) : p.pres,
                 freq = p.frequency ? __ldg(p.frequency + row) : p.freq;
-    for (int s = tid; s < slots; s += kLgHashThreads) {
-        if (!key[s]) continue;
-        const int i = (int)key[s] - 1;
-        const float v = listed_value(p, row, i, elem(in[i]), seen[s], p.bias_count ? biased[s] : 0, rep, pres, freq, allowed);
-        p.listed[row * p.listed_stride + atomicAdd(fill + (unsigned)(i + lead) / kLgPiece, 1)] = LgListed{(unsigned)i, v};
+    LgListed* to = p.listed + row * p.listed_stride;
+    for (int s0 = tid; s0 < slots; s0 += kLgAhead * kLgHashThreads) {
+        int id[kLgAhead];
+        float v[kLgAhead];
+#pragma unroll
+        for (int j = 0; j < kLgAhead; ++j) {        // the logits of several on their way at once
+            const int s = s0 + j * kLgHashThreads;
+            id[j] = s < slots ? (int)key[s] - 1 : -1;
+            v[j] = id[j] >= 0 ? elem(in[id[j]]) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kLgAhead; ++j) {
+            if (id[j] < 0) continue;
+            const int s = s0 + j * kLgHashThreads;
+            to[atomicAdd(&listed, 1)] = LgListed{(unsigned)id[j], listed_value(p, row, id[j], v[j], seen[s], p.bias_count ? biased[s] : 0, rep, pres, freq, allowed)};
+        }
+    }
+    __syncthreads();
+    if (tid == 0) p.n_listed[row] = listed;
+}
+
+template <typename TO>
+__global__ void __launch_bounds__(kLgHashThreads) put_listed_kernel(const __grid_constant__ LgParams p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const long long row = blockIdx.x;
+    const int n = p.n_listed[row];
+    for (int e = threadIdx.x; e < n; e += kLgHashThreads) {
+        const LgListed one = p.listed[row * p.listed_stride + e];
+        put(one.value, (TO*)p.out + row * p.out_stride + one.id);
     }
 }
 
 // The first STREAM threads of a CTA pass over its piece of a row.  The others, if there are any, go through the row's history and its own list
 // of biases meanwhile, and write the ids that stand there once more, behind the others; in place, the others wait until the logits
-// of those ids are read.  Where there are no others, the ids may have been listed by list_ids_kernel, whose end is waited for in the same places.
+// of those ids are read.  Where there are no others, list_ids_kernel may be at work on those ids: in place its end is waited for.
 template <typename TL, typename TO, int STREAM, int SPARSE>
 __global__ void __launch_bounds__(STREAM + SPARSE, SPARSE ? 1 : LG_MINB) adjust_logits_kernel(const __grid_constant__ LgParams p) {
     extern __shared__ uint4 lg_smem[];
     __shared__ int listed;
+    if (SPARSE == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int step = STREAM * 8;
     constexpr unsigned piece = 2 * step;
     const unsigned row = blockIdx.x / (unsigned)p.pieces;
@@ -331,20 +336,8 @@ __global__ void __launch_bounds__(STREAM + SPARSE, SPARSE ? 1 : LG_MINB) adjust_
         else if (allowed) stream<TL, TO, float, true, step>(p, row, in, out, (const float*)p.bias + b, allowed, i0, ready);
         else stream<TL, TO, float, false, step>(p, row, in, out, (const float*)p.bias + b, nullptr, i0, ready);
         if (SPARSE) __syncthreads();
-        if (SPARSE == 0 && p.listed) {
-            if (!p.in_place) asm volatile("griddepcontrol.wait;" ::: "memory");
-            const int* starts = p.starts + (long long)row * (p.pieces + 1) + k;
-            const LgListed* listed_ids = p.listed + row * p.listed_stride;
-            const int end = starts[1];
-            int e = starts[0] + (int)threadIdx.x;
-            LgListed one = e < end ? listed_ids[e] : LgListed{0, 0.f};
-            __syncthreads();            // the piece is written
-            while (e < end) {
-                put(one.value, out + one.id);
-                e += STREAM;
-                if (e < end) one = listed_ids[e];
-            }
-        }
+        // the kernel that then writes the listed ids waits for this one to end, and so for the listing, too
+        if (SPARSE == 0 && p.listed && !p.in_place && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
     if constexpr (SPARSE > 0) {
@@ -461,31 +454,36 @@ LgPlan plan(const bpt_logits_args& a) {
     q.stride = std::min(most, (long long)a.vocab);
     // Every CTA of a row going through all of its history is the shorter way while all CTAs run at once.  B200, bf16: 32 rows of 32000 with
     // histories of 4096 in 128 CTAs 6.6 us against LIST1; 256 rows of 128001 with histories of 2048 LIST2 us against LIST3.
-    q.list = q.sparse && a.rows * pieces(kLgPieceToo) > LG_LIMIT && most <= kLgMostIds && pieces(kLgPiece) <= kLgMostPieces;
+    q.list = q.sparse && a.rows * pieces(kLgPieceToo) > LG_LIMIT && most <= kLgMostIds;
     q.pieces = pieces(q.sparse && !q.list ? kLgPieceToo : kLgPiece);
     q.slots = 1024;
     while (q.slots < kLgSlots && q.slots < 2 * most) q.slots *= 2;
-    q.bytes = q.list ? ((size_t)a.rows * q.stride * sizeof(LgListed) + (size_t)a.rows * (q.pieces + 1) * 4) : 0;
+    q.bytes = q.list ? (size_t)a.rows * (q.stride * sizeof(LgListed) + 4) : 0;
     return q;
 }
 
+template <typename K>
+bool start(K kernel, unsigned grid, int threads, size_t smem, bool dependent, cudaStream_t st, const LgParams& p) {
+    cudaLaunchAttribute attr[1] = {};       // its launch overlaps the kernel before
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess) return true;
+    cudaGetLastError();     // reported by this status, not by the next call of somebody else
+    return false;
+}
 template <typename TL, typename TO, int STREAM, int SPARSE>
 bool run(const LgParams& p, long long rows, size_t smem, bool dependent, cudaStream_t st) {
     if (smem > 40 * 1024 &&     // with the static part, 48 KB is the limit without asking
         cudaFuncSetAttribute(adjust_logits_kernel<TL, TO, STREAM, SPARSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLgPieceToo * 10) != cudaSuccess)
         return false;
-    cudaLaunchAttribute attr[1] = {};
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * p.pieces));
-    cfg.blockDim = dim3(STREAM + SPARSE);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = dependent ? 1 : 0;
-    const bool ok = cudaLaunchKernelEx(&cfg, adjust_logits_kernel<TL, TO, STREAM, SPARSE>, p) == cudaSuccess;
-    if (!ok) cudaGetLastError();        // reported by this status, not by the next call of somebody else
+    const bool ok = start(adjust_logits_kernel<TL, TO, STREAM, SPARSE>, (unsigned)(rows * p.pieces), STREAM + SPARSE, smem, dependent, st, p);
     trace_mark(st, "adjust_logits");
     return ok;
 }
@@ -506,7 +504,9 @@ bpt_status launch(const LgParams& p, const LgPlan& q, long long rows, cudaStream
     if (!q.sparse) {
         ok = run<TL, TO, kLgStream, 0>(p, rows, 0, false, st);
     } else if (q.list) {
-        ok = run_list<TL>(p, rows, q.slots, st) && run<TL, TO, kLgStream, 0>(p, rows, 0, true, st);
+        ok = run_list<TL>(p, rows, q.slots, st) && run<TL, TO, kLgStream, 0>(p, rows, 0, true, st) &&
+             start(put_listed_kernel<TO>, (unsigned)rows, kLgHashThreads, 0, true, st, p);
+        trace_mark(st, "put_listed");
     } else {
         const size_t list = (size_t)std::min<long long>(kLgPieceToo, q.stride) * 2;
         ok = run<TL, TO, kLgStreamToo, kLgSparse>(p, rows, (size_t)kLgPieceToo * (p.bias_count ? 8 : 4) + (list + 15) / 16 * 16, false, st);
@@ -547,7 +547,7 @@ extern "C" bpt_status bpt_adjust_logits(const bpt_logits_args* a, void* out, voi
         if (!workspace || workspace_bytes < q.bytes) return BPT_ERR_WORKSPACE;
         if ((uintptr_t)workspace & 15) return BPT_ERR_INVALID_ARG;
         p.listed = static_cast<LgListed*>(workspace);
-        p.starts = reinterpret_cast<int*>(p.listed + a->rows * q.stride);
+        p.n_listed = reinterpret_cast<int*>(p.listed + a->rows * q.stride);
         p.listed_stride = q.stride;
     }
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -48,7 +48,7 @@ def test_more_refusals(lib):
     big = dict(H, rows=3000, vocab=20000, logits_stride=20000, out_stride=20000, presence=1.0)
     assert need(_args()) == 0 and need(_args(**dict(big, presence=0.0))) == 0 and need(_args(**dict(big, history_len=20000))) == 0
     a = _args(**big)
-    assert need(a) >= 3000 * (5 * 8 + 3 * 4)
+    assert need(a) >= 3000 * (5 * 8 + 4)
     assert call(a, ws=None) == 3 and call(a, n=need(a) - 1) == 3 and call(a, ws=16392) == 1
 
 

@@ -11,6 +11,7 @@
 // so every row of dW is written once.  All sums have one order: bit-reproducible.
 #include <algorithm>
 #include <cmath>
+#include <cooperative_groups.h>
 #include <cstring>
 
 #include "bpt_internal.cuh"
@@ -22,7 +23,6 @@ constexpr int kEmSms = 148;
 constexpr int kEmDigit = 9;                 // bits per sort pass, at most
 constexpr int kEmBins = 1 << kEmDigit;
 constexpr int kEmSortThreads = 1024;
-constexpr int kEmZeroRows = 256;            // rows of dW per CTA that zeroes
 
 struct EmParams {
     const void* ids;
@@ -36,9 +36,11 @@ struct EmParams {
     int D, id64;
     float scale;
     // backward
-    int *hist, *keys[2], *src[2];           // sort: [tiles][kEmBins], id and row of d_out of each place, before and after a pass
-    float* part;                            // [tiles of the sum][2][D]
-    int sort_tile, sort_tiles, sum_tile, sum_tiles, sum_ctas;
+    int* hist;                              // sort: [tiles][kEmBins]
+    int2* list[2];                          // id and row of d_out of each place, before and after a pass
+    float* part;                            // [sum_tiles][2][D]
+    int sort_tile, sort_tiles, sum_tiles, warp_tile, slices, zero_rows, sorted;      // sorted: which of the lists is
+    unsigned zero_ctas;
 };
 
 __device__ __forceinline__ long long load_id(const EmParams& p, long long i) {
@@ -90,54 +92,112 @@ __device__ __forceinline__ void store_vec(T* at, const float (&x)[VEC]) {
     }
 }
 
-template <typename TW, typename TO, int VEC>
+// The id of a row of out, or -1 for a row of zeros.
+__device__ __forceinline__ long long id_of_row(const EmParams& p, unsigned row) {
+    const unsigned b = row / p.out_rows, t = row - b * p.out_rows;
+    if (t >= real_tokens(p, b)) return -1;
+    const long long id = load_id(p, (long long)b * p.tokens + t);
+    if (id >= 0 && id < p.vocab) return id;
+    *p.record = (int)BPT_ERR_INDEX;
+    return -1;
+}
+
+// Rows of whole 16-byte pieces: `lanes` threads per row, kEmRows rows one after another per thread, with the ids and then the pieces of all
+// of them on their way at once.
+constexpr int kEmRows = 4;
+template <typename TW, typename TO>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(EmParams p, int lanes) {
-    const unsigned per_cta = 256 / lanes;
-    const unsigned long long row = (unsigned long long)blockIdx.x * per_cta + threadIdx.x / lanes;
-    if (row >= p.rows) return;
-    const unsigned b = (unsigned)row / p.out_rows, t = (unsigned)row - b * p.out_rows;
+    const unsigned groups = 256 / lanes;
+    const unsigned first = (blockIdx.x * groups + threadIdx.x / lanes) * kEmRows;
     const int lane = threadIdx.x & (lanes - 1);
-    long long id = -1;
-    if (t < real_tokens(p, b)) {
-        id = load_id(p, (long long)b * p.tokens + t);
-        if (id < 0 || id >= p.vocab) {
-            if (lane == 0) *p.record = (int)BPT_ERR_INDEX;
-            id = -1;
+    long long id[kEmRows];
+#pragma unroll
+    for (int r = 0; r < kEmRows; ++r) id[r] = first + r < p.rows ? id_of_row(p, first + r) : -1;
+    for (int c = lane * 8; c < p.D; c += lanes * 8) {
+        float x[kEmRows][8];
+#pragma unroll
+        for (int r = 0; r < kEmRows; ++r) {
+            if (id[r] >= 0) {
+                load_vec<8>((const TW*)p.weight + id[r] * p.D + c, x[r]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[r][i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kEmRows; ++r) {
+            if (first + r >= p.rows) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[r][i] = id[r] >= 0 ? x[r][i] * p.scale : 0.f;
+            store_vec<8>((TO*)p.out + (long long)(first + r) * p.D + c, x[r]);
         }
     }
-    TO* out = (TO*)p.out + (long long)row * p.D;
-    const TW* w = (const TW*)p.weight + id * p.D;
-    for (int c = lane * VEC; c < p.D; c += lanes * VEC) {
-        float x[VEC];
-        if (id < 0) {
+}
+
+// Any width and start: out as one list of elements, 8 of them that lie on a 16-byte boundary per thread, over the ends of rows.
+template <typename TW, typename TO>
+__global__ void __launch_bounds__(256) embed_fwd_flat_kernel(EmParams p) {
+    const int lead = (int)(((uintptr_t)p.out & 15) / sizeof(TO));
+    const long long total = (long long)p.rows * p.D, i0 = ((long long)blockIdx.x * 256 + threadIdx.x) * 8 - lead;
+    if (i0 >= total) return;
+    const long long from = i0 < 0 ? 0 : i0;
+    unsigned row = total <= 0xffffffffll ? (unsigned)from / (unsigned)p.D : (unsigned)(from / p.D);
+    int c = (int)(from - (long long)row * p.D);
+    const int n = (int)(min(i0 + 8, total) - from);
+    long long id = id_of_row(p, row);
+    TO* out = (TO*)p.out + from;
+    float x[8];
+    if (c + 8 <= p.D && n == 8) {
+        const TW* w = (const TW*)p.weight + id * p.D + c;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] = 0.f;
-        } else {
-            load_vec<VEC>(w + c, x);
+        for (int j = 0; j < 8; ++j) x[j] = id >= 0 ? to_f(__ldg(w + j)) * p.scale : 0.f;
+    } else {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] *= p.scale;
+        for (int j = 0; j < 8; ++j) {
+            x[j] = 0.f;
+            if (j >= n) continue;
+            if (c == p.D) {
+                c = 0;
+                id = id_of_row(p, ++row);
+            }
+            if (id >= 0) x[j] = to_f(__ldg((const TW*)p.weight + id * p.D + c)) * p.scale;
+            ++c;
         }
-        store_vec<VEC>(out + c, x);
+    }
+    if (n == 8 && i0 >= 0) {
+        store_vec<8>(out, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) from_f(x[j], out + j);
     }
 }
 
 // ---------------------------------------------------------------------------------------------------------
 // the sort
 // ---------------------------------------------------------------------------------------------------------
-// Id of place i, or `vocab` for a place that adds nothing: behind its sequence's length, at padding_idx, out of range.
-__device__ __forceinline__ int sort_key(const EmParams& p, unsigned i, int* row) {
+// Place i of the list as the sort begins with it: its id, or `vocab` for a place that adds nothing (behind its sequence's length, at padding_idx,
+// out of range), and its row of d_out.
+__device__ __forceinline__ int2 place_of(const EmParams& p, unsigned i, long long id) {
     const unsigned b = i / p.tokens, t = i - b * p.tokens;
-    *row = (int)(b * p.out_rows + t);
-    if (t >= real_tokens(p, b)) return (int)p.vocab;
-    const long long id = load_id(p, i);
-    if (id < 0 || id >= p.vocab) {
-        *p.record = (int)BPT_ERR_INDEX;
-        return (int)p.vocab;
-    }
-    return id == p.padding_idx ? (int)p.vocab : (int)id;
+    const bool real = t < real_tokens(p, b), in = id >= 0 && id < p.vocab;
+    if (real && !in) *p.record = (int)BPT_ERR_INDEX;
+    return make_int2(real && in && id != p.padding_idx ? (int)id : (int)p.vocab, (int)(b * p.out_rows + t));
 }
 __device__ __forceinline__ void pdl_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// The lanes of the warp with the same d, of `bits` bits, among the lanes of `on`.  One vote a bit: match.any takes longer.
+__device__ __forceinline__ unsigned same_digit(int d, int bits, unsigned on) {
+    unsigned peers = on;
+#pragma unroll
+    for (int b = 0; b < kEmDigit; ++b) {
+        if (b >= bits) break;
+        const unsigned ones = __ballot_sync(~0u, (d >> b) & 1);
+        peers &= (d >> b) & 1 ? ones : ~ones;
+    }
+    return peers;
+}
 
 // How often each digit stands in each tile of the list.
 __global__ void __launch_bounds__(kEmSortThreads) embed_hist_kernel(EmParams p, int from, int shift, int bins) {
@@ -148,8 +208,12 @@ __global__ void __launch_bounds__(kEmSortThreads) embed_hist_kernel(EmParams p, 
     pdl_wait();
     const long long first = (long long)blockIdx.x * p.sort_tile, end = min(first + p.sort_tile, (long long)p.M);
     for (long long i = first + threadIdx.x; i < end; i += kEmSortThreads) {
-        int row;
-        const int key = from < 0 ? sort_key(p, (unsigned)i, &row) : p.keys[from][i];
+        int key;
+        if (from < 0) {
+            key = place_of(p, (unsigned)i, load_id(p, i)).x;
+        } else {
+            key = p.list[from][i].x;
+        }
         atomicAdd(&count[(key >> shift) & (bins - 1)], 1);      // whole numbers: any order gives the same
     }
     __syncthreads();
@@ -200,17 +264,16 @@ __global__ void __launch_bounds__(kEmSortThreads) embed_scatter_kernel(EmParams 
     for (long long at = first; at < end; at += kEmSortThreads) {
         const long long i = at + tid;
         const bool on = i < end;
-        int key = 0, row = 0;
+        int2 entry = make_int2(0, 0);
         if (on) {
             if (from < 0) {
-                key = sort_key(p, (unsigned)i, &row);
+                entry = place_of(p, (unsigned)i, load_id(p, i));
             } else {
-                key = p.keys[from][i];
-                row = p.src[from][i];
+                entry = p.list[from][i];
             }
         }
-        const int d = (key >> shift) & (bins - 1);
-        const unsigned peers = __match_any_sync(~0u, on ? d : -1);
+        const int d = (entry.x >> shift) & (bins - 1);
+        const unsigned peers = same_digit(d, 31 - __clz(bins), __ballot_sync(~0u, on));
         const int rank = __popc(peers & ((1u << lane) - 1));
         if (on && rank == 0) in_warp[warp][d] = (unsigned short)__popc(peers);
         __syncthreads();
@@ -225,8 +288,7 @@ __global__ void __launch_bounds__(kEmSortThreads) embed_scatter_kernel(EmParams 
         if (on) {
             int off = base[d] + rank;
             for (int w = 0; w < warp; ++w) off += in_warp[w][d];
-            p.keys[to][off] = key;
-            p.src[to][off] = row;
+            p.list[to][off] = entry;
         }
         __syncthreads();
         if (on && rank == 0) in_warp[warp][d] = 0;
@@ -235,156 +297,361 @@ __global__ void __launch_bounds__(kEmSortThreads) embed_scatter_kernel(EmParams 
     }
 }
 
+// The whole sort of up to kEmClusterMost places in one launch: one cluster, a slice of the list per CTA, in registers.  A warp counts the digits
+// of its own part of the slice, 32 places at a time; counts are added up over the warps, and over the cluster through distributed
+// shared memory.  Between two passes the list goes through global memory (L2): scattered 8-byte stores to the other CTAs' shared memory
+// took three times as long.
+constexpr int kEmClusterThreads = 512, kEmRounds = 16, kEmClusterCtas = 16, kEmClusterMost = kEmClusterCtas * kEmRounds * kEmClusterThreads;
+__global__ void __launch_bounds__(kEmClusterThreads) embed_sort_kernel(EmParams p, int passes, int digit, int rounds) {
+    namespace cg = cooperative_groups;
+    constexpr int warps = kEmClusterThreads / 32;
+    __shared__ int total[kEmBins], base[kEmBins], scan[warps];         // this CTA's counts; where its first place of a digit goes
+    __shared__ unsigned short in_warp[warps * kEmBins];                 // [warps][bins]
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int slice = rounds * kEmClusterThreads, bins = 1 << digit, me = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, first = me * slice + warp * rounds * 32 + lane, M = (int)p.M;
+    pdl_start();
+    int2 entry[kEmRounds];
+    {
+        long long id[kEmRounds];        // all on their way before one is looked at
+#pragma unroll
+        for (int r = 0; r < kEmRounds; ++r)
+            if (r < rounds && first + r * 32 < M) id[r] = load_id(p, first + r * 32);
+#pragma unroll
+        for (int r = 0; r < kEmRounds; ++r)
+            if (r < rounds && first + r * 32 < M) entry[r] = place_of(p, (unsigned)(first + r * 32), id[r]);
+    }
+    unsigned short* mine = in_warp + warp * bins;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * digit;
+        for (int i = lane; i < bins / 2; i += 32) ((unsigned*)mine)[i] = 0;
+        if (pass > 0) {
+#pragma unroll
+            for (int r = 0; r < kEmRounds; ++r)
+                if (r < rounds && first + r * 32 < M) entry[r] = __ldcg(&p.list[(pass + 1) & 1][first + r * 32]);
+        }
+        __syncwarp();
+        int rank[kEmRounds];
+#pragma unroll
+        for (int r = 0; r < kEmRounds; ++r) {
+            if (r >= rounds) break;
+            const bool on = first + r * 32 < M;
+            const int d = on ? (entry[r].x >> shift) & (bins - 1) : 0;
+            const unsigned peers = same_digit(d, digit, __ballot_sync(~0u, on));
+            const int before = mine[d], lower = __popc(peers & ((1u << lane) - 1));
+            __syncwarp();
+            if (on && lower == 0) mine[d] = (unsigned short)(before + __popc(peers));
+            __syncwarp();
+            rank[r] = before + lower;
+        }
+        __syncthreads();
+        if (tid < bins) {
+            unsigned short c[warps];
+#pragma unroll
+            for (int w = 0; w < warps; ++w) c[w] = in_warp[w * bins + tid];
+            int sum = 0;
+#pragma unroll
+            for (int w = 0; w < warps; ++w) {
+                in_warp[w * bins + tid] = (unsigned short)sum;              // places of the digit in the warps before: at most 2^13
+                sum += c[w];
+            }
+            total[tid] = sum;
+        }
+        cluster.sync();
+        int all = 0, before = 0;
+        if (tid < bins)
+#pragma unroll
+            for (int c = 0; c < kEmClusterCtas; ++c) {
+                const int n = c < ctas ? cluster.map_shared_rank(total, c)[tid] : 0;
+                all += n;
+                before += c < me ? n : 0;
+            }
+        int sum = all;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += up;
+        }
+        if (lane == 31) scan[warp] = sum;
+        __syncthreads();
+        if (tid < bins) {
+            int off = sum - all + before;
+#pragma unroll
+            for (int w = 0; w < warps; ++w) off += w < warp ? scan[w] : 0;
+            base[tid] = off;
+        }
+        __syncthreads();
+        int2* to = p.list[pass & 1];
+#pragma unroll
+        for (int r = 0; r < kEmRounds; ++r) {
+            if (r >= rounds) break;
+            if (first + r * 32 >= M) continue;
+            const int d = (entry[r].x >> shift) & (bins - 1);
+            to[base[d] + mine[d] + rank[r]] = entry[r];
+        }
+        // nobody reads this CTA's counts any more; between two passes the list is written
+        if (ctas > 1 || pass + 1 < passes) cluster.sync();
+    }
+}
+
 // ---------------------------------------------------------------------------------------------------------
 // the sums
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kEmSumWarps = 4;
-constexpr int kEmAhead = 8;     // rows of d_out on their way per warp
+constexpr int kEmSumWarps = 8;
+constexpr int kEmSlice = 256;           // columns per CTA, 8 per lane
+constexpr int kEmZeroBytes = 131072;    // of dW per CTA that zeroes, about
 
-// first i with keys[i] >= key
-__device__ int lower_bound(const int* keys, int n, int key) {
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (keys[mid] < key) lo = mid + 1;
-        else hi = mid;
+// A lane's 8 columns of a row, as they lie: next to one another in whole 16-byte pieces, or 32 apart.  Column i of the lane in the slice: col(i).
+template <typename T, bool VEC> struct EmRow {
+    uint4 q[sizeof(T) / 2];
+    static __device__ __forceinline__ int col(int lane, int i) { return lane * 8 + i; }
+    __device__ __forceinline__ void load(const T* row, int lane, int columns) {
+        const T* at = row + (lane * 8 < columns ? lane * 8 : 0);
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) q[j] = __ldg((const uint4*)at + j);
     }
-    return lo;
+    __device__ __forceinline__ float get(int i) const {
+        T e[8];
+        memcpy(e, q, sizeof(e));
+        return to_f(e[i]);
+    }
+};
+template <typename T> struct EmRow<T, false> {
+    T e[8];
+    static __device__ __forceinline__ int col(int lane, int i) { return i * 32 + lane; }
+    __device__ __forceinline__ void load(const T* row, int lane, int columns) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = __ldg(row + (i * 32 + lane < columns ? i * 32 + lane : 0));
+    }
+    __device__ __forceinline__ float get(int i) const { return to_f(e[i]); }
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ void put_row(T* at, int lane, int columns, const float (&x)[8], float scale) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i] * scale;
+    if constexpr (VEC) {
+        if (lane * 8 < columns) store_vec<8>(at + lane * 8, y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i * 32 + lane < columns) from_f(y[i], at + i * 32 + lane);
+    }
 }
 
-template <typename TW, typename TO, int VEC>
-__device__ void sum_tile(const EmParams& p, const int* keys, const int* src, int tile, int slice, int lane) {
-    const int first = tile * p.sum_tile, end = min(first + p.sum_tile, (int)p.M);
-    const int c = (slice * 32 + lane) * VEC;
-    const bool on = c < p.D;
-    const TO* d_out = (const TO*)p.d_out + c;
-    TW* dw = (TW*)p.out + c;
-    const int before = first > 0 ? keys[first - 1] : -1, after = end < (int)p.M ? keys[end] : -1;
-    float acc[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
-    auto flush = [&](int key, bool from_before, bool goes_on) {
-        if (key < (int)p.vocab && on) {
-            if (from_before || goes_on) {
-                float* at = p.part + ((long long)tile * 2 + (from_before ? 0 : 1)) * p.D + c;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) at[i] = acc[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] *= p.scale;
-                store_vec<VEC>(dw + (long long)key * p.D, acc);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
-    };
-    int run = keys[first];
-    bool from_before = run == before;
-    for (int at = first; at < end; at += 32) {
-        const int n = min(32, end - at);
-        const int my_key = lane < n ? keys[at + lane] : -1, my_src = lane < n ? src[at + lane] : 0;
-        for (int r = 0; r < n; r += kEmAhead) {
-            float x[kEmAhead][VEC];
-#pragma unroll
-            for (int j = 0; j < kEmAhead; ++j) {
-                const int key = __shfl_sync(~0u, my_key, (r + j) & 31), row = __shfl_sync(~0u, my_src, (r + j) & 31);
-                if (r + j < n && key < (int)p.vocab && on) load_vec<VEC>(d_out + (long long)row * p.D, x[j]);
-                else
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) x[j][i] = 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < kEmAhead; ++j) {
-                const int key = __shfl_sync(~0u, my_key, (r + j) & 31);
-                if (r + j >= n) break;
-                if (key != run) {
-                    flush(run, from_before, false);
-                    run = key;
-                    from_before = false;
-                }
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] += x[j][i];
-            }
-        }
-    }
-    flush(run, from_before, run == after);
-}
+// What a warp leaves of the runs at the ends of its tile: the ids, and whether the places before and behind the tile belong to them.
+struct EmEnds { int first, last; bool before, behind; };
 
-template <typename TW, typename TO, int VEC>
-__global__ void __launch_bounds__(kEmSumWarps * 32) embed_sum_kernel(EmParams p, int sorted) {
-    __shared__ bool there[kEmZeroRows];
+template <typename TW, typename TO, bool VEC>
+__global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : 4) embed_sum_kernel(EmParams p) {
+    __shared__ float part[kEmSumWarps][2][kEmSlice];        // sums of runs that go on before the warp's tile, and of those that begin in it and go on behind
+    __shared__ EmEnds ends[kEmSumWarps];
+    constexpr int kEmAhead = 4;             // rows of d_out on their way per warp
     pdl_start();
     pdl_wait();
-    const int *keys = p.keys[sorted], *src = p.src[sorted];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (blockIdx.x < (unsigned)p.sum_ctas) {
-        const int slices = (p.D + 32 * VEC - 1) / (32 * VEC);
-        const long long work = (long long)blockIdx.x * kEmSumWarps + warp;
-        const int tile = (int)(work / slices);
-        if (tile < p.sum_tiles) sum_tile<TW, TO, VEC>(p, keys, src, tile, (int)(work - (long long)tile * slices), lane);
+    const int2* list = p.list[p.sorted];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, M = (int)p.M, vocab = (int)p.vocab;
+    // the CTAs that zero stand evenly between those that sum: reading and writing at the same time is the faster way
+    const unsigned zero_before = (unsigned)((unsigned long long)blockIdx.x * p.zero_ctas / gridDim.x);
+    const bool zero = (unsigned long long)(blockIdx.x + 1) * p.zero_ctas / gridDim.x > zero_before;
+    if (!zero) {
+        const unsigned work = blockIdx.x - zero_before;
+        const int tile = (int)(work / (unsigned)p.slices), c0 = (int)(work - (unsigned)tile * p.slices) * kEmSlice, columns = min(kEmSlice, p.D - c0);
+        const TO* d_out = (const TO*)p.d_out + c0;
+        TW* dw = (TW*)p.out + c0;
+        const int a = (tile * kEmSumWarps + warp) * p.warp_tile, n = min(p.warp_tile, M - a);
+        EmEnds me{vocab, vocab, false, false};
+        if (n > 0) {
+            const int2 mine = lane < n ? list[a + lane] : make_int2(vocab, 0);
+            const int my_key = mine.x, my_src = mine.y;
+            const int prev = a > 0 ? list[a - 1].x : -1, next = a + n < M ? list[a + n].x : -1;
+            me.first = __shfl_sync(~0u, my_key, 0);
+            me.last = __shfl_sync(~0u, my_key, n - 1);
+            me.before = me.first < vocab && prev == me.first;
+            me.behind = me.last < vocab && next == me.last;
+            if (me.first < vocab) {
+                const int real = __popc(__ballot_sync(~0u, my_key < vocab));        // places that count come first
+                float acc[8] = {};
+                int run = me.first;
+                bool open = me.before;              // the run began before the tile
+                const auto keep = [&](int slot) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) part[warp][slot][EmRow<TO, VEC>::col(lane, i)] = acc[i];
+                };
+                for (int r = 0; r < real; r += kEmAhead) {
+                    EmRow<TO, VEC> x[kEmAhead];
+#pragma unroll
+                    for (int j = 0; j < kEmAhead; ++j) {
+                        const int row = __shfl_sync(~0u, my_src, r + j < real ? r + j : 0);
+                        x[j].load(d_out + (long long)row * p.D, lane, columns);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kEmAhead; ++j) {
+                        const int key = __shfl_sync(~0u, my_key, (r + j) & 31);
+                        if (r + j >= real) break;
+                        if (key != run) {
+                            if (open) keep(0);
+                            else put_row<TW, VEC>(dw + (long long)run * p.D, lane, columns, acc, p.scale);
+                            open = false;
+                            run = key;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) acc[i] += x[j].get(i);
+                    }
+                }
+                if (open) keep(0);
+                else if (me.behind) keep(1);
+                else put_row<TW, VEC>(dw + (long long)run * p.D, lane, columns, acc, p.scale);
+            }
+        }
+        if (lane == 0) ends[warp] = me;
+        __syncthreads();
+        // runs over several warps, in the warps' order: a column per thread
+        const int c = threadIdx.x;
+        float sum = 0.f;
+        bool from_before = false, open = false;
+        for (int w = 0; w < kEmSumWarps; ++w) {
+            const EmEnds e = ends[w];
+            const bool one = e.first == e.last;
+            if (e.before) {
+                if (w == 0) from_before = true;
+                sum += part[w][0][c];
+                open = one && e.behind;
+                if (!open) {
+                    if (c < columns) {
+                        if (from_before) p.part[(long long)tile * 2 * p.D + c0 + c] = sum;
+                        else from_f(sum * p.scale, dw + (long long)e.first * p.D + c);
+                    }
+                    from_before = false;
+                    sum = 0.f;
+                }
+            }
+            if (e.behind && !(one && e.before)) {
+                sum = part[w][1][c];
+                open = true;
+            }
+        }
+        if (open && c < columns) p.part[((long long)tile * 2 + (from_before ? 0 : 1)) * p.D + c0 + c] = sum;
         return;
     }
-    // rows of ids that occur nowhere
-    const long long first = (long long)(blockIdx.x - p.sum_ctas) * kEmZeroRows, end = min(first + kEmZeroRows, p.vocab);
-    for (int i = threadIdx.x; i < kEmZeroRows; i += kEmSumWarps * 32) there[i] = false;
+    // rows of ids that occur nowhere, in 16-byte pieces of dW as one list of elements, whatever its rows' length
+    bool* there = (bool*)part;                              // [zero_rows]
+    __shared__ int found[2];
+    const long long first = (long long)zero_before * p.zero_rows, end = min(first + p.zero_rows, p.vocab);
+    for (int i = threadIdx.x; i < p.zero_rows; i += kEmSumWarps * 32) there[i] = false;
+    // the places of these ids in the list: its first place with an id from `first` on, and from `end` on, among 256 probes at a time
+    int lo[2] = {0, 0}, hi[2] = {M, M};
+    while (lo[0] < hi[0] || lo[1] < hi[1]) {
+        __syncthreads();
+        if (threadIdx.x < 2) found[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int step = (hi[k] - lo[k] + 255) / 256, i = lo[k] + (int)threadIdx.x * step;
+            const unsigned less = __ballot_sync(~0u, i < hi[k] && list[i].x < (k ? end : first));
+            if (lane == 0) atomicAdd(&found[k], __popc(less));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {       // the last probe that is less lies before the place, the next one not
+            const int step = (hi[k] - lo[k] + 255) / 256, n = found[k];
+            hi[k] = min(hi[k], lo[k] + n * step);
+            lo[k] = n ? lo[k] + (n - 1) * step + 1 : hi[k];
+            if (!n) hi[k] = lo[k] = min(lo[k], hi[k]);
+        }
+    }
+    constexpr int threads = kEmSumWarps * 32;
+    const int rows = (int)(end - first), places = lo[1] - lo[0];
+    if (places < rows * 128) {          // each place marks its row, 8 loads on their way at once
+        for (int i = lo[0] + (int)threadIdx.x; i < lo[1]; i += 8 * threads) {
+            int id[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) id[j] = i + j * threads < lo[1] ? __ldg(&list[i + j * threads].x) : -1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (id[j] >= 0) there[id[j] - first] = true;
+        }
+    } else {                            // few ids in many places: each row looks for one of its own
+        for (int r = threadIdx.x; r < rows; r += threads) {
+            int a = lo[0], b = lo[1];
+            while (a < b) {
+                const int mid = (a + b) >> 1;
+                if (__ldg(&list[mid].x) < first + r) a = mid + 1;
+                else b = mid;
+            }
+            there[r] = a < lo[1] && __ldg(&list[a].x) == first + r;
+        }
+    }
     __syncthreads();
-    const int lo = lower_bound(keys, (int)p.M, (int)first), hi = lower_bound(keys, (int)p.M, (int)end);
-    for (int i = lo + threadIdx.x; i < hi; i += kEmSumWarps * 32) there[keys[i] - first] = true;
-    __syncthreads();
-    const float zero[VEC] = {};
-    for (long long v = first + warp; v < end; v += kEmSumWarps) {
-        if (there[v - first]) continue;
-        for (int c = lane * VEC; c < p.D; c += 32 * VEC) store_vec<VEC>((TW*)p.out + v * p.D + c, zero);
+    TW* from = (TW*)p.out + first * p.D;
+    constexpr int per = 16 / sizeof(TW);
+    const int lead = (int)(((uintptr_t)from & 15) / sizeof(TW)), total = rows * p.D;        // zero_rows * D is below 2^31
+    const int row_step = threads * per / p.D, col_step = threads * per - row_step * p.D;
+    int i = (int)threadIdx.x * per - lead, row = max(i, 0) / p.D, c = max(i, 0) - row * p.D;
+    if (i < 0) {                        // over the start: the elements that are there
+        for (int k = 0; k < i + per && k < total; ++k)
+            if (!there[k / p.D]) from_f(0.f, from + k);
+        i += threads * per;
+        row = i / p.D;
+        c = i - row * p.D;
+    }
+    while (i < total) {
+        if (i + per <= total && c + per <= p.D) {
+            if (!there[row]) *(uint4*)(from + i) = make_uint4(0, 0, 0, 0);
+        } else {
+            for (int k = i, kr = row, kc = c; k < i + per && k < total; ++k, ++kc) {
+                while (kc >= p.D) { kc -= p.D; ++kr; }
+                if (!there[kr]) from_f(0.f, from + k);
+            }
+        }
+        i += threads * per;
+        row += row_step;
+        c += col_step;
+        if (c >= p.D) { c -= p.D; ++row; }
     }
 }
 
-// A run of one id over several tiles: the partial rows of its tiles, in order, split over the warps and joined in the order of the warps.
-// One CTA per tile and 32 columns' vectors; all but those in whose tile such a run starts end at once.
-constexpr int kEmFinishWarps = 8;
-template <typename TW, int VEC>
-__global__ void __launch_bounds__(kEmFinishWarps * 32) embed_finish_kernel(EmParams p, int sorted) {
-    __shared__ float share[kEmFinishWarps][32 * VEC];
+// A run of one id over several CTAs' tiles: the partial rows of its tiles, in order.  One CTA per tile and slice of the columns; all but those
+// in whose tile such a run begins end at once.  Four groups of threads take a quarter of the partial rows each.
+constexpr int kEmFinishGroups = 4;
+template <typename TW>
+__global__ void __launch_bounds__(kEmFinishGroups * kEmSlice) embed_finish_kernel(EmParams p) {
+    __shared__ float share[kEmFinishGroups][kEmSlice];
+    __shared__ int stop;
     pdl_wait();
-    const int* keys = p.keys[sorted];
-    const int tile = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int first = tile * p.sum_tile, next = first + p.sum_tile;
-    if (next >= (int)p.M) return;
-    const int key = keys[next];
-    if (key >= (int)p.vocab || keys[next - 1] != key) return;           // no run of an id goes on
-    if (keys[first] == key && first > 0 && keys[first - 1] == key) return;      // it began in an earlier tile
-    int last = tile + 1;                                                // the last tile that begins with this id
-    for (;;) {
-        const long long t = (long long)last + 1 + lane, i = t * p.sum_tile;
-        const unsigned same = __ballot_sync(~0u, i < (long long)p.M && keys[i < (long long)p.M ? i : 0] == key);
-        const int more = same == ~0u ? 32 : __ffs(~same) - 1;
-        last += more;
-        if (more < 32) break;
+    const int2* list = p.list[p.sorted];
+    const int cta_tile = kEmSumWarps * p.warp_tile, tile = blockIdx.x, first = tile * cta_tile, next = first + cta_tile, M = (int)p.M;
+    if (next >= M) return;
+    const int key = list[next].x, last_here = list[next - 1].x, first_here = list[first].x, prev = first > 0 ? list[first - 1].x : -1;
+    if (key >= (int)p.vocab || last_here != key) return;            // no run of an id goes on
+    if (first_here == key && prev == key) return;                   // it began in an earlier tile
+    // the first tile behind that does not begin with this id
+    int n_tiles = p.sum_tiles;
+    for (int t0 = tile + 2; t0 < p.sum_tiles; t0 += kEmFinishGroups * kEmSlice) {
+        __syncthreads();
+        if (threadIdx.x == 0) stop = p.sum_tiles;
+        __syncthreads();
+        const int t = t0 + (int)threadIdx.x;
+        if (t < p.sum_tiles && list[t * cta_tile].x != key) atomicMin(&stop, t);
+        __syncthreads();
+        n_tiles = stop;
+        if (n_tiles < p.sum_tiles) break;
     }
-    const int n = last - tile + 1;      // slot 1 of the first tile, slot 0 of the others
-    const int per = (n + kEmFinishWarps - 1) / kEmFinishWarps, from = min(n, warp * per), to = min(n, from + per);
-    const int c = ((int)blockIdx.y * 32 + lane) * VEC;
-    float acc[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+    const int n = n_tiles - tile;       // slot 1 of the first tile, slot 0 of the others
+    const int group = threadIdx.x / kEmSlice, in_slice = threadIdx.x % kEmSlice, c = (int)blockIdx.y * kEmSlice + in_slice;
+    const int per = (n + kEmFinishGroups - 1) / kEmFinishGroups, from = min(n, group * per), to = min(n, from + per);
+    float sum = 0.f;
     if (c < p.D) {
-#pragma unroll 4
-        for (int j = from; j < to; ++j) {
-            const float* at = p.part + ((long long)(tile + j) * 2 + (j == 0 ? 1 : 0)) * p.D + c;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[i] += at[i];
-        }
+#pragma unroll 8
+        for (int j = from; j < to; ++j) sum += p.part[((long long)(tile + j) * 2 + (j == 0 ? 1 : 0)) * p.D + c];
     }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) share[warp][lane * VEC + i] = acc[i];
+    share[group][in_slice] = sum;
     __syncthreads();
-    if (warp == 0 && c < p.D) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            float s = share[0][lane * VEC + i];
-            for (int w = 1; w < kEmFinishWarps; ++w) s += share[w][lane * VEC + i];
-            acc[i] = s * p.scale;
-        }
-        store_vec<VEC>((TW*)p.out + (long long)key * p.D + c, acc);
+    if (group == 0 && c < p.D) {
+        for (int g = 1; g < kEmFinishGroups; ++g) sum += share[g][in_slice];
+        from_f(sum * p.scale, (TW*)p.out + (long long)key * p.D + c);
     }
 }
 
@@ -414,8 +681,9 @@ bool on_element(const void* q, int bytes) { return ((uintptr_t)q & (bytes - 1)) 
 int bytes_of(bpt_dtype t) { return t == BPT_F32 ? 4 : 2; }
 
 struct EmPlan {
-    int passes, digit, sort_tile, sort_tiles, sum_tile, sum_tiles;
-    size_t hist, list, part;     // bytes; list: one of the four arrays
+    int passes, digit, sort_tile, sort_tiles, sum_tiles, warp_tile;
+    int ctas, rounds;            // of the sort in one launch; 0: it takes a launch or two a pass
+    size_t hist, list, part;     // bytes; list: one of two
 };
 EmPlan embed_plan(const bpt_embed_args& a) {
     EmPlan q{};
@@ -427,10 +695,18 @@ EmPlan embed_plan(const bpt_embed_args& a) {
     // one CTA per tile and SM, no more: each scatter CTA adds up the counts of all tiles
     q.sort_tile = (int)std::max<long long>(kEmSortThreads, ((M + kEmSms - 1) / kEmSms + 31) / 32 * 32);
     q.sort_tiles = (int)((M + q.sort_tile - 1) / q.sort_tile);
-    q.sum_tile = 32;
-    q.sum_tiles = (int)((M + q.sum_tile - 1) / q.sum_tile);
-    q.hist = (size_t)q.sort_tiles * kEmBins * 4;
-    q.list = ((size_t)M * 4 + 15) / 16 * 16;
+    // places per warp: long tiles leave fewer partial rows, short ones more CTAs to share the work
+    const long long slices = (a.D + kEmSlice - 1) / kEmSlice;
+    q.warp_tile = 32;
+    while (q.warp_tile > 8 && M * slices < kEmSms * kEmSumWarps * q.warp_tile) q.warp_tile /= 2;
+    q.sum_tiles = (int)((M + kEmSumWarps * q.warp_tile - 1) / (kEmSumWarps * q.warp_tile));
+    if (M > 0 && M <= kEmClusterMost) {
+        q.ctas = 1;
+        while (q.ctas < kEmClusterCtas && q.ctas * kEmClusterThreads < M) q.ctas *= 2;
+        q.rounds = (int)((M + q.ctas * kEmClusterThreads - 1) / (q.ctas * kEmClusterThreads));
+    }
+    q.hist = q.ctas ? 0 : (size_t)q.sort_tiles * kEmBins * 4;
+    q.list = ((size_t)M * 8 + 15) / 16 * 16;
     q.part = (size_t)q.sum_tiles * 2 * a.D * 4;
     return q;
 }
@@ -451,16 +727,16 @@ bool start(void (*kernel)(A...), dim3 grid, int threads, cudaStream_t st, bool f
     return false;
 }
 
-template <typename TW, typename TO, int VEC>
-bool run_sum(const EmParams& p, int sorted, cudaStream_t st) {
-    const int slices = (p.D + 32 * VEC - 1) / (32 * VEC);
-    EmParams q = p;
-    q.sum_ctas = (int)(((long long)p.sum_tiles * slices + kEmSumWarps - 1) / kEmSumWarps);
-    const unsigned zero_ctas = (unsigned)((p.vocab + kEmZeroRows - 1) / kEmZeroRows);
-    if (!start(embed_sum_kernel<TW, TO, VEC>, dim3(q.sum_ctas + zero_ctas), kEmSumWarps * 32, st, p.sum_tiles == 0, q, sorted)) return false;
+template <typename TW, typename TO, bool VEC>
+bool run_sum(EmParams p, cudaStream_t st) {
+    p.slices = (p.D + kEmSlice - 1) / kEmSlice;
+    // rows per CTA that zeroes: enough to write, and few enough that their marks fit where the sums would be
+    p.zero_rows = (int)std::min<long long>(4096, std::max<long long>(1, kEmZeroBytes / (int)sizeof(TW) / p.D));
+    p.zero_ctas = (unsigned)((p.vocab + p.zero_rows - 1) / p.zero_rows);
+    if (!start(embed_sum_kernel<TW, TO, VEC>, dim3((unsigned)(p.sum_tiles * p.slices) + p.zero_ctas), kEmSumWarps * 32, st, p.sum_tiles == 0, p)) return false;
     trace_mark(st, "embed_sum");
     if (p.sum_tiles < 2) return true;       // no run crosses tiles
-    if (!start(embed_finish_kernel<TW, VEC>, dim3((unsigned)p.sum_tiles - 1, (unsigned)slices), kEmFinishWarps * 32, st, false, q, sorted)) return false;
+    if (!start(embed_finish_kernel<TW>, dim3((unsigned)p.sum_tiles - 1, (unsigned)p.slices), kEmFinishGroups * kEmSlice, st, false, p)) return false;
     trace_mark(st, "embed_finish");
     return true;
 }
@@ -483,14 +759,15 @@ extern "C" bpt_status bpt_embed_fwd(const bpt_embed_args* a, void* out, void* cu
     if (!p.record) return BPT_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const bool vec = a->D % 8 == 0 && on_16(a->weight) && on_16(out);       // whole 16-byte pieces in both
-    const int pieces = vec ? a->D / 8 : a->D;
     int lanes = 1;
-    while (lanes < pieces && lanes < 32) lanes *= 2;
-    const unsigned grid = (unsigned)(((unsigned long long)p.rows + 256 / lanes - 1) / (256 / lanes));
+    while (lanes < a->D / 8 && lanes < 32) lanes *= 2;
+    const int rows_per_cta = 256 / lanes * kEmRows;
+    const unsigned grid = vec ? (unsigned)(((unsigned long long)p.rows + rows_per_cta - 1) / rows_per_cta)
+                              : (unsigned)(((unsigned long long)p.rows * p.D + 7 + 8 * 256 - 1) / (8 * 256));        // wherever out starts
     typedef __nv_bfloat16 bf;
     const bool wf = a->weight_dtype == BPT_F32, of = a->out_dtype == BPT_F32;
-#define BPT_EMBED_FWD(TW, TO) (vec ? start(embed_fwd_kernel<TW, TO, 8>, dim3(grid), 256, st, true, p, lanes) \
-                                   : start(embed_fwd_kernel<TW, TO, 1>, dim3(grid), 256, st, true, p, lanes))
+#define BPT_EMBED_FWD(TW, TO) (vec ? start(embed_fwd_kernel<TW, TO>, dim3(grid), 256, st, true, p, lanes) \
+                                   : start(embed_fwd_flat_kernel<TW, TO>, dim3(grid), 256, st, true, p))
     const bool ok = wf ? (of ? BPT_EMBED_FWD(float, float) : BPT_EMBED_FWD(float, bf)) : (of ? BPT_EMBED_FWD(bf, float) : BPT_EMBED_FWD(bf, bf));
 #undef BPT_EMBED_FWD
     trace_mark(st, "embed_fwd");
@@ -500,7 +777,7 @@ extern "C" bpt_status bpt_embed_fwd(const bpt_embed_args* a, void* out, void* cu
 extern "C" size_t bpt_embed_bwd_workspace_bytes(const bpt_embed_args* a) {
     if (check_embed(a) != BPT_OK) return 0;
     const EmPlan q = embed_plan(*a);
-    return std::max<size_t>(16, q.hist + 4 * q.list + q.part);
+    return std::max<size_t>(16, q.hist + 2 * q.list + q.part);
 }
 
 extern "C" bpt_status bpt_embed_bwd(const bpt_embed_args* a, const void* d_out, void* d_weight, void* workspace, size_t workspace_bytes,
@@ -522,14 +799,29 @@ extern "C" bpt_status bpt_embed_bwd(const bpt_embed_args* a, const void* d_out, 
     char* at = static_cast<char*>(workspace);
     p.hist = reinterpret_cast<int*>(at); at += q.hist;
     for (int i = 0; i < 2; ++i) {
-        p.keys[i] = reinterpret_cast<int*>(at); at += q.list;
-        p.src[i] = reinterpret_cast<int*>(at); at += q.list;
+        p.list[i] = reinterpret_cast<int2*>(at); at += q.list;
     }
     p.part = reinterpret_cast<float*>(at);
-    p.sort_tile = q.sort_tile; p.sort_tiles = q.sort_tiles; p.sum_tile = q.sum_tile; p.sum_tiles = q.sum_tiles;
+    p.sort_tile = q.sort_tile; p.sort_tiles = q.sort_tiles; p.sum_tiles = q.sum_tiles; p.warp_tile = q.warp_tile;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    int sorted = 0;
-    if (M > 0) {
+    if (M > 0 && q.ctas) {
+        if (q.ctas > 8 && cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return BPT_ERR_CUDA;
+        cudaLaunchAttribute attr[1] = {};
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim = {(unsigned)q.ctas, 1, 1};
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)q.ctas);
+        cfg.blockDim = dim3(kEmClusterThreads);
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaLaunchKernelEx(&cfg, embed_sort_kernel, p, q.passes, q.digit, q.rounds) != cudaSuccess) {
+            cudaGetLastError();
+            return BPT_ERR_CUDA;
+        }
+        trace_mark(st, "embed_sort");
+        p.sorted = (q.passes - 1) & 1;
+    } else if (M > 0) {
         const int bins = 1 << q.digit;
         for (int i = 0; i < q.passes; ++i) {
             const int from = i == 0 ? -1 : (i - 1) & 1, to = i & 1;
@@ -537,13 +829,13 @@ extern "C" bpt_status bpt_embed_bwd(const bpt_embed_args* a, const void* d_out, 
             trace_mark(st, "embed_hist");
             if (!start(embed_scatter_kernel, dim3(q.sort_tiles), kEmSortThreads, st, false, p, from, to, i * q.digit, bins)) return BPT_ERR_CUDA;
             trace_mark(st, "embed_scatter");
-            sorted = to;
+            p.sorted = to;
         }
     }
     const bool vec = a->D % 8 == 0 && on_16(d_weight) && on_16(d_out);
     typedef __nv_bfloat16 bf;
     const bool wf = a->weight_dtype == BPT_F32, of = a->out_dtype == BPT_F32;
-#define BPT_EMBED_SUM(TW, TO) (vec ? run_sum<TW, TO, 8>(p, sorted, st) : run_sum<TW, TO, 1>(p, sorted, st))
+#define BPT_EMBED_SUM(TW, TO) (vec ? run_sum<TW, TO, true>(p, st) : run_sum<TW, TO, false>(p, st))
     const bool ok = wf ? (of ? BPT_EMBED_SUM(float, float) : BPT_EMBED_SUM(float, bf)) : (of ? BPT_EMBED_SUM(bf, float) : BPT_EMBED_SUM(bf, bf));
 #undef BPT_EMBED_SUM
     return ok ? BPT_OK : BPT_ERR_CUDA;

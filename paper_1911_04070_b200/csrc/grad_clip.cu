@@ -19,18 +19,6 @@ namespace bpt {
 namespace {
 
 constexpr int kGcSms = 148;
-#ifndef GC_AHEAD
-#define GC_AHEAD 4
-#endif
-#ifndef GC_CS
-#define GC_CS ""
-#endif
-#ifndef GC_LD
-#define GC_LD ""
-#endif
-#ifndef GC_BLK
-#define GC_BLK 1
-#endif
 constexpr int kGcUnit = 2048;       // elements; 8 per thread
 constexpr int kGcThreads = 256;
 constexpr int kGcMost = 960;        // tensors per launch: 32 bytes each, in at most 32 KB of arguments
@@ -90,7 +78,7 @@ __device__ __forceinline__ int lead_of(const GcTensor& t) { return (int)(t.flags
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
     uint4 q;
-    __device__ __forceinline__ void load(const void* at) { asm volatile("ld.global" GC_LD ".v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(at)); }
+    __device__ __forceinline__ void load(const void* at) { asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(at)); }
     __device__ __forceinline__ void get(float (&x)[8]) const {
         const unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -103,7 +91,7 @@ template <> struct Raw8<__nv_bfloat16> {
 template <> struct Raw8<float> {
     float f[8];
     __device__ __forceinline__ void load(const void* at) {
-        asm volatile("ld.global" GC_LD ".v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(at));
     }
     __device__ __forceinline__ void get(float (&x)[8]) const {
@@ -116,7 +104,7 @@ __device__ __forceinline__ float elem(__nv_bfloat16 x) { return __bfloat162float
 
 // This thread's groups of 8 elements in units u0 .. u1 of a tensor: body(index of the group's first element, its values, whether all 8
 // belong to the tensor; those that do not are 0).  kGcAhead groups are on their way at a time.
-constexpr int kGcAhead = GC_AHEAD;
+constexpr int kGcAhead = 4;
 template <typename T, bool BACK, typename F>
 __device__ __forceinline__ void groups_of(const GcTensor& t, unsigned u0, unsigned u1, F&& body) {
     const int lead = lead_of(t);
@@ -163,7 +151,7 @@ __device__ __forceinline__ void groups(const GcTensor& t, unsigned u0, unsigned 
 }
 
 template <int N>
-__global__ void __launch_bounds__(kGcThreads, GC_BLK) grad_norm_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
+__global__ void __launch_bounds__(kGcThreads) grad_norm_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
     __shared__ double share[kGcThreads / 32];
     __shared__ unsigned largest[kGcThreads / 32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -231,7 +219,7 @@ __device__ float whole_norm(const GcParams& p) {
 }
 
 __device__ __forceinline__ void store8(float* at, const float (&x)[8]) {
-    asm volatile("st.global" GC_CS ".v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  :: "l"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
 }
 __device__ __forceinline__ void store8(__nv_bfloat16* at, const float (&x)[8]) {
@@ -240,7 +228,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16* at, const float (&x)[8]) {
     for (int j = 0; j < 4; ++j) q[j] = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
     uint4 w;
     memcpy(&w, q, 16);
-    asm volatile("st.global" GC_CS ".v4.b32 [%0], {%1, %2, %3, %4};" :: "l"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+    asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" :: "l"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
 }
 __device__ __forceinline__ void put(float x, float* y) { *y = x; }
 __device__ __forceinline__ void put(float x, __nv_bfloat16* y) { *y = __float2bfloat16(x); }
@@ -264,7 +252,7 @@ __device__ __forceinline__ void scale_units(const GcTensor& t, unsigned u0, unsi
 }
 
 template <int N>
-__global__ void __launch_bounds__(kGcThreads, GC_BLK) grad_scale_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
+__global__ void __launch_bounds__(kGcThreads) grad_scale_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float norm = whole_norm(p);

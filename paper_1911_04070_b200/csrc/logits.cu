@@ -11,7 +11,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <cstdlib>
 #include <type_traits>
 
 #include "bpt_internal.cuh"
@@ -20,16 +19,10 @@ namespace bpt {
 namespace {
 
 constexpr int kLgSms = 148;
-#ifndef LG_LIMIT
-#define LG_LIMIT (2 * kLgSms)
-#endif
 // Threads that pass over a piece, 16 elements each, where that is all a CTA does; where it also goes through the history, and
 // then the threads that do that.
 constexpr int kLgStream = 256, kLgStreamToo = 512, kLgSparse = 512;
 constexpr int kLgPiece = kLgStream * 16, kLgPieceToo = kLgStreamToo * 16;
-#ifndef LG_MINB
-#define LG_MINB 4
-#endif
 
 struct LgListed { unsigned id; float value; };
 struct LgParams {
@@ -308,7 +301,7 @@ __global__ void __launch_bounds__(kLgHashThreads) put_listed_kernel(const __grid
 // of biases meanwhile, and write the ids that stand there once more, behind the others; in place, the others wait until the logits
 // of those ids are read.  Where there are no others, list_ids_kernel may be at work on those ids: in place its end is waited for.
 template <typename TL, typename TO, int STREAM, int SPARSE>
-__global__ void __launch_bounds__(STREAM + SPARSE, SPARSE ? 1 : LG_MINB) adjust_logits_kernel(const __grid_constant__ LgParams p) {
+__global__ void __launch_bounds__(STREAM + SPARSE, SPARSE ? 1 : 4) adjust_logits_kernel(const __grid_constant__ LgParams p) {
     extern __shared__ uint4 lg_smem[];
     __shared__ int listed;
     if (SPARSE == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -452,9 +445,10 @@ LgPlan plan(const bpt_logits_args& a) {
     q.sparse = most > 0;
     const auto pieces = [&](int piece) { return (int)((a.vocab + 16 / bytes_of(a.dtype) - 1 + piece - 1) / piece); };     // wherever the row starts
     q.stride = std::min(most, (long long)a.vocab);
-    // Every CTA of a row going through all of its history is the shorter way while all CTAs run at once.  B200, bf16: 32 rows of 32000 with
-    // histories of 4096 in 128 CTAs 6.6 us against LIST1; 256 rows of 128001 with histories of 2048 LIST2 us against LIST3.
-    q.list = q.sparse && a.rows * pieces(kLgPieceToo) > LG_LIMIT && most <= kLgMostIds;
+    // Every CTA of a row going through all of its history is the shorter way while there are few CTAs to a row or to an SM.  B200, bf16 with a mask,
+    // microseconds of one launch | of listing apart: 32 rows of 32000, histories of 8000 10 | 23; 128 rows of 32000, 2000 14 | 14; 32 rows of 128000,
+    // 8000 21 | 27; 256 rows of 32000, 1000 23 | 16; 64 rows of 128000, 500 21 | 12, 8000 33 | 29; 512 rows of 5000, 2000 19 | 23.
+    q.list = q.sparse && pieces(kLgPieceToo) >= 4 && a.rows * pieces(kLgPieceToo) > 5 * kLgSms && most <= kLgMostIds;
     q.pieces = pieces(q.sparse && !q.list ? kLgPieceToo : kLgPiece);
     q.slots = 1024;
     while (q.slots < kLgSlots && q.slots < 2 * most) q.slots *= 2;

@@ -70,7 +70,8 @@ def _table(V, D, dtype=BF16, seed=2):
 # one token to many tiles of the sort and the sums; the ends of a digit's range (511 | 512 ids are one | two passes, 262143 | 262144 two | three)
 @pytest.mark.parametrize("shape,V,D", [((1,), 1, 1), ((1, 1), 7, 8), ((3, 31), 5, 7), ((2, 33), 511, 64), ((2, 512), 512, 201), ((1, 1025), 3, 256),
                                        ((4, 1000), 256, 264), ((2, 2, 77), 1000, 40), ((1, 4097), 262143, 8), ((1, 300), 262144, 16),
-                                       ((3, 70001), 97, 8), ((1, 160000), 70000, 3)])
+                                       ((3, 70001), 97, 8), ((1, 160000), 70000, 3), ((2, 50001), 3000, 8),
+                                       ((1, 131072), 300000, 2), ((1, 8192), 2, 24), ((1, 131073), 40, 9)])
 @pytest.mark.parametrize("wt,ot", [(BF16, BF16), (F32, BF16), (BF16, F32), (F32, F32)])
 def test_sizes_and_types(layer, shape, V, D, wt, ot):
     _check(layer, _ids(*shape, V=V, dtype=torch.int32 if D % 2 else torch.int64), _table(V, D, wt), scale=1.5, spans=shape[-1] - 1, dtype=ot)

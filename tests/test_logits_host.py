@@ -45,7 +45,7 @@ def test_more_refusals(lib):
     assert call(_args(), out=None) == 1 and call(_args(), out=8193) == 1
     assert call(_args(rows=0, logits=None, history_len=4, bias_count=3), out=None) == 0
     # many pieces of rows with a history: listed apart, in a workspace
-    big = dict(H, rows=3000, vocab=20000, logits_stride=20000, out_stride=20000, presence=1.0)
+    big = dict(H, rows=3000, vocab=50000, logits_stride=50000, out_stride=50000, presence=1.0)
     assert need(_args()) == 0 and need(_args(**dict(big, presence=0.0))) == 0 and need(_args(**dict(big, history_len=20000))) == 0
     a = _args(**big)
     assert need(a) >= 3000 * (5 * 8 + 4)

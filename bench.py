@@ -616,6 +616,37 @@ def run_model(args):
             torch.cuda.empty_cache()
 
 
+def run_training(args):
+    """Training steps of a byte-level language model over the stack of run_model: ids to states, stack, logits, cross entropy, backward
+    pass, clipping, AdamW.  8192 random ids per batch.  One JSON line per sequence length."""
+    import torch
+    from paper_1911_04070_b200 import layer
+    torch.cuda.set_device(0)
+    torch.manual_seed(0)
+    for n in (512, 2048, 8192):
+        B, vocab = 8192 // n, 256
+        form = dict(gated="silu", sandwich=True) if args.form == "gated" else {}
+        model = layer.BPTLanguageModel(vocab, n, 64, 512, 8, 1368 if form else 2048, 6, device="cuda:0", **form).to("cuda:0", torch.bfloat16)
+        opt = torch.optim.AdamW(model.parameters(), lr=1e-4, fused=True)
+        ids = torch.randint(0, vocab, (B, n), device="cuda:0")
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        for _ in range(3):
+            layer.training_step(model, opt, ids)
+        torch.cuda.synchronize()
+        steps = max(3, min(args.steps, 10))
+        e0.record()
+        for _ in range(steps):
+            loss, norm = layer.training_step(model, opt, ids)
+        e1.record()
+        torch.cuda.synchronize()
+        ms = e0.elapsed_time(e1) / steps
+        print(json.dumps({"workload": "training step of a byte-level language model, 6 layers, d=512, 8 heads, k=64, 8192 tokens per batch, bf16",
+                          "form": "gated (silu), sandwich norms" if form else "Algorithm 2", "n": n, "batch": B, "step_ms": ms,
+                          "tokens_per_s": 8192 / (ms * 1e-3), "loss": float(loss), "gradient_norm": float(norm)}), flush=True)
+        del model, opt
+        torch.cuda.empty_cache()
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -629,6 +660,8 @@ def main():
     ap.add_argument("--batch", type=int, default=0, help="override the batch size (profiling of a smaller case)")
     ap.add_argument("--sweep", action="store_true", help="run the n x k scaling sweep instead: one JSON line per point")
     ap.add_argument("--model", action="store_true", help="time a 6-layer BPT stack (Sec. 4.4 setting) instead: one JSON line per point")
+    ap.add_argument("--train", action="store_true",
+                    help="with --model: training steps of a language model over the stack (bytes in, clipped gradients, AdamW) instead")
     ap.add_argument("--form", default="paper", choices=["paper", "gated"],
                     help="with --model: the layers of Algorithm 2, or gated feed-forward blocks between sandwich norms")
     args = ap.parse_args()
@@ -636,7 +669,7 @@ def main():
     if args.sweep:
         return run_sweep(args)
     if args.model:
-        return run_model(args)
+        return run_training(args) if args.train else run_model(args)
     cfgs = all_configs()
     if args.config not in cfgs:
         raise SystemExit("unknown config %s; choose from %s" % (args.config, ", ".join(sorted(cfgs))))

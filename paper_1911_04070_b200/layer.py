@@ -333,7 +333,13 @@ class BPTEncoder(nn.Module):
         B, n, D = tokens.shape
         if n != self.n:
             raise ValueError("expected %d token states per sequence, got %d" % (self.n, n))
-        h = torch.cat([tokens, tokens.new_zeros(B, n - 1, D)], dim=1)
+        return self.forward_nodes(torch.cat([tokens, tokens.new_zeros(B, n - 1, D)], dim=1), lengths, readout)
+
+    def forward_nodes(self, h, lengths=None, readout: str = "tokens"):
+        """The same from the states of all nodes [B, 2n-1, D] (token_states makes them from ids)."""
+        n = self.n
+        if h.shape[1] != 2 * n - 1:
+            raise ValueError("expected the states of %d nodes per sequence, got %d" % (2 * n - 1, h.shape[1]))
         if self.sandwich:
             y = None
             for layer, norm in zip(self.layers, [l.pre1 for l in self.layers[1:]] + [self.norm_out]):
@@ -411,3 +417,79 @@ class BPTDecoder:
             norm = self.enc.norm_out
             out = residual_norm(out, None, norm.weight, norm.bias, eps=norm.eps)
         return out
+
+
+class BPTLanguageModel(nn.Module):
+    """Token ids to logits with a left-only BPTEncoder (Sec. 4.2): node states from a table of embeddings scaled by sqrt(d_model), the stack,
+    and a projection to the vocabulary by the same table (tied) or by one of its own.
+
+    vocab: ids 0 .. vocab - 1; padding_idx: an id whose embedding is not trained by its own places; the other arguments are BPTEncoder's."""
+
+    def __init__(self, vocab: int, n: int, k: int, d_model: int, n_heads: int, d_ff: int, n_layers: int, tied: bool = True, padding_idx=None,
+                 device="cuda", **form):
+        super().__init__()
+        if vocab < 1 or (padding_idx is not None and not 0 <= padding_idx < vocab):
+            raise ValueError("vocab must be at least 1, and padding_idx None or an id below it")
+        self.vocab, self.padding_idx, self.scale = vocab, padding_idx, math.sqrt(d_model)
+        self.embedding = nn.Parameter(torch.randn(vocab, d_model) * d_model ** -0.5)
+        self.encoder = BPTEncoder(n, k, d_model, n_heads, d_ff, n_layers, left_only=True, device=device, **form)
+        self.head = None if tied else nn.Linear(d_model, vocab, bias=False)
+
+    def logits(self, h):
+        """[..., d_model] states of tokens to [..., vocab] logits of what follows them."""
+        return torch.nn.functional.linear(h, self.embedding if self.head is None else self.head.weight)
+
+    def forward(self, ids, lengths=None):
+        """ids: [B, n] int32 or int64, n the encoder's; lengths: int32 [B], or None (all n; what stands behind a length is not looked at).
+        Returns the logits [B, n, vocab]; those behind a length mean nothing."""
+        n = self.encoder.n
+        if ids.dim() != 2 or ids.shape[1] != n:
+            raise ValueError("expected %d ids per sequence (pad shorter ones and give lengths)" % n)
+        h = token_states(ids, self.embedding, self.scale, n - 1, lengths, self.padding_idx)
+        return self.logits(self.encoder.forward_nodes(h, lengths))
+
+    def loss(self, ids, lengths=None):
+        """The mean cross entropy, in float32, of each token given those before it."""
+        x = self(ids, lengths)[:, :-1].float()
+        want = ids[:, 1:].long()
+        if lengths is not None:
+            want = want.masked_fill(torch.arange(1, ids.shape[1], device=ids.device) >= lengths[:, None], -100)
+        return torch.nn.functional.cross_entropy(x.reshape(-1, self.vocab), want.reshape(-1), ignore_index=-100)
+
+    @torch.no_grad()
+    def generate(self, prompt, steps: int, temperature: float = 0.0, generator=None, allowed=None, **settings):
+        """Continues the prompts [B, P] (P >= 1 ids each, int32 or int64) by `steps` ids, token by token with cached states (BPTDecoder).
+
+        allowed: the ids that may follow, as adjust_logits takes them, or a function of the ids so far [B, t] that returns them (a grammar).
+        settings: repetition, presence, frequency, bias, bias_ids, bias_values, see adjust_logits; the prompt counts for repetition only.
+        temperature 0 takes the largest logit (the lowest id of equal ones), another one draws from softmax(logits / temperature) with
+        torch's `generator`.  Returns [B, P + steps] ids."""
+        B, P = prompt.shape
+        if P < 1 or steps < 0 or P + steps > self.encoder.n:
+            raise ValueError("a prompt of at least one id and room for it and the steps in %d ids are needed" % self.encoder.n)
+        if temperature < 0:
+            raise ValueError("temperature must not be negative")
+        ids = torch.cat([prompt, prompt.new_zeros(B, steps)], dim=1)
+        lengths, prompts = (torch.full((B,), P, dtype=torch.int32, device=ids.device) for _ in range(2))
+        dec = BPTDecoder(self.encoder, B, dtype=self.embedding.dtype)
+        for t in range(P + steps - 1):
+            state = dec.step(token_states(ids[:, t], self.embedding, self.scale))
+            if t < P - 1:
+                continue
+            # in float32 from here on, in place
+            x = self.logits(state).float()
+            adjust_logits(x, ids, lengths, prompts, allowed=allowed(ids[:, :t + 1]) if callable(allowed) else allowed, out=x, **settings)
+            lengths += 1
+            ids[:, t + 1] = x.argmax(-1) if temperature == 0 else torch.multinomial(torch.softmax(x / temperature, -1), 1, generator=generator)[:, 0]
+        return ids
+
+
+def training_step(model, optimizer, ids, lengths=None, max_norm: float = 1.0):
+    """One step of a BPTLanguageModel: loss, backward pass, clipping of all gradients by their norm, the optimizer's step.  Returns (loss, norm
+    before clipping) as tensors on the device; nothing is read back."""
+    optimizer.zero_grad(set_to_none=True)
+    loss = model.loss(ids, lengths)
+    loss.backward()
+    norm = clip_gradients([p.grad for p in model.parameters()], max_norm)
+    optimizer.step()
+    return loss.detach(), norm

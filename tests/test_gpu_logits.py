@@ -48,8 +48,8 @@ def _oracle(x, history=None, lengths=None, prompt_lengths=None, repetition=1.0, 
                 y[b, v] += w
                 mag[b, v] += abs(w)
         if allowed is not None:
-            words = (allowed if allowed.dim() == 1 else allowed[b % allowed.shape[0]]).tolist()
-            ok = torch.tensor([(words[v // 32] >> (v % 32)) & 1 for v in range(V)], dtype=torch.bool)
+            words = (allowed if allowed.dim() == 1 else allowed[b % allowed.shape[0]]).cpu().long() & 0xffffffff
+            ok = ((words[:, None] >> torch.arange(32)) & 1).bool().reshape(-1)[:V]
             y[b] = torch.where(ok, y[b], torch.full_like(y[b], -float("inf")))
     return y, mag
 
@@ -245,6 +245,40 @@ def test_another_stream(layer):
         got = layer.adjust_logits(x, h, repetition=1.2)
     torch.cuda.synchronize()
     assert torch.equal(want, got)
+
+
+# rows of several pieces each, more of them than run at once: ids of the histories are listed apart
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("lt,ot", [(BF16, BF16), (F32, F32), (BF16, F32)])
+def test_large_batches(layer, in_place, lt, ot):
+    if in_place and lt != ot:
+        pytest.skip("another type cannot be written in place")
+    d = _Draw(15)
+    B, V, T, K = 200, 32801, 60, 9
+    x = d.logits(B, V, lt)
+    h, bi = d.ids(-2, V + 2, B, T), d.ids(-1, V + 1, B, K)
+    h[0], h[1, ::2], bi[1, 3:] = 7, V - 1, 11
+    kw = dict(history=h, lengths=d.ids(0, T + 1, B, dtype=torch.int32), prompt_lengths=d.ids(0, T + 1, B, dtype=torch.int32), repetition=d.real(B, lo=0.5, hi=2),
+              presence=d.real(B, lo=-1), frequency=d.real(B, lo=-0.5))
+    full = dict(kw, bias=d.real(V, lo=-2, hi=2), bias_ids=bi, bias_values=d.real(B, K, lo=-9, hi=9), allowed=d.bits(B, (V + 31) // 32))
+    want = _check(layer, x, out=torch.empty(B, V, device="cuda", dtype=ot), **full)
+    some = _check(layer, x, out=torch.empty(B, V, device="cuda", dtype=ot), **kw)
+    if in_place:
+        y, z = x.clone(), x
+        assert torch.equal(layer.adjust_logits(y, out=y, **full), want) and torch.equal(layer.adjust_logits(z, out=z, **kw), some)
+
+
+def test_long_histories_of_large_batches(layer):
+    """As many different ids as the table of a row takes, and one more than that."""
+    d = _Draw(16)
+    B, V = 190, 32768
+    x = d.logits(B, V)
+    for T in (12288, 12289):
+        h = torch.stack([torch.randperm(V, generator=d.g)[:T] for _ in range(3)]).repeat(64, 1)[:B].to("cuda")
+        y = layer.adjust_logits(x, h, presence=1.0, repetition=2.0)
+        r = torch.where(x > 0, x / 2, x * 2) - 1
+        want = x.clone().scatter_(1, h, r.gather(1, h))
+        assert torch.equal(y, want)
 
 
 _CAPTURE = r"""

@@ -419,7 +419,7 @@ bpt_status bpt_clip_grads(const bpt_grad* grads, int32_t n, int32_t norm_type, f
  *     x += bias[b, v];    x += bias_values[b, j] for the last j with bias_ids[b, j] = v;     out[b, v] = allowed(b, v) ? x : -infinity
  * in fp32, rounded once.  What a mask forbids is -infinity whatever stands there (NaN too); a row without an allowed id is all -infinity.
  * logits: [rows, vocab] of `dtype`, rows logits_stride elements apart; out: of out_dtype, rows out_stride apart; out may be the logits
- * themselves (same address, type and stride) and must otherwise not overlap them.
+ * themselves (same address, type and stride) and must otherwise not overlap them, nor any other argument.
  * history: [rows, history_len] of history_bytes 4 or 8, rows history_stride apart; history_len 0: none.  lengths, prompt_lengths: [rows]
  * (clamped to 0 .. history_len and 0 .. lengths[b]) or NULL (history_len; 0).  Ids outside 0 .. vocab - 1 count for nothing.
  * repetition (> 0), presence, frequency: numbers, or where the _rows pointer is not NULL one fp32 value per row.

@@ -457,6 +457,8 @@ py::object clip_gradients(const py::object& grads, const py::object& into, int64
         if (g[i].layout() != at::kStrided || !g[i].is_cuda() || (first && g[i].device() != first->device()) || !type_code(g[i], &e.dtype)) return py::none();
         if (!first) first = &g[i];
         Tensor src = g[i], dst;
+        // parameters in the place of their gradients, as other interfaces take them, would be scaled themselves
+        if (clip && (o.empty() ? g[i] : o[i]).defined() && (o.empty() ? g[i] : o[i]).is_leaf() && (o.empty() ? g[i] : o[i]).requires_grad()) return py::none();
         if (!o.empty()) {
             if (!o[i].defined()) return py::none();
             check_tangents({&o[i]}, "clip_gradients");
@@ -466,6 +468,8 @@ py::object clip_gradients(const py::object& grads, const py::object& into, int64
                 src = src.contiguous();
                 if (!dst.is_contiguous()) {
                     if (at::has_internal_overlap(dst) == at::MemOverlap::Yes) return py::none();
+                    for (const auto& other : back)      // the library sees copies only
+                        if (other.second.data_ptr() == dst.data_ptr() && other.second.strides() == dst.strides()) return py::none();
                     held.push_back(at::empty(dst.sizes(), dst.options()));
                     back.emplace_back(held.back(), dst);
                     dst = held.back();
@@ -523,6 +527,17 @@ bool rows_meet(const Tensor& a, const Tensor& b) {
     if (step(a) != step(b) || a.size(0) < 2) return true;
     const int64_t d = ((from(b) - from(a)) % step(a) + step(a)) % step(a);
     return d < width(a) || d + width(b) > step(a);
+}
+
+// Whether the memory from the first to the last element of one meets that of the other.
+bool spans_meet(const Tensor& a, const Tensor& b) {
+    if (!a.numel() || !b.numel()) return false;
+    const auto end = [](const Tensor& t) {
+        int64_t n = t.element_size();
+        for (int64_t i = 0; i < t.dim(); ++i) n += (t.size(i) - 1) * t.stride(i) * (int64_t)t.element_size();
+        return (const char*)t.data_ptr() + n;
+    };
+    return (const char*)a.data_ptr() < end(b) && (const char*)b.data_ptr() < end(a);
 }
 
 // A number, or one float32 per row.
@@ -619,6 +634,8 @@ py::object adjust_logits(const Tensor& logits_, const Opt& history_, const Opt& 
         if (!(out.data_ptr() == logits.data_ptr() && out.scalar_type() == logits.scalar_type() && row_stride(out) == row_stride(logits)) &&
             rows_meet(out, logits))
             return py::none();
+        for (const Tensor& t : held)
+            if (spans_meet(out, t)) return py::none();
     } else {
         out = at::empty({B, V}, logits.options());
     }

@@ -159,6 +159,12 @@ def token_states(ids, weight, scale=1.0, span_rows=0, lengths=None, padding_idx=
         cont = lambda t: t if t is None else t.contiguous()
         binding.bpt_embed_fwd(cont(ids), cont(weight), scale, span_rows, cont(lengths), dtype)                     # says what is wrong
         raise RuntimeError("token_states: refused")
+    if binding.CHECK_DEVICE_STATUS:
+        status = binding.bpt_check_device(ids.device)
+        if status == 8:
+            raise IndexError("token_states: an id is outside the table")
+        if status:
+            raise RuntimeError("a device-side wait timed out before token_states")
     return out
 
 
@@ -172,7 +178,9 @@ def _clip(grads, out, norm_type, clip, max_norm, eps):
         if out is not None and len(as_list(out)) != len(as_list(grads)):
             raise ValueError("out must have an entry for every gradient")
         pairs = [(g, o) for g, o in zip(as_list(grads), as_list(grads if out is None else out)) if g is not None]
-        grads, into = [g.contiguous() for g, _ in pairs], None if out is None else [o for _, o in pairs]
+        if clip and any(t is not None and t.is_leaf and t.requires_grad for t in (as_list(grads) if out is None else as_list(out))):
+            raise ValueError("leaves that require a gradient are not written: give the gradients, not the parameters")
+        grads, into = [g.contiguous() for g, _ in pairs], None if out is None else [o if o is None else o.new_empty(o.shape) for _, o in pairs]
         if out is not None and any(o is None for o in into):
             raise ValueError("out must have a tensor for every gradient")
         binding._grad_list(grads, into, norm_type)
@@ -195,7 +203,8 @@ def clip_gradients(grads, max_norm, norm_type=2.0, eps=1e-6, out=None):
     grads: a list of tensors, float32 or bfloat16 mixed, on one device (``[p.grad for p in model.parameters()]``; None entries are passed over).
     They are scaled in place, and not written where the norm is below max_norm; or, with out (a list of as many tensors, float32 or
     bfloat16, say the gradients of an optimizer's 32-bit master weights), left as they are and the scaled values written there.  Any
-    strides; no tensor twice and no overlaps between what is written and anything else.  A NaN makes the norm and all results NaN.  Nothing
+    strides; no tensor twice and no overlaps between what is written and anything else; no leaf that requires a gradient is written (a parameter
+    given for its gradient is refused).  A NaN makes the norm and all results NaN.  Nothing
     is read back to the host: can be captured in a CUDA graph, which then uses these very tensors."""
     return _clip(grads, out, norm_type, True, max_norm, eps)
 
@@ -211,7 +220,7 @@ def adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, repet
     bias: [V] or [B, V], float32 or bfloat16.  bias_ids (int32 or int64), bias_values (float32): [B, K], a few biased ids per row (outside the
     vocabulary: no effect; given twice: the last one counts).  allowed: int32 [ceil(V / 32)] or [B, ceil(V / 32)], bit v % 32 of word v // 32 set
     where id v is allowed.  out: a tensor [B, V], float32 or bfloat16, the logits themselves for one (default: a new one of the logits'
-    type).  Any strides.  Computed in float32, rounded once.  For inference: arguments that require a gradient are refused."""
+    type), apart from all other arguments.  Any strides.  Computed in float32, rounded once.  For inference: arguments that require a gradient are refused."""
     got = binding.load_native().adjust_logits(logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias, bias_ids, bias_values,
                                               allowed, out)
     if got is None:
@@ -221,7 +230,7 @@ def adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, repet
             raise ValueError("out must be [B, V] on the device of the logits, its rows without gaps")
         binding.bpt_adjust_logits(*map(cont, (logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias, bias_ids, bias_values,
                                               allowed)), None if out is None else out.new_empty(out.shape))      # says what is wrong
-        raise ValueError("out overlaps the logits without being them")
+        raise ValueError("out overlaps the logits without being them, or another argument")
     return got
 
 

@@ -126,6 +126,18 @@ def test_ids_outside_the_table(layer, bad, dtype):
     assert binding.bpt_check_device() == 8 and binding.bpt_check_device() == 0
 
 
+def test_ids_outside_the_table_while_the_status_is_looked_at(layer, monkeypatch):
+    from paper_1911_04070_b200 import binding
+    ids, w = _ids(2, 100, V=50), _table(50, 24)
+    monkeypatch.setattr(binding, "CHECK_DEVICE_STATUS", True)
+    binding.bpt_check_device()
+    layer.token_states(ids, w)
+    ids[1, 5] = 50
+    with pytest.raises(IndexError):
+        layer.token_states(ids, w)
+    assert binding.bpt_check_device() == 0
+
+
 @pytest.mark.parametrize("shape,V", [((0,), 4), ((0, 5), 4), ((3, 0), 4)])
 def test_no_tokens(layer, shape, V):
     w = _table(V, 16)

@@ -108,6 +108,20 @@ def test_strides(layer):
     for bad in ([row], [big[:, :32], big[:, :32]], [row.contiguous()] * 2, [views[2], views[2].t()]):
         with pytest.raises(ValueError, match="overlaps"):
             layer.clip_gradients(bad, 0.1)
+    with pytest.raises(ValueError, match="overlaps"):
+        layer.clip_gradients([_rnd(40, 32), _rnd(40, 32)], 0.1, out=[big[:, :32], big[:, :32]])
+
+
+def test_parameters_are_not_taken_for_gradients(layer):
+    p = torch.nn.Parameter(_rnd(5))
+    keep = p.detach().clone()
+    for call in (lambda: layer.clip_gradients([p], 0.1), lambda: layer.clip_gradients(p, 0.1), lambda: layer.clip_gradients([_rnd(5)], 0.1, out=[p])):
+        with pytest.raises(ValueError, match="not the parameters"):
+            call()
+    assert torch.equal(p, keep) and abs(float(layer.gradient_norm([p])) - _norm64([p], 2.0)) <= 5 * U * _norm64([p], 2.0)
+    g, = torch.autograd.grad((p ** 3).sum(), [p], create_graph=True)        # not a leaf
+    layer.clip_gradients([g], 0.1)
+    assert abs(_norm64([g], 2.0) - 0.1) < 1e-6
 
 
 @pytest.mark.parametrize("std", [1e-42, 1e-30, 1e-22, 1e-12, 1e12, 1e19, 1e30])

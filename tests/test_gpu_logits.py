@@ -226,6 +226,10 @@ def test_refusals_on_the_device(layer):
     big = d.logits(1, 200)[0]
     with pytest.raises(ValueError, match="overlaps"):
         layer.adjust_logits(big[:120].view(3, 40), out=big[8:128].view(3, 40))
+    for name in ("bias", "bias_values"):
+        z = d.real(3, 40)
+        with pytest.raises(ValueError, match="another argument"):
+            layer.adjust_logits(x, **{"bias_ids": d.ids(0, 40, 3, 40)} if name == "bias_values" else {}, **{name: z}, out=z)
     with pytest.raises(TypeError):
         layer.adjust_logits(x, out=x.half())
     with pytest.raises(TypeError):

@@ -6,6 +6,11 @@
 // contiguous share of the units, so that a few large and many small tensors balance.  The second kernel walks a CTA's share backwards:
 // what the first one read last is still in L2.
 //
+// B200, on the GPU: 9 tensors of 0.26 million values 6.2 us (two short launches; one launch of a cluster of 16 CTAs took 8 to 10); 50 MB of
+// bf16 in 54 tensors, norm only, 18 us; the same scaled into fp32 41 us (150 MB read and written once are 23, the norm's own read of 50 MB from
+// memory and a second launch come on top); 1.2 GB in 432 tensors scaled into bf16 608 us (norm 6.2 TB/s, scaling 5.6).  Eight groups of 8 elements on
+// their way per thread instead of four: 25 / 53 / 597; units dealt out in turn instead of in one range per CTA: 20 / 44 / 595.
+//
 // Squares are summed in fp32 over 8 elements and then in fp64, which costs one addition per 16 or 32 bytes; where a sum of 8 squares
 // leaves the range in which fp32 loses nothing, those 8 are squared in fp64: no gradient is too large or too small for its norm.
 #include <algorithm>

@@ -1,10 +1,14 @@
 // What a decoding step does to its logits before a token is taken: penalties for tokens that stand in the history, biases, masks.
 // See bpt_adjust_logits in include/bpt.h.
 //
-// Bound by memory for a large batch, by latency for a small one.  One launch, one pass over the logits: a CTA takes a piece of
-// one row's vocabulary, asks for its logits, and while they are on their way goes through the row's history and counts, in shared
-// memory, the ids that fall into its piece.  Counts are whole numbers, so the order of the atomics does not show.  The history is read
-// once per piece, from L2 after the first; a table of counts in global memory would have to be cleared, filled and read by a launch each.
+// Bound by memory for a large batch, by latency for a small one.  Few ids of a vocabulary stand in a history: one pass computes
+// allowed ? logits + bias : -inf for every element, as if there were none, and the ids that stand there or in the row's own list of biases are found,
+// once each, and written once more.  Counts are whole numbers in shared memory, so the order of the atomics does not show.
+// Two ways, by the rule at plan(): in one launch, each CTA finding the ids of its own piece of the row while its other threads pass over that
+// (one sequence, 256 ids, history of 8192: 5.5 us; 32 rows of 32000, histories of 4096: 6.6 us); or, for many pieces, a launch that lists each
+// row's ids by a hash table beside the pass, and one that writes them behind it (256 rows of 128001 in bf16 with bias and mask: the pass
+// 34 us without a history, 3.9 TB/s, where a copy of the logits takes 28; 48 us with histories of 2048, of which listing leaves
+// the pass fewer SMs at first and the last launch is the tail.  With the ids found by every piece for itself 95 us).
 //
 // Rows may start anywhere (an odd vocabulary, a slice of a larger tensor): a row's elements are taken in groups of 8 that lie on
 // 16-byte boundaries of the logits, whatever their index.

@@ -19,6 +19,7 @@
 #include <cooperative_groups.h>
 #include <cstring>
 
+#include "any8.cuh"
 #include "bpt_internal.cuh"
 
 namespace bpt {
@@ -28,6 +29,16 @@ constexpr int kEmSms = 148;
 constexpr int kEmDigit = 9;                 // bits per sort pass, at most
 constexpr int kEmBins = 1 << kEmDigit;
 constexpr int kEmSortThreads = 1024;
+
+// n / d of n < 2^31 by a multiplication: with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1 it is (floor(m n / 2^32) + n) >> s.
+struct FastDiv {
+    unsigned d, m, s;
+    explicit FastDiv(unsigned by = 1) : d(by), m(1), s(0) {
+        while ((1ull << s) < by) ++s;
+        m = (unsigned)(((1ull << 32) * ((1ull << s) - by)) / by + 1);
+    }
+    __device__ __forceinline__ unsigned div(unsigned n) const { return (__umulhi(m, n) + n) >> s; }
+};
 
 struct EmParams {
     const void* ids;
@@ -46,6 +57,7 @@ struct EmParams {
     float* part;                            // [sum_tiles][2][D]
     int sort_tile, sort_tiles, sum_tiles, warp_tile, slices, zero_rows, sorted;      // sorted: which of the lists is
     unsigned zero_ctas;
+    FastDiv by_D, by_tokens, by_out_rows;
 };
 
 __device__ __forceinline__ long long load_id(const EmParams& p, long long i) {
@@ -99,7 +111,7 @@ __device__ __forceinline__ void store_vec(T* at, const float (&x)[VEC]) {
 
 // The id of a row of out, or -1 for a row of zeros.
 __device__ __forceinline__ long long id_of_row(const EmParams& p, unsigned row) {
-    const unsigned b = row / p.out_rows, t = row - b * p.out_rows;
+    const unsigned b = p.by_out_rows.div(row), t = row - b * p.out_rows;
     if (t >= real_tokens(p, b)) return -1;
     const long long id = load_id(p, (long long)b * p.tokens + t);
     if (id >= 0 && id < p.vocab) return id;
@@ -146,16 +158,27 @@ __global__ void __launch_bounds__(256) embed_fwd_flat_kernel(EmParams p) {
     const long long total = (long long)p.rows * p.D, i0 = ((long long)blockIdx.x * 256 + threadIdx.x) * 8 - lead;
     if (i0 >= total) return;
     const long long from = i0 < 0 ? 0 : i0;
-    unsigned row = total <= 0xffffffffll ? (unsigned)from / (unsigned)p.D : (unsigned)(from / p.D);
+    unsigned row = total <= 0x7fffffffll ? p.by_D.div((unsigned)from) : (unsigned)(from / p.D);
     int c = (int)(from - (long long)row * p.D);
     const int n = (int)(min(i0 + 8, total) - from);
     long long id = id_of_row(p, row);
     TO* out = (TO*)p.out + from;
     float x[8];
     if (c + 8 <= p.D && n == 8) {
-        const TW* w = (const TW*)p.weight + id * p.D + c;
+        const TW* w = (const TW*)p.weight + (id >= 0 ? id * p.D + c : 0);
+        if (id < 0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = id >= 0 ? to_f(__ldg(w + j)) * p.scale : 0.f;
+            for (int j = 0; j < 8; ++j) x[j] = 0.f;
+        } else if (any8_inside(w, (const TW*)p.weight, p.vocab * p.D)) {
+            Any8<TW> row;
+            row.load(w);
+            row.get(x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] *= p.scale;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = to_f(__ldg(w + j)) * p.scale;
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -184,7 +207,7 @@ __global__ void __launch_bounds__(256) embed_fwd_flat_kernel(EmParams p) {
 // Place i of the list as the sort begins with it: its id, or `vocab` for a place that adds nothing (behind its sequence's length, at padding_idx,
 // out of range), and its row of d_out.
 __device__ __forceinline__ int2 place_of(const EmParams& p, unsigned i, long long id) {
-    const unsigned b = i / p.tokens, t = i - b * p.tokens;
+    const unsigned b = p.by_tokens.div(i), t = i - b * p.tokens;
     const bool real = t < real_tokens(p, b), in = id >= 0 && id < p.vocab;
     if (real && !in) *p.record = (int)BPT_ERR_INDEX;
     return make_int2(real && in && id != p.padding_idx ? (int)id : (int)p.vocab, (int)(b * p.out_rows + t));
@@ -406,30 +429,41 @@ constexpr int kEmSumWarps = 8;
 constexpr int kEmSlice = 256;           // columns per CTA, 8 per lane
 constexpr int kEmZeroBytes = 131072;    // of dW per CTA that zeroes, about
 
-// A lane's 8 columns of a row, as they lie: next to one another in whole 16-byte pieces, or 32 apart.  Column i of the lane in the slice: col(i).
+// A lane's 8 columns of a row of d_out, 8 * lane and on, as they lie: in whole 16-byte pieces, or anywhere.  Lanes behind the last column take the
+// first ones, which nobody looks at.
 template <typename T, bool VEC> struct EmRow {
     uint4 q[sizeof(T) / 2];
-    static __device__ __forceinline__ int col(int lane, int i) { return lane * 8 + i; }
-    __device__ __forceinline__ void load(const T* row, int lane, int columns) {
+    __device__ __forceinline__ void load(const T* row, int lane, int columns, const T*, long long) {
         const T* at = row + (lane * 8 < columns ? lane * 8 : 0);
 #pragma unroll
         for (int j = 0; j < (int)sizeof(T) / 2; ++j) q[j] = __ldg((const uint4*)at + j);
     }
-    __device__ __forceinline__ float get(int i) const {
+    __device__ __forceinline__ void get(float (&x)[8]) const {
         T e[8];
         memcpy(e, q, sizeof(e));
-        return to_f(e[i]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = to_f(e[i]);
     }
 };
 template <typename T> struct EmRow<T, false> {
-    T e[8];
-    static __device__ __forceinline__ int col(int lane, int i) { return i * 32 + lane; }
-    __device__ __forceinline__ void load(const T* row, int lane, int columns) {
+    Any8<T> raw;
+    __device__ __forceinline__ void load(const T* row, int lane, int columns, const T* tensor, long long n) {
+        const int c = lane * 8 < columns ? lane * 8 : 0;
+        if (any8_inside(row + c, tensor, n)) {
+            raw.load(row + c);
+        } else {                            // at the ends of the tensor
+            T e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = __ldg(row + (i * 32 + lane < columns ? i * 32 + lane : 0));
+            for (int i = 0; i < 8; ++i) e[i] = c + i < columns ? __ldg(row + c + i) : T(0.f);
+            memcpy(raw.q, e, sizeof(e));
+            raw.s = 0;
+        }
     }
-    __device__ __forceinline__ float get(int i) const { return to_f(e[i]); }
+    __device__ __forceinline__ void get(float (&x)[8]) const { raw.get(x); }
 };
+
+// A row of dW from a warp's columns, 8 to a lane.  One that starts anywhere is written in whole 16-byte pieces, too, put together from a lane's
+// own values and the last ones of the lane before; element by element at its ends.
 template <typename T, bool VEC>
 __device__ __forceinline__ void put_row(T* at, int lane, int columns, const float (&x)[8], float scale) {
     float y[8];
@@ -437,18 +471,67 @@ __device__ __forceinline__ void put_row(T* at, int lane, int columns, const floa
     for (int i = 0; i < 8; ++i) y[i] = x[i] * scale;
     if constexpr (VEC) {
         if (lane * 8 < columns) store_vec<8>(at + lane * 8, y);
+        return;
+    }
+    const int s = (int)((uintptr_t)at & 15) / (int)sizeof(T);       // column c of this lane goes to the pieces that begin at column 8 * lane - s
+    T e[8];                                                         // columns 8 * lane - s and on
+    if constexpr (sizeof(T) == 2) {
+        unsigned w[9];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __nv_bfloat162 two = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+            memcpy(&w[4 + i], &two, 4);
+            w[i] = __shfl_up_sync(~0u, w[4 + i], 1);
+        }
+        w[8] = 0;
+        const int from = 8 - s;             // of the 16 values: 1 .. 8
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = from & 2 ? w[i + 1] : w[i];
+#pragma unroll
+        for (int i = 0; i < 7; ++i) w[i] = from & 4 ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = from & 8 ? w[i + 4] : w[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = from & 1 ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+        memcpy(e, w, sizeof(e));
     } else {
+        float z[11];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[3 + i] = y[i];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) z[i] = __shfl_up_sync(~0u, y[5 + i], 1);
+        const int from = 3 - s;             // of the 11 values: 0 .. 3
+#pragma unroll
+        for (int i = 0; i < 10; ++i) z[i] = from & 1 ? z[i + 1] : z[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = from & 2 ? z[i + 2] : z[i];
+        memcpy(e, z, sizeof(e));
+    }
+    const int c = lane * 8 - s;
+    constexpr int per = 16 / sizeof(T);
+#pragma unroll
+    for (int j = 0; j < 8; j += per) {
+        if (c + j >= 0 && c + j + per <= columns) {
+            uint4 q;
+            memcpy(&q, e + j, 16);
+            *(uint4*)(at + c + j) = q;
+        } else {
+#pragma unroll
+            for (int i = j; i < j + per; ++i)
+                if (c + i >= 0 && c + i < columns) at[c + i] = e[i];
+        }
+    }
+    if (lane == 31)                         // what is left behind the last pieces
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i * 32 + lane < columns) from_f(y[i], at + i * 32 + lane);
-    }
+            if (8 - i <= s && lane * 8 + i < columns) from_f(y[i], at + lane * 8 + i);
 }
 
 // What a warp leaves of the runs at the ends of its tile: the ids, and whether the places before and behind the tile belong to them.
 struct EmEnds { int first, last; bool before, behind; };
 
 template <typename TW, typename TO, bool VEC>
-__global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : 4) embed_sum_kernel(EmParams p) {
+__global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : VEC ? 4 : 3) embed_sum_kernel(EmParams p) {
     __shared__ float part[kEmSumWarps][2][kEmSlice];        // sums of runs that go on before the warp's tile, and of those that begin in it and go on behind
     __shared__ EmEnds ends[kEmSumWarps];
     constexpr int kEmAhead = 4;             // rows of d_out on their way per warp
@@ -481,14 +564,14 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : 4) emb
                 bool open = me.before;              // the run began before the tile
                 const auto keep = [&](int slot) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) part[warp][slot][EmRow<TO, VEC>::col(lane, i)] = acc[i];
+                    for (int i = 0; i < 8; ++i) part[warp][slot][lane * 8 + i] = acc[i];
                 };
                 for (int r = 0; r < real; r += kEmAhead) {
                     EmRow<TO, VEC> x[kEmAhead];
 #pragma unroll
                     for (int j = 0; j < kEmAhead; ++j) {
                         const int row = __shfl_sync(~0u, my_src, r + j < real ? r + j : 0);
-                        x[j].load(d_out + (long long)row * p.D, lane, columns);
+                        x[j].load(d_out + (long long)row * p.D, lane, columns, (const TO*)p.d_out, (long long)p.rows * p.D);
                     }
 #pragma unroll
                     for (int j = 0; j < kEmAhead; ++j) {
@@ -502,8 +585,10 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : 4) emb
 #pragma unroll
                             for (int i = 0; i < 8; ++i) acc[i] = 0.f;
                         }
+                        float v[8];
+                        x[j].get(v);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) acc[i] += x[j].get(i);
+                        for (int i = 0; i < 8; ++i) acc[i] += v[i];
                     }
                 }
                 if (open) keep(0);
@@ -678,6 +763,7 @@ EmParams embed_params(const bpt_embed_args& a) {
     p.vocab = a.vocab; p.padding_idx = a.padding_idx;
     p.rows = (unsigned)(a.batch * a.out_rows); p.tokens = (unsigned)a.tokens; p.out_rows = (unsigned)a.out_rows;
     p.M = (unsigned)(a.batch * a.tokens);
+    p.by_D = FastDiv((unsigned)a.D); p.by_tokens = FastDiv((unsigned)std::max<long long>(1, a.tokens)); p.by_out_rows = FastDiv((unsigned)std::max<long long>(1, a.out_rows));
     p.D = a.D; p.id64 = a.id_bytes == 8; p.scale = a.scale;
     return p;
 }

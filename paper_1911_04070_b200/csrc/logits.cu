@@ -17,6 +17,7 @@
 #include <cstring>
 #include <type_traits>
 
+#include "any8.cuh"
 #include "bpt_internal.cuh"
 
 namespace bpt {
@@ -85,48 +86,6 @@ __device__ __forceinline__ long long id_at(const void* ids, int is64, long long 
 constexpr unsigned kLgPrompt = 0x80000000u;     // of an id's word: it stands in the prompt; the other bits count the places behind it
 constexpr int kLgAhead = 4;                     // ids of the history a thread asks for at once
 
-// 8 values of a bias that start anywhere: the 16-byte pieces around them, and the values out of those.
-template <typename B> struct Bias8;
-template <> struct Bias8<float> {
-    uint4 q[3];
-    int s;
-    __device__ __forceinline__ void load(const float* at) {
-        s = (int)((uintptr_t)at & 15) / 4;
-#pragma unroll
-        for (int j = 0; j < 3; ++j) q[j] = __ldg((const uint4*)(at - s) + j);
-    }
-    __device__ __forceinline__ void get(float (&z)[8]) const {
-        unsigned w[12];
-        memcpy(w, q, sizeof(w));
-#pragma unroll
-        for (int j = 0; j < 11; ++j) w[j] = s & 1 ? w[j + 1] : w[j];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(s & 2 ? w[j + 2] : w[j]);
-    }
-};
-template <> struct Bias8<__nv_bfloat16> {
-    uint4 q[2];
-    int s;
-    __device__ __forceinline__ void load(const __nv_bfloat16* at) {
-        s = (int)((uintptr_t)at & 15) / 2;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) q[j] = __ldg((const uint4*)(at - s) + j);
-    }
-    __device__ __forceinline__ void get(float (&z)[8]) const {
-        unsigned w[8];
-        memcpy(w, q, sizeof(w));
-#pragma unroll
-        for (int j = 0; j < 7; ++j) w[j] = s & 2 ? w[j + 1] : w[j];
-#pragma unroll
-        for (int j = 0; j < 5; ++j) w[j] = s & 4 ? w[j + 2] : w[j];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const unsigned two = s & 1 ? __funnelshift_r(w[j], w[j + 1], 16) : w[j];
-            z[2 * j] = __uint_as_float(two << 16);
-            z[2 * j + 1] = __uint_as_float(two & 0xffff0000u);
-        }
-    }
-};
 struct NoBias {};
 
 __device__ __forceinline__ float bias_at(const LgParams& p, long long row, int i) {
@@ -157,7 +116,7 @@ __device__ __forceinline__ void stream(const LgParams& p, long long row, const T
     const int vocab = (int)p.vocab, ib = ia + STEP;
     const bool inside = ia >= 16 && ib <= vocab - 24;
     uint4 raw[2][pieces];
-    Bias8<std::conditional_t<BIAS, B, float>> z[2];
+    Any8<std::conditional_t<BIAS, B, float>> z[2];
     unsigned lo[2], hi[2];
     if (inside) {
 #pragma unroll

@@ -166,6 +166,40 @@ def test_views_and_strides(layer):
     assert torch.equal(a, b)
 
 
+# every start of table, states and their gradients against a 16-byte boundary, widths around the ends of pieces, lanes and slices of 256
+@pytest.mark.parametrize("D", [1, 3, 6, 9, 15, 17, 250, 255, 257, 263, 511, 519])
+@pytest.mark.parametrize("wt,ot", [(BF16, BF16), (F32, BF16), (BF16, F32), (F32, F32)])
+def test_any_width_and_start(layer, D, wt, ot):
+    ids = torch.cat([_ids(90, V=13), torch.full((70,), 4, device="cuda")])
+    for first in range(0, 8, 1 if D < 20 else 3):
+        flat = torch.randn(first + 13 * D + 3, generator=torch.Generator().manual_seed(first)).to("cuda", wt)
+        w = flat[first:first + 13 * D].view(13, D).requires_grad_(True)
+        y, dw = _check(layer, ids, w, scale=2.0, spans=3, dtype=ot, seed=first)
+        buf = torch.full((y.numel() + 16,), float("nan"), device="cuda", dtype=ot)      # gradients that start anywhere, with NaN around them
+        d = buf[first:first + y.numel()].view(y.shape)
+        d.copy_(torch.randn(y.shape, generator=torch.Generator("cuda").manual_seed(first), device="cuda").to(ot))
+        d[160:] = float("nan")                                                              # and in the rows behind the tokens
+        got, = torch.autograd.grad(layer.token_states(ids, w, scale=2.0, span_rows=3, dtype=ot), [w], d)
+        d2 = d.clone()
+        d2[160:] = 0
+        want, = torch.autograd.grad(layer.token_states(ids, w, scale=2.0, span_rows=3, dtype=ot), [w], d2)
+        assert torch.equal(got, want)
+
+
+def test_what_is_beside_a_gradient_stays(layer):
+    """d_weight of the binding, at any start, in the middle of a larger buffer."""
+    from paper_1911_04070_b200 import binding
+    ids = _ids(300, V=40)
+    for D in (5, 24, 201, 259):
+        for wt in (BF16, F32):
+            d = torch.randn(300, D, device="cuda")
+            want = binding.bpt_embed_bwd(ids, d, 40, wt)
+            for first in range(9):
+                buf = torch.full((40 * D + 20,), 7.0, device="cuda", dtype=wt)
+                got = binding.bpt_embed_bwd(ids, d, 40, wt, d_weight=buf[first:first + 40 * D].view(40, D))
+                assert torch.equal(got, want) and bool((buf[:first] == 7).all()) and bool((buf[first + 40 * D:] == 7).all())
+
+
 def test_gradient_against_differences(layer):
     """The function is linear in the table: a step along any direction gives the gradient's product with it, but for roundings: at most
     (places + 2) 2^-24 <= 27 x 2^-24 of the absolute values in the gradient, 3 x 2^-24 in each value of the function."""

@@ -151,54 +151,65 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmParams p, int lanes) {
     }
 }
 
-// Any width and start: out as one list of elements, 8 of them that lie on a 16-byte boundary per thread, over the ends of rows.
+// scale * 8 elements from column c on of an id's row, which may begin before the row or end behind it; zeros without an id.
+template <typename TW>
+__device__ __forceinline__ void scaled8(const EmParams& p, long long id, int c, float (&x)[8]) {
+    if (id < 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = 0.f;
+        return;
+    }
+    const TW* w = (const TW*)p.weight + id * p.D + c;
+    if (any8_inside(w, (const TW*)p.weight, p.vocab * p.D)) {
+        Any8<TW> raw;
+        raw.load(w);
+        raw.get(x);
+    } else {                                    // at the ends of the table
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {
+            const long long at = id * p.D + c + j;
+            const float v = at >= 0 && at < p.vocab * p.D ? to_f(__ldg(w + j)) : 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = k == j ? v : x[k];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= p.scale;
+}
+// Any width from 8 on and any start: out as one list of elements, 8 of them that lie on a 16-byte boundary per thread, out of one row or the ends of two.
 template <typename TW, typename TO>
 __global__ void __launch_bounds__(256) embed_fwd_flat_kernel(EmParams p) {
     const int lead = (int)(((uintptr_t)p.out & 15) / sizeof(TO));
     const long long total = (long long)p.rows * p.D, i0 = ((long long)blockIdx.x * 256 + threadIdx.x) * 8 - lead;
     if (i0 >= total) return;
     const long long from = i0 < 0 ? 0 : i0;
-    unsigned row = total <= 0x7fffffffll ? p.by_D.div((unsigned)from) : (unsigned)(from / p.D);
-    int c = (int)(from - (long long)row * p.D);
-    const int n = (int)(min(i0 + 8, total) - from);
-    long long id = id_of_row(p, row);
-    TO* out = (TO*)p.out + from;
+    const unsigned row = total <= 0x7fffffffll ? p.by_D.div((unsigned)from) : (unsigned)(from / p.D);
+    const int c = (int)(from - (long long)row * p.D), n = (int)(min(i0 + 8, total) - from), left = p.D - c;
     float x[8];
-    if (c + 8 <= p.D && n == 8) {
-        const TW* w = (const TW*)p.weight + (id >= 0 ? id * p.D + c : 0);
-        if (id < 0) {
+    scaled8<TW>(p, id_of_row(p, row), c, x);
+    if (left < n) {
+        float y[8];
+        scaled8<TW>(p, id_of_row(p, row + 1), -left, y);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = 0.f;
-        } else if (any8_inside(w, (const TW*)p.weight, p.vocab * p.D)) {
-            Any8<TW> row;
-            row.load(w);
-            row.get(x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] *= p.scale;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = to_f(__ldg(w + j)) * p.scale;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            x[j] = 0.f;
-            if (j >= n) continue;
-            if (c == p.D) {
-                c = 0;
-                id = id_of_row(p, ++row);
-            }
-            if (id >= 0) x[j] = to_f(__ldg((const TW*)p.weight + id * p.D + c)) * p.scale;
-            ++c;
-        }
+        for (int j = 0; j < 8; ++j) x[j] = j < left ? x[j] : y[j];
     }
-    if (n == 8 && i0 >= 0) {
+    TO* out = (TO*)p.out + from;
+    if (n == 8) {                       // then i0 >= 0, and a whole piece or two of out
         store_vec<8>(out, x);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n) from_f(x[j], out + j);
     }
+}
+// Narrower than that: an element per thread.
+template <typename TW, typename TO>
+__global__ void __launch_bounds__(256) embed_fwd_narrow_kernel(EmParams p) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (long long)p.rows * p.D) return;
+    const unsigned row = (unsigned)(i / p.D);
+    const long long id = id_of_row(p, row);
+    from_f(id >= 0 ? to_f(__ldg((const TW*)p.weight + id * p.D + (i - (long long)row * p.D))) * p.scale : 0.f, (TO*)p.out + i);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -433,7 +444,7 @@ constexpr int kEmZeroBytes = 131072;    // of dW per CTA that zeroes, about
 // first ones, which nobody looks at.
 template <typename T, bool VEC> struct EmRow {
     uint4 q[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* row, int lane, int columns, const T*, long long) {
+    __device__ __forceinline__ void load(const T* row, int lane, int columns, bool) {
         const T* at = row + (lane * 8 < columns ? lane * 8 : 0);
 #pragma unroll
         for (int j = 0; j < (int)sizeof(T) / 2; ++j) q[j] = __ldg((const uint4*)at + j);
@@ -447,11 +458,12 @@ template <typename T, bool VEC> struct EmRow {
 };
 template <typename T> struct EmRow<T, false> {
     Any8<T> raw;
-    __device__ __forceinline__ void load(const T* row, int lane, int columns, const T* tensor, long long n) {
+    // inner: whatever lies around a row's elements belongs to the tensor
+    __device__ __forceinline__ void load(const T* row, int lane, int columns, bool inner) {
         const int c = lane * 8 < columns ? lane * 8 : 0;
-        if (any8_inside(row + c, tensor, n)) {
+        if (inner) {
             raw.load(row + c);
-        } else {                            // at the ends of the tensor
+        } else {
             T e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) e[i] = c + i < columns ? __ldg(row + c + i) : T(0.f);
@@ -547,6 +559,7 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : VEC ? 
         const int tile = (int)(work / (unsigned)p.slices), c0 = (int)(work - (unsigned)tile * p.slices) * kEmSlice, columns = min(kEmSlice, p.D - c0);
         const TO* d_out = (const TO*)p.d_out + c0;
         TW* dw = (TW*)p.out + c0;
+        const bool wide = p.D >= 16;            // a row before and one behind hold the pieces around a row's ends
         const int a = (tile * kEmSumWarps + warp) * p.warp_tile, n = min(p.warp_tile, M - a);
         EmEnds me{vocab, vocab, false, false};
         if (n > 0) {
@@ -571,7 +584,7 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : VEC ? 
 #pragma unroll
                     for (int j = 0; j < kEmAhead; ++j) {
                         const int row = __shfl_sync(~0u, my_src, r + j < real ? r + j : 0);
-                        x[j].load(d_out + (long long)row * p.D, lane, columns, (const TO*)p.d_out, (long long)p.rows * p.D);
+                        x[j].load(d_out + (long long)row * p.D, lane, columns, wide && row > 0 && row + 1 < (int)p.rows);
                     }
 #pragma unroll
                     for (int j = 0; j < kEmAhead; ++j) {
@@ -854,11 +867,13 @@ extern "C" bpt_status bpt_embed_fwd(const bpt_embed_args* a, void* out, void* cu
     while (lanes < a->D / 8 && lanes < 32) lanes *= 2;
     const int rows_per_cta = 256 / lanes * kEmRows;
     const unsigned grid = vec ? (unsigned)(((unsigned long long)p.rows + rows_per_cta - 1) / rows_per_cta)
-                              : (unsigned)(((unsigned long long)p.rows * p.D + 7 + 8 * 256 - 1) / (8 * 256));        // wherever out starts
+                         : a->D >= 8 ? (unsigned)(((unsigned long long)p.rows * p.D + 7 + 8 * 256 - 1) / (8 * 256))        // wherever out starts
+                                     : (unsigned)(((unsigned long long)p.rows * p.D + 255) / 256);
     typedef __nv_bfloat16 bf;
     const bool wf = a->weight_dtype == BPT_F32, of = a->out_dtype == BPT_F32;
 #define BPT_EMBED_FWD(TW, TO) (vec ? start(embed_fwd_kernel<TW, TO>, dim3(grid), 256, st, true, p, lanes) \
-                                   : start(embed_fwd_flat_kernel<TW, TO>, dim3(grid), 256, st, true, p))
+                         : a->D >= 8 ? start(embed_fwd_flat_kernel<TW, TO>, dim3(grid), 256, st, true, p) \
+                                     : start(embed_fwd_narrow_kernel<TW, TO>, dim3(grid), 256, st, true, p))
     const bool ok = wf ? (of ? BPT_EMBED_FWD(float, float) : BPT_EMBED_FWD(float, bf)) : (of ? BPT_EMBED_FWD(bf, float) : BPT_EMBED_FWD(bf, bf));
 #undef BPT_EMBED_FWD
     trace_mark(st, "embed_fwd");

@@ -10,8 +10,8 @@
 // lies inside the tile straight to dW; the ends of runs that cross warps are joined in shared memory, of those that cross CTAs in
 // embed_finish, both in the order of the list.  Rows of ids that occur nowhere are zeroed by CTAs of their own between those that sum, so
 // every row of dW is written once.  All sums have one order: bit-reproducible.
-// B200, forward + backward on the GPU: 4 x 8192 ids of 256, 512 wide, 43 us (forward 16, sort 10, sums and zeros about 10, finish about 6);
-// 16 x 512 ids of 32001 x 201 in fp32 40 us (forward 8, sort 10); 8 x 8192 ids of 131072 x 2048 242 us (forward 68, sort 22, sums and zeros of
+// B200, forward + backward on the GPU: 4 x 8192 ids of 256, 512 wide, 42 us (forward 16, sort 9.5, sums and zeros about 10, finish about 6);
+// 16 x 512 ids of 32001 x 201 in fp32 37 us (forward 8, sort 9.5); 8 x 8192 ids of 131072 x 2048 239 us (forward 68, sort 22, sums and zeros of
 // 268 MB read and 537 MB written about 135).  What it took: sorting by two launches a pass and tiles per warp only 57 / 45 / 300; zeroing all of dW beside
 // the sort 289 for the last (a kernel that only writes is the slower way); CTAs that zero 32 KB instead of 128 KB 290.
 #include <algorithm>
@@ -33,7 +33,7 @@ constexpr int kEmSortThreads = 1024;
 // n / d of n < 2^31 by a multiplication: with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1 it is (floor(m n / 2^32) + n) >> s.
 struct FastDiv {
     unsigned d, m, s;
-    explicit FastDiv(unsigned by = 1) : d(by), m(1), s(0) {
+    FastDiv(unsigned by = 1) : d(by), m(1), s(0) {
         while ((1ull << s) < by) ++s;
         m = (unsigned)(((1ull << 32) * ((1ull << s) - by)) / by + 1);
     }
@@ -911,7 +911,10 @@ extern "C" bpt_status bpt_embed_bwd(const bpt_embed_args* a, const void* d_out, 
     p.sort_tile = q.sort_tile; p.sort_tiles = q.sort_tiles; p.sum_tiles = q.sum_tiles; p.warp_tile = q.warp_tile;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (M > 0 && q.ctas) {
-        if (q.ctas > 8 && cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return BPT_ERR_CUDA;
+        if (q.ctas > 8 && cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+            cudaGetLastError();     // reported by this status, not by the next call of somebody else
+            return BPT_ERR_CUDA;
+        }
         cudaLaunchAttribute attr[1] = {};
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim = {(unsigned)q.ctas, 1, 1};

@@ -438,8 +438,10 @@ bool start(K kernel, unsigned grid, int threads, size_t smem, bool dependent, cu
 template <typename TL, typename TO, int STREAM, int SPARSE>
 bool run(const LgParams& p, long long rows, size_t smem, bool dependent, cudaStream_t st) {
     if (smem > 40 * 1024 &&     // with the static part, 48 KB is the limit without asking
-        cudaFuncSetAttribute(adjust_logits_kernel<TL, TO, STREAM, SPARSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLgPieceToo * 10) != cudaSuccess)
+        cudaFuncSetAttribute(adjust_logits_kernel<TL, TO, STREAM, SPARSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLgPieceToo * 10) != cudaSuccess) {
+        cudaGetLastError();     // reported by this status, not by the next call of somebody else
         return false;
+    }
     const bool ok = start(adjust_logits_kernel<TL, TO, STREAM, SPARSE>, (unsigned)(rows * p.pieces), STREAM + SPARSE, smem, dependent, st, p);
     trace_mark(st, "adjust_logits");
     return ok;
@@ -448,8 +450,10 @@ template <typename TL>
 bool run_list(const LgParams& p, long long rows, int slots, cudaStream_t st) {
     const size_t smem = (size_t)slots * (p.bias_count ? 12 : 8);
     if (smem > 40 * 1024 &&
-        cudaFuncSetAttribute(list_ids_kernel<TL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLgSlots * 12) != cudaSuccess)
+        cudaFuncSetAttribute(list_ids_kernel<TL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLgSlots * 12) != cudaSuccess) {
+        cudaGetLastError();
         return false;
+    }
     list_ids_kernel<TL><<<(unsigned)rows, kLgHashThreads, smem, st>>>(p, slots);
     const bool ok = cudaGetLastError() == cudaSuccess;
     trace_mark(st, "list_ids");

@@ -1,7 +1,8 @@
 """BP-Transformer layers on top of the graph self-attention library (arXiv 1911.04070, Sec. 3.3,
 Algorithm 2): PyTorch modules whose attention runs in libbpt.so.
 
-The graph self-attention, the gated feed-forward block and the seam between two blocks (norms, gate, residual) are this
+The graph self-attention, the gated feed-forward block, the seam between two blocks (norms, gate, residual), and at the ends of a
+language model the way from ids to node states, the clipping of gradients and the adjustment of logits are this
 package's own operators; the projections, and in the paper's form of the layer the feed-forward block and the norms, are plain
 PyTorch operators around them, so that each can be dropped into a model and trained.  Nothing here falls back to another
 implementation of an operator: a gated block in float32 is written out in PyTorch operators.
@@ -211,7 +212,7 @@ def clip_gradients(grads, max_norm, norm_type=2.0, eps=1e-6, out=None):
 
 def adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None,
                   bias_ids=None, bias_values=None, allowed=None, out=None):
-    """What a decoding step does to its logits [B, V] before a token is taken, in one kernel.  For an id that stands in history[b, :lengths[b]]:
+    """What a decoding step does to its logits [B, V] before a token is taken.  For an id that stands in history[b, :lengths[b]]:
     x / repetition where x > 0, else x * repetition; for one that stands n > 0 times behind the prompt, in history[b, prompt_lengths[b]:lengths[b]]:
     x - frequency * n - presence; then x + bias, and -inf for what is not allowed (NaN there, too; a row without an allowed id is all -inf).
 
@@ -219,7 +220,7 @@ def adjust_logits(logits, history=None, lengths=None, prompt_lengths=None, repet
     vocabulary count for nothing.  repetition (above 0), presence, frequency: numbers, or float32 tensors [B], one setting per row.
     bias: [V] or [B, V], float32 or bfloat16.  bias_ids (int32 or int64), bias_values (float32): [B, K], a few biased ids per row (outside the
     vocabulary: no effect; given twice: the last one counts).  allowed: int32 [ceil(V / 32)] or [B, ceil(V / 32)], bit v % 32 of word v // 32 set
-    where id v is allowed.  out: a tensor [B, V], float32 or bfloat16, the logits themselves for one (default: a new one of the logits'
+    where id v is allowed.  out: a tensor [B, V], float32 or bfloat16, its rows without gaps, the logits themselves for one (default: a new one of the logits'
     type), apart from all other arguments.  Any strides.  Computed in float32, rounded once.  For inference: arguments that require a gradient are refused."""
     got = binding.load_native().adjust_logits(logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias, bias_ids, bias_values,
                                               allowed, out)

@@ -74,38 +74,30 @@ __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float
 __device__ __forceinline__ void from_f(float x, float* y) { *y = x; }
 __device__ __forceinline__ void from_f(float x, __nv_bfloat16* y) { *y = __float2bfloat16(x); }
 
-// VEC elements in fp32, in pieces of at most 16 bytes
-template <int VEC, typename T>
-__device__ __forceinline__ void load_vec(const T* at, float (&x)[VEC]) {
-    if constexpr (VEC == 1) {
-        x[0] = to_f(__ldg(at));
-    } else {
-        constexpr int per = 16 / sizeof(T);
+// 8 elements in fp32, in whole 16-byte pieces
+template <typename T>
+__device__ __forceinline__ void load8(const T* at, float (&x)[8]) {
+    constexpr int per = 16 / sizeof(T);
 #pragma unroll
-        for (int j = 0; j < VEC / per; ++j) {
-            const uint4 q = __ldg((const uint4*)at + j);
-            T e[per];
-            memcpy(e, &q, 16);
+    for (int j = 0; j < 8 / per; ++j) {
+        const uint4 q = __ldg((const uint4*)at + j);
+        T e[per];
+        memcpy(e, &q, 16);
 #pragma unroll
-            for (int i = 0; i < per; ++i) x[j * per + i] = to_f(e[i]);
-        }
+        for (int i = 0; i < per; ++i) x[j * per + i] = to_f(e[i]);
     }
 }
-template <int VEC, typename T>
-__device__ __forceinline__ void store_vec(T* at, const float (&x)[VEC]) {
-    if constexpr (VEC == 1) {
-        from_f(x[0], at);
-    } else {
-        constexpr int per = 16 / sizeof(T);
+template <typename T>
+__device__ __forceinline__ void store8(T* at, const float (&x)[8]) {
+    constexpr int per = 16 / sizeof(T);
 #pragma unroll
-        for (int j = 0; j < VEC / per; ++j) {
-            T e[per];
+    for (int j = 0; j < 8 / per; ++j) {
+        T e[per];
 #pragma unroll
-            for (int i = 0; i < per; ++i) from_f(x[j * per + i], e + i);
-            uint4 q;
-            memcpy(&q, e, 16);
-            *((uint4*)at + j) = q;
-        }
+        for (int i = 0; i < per; ++i) from_f(x[j * per + i], e + i);
+        uint4 q;
+        memcpy(&q, e, 16);
+        *((uint4*)at + j) = q;
     }
 }
 
@@ -135,7 +127,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmParams p, int lanes) {
 #pragma unroll
         for (int r = 0; r < kEmRows; ++r) {
             if (id[r] >= 0) {
-                load_vec<8>((const TW*)p.weight + id[r] * p.D + c, x[r]);
+                load8((const TW*)p.weight + id[r] * p.D + c, x[r]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[r][i] = 0.f;
@@ -146,7 +138,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmParams p, int lanes) {
             if (first + r >= p.rows) break;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[r][i] = id[r] >= 0 ? x[r][i] * p.scale : 0.f;
-            store_vec<8>((TO*)p.out + (long long)(first + r) * p.D + c, x[r]);
+            store8((TO*)p.out + (long long)(first + r) * p.D + c, x[r]);
         }
     }
 }
@@ -195,7 +187,7 @@ __global__ void __launch_bounds__(256) embed_fwd_flat_kernel(EmParams p) {
     }
     TO* out = (TO*)p.out + from;
     if (n == 8) {                       // then i0 >= 0, and a whole piece or two of out
-        store_vec<8>(out, x);
+        store8(out, x);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -317,8 +309,7 @@ __global__ void __launch_bounds__(kEmSortThreads) embed_scatter_kernel(EmParams 
         if (on && rank == 0) in_warp[warp][d] = (unsigned short)__popc(peers);
         __syncthreads();
         if (tid < bins) {                           // counts of the warps to places
-            int off = base[tid];
-            int next = off;
+            int next = base[tid];
 #pragma unroll
             for (int w = 0; w < 32; ++w) next += in_warp[w][tid];
             total[tid] = next;
@@ -482,7 +473,7 @@ __device__ __forceinline__ void put_row(T* at, int lane, int columns, const floa
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = x[i] * scale;
     if constexpr (VEC) {
-        if (lane * 8 < columns) store_vec<8>(at + lane * 8, y);
+        if (lane * 8 < columns) store8(at + lane * 8, y);
         return;
     }
     const int s = (int)((uintptr_t)at & 15) / (int)sizeof(T);       // column c of this lane goes to the pieces that begin at column 8 * lane - s

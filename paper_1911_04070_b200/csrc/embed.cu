@@ -15,6 +15,7 @@
 // 268 MB read and 537 MB written about 135).  What it took: sorting by two launches a pass and tiles per warp only 57 / 45 / 300; zeroing all of dW beside
 // the sort 289 for the last (a kernel that only writes is the slower way); CTAs that zero 32 KB instead of 128 KB 290.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cooperative_groups.h>
 #include <cstring>
@@ -327,11 +328,11 @@ __global__ void __launch_bounds__(kEmSortThreads) embed_scatter_kernel(EmParams 
     }
 }
 
-// The whole sort of up to kEmClusterMost places in one launch: one cluster, a slice of the list per CTA, in registers.  A warp counts the digits
+// The whole sort of up to 131072 places (16 CTAs of 512 threads, 16 places each) in one launch: one cluster, a slice of the list per CTA, in registers.  A warp counts the digits
 // of its own part of the slice, 32 places at a time; counts are added up over the warps, and over the cluster through distributed
 // shared memory.  Between two passes the list goes through global memory (L2): scattered 8-byte stores to the other CTAs' shared memory
 // took three times as long.
-constexpr int kEmClusterThreads = 512, kEmRounds = 16, kEmClusterCtas = 16, kEmClusterMost = kEmClusterCtas * kEmRounds * kEmClusterThreads;
+constexpr int kEmClusterThreads = 512, kEmRounds = 16, kEmClusterCtas = 16;
 __global__ void __launch_bounds__(kEmClusterThreads) embed_sort_kernel(EmParams p, int passes, int digit, int rounds) {
     namespace cg = cooperative_groups;
     constexpr int warps = kEmClusterThreads / 32;
@@ -775,6 +776,28 @@ bool on_16(const void* q) { return ((uintptr_t)q & 15) == 0; }
 bool on_element(const void* q, int bytes) { return ((uintptr_t)q & (bytes - 1)) == 0; }
 int bytes_of(bpt_dtype t) { return t == BPT_F32 ? 4 : 2; }
 
+// Whether the current device can run a cluster of 16 CTAs of the sort (8 always fit): asked once per device.
+bool wide_clusters() {
+    static std::atomic<int> known[64];      // by device ordinal: 0 not asked yet, 1 no, 2 yes
+    int device;
+    if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return true; }     // a size query without a device
+    if (device < 64 && known[device].load(std::memory_order_acquire)) return known[device].load(std::memory_order_acquire) == 2;
+    cudaLaunchAttribute attr[1] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)kEmClusterCtas, 1, 1};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)kEmClusterCtas);
+    cfg.blockDim = dim3(kEmClusterThreads);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    const bool yes = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                     cudaOccupancyMaxActiveClusters(&n, embed_sort_kernel, &cfg) == cudaSuccess && n > 0;
+    if (!yes) cudaGetLastError();
+    if (device < 64) known[device].store(yes ? 2 : 1, std::memory_order_release);
+    return yes;
+}
+
 struct EmPlan {
     int passes, digit, sort_tile, sort_tiles, sum_tiles, warp_tile;
     int ctas, rounds;            // of the sort in one launch; 0: it takes a launch or two a pass
@@ -795,9 +818,10 @@ EmPlan embed_plan(const bpt_embed_args& a) {
     q.warp_tile = 32;
     while (q.warp_tile > 8 && M * slices < kEmSms * kEmSumWarps * q.warp_tile) q.warp_tile /= 2;
     q.sum_tiles = (int)((M + kEmSumWarps * q.warp_tile - 1) / (kEmSumWarps * q.warp_tile));
-    if (M > 0 && M <= kEmClusterMost) {
+    const int most_ctas = M > 8 * kEmClusterThreads && wide_clusters() ? kEmClusterCtas : 8;
+    if (M > 0 && M <= most_ctas * kEmRounds * kEmClusterThreads) {
         q.ctas = 1;
-        while (q.ctas < kEmClusterCtas && q.ctas * kEmClusterThreads < M) q.ctas *= 2;
+        while (q.ctas < most_ctas && q.ctas * kEmClusterThreads < M) q.ctas *= 2;
         q.rounds = (int)((M + q.ctas * kEmClusterThreads - 1) / (q.ctas * kEmClusterThreads));
     }
     q.hist = q.ctas ? 0 : (size_t)q.sort_tiles * kEmBins * 4;
@@ -902,10 +926,6 @@ extern "C" bpt_status bpt_embed_bwd(const bpt_embed_args* a, const void* d_out, 
     p.sort_tile = q.sort_tile; p.sort_tiles = q.sort_tiles; p.sum_tiles = q.sum_tiles; p.warp_tile = q.warp_tile;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (M > 0 && q.ctas) {
-        if (q.ctas > 8 && cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-            cudaGetLastError();     // reported by this status, not by the next call of somebody else
-            return BPT_ERR_CUDA;
-        }
         cudaLaunchAttribute attr[1] = {};
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim = {(unsigned)q.ctas, 1, 1};

@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(kEmClusterThreads) embed_sort_kernel(EmParams 
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kEmSumWarps = 8;
 constexpr int kEmSlice = 256;           // columns per CTA, 8 per lane
-constexpr int kEmZeroBytes = 131072;    // of dW per CTA that zeroes, about
+constexpr int kEmZeroBytes = 131072, kEmZeroLeast = 4096;       // of dW per CTA that zeroes, about: at most, at least
 
 // A lane's 8 columns of a row of d_out, 8 * lane and on, as they lie: in whole 16-byte pieces, or anywhere.  Lanes behind the last column take the
 // first ones, which nobody looks at.
@@ -693,9 +693,14 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : VEC ? 
         c = i - row * p.D;
     }
     while (i < total) {
-        if (i + per <= total && c + per <= p.D) {
-            if (!there[row]) *(uint4*)(from + i) = make_uint4(0, 0, 0, 0);
-        } else {
+        bool none = !there[row], all = !none;           // the rows that the piece lies in: none or all of them have a token
+        for (int kr = row + 1, kc = c + per - p.D; kc > 0 && kr < rows; ++kr, kc -= p.D) {
+            none = none && !there[kr];
+            all = all && there[kr];
+        }
+        if (none && i + per <= total) {
+            *(uint4*)(from + i) = make_uint4(0, 0, 0, 0);
+        } else if (!all) {
             for (int k = i, kr = row, kc = c; k < i + per && k < total; ++k, ++kc) {
                 while (kc >= p.D) { kc -= p.D; ++kr; }
                 if (!there[kr]) from_f(0.f, from + k);
@@ -850,7 +855,8 @@ template <typename TW, typename TO, bool VEC>
 bool run_sum(EmParams p, cudaStream_t st) {
     p.slices = (p.D + kEmSlice - 1) / kEmSlice;
     // rows per CTA that zeroes: enough to write, and few enough that their marks fit where the sums would be
-    p.zero_rows = (int)std::min<long long>(4096, std::max<long long>(1, kEmZeroBytes / (int)sizeof(TW) / p.D));
+    const long long row = (long long)sizeof(TW) * p.D, share = p.vocab * row / (2 * kEmSms);
+    p.zero_rows = (int)std::min<long long>(4096, std::max<long long>(1, std::min<long long>(kEmZeroBytes, std::max<long long>(kEmZeroLeast, share)) / row));
     p.zero_ctas = (unsigned)((p.vocab + p.zero_rows - 1) / p.zero_rows);
     if (!start(embed_sum_kernel<TW, TO, VEC>, dim3((unsigned)(p.sum_tiles * p.slices) + p.zero_ctas), kEmSumWarps * 32, st, p.sum_tiles == 0, p)) return false;
     trace_mark(st, "embed_sum");

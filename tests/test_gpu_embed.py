@@ -186,6 +186,14 @@ def test_any_width_and_start(layer, D, wt, ot):
         assert torch.equal(got, want)
 
 
+# rows without a token and rows with one in one 16-byte piece, of two rows or of many; in runs, alone and all over
+@pytest.mark.parametrize("D", [1, 2, 3, 4, 5, 7, 9, 11, 20, 31])
+@pytest.mark.parametrize("wt", [BF16, F32])
+def test_rows_without_a_token_between_rows_with_one(layer, D, wt):
+    for V, ids in ((5000, [7, 9, 10, 4999, 0, 2500]), (777, list(range(0, 777, 2))), (777, list(range(777))), (64, [63]), (4097, list(range(100, 200)) + list(range(4000, 4097)))):
+        _check(layer, torch.tensor(ids, device="cuda"), _table(V, D, wt))
+
+
 def test_what_is_beside_a_gradient_stays(layer):
     """d_weight of the binding, at any start, in the middle of a larger buffer."""
     from paper_1911_04070_b200 import binding

@@ -11,9 +11,10 @@
 // embed_finish, both in the order of the list.  Rows of ids that occur nowhere are zeroed by CTAs of their own between those that sum, so
 // every row of dW is written once.  All sums have one order: bit-reproducible.
 // B200, forward + backward on the GPU: 4 x 8192 ids of 256, 512 wide, 42 us (forward 16, sort 9.5, sums and zeros about 10, finish about 6);
-// 16 x 512 ids of 32001 x 201 in fp32 37 us (forward 8, sort 9.5); 8 x 8192 ids of 131072 x 2048 239 us (forward 68, sort 22, sums and zeros of
+// 16 x 512 ids of 32001 x 201 in fp32 31 us (forward 8, sort 9.5); 8 x 8192 ids of 131072 x 2048 240 us (forward 68, sort 22, sums and zeros of
 // 268 MB read and 537 MB written about 135).  What it took: sorting by two launches a pass and tiles per warp only 57 / 45 / 300; zeroing all of dW beside
-// the sort 289 for the last (a kernel that only writes is the slower way); CTAs that zero 32 KB instead of 128 KB 290.
+// the sort 289 for the last (a kernel that only writes is the slower way); CTAs that zero 32 KB instead of 128 KB there 290, and 128 KB
+// instead of a share of the table's size 37 instead of 31 for the second.
 #include <algorithm>
 #include <atomic>
 #include <cmath>

@@ -222,13 +222,8 @@ def _own_embed(s):
 
 def _own_clip(s):
     from paper_1911_04070_b200 import layer
-    into, flat = (s["into"], s["flat_into"]) if s["into"] is not None else (None, s["flat"])
-    if into is None and s["most"] < 1e6:        # cut in place, the next pass would start from other gradients than the plain form's does
-        if "kept" not in s:
-            s["kept"] = _in_one_buffer([v.shape for v in s["grads"]], [_name(v) for v in s["grads"]])
-        into, flat = s["kept"]
-    norm = layer.clip_gradients(s["grads"], s["most"], norm_type=float(s["norm"]), out=into)
-    return {"norm": norm, "grads": flat}
+    norm = layer.clip_gradients(s["grads"], s["most"], norm_type=float(s["norm"]), out=s["into"])
+    return {"norm": norm, "grads": s["flat"] if s["into"] is None else s["flat_into"]}
 
 
 def _own_logits(s):

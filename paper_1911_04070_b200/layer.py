@@ -459,9 +459,11 @@ class BPTLanguageModel(nn.Module):
         return self.logits(self.encoder.forward_nodes(h, lengths))
 
     def loss(self, ids, lengths=None):
-        """The mean cross entropy, in float32, of each token given those before it."""
+        """The mean cross entropy, in float32, of each token given those before it.  An id outside the vocabulary is no target; token_states
+        reports it."""
         x = self(ids, lengths)[:, :-1].float()
         want = ids[:, 1:].long()
+        want = want.masked_fill((want < 0) | (want >= self.vocab), -100)        # cross_entropy would end the process's use of the device
         if lengths is not None:
             want = want.masked_fill(torch.arange(1, ids.shape[1], device=ids.device) >= lengths[:, None], -100)
         return torch.nn.functional.cross_entropy(x.reshape(-1, self.vocab), want.reshape(-1), ignore_index=-100)

@@ -1,0 +1,31 @@
+"""BPTLanguageModel on the GPU with the inputs at the edge of what its calls define."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _model(vocab=37, n=32, k=3, seed=3, **form):
+    from paper_1911_04070_b200 import layer
+    torch.manual_seed(seed)
+    return layer.BPTLanguageModel(vocab, n, k, 64, 2, 96, 2, device="cuda:0", **form).to("cuda:0")
+
+
+@pytest.mark.parametrize("bad", [37, -1, -100, 2 ** 40])
+def test_an_id_outside_the_table_in_a_training_step(bad):
+    """Reported, not a target, and the parameters' gradients are those of a loss without it."""
+    from paper_1911_04070_b200 import binding, layer
+    m = _model()
+    opt = torch.optim.SGD(m.parameters(), lr=0.0)
+    ids = torch.randint(0, 37, (3, 32), generator=torch.Generator().manual_seed(1)).to("cuda:0")
+    ids[1, 5] = bad
+    binding.bpt_check_device()
+    loss, norm = layer.training_step(m, opt, ids, max_norm=1e9)
+    assert binding.bpt_check_device() == 8 and binding.bpt_check_device() == 0
+    assert bool(torch.isfinite(loss)) and bool(torch.isfinite(norm)) and all(bool(torch.isfinite(p.grad).all()) for p in m.parameters())
+    p = m(ids)[:, :-1].detach().double().log_softmax(-1)
+    on = torch.ones(3, 31, dtype=torch.bool, device="cuda:0")
+    on[1, 4] = False
+    want = -p[on].gather(1, ids[:, 1:][on][:, None]).mean()
+    # as on the host: at most 7 + 37 + 93 roundings of values up to the largest one
+    assert abs(float(loss) - float(want)) <= 150 * 2.0 ** -24 * float(p.abs().max())

@@ -469,21 +469,27 @@ class BPTLanguageModel(nn.Module):
         return torch.nn.functional.cross_entropy(x.reshape(-1, self.vocab), want.reshape(-1), ignore_index=-100)
 
     @torch.no_grad()
-    def generate(self, prompt, steps: int, temperature: float = 0.0, generator=None, allowed=None, **settings):
+    def generate(self, prompt, steps: int, temperature: float = 0.0, generator=None, allowed=None, end_id=None, **settings):
         """Continues the prompts [B, P] (P >= 1 ids each, int32 or int64) by `steps` ids, token by token with cached states (BPTDecoder).
 
         allowed: the ids that may follow, as adjust_logits takes them, or a function of the ids so far [B, t] that returns them (a grammar).
         settings: repetition, presence, frequency, bias, bias_ids, bias_values, see adjust_logits; the prompt counts for repetition only.
         temperature 0 takes the largest logit (the lowest id of equal ones), another one draws from softmax(logits / temperature) with
-        torch's `generator`.  Returns [B, P + steps] ids."""
+        torch's `generator`.  A sequence has ended at the first step at which its mask or bias leaves it no id (logits of -inf only): it takes
+        end_id there and at all steps behind; without an end_id it raises ValueError when the steps are through.  Returns [B, P + steps] ids."""
         B, P = prompt.shape
         if P < 1 or steps < 0 or P + steps > self.encoder.n:
             raise ValueError("a prompt of at least one id and room for it and the steps in %d ids are needed" % self.encoder.n)
         if temperature < 0:
             raise ValueError("temperature must not be negative")
+        if end_id is not None and not 0 <= end_id < self.vocab:
+            raise ValueError("end_id must be None or an id of the vocabulary")
         ids = torch.cat([prompt, prompt.new_zeros(B, steps)], dim=1)
         lengths, prompts = (torch.full((B,), P, dtype=torch.int32, device=ids.device) for _ in range(2))
         dec = BPTDecoder(self.encoder, B, dtype=self.embedding.dtype)
+        ended = None        # [B]; nothing ends where nothing is forbidden
+        if allowed is not None or settings.get("bias") is not None or settings.get("bias_values") is not None:
+            ended = torch.zeros(B, dtype=torch.bool, device=ids.device)
         for t in range(P + steps - 1):
             state = dec.step(token_states(ids[:, t], self.embedding, self.scale))
             if t < P - 1:
@@ -492,7 +498,13 @@ class BPTLanguageModel(nn.Module):
             x = self.logits(state).float()
             adjust_logits(x, ids, lengths, prompts, allowed=allowed(ids[:, :t + 1]) if callable(allowed) else allowed, out=x, **settings)
             lengths += 1
-            ids[:, t + 1] = x.argmax(-1) if temperature == 0 else torch.multinomial(torch.softmax(x / temperature, -1), 1, generator=generator)[:, 0]
+            if ended is not None:
+                ended |= x.amax(-1) == -math.inf
+                x.masked_fill_(ended[:, None], 0.0)         # there is a softmax, for a draw that nobody looks at
+            new = x.argmax(-1) if temperature == 0 else torch.multinomial(torch.softmax(x / temperature, -1), 1, generator=generator)[:, 0]
+            ids[:, t + 1] = new if ended is None else new.masked_fill(ended, end_id or 0)
+        if ended is not None and end_id is None and bool(ended.any()):
+            raise ValueError("a sequence was left without an allowed id; an end_id is what such a sequence takes from there on")
         return ids
 
 

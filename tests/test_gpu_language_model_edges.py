@@ -29,3 +29,27 @@ def test_an_id_outside_the_table_in_a_training_step(bad):
     want = -p[on].gather(1, ids[:, 1:][on][:, None]).mean()
     # as on the host: at most 7 + 37 + 93 roundings of values up to the largest one
     assert abs(float(loss) - float(want)) <= 150 * 2.0 ** -24 * float(p.abs().max())
+
+
+@pytest.mark.parametrize("temperature", [0.0, 1.5])
+@torch.no_grad()
+def test_a_sequence_that_its_grammar_ends(temperature):
+    """Sequence 1 has nothing allowed at its third id, sequence 0 and 2 go on as if it were not there."""
+    m = _model()
+    prompt = torch.randint(0, 37, (3, 4), generator=torch.Generator().manual_seed(2)).to("cuda:0")
+    always = torch.tensor([0x7ffffffe, 0], dtype=torch.int32, device="cuda:0")
+
+    def grammar(ids):
+        w = always.repeat(3, 1)
+        if ids.shape[1] == 6:
+            w[1] = 0
+        return w
+
+    call = lambda **kw: m.generate(prompt, 10, temperature, torch.Generator("cuda:0").manual_seed(5), repetition=1.1, **kw)
+    got, free = call(allowed=grammar, end_id=36), call(allowed=always)
+    assert torch.equal(got[::2], free[::2]) and torch.equal(got[1, :6], free[1, :6]) and bool((got[1, 6:] == 36).all())
+    assert bool((free[:, 4:] >= 1).all()) and bool((free[:, 4:] < 31).all())
+    with pytest.raises(ValueError, match="end_id"):
+        call(allowed=grammar)
+    ban = torch.full((37,), -float("inf"), device="cuda:0")         # a bias that leaves nothing, from the first step on
+    assert bool((call(bias=ban, end_id=0)[:, 4:] == 0).all())

@@ -35,3 +35,57 @@ def test_ids_outside_the_vocabulary_are_no_targets(dtype, ragged, bad):
     assert abs(float(loss) - float(want)) <= 50 * 2.0 ** -24 * float(p.abs().max())
     dx, = torch.autograd.grad(loss, [x])
     assert bool(torch.isfinite(dx).all()) and not dx[:, -1].any() and not dx[:, :-1][~on].any() and bool((dx[:, :-1][on].abs().sum(-1) > 0).all())
+
+
+class _Steps:
+    """Stands for a model in generate: step by step, the logits are given for every last id and row."""
+
+    def __init__(self, table):          # [steps at most, B, V]
+        self.table, self.vocab, self.scale, self.padding_idx, self.embedding, self.encoder = table, table.shape[-1], 1.0, None, torch.zeros(1), self
+        self.n, self.t = table.shape[0], 0
+
+    def step(self, state):
+        self.t += 1
+        return self.table[self.t - 1]
+
+    def logits(self, state):
+        return state.clone()
+
+
+def _masked(x, history, lengths, prompts, allowed=None, bias=None, out=None, **settings):
+    words = allowed.expand(x.shape[0], -1).long() & 0xffffffff
+    ok = ((words[:, torch.arange(x.shape[1]) // 32] >> (torch.arange(x.shape[1]) % 32)) & 1).bool()
+    out.copy_(torch.where(ok, x, torch.full_like(x, -float("inf"))))
+
+
+def _generate(monkeypatch, table, prompt, steps, **kw):
+    m = _Steps(table)
+    monkeypatch.setattr(layer, "BPTDecoder", lambda encoder, B, dtype: m)
+    monkeypatch.setattr(layer, "token_states", lambda ids, weight, scale: ids)
+    monkeypatch.setattr(layer, "adjust_logits", _masked)
+    return layer.BPTLanguageModel.generate(m, prompt, steps, **kw)
+
+
+@pytest.mark.parametrize("temperature", [0.0, 0.7])
+def test_a_sequence_without_an_allowed_id_has_ended(monkeypatch, temperature):
+    """Row 1 has nothing allowed at the third id of the answer, and something again from the fifth on; rows 0 and 2 always do."""
+    g = torch.Generator().manual_seed(3)
+    table, prompt = torch.randn(12, 3, 20, generator=g), torch.randint(0, 20, (3, 2), generator=g)
+
+    def grammar(ids):
+        w = torch.full((3, 1), 0b11111111110, dtype=torch.int32)
+        if ids.shape[1] == 4 or ids.shape[1] == 5:
+            w[1] = 0
+        return w
+
+    call = lambda **kw: _generate(monkeypatch, table, prompt, 8, temperature=temperature, generator=torch.Generator().manual_seed(7), **kw)
+    got = call(allowed=grammar, end_id=19)
+    free = call(allowed=torch.tensor([0b11111111110], dtype=torch.int32))       # the same draws, nothing ever forbidden altogether
+    assert torch.equal(got[0], free[0]) and torch.equal(got[2], free[2]) and torch.equal(got[1, :4], free[1, :4])
+    assert bool((got[1, 4:] == 19).all())
+    with pytest.raises(ValueError, match="end_id"):
+        call(allowed=grammar)
+    assert torch.equal(call(allowed=torch.tensor([0b11111111110], dtype=torch.int32), end_id=0), free)
+    for bad in (-1, 20):
+        with pytest.raises(ValueError, match="end_id"):
+            call(allowed=grammar, end_id=bad)

@@ -6,7 +6,6 @@
 // which PyTorch's engine takes about 40; single tokens and short sequences are bound by that.
 //
 // Functions return None for arguments that the operators refuse; the caller then goes through binding.py, which says why.
-#include <ATen/MemoryOverlap.h>
 #include <ATen/cuda/CUDAContext.h>
 #include <ATen/cuda/CUDAGraphsUtils.cuh>
 #include <c10/cuda/CUDAGuard.h>
@@ -15,6 +14,8 @@
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
+#include <algorithm>
+#include <functional>
 #include <unordered_set>
 
 #include "../../include/bpt.h"
@@ -438,6 +439,76 @@ bool take_tensors(const py::object& from, std::vector<Tensor>* to) {
     return true;
 }
 
+// Whether some element of a and one of b share a byte; with b the same tensor as a, whether two different elements do.  The distance of two elements is the
+// distance of the tensors' starts plus whole multiples of the strides, each in its range; strides that both have count once.  From the
+// largest stride on, only the multiples that the smaller strides can still make up for are tried: a few where strides
+// nest as those of views do.  Where they do not, and it would take long, the answer is that they meet.
+bool share_memory(const Tensor& a, const Tensor& b) {
+    if (!a.numel() || !b.numel()) return false;
+    const bool self = &a == &b;
+    struct Step { int64_t bytes, lo, hi; };         // lo .. hi multiples
+    std::vector<Step> steps;
+    for (const Tensor* t : {&a, &b}) {
+        for (int64_t i = 0; i < t->dim(); ++i) {
+            const int64_t n = t->size(i) - 1, bytes = t->stride(i) * (int64_t)t->element_size();
+            if (n == 0) continue;
+            if (bytes == 0) {
+                if (self) return true;
+                continue;
+            }
+            auto same = std::find_if(steps.begin(), steps.end(), [&](const Step& s) { return s.bytes == bytes; });
+            if (self && same != steps.end()) return true;
+            if (same == steps.end()) same = steps.insert(steps.end(), Step{bytes, 0, 0});
+            if (t == &a) same->hi += n;
+            if (t == &b) same->lo -= n;
+        }
+        if (self) break;
+    }
+    std::sort(steps.begin(), steps.end(), [](const Step& x, const Step& y) { return x.bytes > y.bytes; });
+    std::vector<int64_t> low(steps.size() + 1, 0), high(steps.size() + 1, 0);      // what the steps from k on reach
+    for (size_t k = steps.size(); k-- > 0;) {
+        low[k] = low[k + 1] + steps[k].lo * steps[k].bytes;
+        high[k] = high[k + 1] + steps[k].hi * steps[k].bytes;
+    }
+    // the start of a's element minus that of b's lies between these where they share a byte
+    const int64_t least = 1 - (int64_t)a.element_size(), most = (int64_t)b.element_size() - 1;
+    const auto down = [](int64_t x, int64_t y) { return x >= 0 ? x / y : -((-x + y - 1) / y); };
+    int tries = 100000;
+    const std::function<bool(size_t, int64_t, bool)> from = [&](size_t k, int64_t d, bool other) {
+        if (k == steps.size()) return other && d >= least && d <= most;
+        const int64_t s = steps[k].bytes;
+        const int64_t first = std::max(steps[k].lo, -down(d + high[k + 1] - least, s)), last = std::min(steps[k].hi, down(most - d - low[k + 1], s));
+        for (int64_t c = first; c <= last; ++c)
+            if (--tries < 0 || from(k + 1, d + c * s, other || c != 0)) return true;
+        return false;
+    };
+    return from(0, (int64_t)((uintptr_t)a.data_ptr() - (uintptr_t)b.data_ptr()), !self);
+}
+
+// Whether anything that clip_gradients writes -- the results, or without any the gradients -- shares memory with another tensor of the call or with
+// itself.  A result may be its own gradient.
+bool overlaps(const std::vector<Tensor>& g, const std::vector<Tensor>& o) {
+    struct View { const Tensor* t; uintptr_t from, to; size_t who; bool write; };
+    std::vector<View> views;
+    const auto add = [&](const Tensor& t, size_t who, bool write) {
+        uintptr_t bytes = t.element_size();
+        for (int64_t i = 0; i < t.dim(); ++i) bytes += (t.size(i) - 1) * t.stride(i) * t.element_size();
+        views.push_back({&t, (uintptr_t)t.data_ptr(), (uintptr_t)t.data_ptr() + bytes, who, write});
+    };
+    for (size_t i = 0; i < g.size(); ++i) {
+        if (!g[i].defined() || !g[i].numel()) continue;
+        const Tensor& to = o.empty() ? g[i] : o[i];
+        if (!to.is_non_overlapping_and_dense() && share_memory(to, to)) return true;
+        add(to, i, true);
+        if (!o.empty() && !(to.data_ptr() == g[i].data_ptr() && to.strides() == g[i].strides() && to.scalar_type() == g[i].scalar_type())) add(g[i], i, false);
+    }
+    std::sort(views.begin(), views.end(), [](const View& x, const View& y) { return x.from < y.from; });
+    for (size_t i = 0; i < views.size(); ++i)
+        for (size_t j = i + 1; j < views.size() && views[j].from < views[i].to; ++j)
+            if ((views[i].write || views[j].write) && share_memory(*views[i].t, *views[j].t)) return true;
+    return false;
+}
+
 // Elements lie one after another in memory, in whatever order, so that a tensor is a list of numbers.
 py::object clip_gradients(const py::object& grads, const py::object& into, int64_t norm_type, bool clip, double max_norm, double eps) {
     check_tracing("clip_gradients");
@@ -467,9 +538,6 @@ py::object clip_gradients(const py::object& grads, const py::object& into, int64
             if (!(src.strides() == dst.strides() && src.is_non_overlapping_and_dense())) {
                 src = src.contiguous();
                 if (!dst.is_contiguous()) {
-                    if (at::has_internal_overlap(dst) == at::MemOverlap::Yes) return py::none();
-                    for (const auto& other : back)      // the library sees copies only
-                        if (other.second.data_ptr() == dst.data_ptr() && other.second.strides() == dst.strides()) return py::none();
                     held.push_back(at::empty(dst.sizes(), dst.options()));
                     back.emplace_back(held.back(), dst);
                     dst = held.back();
@@ -478,9 +546,6 @@ py::object clip_gradients(const py::object& grads, const py::object& into, int64
             }
             written.push_back(&o[i]);
         } else if (!src.is_non_overlapping_and_dense()) {
-            if (clip && at::has_internal_overlap(src) == at::MemOverlap::Yes) return py::none();
-            for (const auto& other : back)          // the library sees copies only
-                if (other.second.data_ptr() == src.data_ptr() && other.second.strides() == src.strides()) return py::none();
             src = src.contiguous();
             held.push_back(src);
             if (clip) back.emplace_back(src, g[i]);
@@ -491,6 +556,7 @@ py::object clip_gradients(const py::object& grads, const py::object& into, int64
         e.numel = src.numel();
         list.push_back(e);
     }
+    if (clip && !held.empty() && overlaps(g, o)) return py::none();     // the library sees copies
     const c10::cuda::OptionalCUDAGuard guard(first ? std::optional<at::Device>(first->device()) : std::nullopt);
     const auto options = at::TensorOptions().device(first ? first->device() : at::Device(at::kCUDA, c10::cuda::current_device()));
     const Tensor norm = at::empty({}, options.dtype(at::kFloat));
@@ -675,5 +741,6 @@ PYBIND11_MODULE(_bpt_torch, m) {
     m.def("gated_feed_forward", &gated_feed_forward);
     m.def("token_states", &token_states);
     m.def("clip_gradients", &clip_gradients);
+    m.def("share_memory", [](const Tensor& a, const std::optional<Tensor>& b) { return share_memory(a, b.has_value() ? *b : a); }, py::arg("a"), py::arg("b") = py::none());
     m.def("adjust_logits", &adjust_logits);
 }

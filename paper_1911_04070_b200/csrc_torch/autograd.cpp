@@ -582,30 +582,6 @@ Tensor by_rows(const Tensor& t) {
 }
 int64_t row_stride(const Tensor& t) { return t.size(0) < 2 ? t.size(1) : t.stride(0); }
 
-// Whether rows of one lie on rows of the other (rows apart by the same number of bytes may lie side by side).
-bool rows_meet(const Tensor& a, const Tensor& b) {
-    if (!a.numel() || !b.numel()) return false;
-    const auto from = [](const Tensor& t) { return (int64_t)(uintptr_t)t.data_ptr(); };
-    const auto step = [](const Tensor& t) { return row_stride(t) * (int64_t)t.element_size(); };
-    const auto width = [](const Tensor& t) { return t.size(1) * (int64_t)t.element_size(); };
-    const auto end = [&](const Tensor& t) { return from(t) + (t.size(0) - 1) * step(t) + width(t); };
-    if (end(a) <= from(b) || end(b) <= from(a)) return false;
-    if (step(a) != step(b) || a.size(0) < 2) return true;
-    const int64_t d = ((from(b) - from(a)) % step(a) + step(a)) % step(a);
-    return d < width(a) || d + width(b) > step(a);
-}
-
-// Whether the memory from the first to the last element of one meets that of the other.
-bool spans_meet(const Tensor& a, const Tensor& b) {
-    if (!a.numel() || !b.numel()) return false;
-    const auto end = [](const Tensor& t) {
-        int64_t n = t.element_size();
-        for (int64_t i = 0; i < t.dim(); ++i) n += (t.size(i) - 1) * t.stride(i) * (int64_t)t.element_size();
-        return (const char*)t.data_ptr() + n;
-    };
-    return (const char*)a.data_ptr() < end(b) && (const char*)b.data_ptr() < end(a);
-}
-
 // A number, or one float32 per row.
 bool setting(const py::object& v, const Tensor& logits, std::vector<Tensor>* held, float* number, const float** rows) {
     if (!THPVariable_Check(v.ptr())) {
@@ -698,10 +674,10 @@ py::object adjust_logits(const Tensor& logits_, const Opt& history_, const Opt& 
         if (out.sizes() != logits.sizes() || out.device() != device || !by_rows(out).is_same(out)) return py::none();
         // the logits themselves, or somewhere else
         if (!(out.data_ptr() == logits.data_ptr() && out.scalar_type() == logits.scalar_type() && row_stride(out) == row_stride(logits)) &&
-            rows_meet(out, logits))
+            share_memory(out, logits))
             return py::none();
         for (const Tensor& t : held)
-            if (spans_meet(out, t)) return py::none();
+            if (share_memory(out, t)) return py::none();
     } else {
         out = at::empty({B, V}, logits.options());
     }

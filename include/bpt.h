@@ -139,11 +139,11 @@ bpt_status bpt_check(const void* workspace, void* cuda_stream);
 /*
  * Waits for `cuda_stream` and reports whether a bounded device-side wait of any gated feed-forward call
  * (bpt_gated_ff_fwd, bpt_gated_ff_bwd, with or without a status block) or of the wait self-test expired on
- * the current device since the last such report: BPT_OK or BPT_ERR_TIMEOUT, which clears the record; or
- * BPT_ERR_INDEX, where a token id was outside its table (of both, what was stored last).  For
+ * the current device since the last such report: BPT_OK, or BPT_ERR_TIMEOUT; or BPT_ERR_INDEX, where a token id was outside
+ * its table.  What is reported is cleared; of both, the timeout is reported first and the id by the next call.  For
  * training loops: once per step, where the step's calls ran inside an autograd engine that keeps no status
  * blocks.  Covers the work that `cuda_stream` has waited for; work that still runs on other streams
- * is reported by a later call.  BPT_ERR_CUDA when the synchronisation or a copy fails.  Host-synchronous: not
+ * is reported by a later call.  BPT_ERR_CUDA when the synchronisation, a copy or a launch fails.  Host-synchronous: not
  * for use inside a stream capture.
  */
 bpt_status bpt_check_device(void* cuda_stream);

@@ -316,7 +316,7 @@ def bpt_check(workspace) -> int:
 def bpt_check_device(device=None) -> int:
     """Waits for the current stream of `device` (the current one) and returns 0, or 5 when a bounded device-side wait of a gated
     feed-forward call, forward or backward, expired there since the last such question: what was computed since is invalid; or 8 when
-    a token id was outside its table."""
+    a token id was outside its table (of both, 5 first, and 8 by the next call)."""
     with torch.cuda.device(device):
         return int(load_library().bpt_check_device(_stream()))
 

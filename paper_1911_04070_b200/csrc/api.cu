@@ -23,6 +23,8 @@ int* device_record() {
     if (device < 64) known[device].store(at, std::memory_order_release);
     return at;
 }
+// Takes a bit out of the record; what other streams report meanwhile stays.
+__global__ void clear_record_kernel(int* record, int bit) { atomicAnd(record, ~bit); }
 }  // namespace bpt
 
 using namespace bpt;
@@ -71,8 +73,10 @@ extern "C" bpt_status bpt_check_device(void* cuda_stream) {
     if (!record || cudaMemcpyAsync(&word, record, sizeof(word), cudaMemcpyDeviceToHost, st) != cudaSuccess) return BPT_ERR_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return BPT_ERR_CUDA;
     if (word == 0) return BPT_OK;
-    if (cudaMemsetAsync(record, 0, sizeof(word), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return BPT_ERR_CUDA;
-    return word == (int32_t)BPT_ERR_TIMEOUT || word == (int32_t)BPT_ERR_INDEX ? (bpt_status)word : BPT_ERR_CUDA;
+    const int bit = word & kRecordTimeout ? kRecordTimeout : kRecordIndex;      // the one that makes results invalid first
+    clear_record_kernel<<<1, 1, 0, st>>>(record, bit);
+    if (cudaGetLastError() != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return BPT_ERR_CUDA;
+    return bit == kRecordTimeout ? BPT_ERR_TIMEOUT : BPT_ERR_INDEX;
 }
 
 static bool options_ok(const bpt_attn_options* opt) {

@@ -37,12 +37,14 @@ struct AttnProblem {
     cudaStream_t stream;
 };
 
-// The word of the current device that bpt_check_device reads, or nullptr when the runtime fails.
+// The word of the current device that bpt_check_device reads, or nullptr when the runtime fails: a bit for each thing that can be reported, so that none
+// covers another.
 int* device_record();
+constexpr int kRecordTimeout = 1, kRecordIndex = 2;
 // What a kernel does with a bounded wait that ran out: into the call's status block, if it has one, and into the device's record.
 __device__ __forceinline__ void report_timeout(int* status, int* record) {
     if (status) status[0] = (int)BPT_ERR_TIMEOUT;
-    *record = (int)BPT_ERR_TIMEOUT;
+    atomicOr(record, kRecordTimeout);
 }
 
 // Optional per-launch timing (see bpt_trace_begin): a mark after every kernel launch.

@@ -109,7 +109,7 @@ __device__ __forceinline__ long long id_of_row(const EmParams& p, unsigned row) 
     if (t >= real_tokens(p, b)) return -1;
     const long long id = load_id(p, (long long)b * p.tokens + t);
     if (id >= 0 && id < p.vocab) return id;
-    *p.record = (int)BPT_ERR_INDEX;
+    atomicOr(p.record, kRecordIndex);
     return -1;
 }
 
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(256) embed_fwd_narrow_kernel(EmParams p) {
 __device__ __forceinline__ int2 place_of(const EmParams& p, unsigned i, long long id) {
     const unsigned b = p.by_tokens.div(i), t = i - b * p.tokens;
     const bool real = t < real_tokens(p, b), in = id >= 0 && id < p.vocab;
-    if (real && !in) *p.record = (int)BPT_ERR_INDEX;
+    if (real && !in) atomicOr(p.record, kRecordIndex);
     return make_int2(real && in && id != p.padding_idx ? (int)id : (int)p.vocab, (int)(b * p.out_rows + t));
 }
 __device__ __forceinline__ void pdl_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -15,7 +15,7 @@ def test_neither_covers_the_other(order):
     ids, w = torch.tensor([1, 2, 99], device="cuda:0"), torch.ones(5, 8, device="cuda:0")
     while binding.bpt_check_device():
         pass
-    acts = {"wait": lambda: binding.bpt_selftest_wait_timeout(block, 2000), "forward": lambda: binding.bpt_embed_fwd(ids, w),
+    acts = {"wait": lambda: binding.bpt_selftest_wait_timeout(block, 2000, arrive=False), "forward": lambda: binding.bpt_embed_fwd(ids, w),
             "backward": lambda: binding.bpt_embed_bwd(ids, torch.ones(3, 8, device="cuda:0"), 5, torch.float32)}
     for a in order:
         acts[a]()

@@ -153,7 +153,8 @@ def token_states(ids, weight, scale=1.0, span_rows=0, lengths=None, padding_idx=
     Capture, modes of differentiation and tracing as in residual_norm."""
     if type(scale) is not float:
         _check_constant("scale", scale, "token_states", "weight")
-    out = binding.load_native().token_states(ids, weight, lengths, scale, span_rows, -1 if padding_idx is None else padding_idx, dtype)
+    padding = -1 if padding_idx is None else padding_idx if padding_idx >= 0 else -2       # -1 is none, below that is refused
+    out = binding.load_native().token_states(ids, weight, lengths, scale, span_rows, padding, dtype)
     if out is None:
         if weight.dim() == 2 and padding_idx is not None and not 0 <= padding_idx < weight.shape[0]:
             raise ValueError("padding_idx must be None or an id of the table")

@@ -393,7 +393,8 @@ bpt_status bpt_embed_bwd(const bpt_embed_args* args, const void* d_out, void* d_
  * tensor given twice, for one; refused.  bpt_grad_norm writes no tensor (out is not looked at) and counts a tensor given twice twice.
  * norm: device, fp32 [1].  A NaN among the gradients, or an infinity with BPT_GRAD_NORM_L2, makes norm NaN or infinite as it would by
  * the formula, and c NaN or 0; nothing is hidden.  Squares are summed in fp64 where fp32 would lose them, so
- * the norm is right for gradients of any size; c and the products are fp32, one rounding.  Fixed order, no atomics: bit-reproducible.
+ * the norm is right for gradients of any size; c and the products are fp32, one rounding.  A norm that fp32 has no number for comes out
+ * infinite in `norm`; c is that of the sum itself.  Fixed order, no atomics: bit-reproducible.
  * n = 0, or nothing in any tensor: norm 0.  max_norm >= 0 (infinite: nothing is scaled), eps >= 0.
  * `workspace`: bpt_grad_norm_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a status block, 16-byte
  * aligned; two calls whose GPU work overlaps need one each.  Two launches for up to 960 tensors.

@@ -12,8 +12,10 @@
 // their way per thread instead of four: 25 / 53 / 597; units dealt out in turn instead of in one range per CTA: 20 / 44 / 595.
 //
 // Squares are summed in fp32 over 8 elements and then in fp64, which costs one addition per 16 or 32 bytes; where a sum of 8 squares
-// leaves the range in which fp32 loses nothing, those 8 are squared in fp64: no gradient is too large or too small for its norm.
+// leaves the range in which fp32 loses nothing, those 8 are squared in fp64: no gradient is too large or too small for its norm.  Where that
+// norm or the factor leaves fp32's normal range, the factor is taken from the norm as it was summed and applied in two steps (factor_of).
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -204,7 +206,7 @@ __global__ void __launch_bounds__(kGcThreads) grad_norm_kernel(const __grid_cons
 }
 
 // The norm from the shares, the same in every CTA: thread by thread, then over the warps, in one order.
-__device__ float whole_norm(const GcParams& p) {
+__device__ double whole_norm(const GcParams& p) {
     __shared__ double share[kGcThreads / 32];
     double v = 0;
     if (p.inf) {
@@ -220,7 +222,7 @@ __device__ float whole_norm(const GcParams& p) {
     __syncthreads();
     v = share[0];
     for (int w = 1; w < kGcThreads / 32; ++w) v = join(v, share[w]);
-    return (float)(p.inf ? v : sqrt(v));
+    return p.inf ? v : sqrt(v);
 }
 
 __device__ __forceinline__ void store8(float* at, const float (&x)[8]) {
@@ -238,14 +240,30 @@ __device__ __forceinline__ void store8(__nv_bfloat16* at, const float (&x)[8]) {
 __device__ __forceinline__ void put(float x, float* y) { *y = x; }
 __device__ __forceinline__ void put(float x, __nv_bfloat16* y) { *y = __float2bfloat16(x); }
 
+// The factor as two, whose product it is: (g * step) * c.  step is 1 but for factors below fp32's normal numbers.
+struct GcFactor {
+    float c, step;
+};
+// max_norm / (norm + eps) where fp32 holds the norm and the quotient as normal numbers, which is as good as always; in fp64 otherwise.  A quotient q
+// below 2^-126 is taken in two steps that lose nothing: what is left of a gradient at all, at least 2^-150 of it, was at least 2^-150 / q,
+// which is 2^-24 (2^70 for q below 2^-220) and with the step 2^-124 (2^-79); and q / step is normal down to q = 2^-275, below which
+// results are at most a few of the smallest numbers.
+__device__ __forceinline__ GcFactor factor_of(const GcParams& p, double norm) {
+    const float norm32 = (float)norm, c = p.max_norm / (norm32 + p.eps);
+    if (norm32 >= FLT_MIN && norm32 <= FLT_MAX && c >= FLT_MIN) return {c, 1.f};
+    const double q = (double)p.max_norm / (norm + (double)p.eps);
+    const float step = q < 0x1p-220 ? 0x1p-149f : q < 0x1p-126 ? 0x1p-100f : 1.f;
+    return {(float)(q / (double)step), step};
+}
+
 // c * the elements of units u0 .. u1 into a result of type T
 template <typename T>
-__device__ __forceinline__ void scale_units(const GcTensor& t, unsigned u0, unsigned u1, float c) {
+__device__ __forceinline__ void scale_units(const GcTensor& t, unsigned u0, unsigned u1, const GcFactor& by) {
     T* out = (T*)(t.out ? t.out : const_cast<void*>(t.grad));
     const bool same_start = t.flags & kGcSameStart;
     groups<true>(t, u0, u1, [&](long long i, float (&x)[8], bool whole) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= c;
+        for (int j = 0; j < 8; ++j) x[j] = x[j] * by.step * by.c;
         if (whole && same_start) {
             store8(out + i, x);
         } else {
@@ -260,22 +278,22 @@ template <int N>
 __global__ void __launch_bounds__(kGcThreads) grad_scale_kernel(const __grid_constant__ GcList<N> list, const __grid_constant__ GcParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const float norm = whole_norm(p);
-    if (p.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
-    const float q = p.max_norm / (norm + p.eps);
-    const bool cut = !(q >= 1.f);       // NaN cuts, too: a NaN norm leaves no gradient that looks sound
-    const float c = cut ? q : 1.f;      // times 1 changes no value
+    const double norm = whole_norm(p);
+    if (p.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
+    GcFactor by = factor_of(p, norm);
+    const bool cut = by.step < 1.f || !(by.c >= 1.f);       // NaN cuts, too: a NaN norm leaves no gradient that looks sound
+    if (!cut) by.c = 1.f;                                   // times 1 changes no value
     if (!cut && !p.into) return;
     walk<N, true>(list, p, [&](const GcTensor& t, unsigned u0, unsigned u1) {
         if (!cut && !t.out) return;
-        if (t.flags & kGcOutBf16) scale_units<__nv_bfloat16>(t, u0, u1, c);
-        else scale_units<float>(t, u0, u1, c);
+        if (t.flags & kGcOutBf16) scale_units<__nv_bfloat16>(t, u0, u1, by);
+        else scale_units<float>(t, u0, u1, by);
     });
 }
 
 __global__ void __launch_bounds__(kGcThreads) grad_norm_finish_kernel(const __grid_constant__ GcParams p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const float norm = whole_norm(p);
+    const float norm = (float)whole_norm(p);
     if (threadIdx.x == 0) *p.norm = norm;
 }
 

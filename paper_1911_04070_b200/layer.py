@@ -195,7 +195,7 @@ def _clip(grads, out, norm_type, clip, max_norm, eps):
 def gradient_norm(grads, norm_type=2.0):
     """The 2-norm (norm_type=float("inf"): the largest absolute value) over all elements of a list of tensors, float32 or bfloat16 mixed, as
     a float32 tensor [].  None entries count for nothing; nothing at all gives 0.  Squares are summed in 64 bits where 32 would
-    lose them: right for gradients of any size.  Two launches whatever the number of tensors up to 960; bit-reproducible; can be captured."""
+    lose them: right for gradients of any size (infinite where float32 has no such number).  Two launches whatever the number of tensors up to 960; bit-reproducible; can be captured."""
     return _clip(grads, None, norm_type, False, 0.0, 0.0)
 
 
@@ -206,7 +206,7 @@ def clip_gradients(grads, max_norm, norm_type=2.0, eps=1e-6, out=None):
     They are scaled in place, and not written where the norm is below max_norm; or, with out (a list of as many tensors, float32 or
     bfloat16, say the gradients of an optimizer's 32-bit master weights), left as they are and the scaled values written there.  Any
     strides; no tensor twice and no overlaps between what is written and anything else; no leaf that requires a gradient is written (a parameter
-    given for its gradient is refused).  A NaN makes the norm and all results NaN.  Nothing
+    given for its gradient is refused).  Gradients whose norm is beyond float32 are scaled by it all the same.  A NaN makes the norm and all results NaN.  Nothing
     is read back to the host: can be captured in a CUDA graph, which then uses these very tensors."""
     return _clip(grads, out, norm_type, True, max_norm, eps)
 

@@ -395,7 +395,7 @@ bpt_status bpt_embed_bwd(const bpt_embed_args* args, const void* d_out, void* d_
  * the formula, and c NaN or 0; nothing is hidden.  Squares are summed in fp64 where fp32 would lose them, so
  * the norm is right for gradients of any size; c and the products are fp32, one rounding.  A norm that fp32 has no number for comes out
  * infinite in `norm`; c is that of the sum itself.  Fixed order, no atomics: bit-reproducible.
- * n = 0, or nothing in any tensor: norm 0.  max_norm >= 0 (infinite: nothing is scaled), eps >= 0.
+ * n = 0, or nothing in any tensor: norm 0.  max_norm >= 0 (infinite: nothing is scaled, whatever the norm), eps >= 0.
  * `workspace`: bpt_grad_norm_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a status block, 16-byte
  * aligned; two calls whose GPU work overlaps need one each.  Two launches for up to 960 tensors.
  * Errors: INVALID_ARG, UNSUPPORTED (numel > 2^40, 2^42 elements in all), WORKSPACE, CUDA.

@@ -249,6 +249,7 @@ struct GcFactor {
 // which is 2^-24 (2^70 for q below 2^-220) and with the step 2^-124 (2^-79); and q / step is normal down to q = 2^-275, below which
 // results are at most a few of the smallest numbers.
 __device__ __forceinline__ GcFactor factor_of(const GcParams& p, double norm) {
+    if (p.max_norm > FLT_MAX) return {1.f, 1.f};        // no limit: not infinity / infinity
     const float norm32 = (float)norm, c = p.max_norm / (norm32 + p.eps);
     if (norm32 >= FLT_MIN && norm32 <= FLT_MAX && c >= FLT_MIN) return {c, 1.f};
     const double q = (double)p.max_norm / (norm + (double)p.eps);

@@ -206,7 +206,8 @@ def clip_gradients(grads, max_norm, norm_type=2.0, eps=1e-6, out=None):
     They are scaled in place, and not written where the norm is below max_norm; or, with out (a list of as many tensors, float32 or
     bfloat16, say the gradients of an optimizer's 32-bit master weights), left as they are and the scaled values written there.  Any
     strides; no tensor twice and no overlaps between what is written and anything else; no leaf that requires a gradient is written (a parameter
-    given for its gradient is refused).  Gradients whose norm is beyond float32 are scaled by it all the same.  A NaN makes the norm and all results NaN.  Nothing
+    given for its gradient is refused).  Gradients whose norm is beyond float32 are scaled by it all the same.  A NaN makes the norm and all results NaN (an
+    infinite max_norm scales nothing, whatever the norm).  Nothing
     is read back to the host: can be captured in a CUDA graph, which then uses these very tensors."""
     return _clip(grads, out, norm_type, True, max_norm, eps)
 

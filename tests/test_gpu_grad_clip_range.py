@@ -63,3 +63,17 @@ def test_no_limit(layer):
         g = torch.full((50,), big, device="cuda")
         layer.clip_gradients([g], float("inf"))
         assert bool((g == torch.tensor(big)).all())
+
+
+@pytest.mark.parametrize("kind", [2.0, float("inf")])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_no_limit_scales_nothing_whatever_the_norm(layer, kind, bad):
+    g = [torch.randn(3000, generator=torch.Generator().manual_seed(4)).to("cuda"), torch.randn(70, generator=torch.Generator().manual_seed(5)).to("cuda", BF16)]
+    g[0][1234] = bad
+    keep = [t.clone() for t in g]
+    same = lambda a, b: torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    norm = layer.clip_gradients(g, float("inf"), norm_type=kind)
+    assert not bool(torch.isfinite(norm)) and all(same(a, b) for a, b in zip(g, keep))
+    out = [torch.empty_like(t) for t in g]
+    layer.clip_gradients(g, float("inf"), norm_type=kind, out=out)
+    assert all(torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) for a, b in zip(out, keep))

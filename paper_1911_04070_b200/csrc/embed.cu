@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kEmClusterThreads) embed_sort_kernel(EmParams 
     namespace cg = cooperative_groups;
     constexpr int warps = kEmClusterThreads / 32;
     __shared__ int total[kEmBins], base[kEmBins], scan[warps];         // this CTA's counts; where its first place of a digit goes
-    __shared__ unsigned short in_warp[warps * kEmBins];                 // [warps][bins]
+    __shared__ __align__(16) unsigned short in_warp[warps * kEmBins];   // [warps][bins]; cleared two at a time
     const cg::cluster_group cluster = cg::this_cluster();
     const int slice = rounds * kEmClusterThreads, bins = 1 << digit, me = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, first = me * slice + warp * rounds * 32 + lane, M = (int)p.M;

@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : VEC ? 
     constexpr int kEmAhead = 4;             // rows of d_out on their way per warp
     pdl_start();
     pdl_wait();
-    const int2* list = p.list[p.sorted];
+    const int2* list = p.list[p.sorted];        // written while this kernel may have started: never through the read-only path (__ldg)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, M = (int)p.M, vocab = (int)p.vocab;
     // the CTAs that zero stand evenly between those that sum: reading and writing at the same time is the faster way
     const unsigned zero_before = (unsigned)((unsigned long long)blockIdx.x * p.zero_ctas / gridDim.x);
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : VEC ? 
         for (int i = lo[0] + (int)threadIdx.x; i < lo[1]; i += 8 * threads) {
             int id[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) id[j] = i + j * threads < lo[1] ? __ldg(&list[i + j * threads].x) : -1;
+            for (int j = 0; j < 8; ++j) id[j] = i + j * threads < lo[1] ? list[i + j * threads].x : -1;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (id[j] >= 0) there[id[j] - first] = true;
@@ -674,10 +674,10 @@ __global__ void __launch_bounds__(kEmSumWarps * 32, sizeof(TO) == 4 ? 2 : VEC ? 
             int a = lo[0], b = lo[1];
             while (a < b) {
                 const int mid = (a + b) >> 1;
-                if (__ldg(&list[mid].x) < first + r) a = mid + 1;
+                if (list[mid].x < first + r) a = mid + 1;
                 else b = mid;
             }
-            there[r] = a < lo[1] && __ldg(&list[a].x) == first + r;
+            there[r] = a < lo[1] && list[a].x == first + r;
         }
     }
     __syncthreads();

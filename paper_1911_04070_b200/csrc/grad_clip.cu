@@ -6,10 +6,11 @@
 // contiguous share of the units, so that a few large and many small tensors balance.  The second kernel walks a CTA's share backwards:
 // what the first one read last is still in L2.
 //
-// B200, on the GPU: 9 tensors of 0.26 million values 6.2 us (two short launches; one launch of a cluster of 16 CTAs took 8 to 10); 50 MB of
-// bf16 in 54 tensors, norm only, 18 us; the same scaled into fp32 41 us (150 MB read and written once are 23, the norm's own read of 50 MB from
-// memory and a second launch come on top); 1.2 GB in 432 tensors scaled into bf16 608 us (norm 6.2 TB/s, scaling 5.6).  Eight groups of 8 elements on
-// their way per thread instead of four: 25 / 53 / 597; units dealt out in turn instead of in one range per CTA: 20 / 44 / 595.
+// B200, on the GPU: 9 tensors of 0.26 million values 6.2 to 7.3 us (two short launches; one launch of a cluster of 16 CTAs took 8 to 10).  50 MB of
+// bf16 in 54 tensors: the norm alone 16.4 us, below the limit 17, of which grad_norm is 12.3 (4.1 TB/s; a reduction of 67 MB of PyTorch's takes
+// 24) and the launch behind it the rest; cut in place 31; cut into fp32 41 (150 MB read and written once are 23, the norm's own read
+// comes on top).  1.2 GB in 432 tensors scaled into bf16 608 us (norm 6.2 TB/s, scaling 5.6).  Eight groups of 8 elements on their way per thread
+// instead of four: 25 (below the limit) / 53 (into fp32) / 597 where four took 17.8 / 41 / 608; units dealt out in turn instead of in one range per CTA: 20 / 44 / 595.
 //
 // Squares are summed in fp32 over 8 elements and then in fp64, which costs one addition per 16 or 32 bytes; where a sum of 8 squares
 // leaves the range in which fp32 loses nothing, those 8 are squared in fp64: no gradient is too large or too small for its norm.  Where that
@@ -400,7 +401,7 @@ bool launch(const bpt_grad* g, int from, const GcPlan& q, GcParams p, bool scale
     return ok;
 }
 bool launch(const bpt_grad* g, int from, const GcPlan& q, const GcParams& p, bool scale, bool dependent, cudaStream_t st) {
-    if (q.n <= 24) return launch<24>(g, from, q, p, scale, dependent, st);
+    // a launch's arguments are copied: 9 tensors in the long list 12.8 us a call, in the short one 9.8 (one of 24 entries: 9.9); 117 tensors 26 and 23
     if (q.n <= 120) return launch<120>(g, from, q, p, scale, dependent, st);
     return launch<kGcMost>(g, from, q, p, scale, dependent, st);
 }

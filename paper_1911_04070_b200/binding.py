@@ -557,7 +557,8 @@ def bpt_embed_bwd(ids, d_out, vocab: int, weight_dtype, scale: float = 1.0, leng
     """The gradient of the table of bpt_embed_fwd: [vocab, D] of weight_dtype, zeros where no token stands and at padding_idx.
     d_out: [..., n + span_rows, D], contiguous.  Bit-reproducible."""
     _check_float_type(weight_dtype, d_out.dtype)
-    if d_out.dim() != ids.dim() + 1 or d_out.shape[:-2] != ids.shape[:-1] or d_out.shape[-2] < ids.shape[-1] or not d_out.is_contiguous()             or d_out.get_device() != ids.get_device():
+    if d_out.dim() != ids.dim() + 1 or d_out.shape[:-2] != ids.shape[:-1] or d_out.shape[-2] < ids.shape[-1] or not d_out.is_contiguous() \
+            or d_out.get_device() != ids.get_device():
         raise ValueError("d_out must be contiguous, [..., n + span_rows, D] on the device of ids")
     D = d_out.shape[-1]
     args, dev = _embed_args(ids, lengths, None, vocab, D, weight_dtype, d_out.dtype, scale, d_out.shape[-2] - ids.shape[-1], padding_idx)

@@ -1,7 +1,8 @@
 // Token ids to node states, and the gradient of the table.  See bpt_embed_fwd / bpt_embed_bwd in include/bpt.h.
 //
-// Forward: out[b, t] = scale * weight[ids[b, t]], zero rows behind the tokens.  Bound by what it writes: 67 MB (4 x 16383 rows of 512 in bf16, 8192
-// tokens each) in 16.4 us, 268 MB in 68, the 4 TB/s at which this device writes where little is read.
+// Forward: out[b, t] = scale * weight[ids[b, t]], zero rows behind the tokens.  It mostly writes: 67 MB (4 x 16383 rows of 512 in bf16, 8192
+// tokens each) in 16.4 us, 4.1 TB/s, and 268 MB in 47 (8 x 8192 ids of 256, 2048 wide) or 69 (of 131072, drawn as words are, whose rows it reads from
+// memory).  Timed the same way PyTorch's fill_ and zero_ of 67 MB take 20.5 us, of 268 MB 72.
 //
 // Backward: dW[v] = scale * sum of d_out over the places where v stands.  Float atomics would add in another order every time, and a
 // table of counts per id is as long as the vocabulary; so the places are sorted by id (stable, digits of at most 9 bits: one pass up to 511
@@ -13,7 +14,7 @@
 // B200, forward + backward on the GPU: 4 x 8192 ids of 256, 512 wide, 42 us (forward 16, sort 9.5, sums and zeros about 10, finish about 6);
 // 16 x 512 ids of 32001 x 201 in fp32 31 us (forward 8, sort 9.5); 8 x 8192 ids of 131072 x 2048 240 us (forward 68, sort 22, sums and zeros of
 // 268 MB read and 537 MB written about 135).  What it took: sorting by two launches a pass and tiles per warp only 57 / 45 / 300; zeroing all of dW beside
-// the sort 289 for the last (a kernel that only writes is the slower way); CTAs that zero 32 KB instead of 128 KB there 290, and 128 KB
+// the sort 289 for the last (a kernel that only zeroes is the slower way: 3.9 TB/s); CTAs that zero 32 KB instead of 128 KB there 290, and 128 KB
 // instead of a share of the table's size 37 instead of 31 for the second.
 #include <algorithm>
 #include <atomic>
@@ -32,7 +33,7 @@ constexpr int kEmDigit = 9;                 // bits per sort pass, at most
 constexpr int kEmBins = 1 << kEmDigit;
 constexpr int kEmSortThreads = 1024;
 
-// n / d of n < 2^31 by a multiplication: with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1 it is (floor(m n / 2^32) + n) >> s.
+// n / d of n < 2^31 by a multiplication (Granlund and Montgomery, Division by Invariant Integers using Multiplication, 1994): with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1 it is (floor(m n / 2^32) + n) >> s.
 struct FastDiv {
     unsigned d, m, s;
     FastDiv(unsigned by = 1) : d(by), m(1), s(0) {

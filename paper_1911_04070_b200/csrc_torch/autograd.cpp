@@ -439,6 +439,13 @@ bool take_tensors(const py::object& from, std::vector<Tensor>* to) {
     return true;
 }
 
+// The bytes from the first to the last element of a tensor that has some.
+std::pair<uintptr_t, uintptr_t> span(const Tensor& t) {
+    uintptr_t bytes = t.element_size();
+    for (int64_t i = 0; i < t.dim(); ++i) bytes += (t.size(i) - 1) * t.stride(i) * t.element_size();
+    return {(uintptr_t)t.data_ptr(), (uintptr_t)t.data_ptr() + bytes};
+}
+
 // Whether some element of a and one of b share a byte; with b the same tensor as a, whether two different elements do.  The distance of two elements is the
 // distance of the tensors' starts plus whole multiples of the strides, each in its range; strides that both have count once.  From the
 // largest stride on, only the multiples that the smaller strides can still make up for are tried: a few where strides
@@ -446,6 +453,8 @@ bool take_tensors(const py::object& from, std::vector<Tensor>* to) {
 bool share_memory(const Tensor& a, const Tensor& b) {
     if (!a.numel() || !b.numel()) return false;
     const bool self = &a == &b;
+    const auto from_a = span(a), from_b = span(b);
+    if (!self && (from_a.second <= from_b.first || from_b.second <= from_a.first)) return false;
     struct Step { int64_t bytes, lo, hi; };         // lo .. hi multiples
     std::vector<Step> steps;
     for (const Tensor* t : {&a, &b}) {
@@ -482,25 +491,24 @@ bool share_memory(const Tensor& a, const Tensor& b) {
             if (--tries < 0 || from(k + 1, d + c * s, other || c != 0)) return true;
         return false;
     };
-    return from(0, (int64_t)((uintptr_t)a.data_ptr() - (uintptr_t)b.data_ptr()), !self);
+    return from(0, (int64_t)(from_a.first - from_b.first), !self);
 }
 
 // Whether anything that clip_gradients writes -- the results, or without any the gradients -- shares memory with another tensor of the call or with
 // itself.  A result may be its own gradient.
 bool overlaps(const std::vector<Tensor>& g, const std::vector<Tensor>& o) {
-    struct View { const Tensor* t; uintptr_t from, to; size_t who; bool write; };
+    struct View { const Tensor* t; uintptr_t from, to; bool write; };
     std::vector<View> views;
-    const auto add = [&](const Tensor& t, size_t who, bool write) {
-        uintptr_t bytes = t.element_size();
-        for (int64_t i = 0; i < t.dim(); ++i) bytes += (t.size(i) - 1) * t.stride(i) * t.element_size();
-        views.push_back({&t, (uintptr_t)t.data_ptr(), (uintptr_t)t.data_ptr() + bytes, who, write});
+    const auto add = [&](const Tensor& t, bool write) {
+        const auto at = span(t);
+        views.push_back({&t, at.first, at.second, write});
     };
     for (size_t i = 0; i < g.size(); ++i) {
         if (!g[i].defined() || !g[i].numel()) continue;
         const Tensor& to = o.empty() ? g[i] : o[i];
         if (!to.is_non_overlapping_and_dense() && share_memory(to, to)) return true;
-        add(to, i, true);
-        if (!o.empty() && !(to.data_ptr() == g[i].data_ptr() && to.strides() == g[i].strides() && to.scalar_type() == g[i].scalar_type())) add(g[i], i, false);
+        add(to, true);
+        if (!o.empty() && !(to.data_ptr() == g[i].data_ptr() && to.strides() == g[i].strides() && to.scalar_type() == g[i].scalar_type())) add(g[i], false);
     }
     std::sort(views.begin(), views.end(), [](const View& x, const View& y) { return x.from < y.from; });
     for (size_t i = 0; i < views.size(); ++i)

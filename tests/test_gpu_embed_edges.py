@@ -72,3 +72,13 @@ def test_sorts_of_many_passes(layer, total, V, D):
     w = torch.zeros(V, D, device="cuda", requires_grad=True)
     dw, = torch.autograd.grad(layer.token_states(ids, w), [w], d)
     assert torch.equal(dw, torch.zeros(V, D, device="cuda").index_add_(0, ids, d))
+
+
+def test_forward_mode_over_the_backward_pass_is_refused(layer):
+    from torch.autograd import forward_ad
+    ids, w = torch.zeros(3, 4, dtype=torch.int64, device="cuda"), torch.zeros(5, 8, device="cuda", requires_grad=True)
+    with forward_ad.dual_level():
+        y = layer.token_states(ids, w)
+        up = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
+        with pytest.raises(NotImplementedError, match="forward-mode"):
+            torch.autograd.grad(y, w, up)

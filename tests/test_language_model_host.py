@@ -89,3 +89,9 @@ def test_a_sequence_without_an_allowed_id_has_ended(monkeypatch, temperature):
     for bad in (-1, 20):
         with pytest.raises(ValueError, match="end_id"):
             call(allowed=grammar, end_id=bad)
+
+
+@pytest.mark.parametrize("call", [lambda t: layer.clip_gradients([t], 1.0), lambda t: layer.clip_gradients([t], 1.0, out=[t]), lambda t: layer.gradient_norm(t)])
+def test_clipping_is_not_traced(call):
+    with pytest.raises(NotImplementedError, match="traced"):
+        torch.jit.trace(call, (torch.ones(4),), check_trace=False)

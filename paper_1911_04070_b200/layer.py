@@ -478,7 +478,8 @@ class BPTLanguageModel(nn.Module):
         settings: repetition, presence, frequency, bias, bias_ids, bias_values, see adjust_logits; the prompt counts for repetition only.
         temperature 0 takes the largest logit (the lowest id of equal ones), another one draws from softmax(logits / temperature) with
         torch's `generator`.  A sequence has ended at the first step at which its mask or bias leaves it no id (logits of -inf only): it takes
-        end_id there and at all steps behind; without an end_id it raises ValueError when the steps are through.  Returns [B, P + steps] ids."""
+        end_id there and at all steps behind; without an end_id it raises ValueError when the steps are through.  So does a draw from logits that are
+        not finite, or not after the division.  Returns [B, P + steps] ids."""
         B, P = prompt.shape
         if P < 1 or steps < 0 or P + steps > self.encoder.n:
             raise ValueError("a prompt of at least one id and room for it and the steps in %d ids are needed" % self.encoder.n)
@@ -489,9 +490,9 @@ class BPTLanguageModel(nn.Module):
         ids = torch.cat([prompt, prompt.new_zeros(B, steps)], dim=1)
         lengths, prompts = (torch.full((B,), P, dtype=torch.int32, device=ids.device) for _ in range(2))
         dec = BPTDecoder(self.encoder, B, dtype=self.embedding.dtype)
-        ended = None        # [B]; nothing ends where nothing is forbidden
-        if allowed is not None or settings.get("bias") is not None or settings.get("bias_values") is not None:
-            ended = torch.zeros(B, dtype=torch.bool, device=ids.device)
+        # a step's largest logits say whether there was anything to take; they are looked at when all steps are through
+        forbids = allowed is not None or settings.get("bias") is not None or settings.get("bias_values") is not None
+        tops, ended = [], torch.zeros(B, dtype=torch.bool, device=ids.device)
         for t in range(P + steps - 1):
             state = dec.step(token_states(ids[:, t], self.embedding, self.scale))
             if t < P - 1:
@@ -500,13 +501,29 @@ class BPTLanguageModel(nn.Module):
             x = self.logits(state).float()
             adjust_logits(x, ids, lengths, prompts, allowed=allowed(ids[:, :t + 1]) if callable(allowed) else allowed, out=x, **settings)
             lengths += 1
-            if ended is not None:
-                ended |= x.amax(-1) == -math.inf
-                x.masked_fill_(ended[:, None], 0.0)         # there is a softmax, for a draw that nobody looks at
-            new = x.argmax(-1) if temperature == 0 else torch.multinomial(torch.softmax(x / temperature, -1), 1, generator=generator)[:, 0]
-            ids[:, t + 1] = new if ended is None else new.masked_fill(ended, end_id or 0)
-        if ended is not None and end_id is None and bool(ended.any()):
-            raise ValueError("a sequence was left without an allowed id; an end_id is what such a sequence takes from there on")
+            if temperature > 0:
+                tops.append(x.amax(-1))
+                p = torch.softmax(x / temperature, -1).nan_to_num_(nan=1.0)         # a row of NaN is no row to draw from; what is drawn there is dropped
+                new = torch.multinomial(p, 1, generator=generator)[:, 0]
+            elif forbids:
+                top, new = x.max(-1)
+                tops.append(top)
+            else:
+                new = x.argmax(-1)
+            if callable(allowed):           # which is shown the ids
+                ended |= tops[-1] == -math.inf
+                new = new.masked_fill(ended, end_id or 0)
+            ids[:, t + 1] = new
+        if tops:
+            top = torch.stack(tops, 1)
+            divided = top / temperature if temperature > 0 else None
+            if divided is not None and bool((~(divided < math.inf) | (divided == -math.inf) & (top > -math.inf)).any()):
+                raise ValueError("logits were not finite, or not after the division by the temperature")
+            over = (top == -math.inf).cumsum(1) > 0
+            if end_id is not None:
+                ids[:, P:].masked_fill_(over, end_id)
+            elif bool(over.any()):
+                raise ValueError("a sequence was left without an allowed id; an end_id is what such a sequence takes from there on")
         return ids
 
 

@@ -54,3 +54,20 @@ def test_a_sequence_that_its_grammar_ends(temperature):
         call(allowed=grammar)
     ban = torch.full((37,), -float("inf"), device="cuda:0")         # a bias that leaves nothing, from the first step on
     assert bool((call(bias=ban, end_id=0)[:, 4:] == 0).all())
+
+
+@torch.no_grad()
+def test_logits_that_are_not_finite_are_not_drawn_from():
+    """Said in words; the device takes calls as before."""
+    prompt = torch.randint(0, 37, (3, 4), generator=torch.Generator().manual_seed(2)).to("cuda:0")
+    m = _model(tied=False)
+    want = m.generate(prompt, 6, 1.0, torch.Generator("cuda:0").manual_seed(5))
+    keep = m.head.weight[5].clone()
+    for bad in (float("nan"), float("inf")):
+        m.head.weight[5] = bad
+        with pytest.raises(ValueError, match="not finite"):
+            m.generate(prompt, 6, 1.0, torch.Generator("cuda:0").manual_seed(5))
+    m.head.weight[5] = keep
+    with pytest.raises(ValueError, match="not finite"):
+        m.generate(prompt, 6, 1e-42, torch.Generator("cuda:0").manual_seed(5))
+    assert torch.equal(m.generate(prompt, 6, 1.0, torch.Generator("cuda:0").manual_seed(5)), want)

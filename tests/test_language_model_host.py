@@ -53,6 +53,8 @@ class _Steps:
 
 
 def _masked(x, history, lengths, prompts, allowed=None, bias=None, out=None, **settings):
+    if allowed is None:
+        return
     words = allowed.expand(x.shape[0], -1).long() & 0xffffffff
     ok = ((words[:, torch.arange(x.shape[1]) // 32] >> (torch.arange(x.shape[1]) % 32)) & 1).bool()
     out.copy_(torch.where(ok, x, torch.full_like(x, -float("inf"))))
@@ -95,3 +97,50 @@ def test_a_sequence_without_an_allowed_id_has_ended(monkeypatch, temperature):
 def test_clipping_is_not_traced(call):
     with pytest.raises(NotImplementedError, match="traced"):
         torch.jit.trace(call, (torch.ones(4),), check_trace=False)
+
+
+def _checked(draw):
+    def multinomial(p, *a, **k):
+        assert bool((p >= 0).all()) and bool(torch.isfinite(p).all()) and bool((p.sum(-1) > 0).all())
+        return draw(p, *a, **k)
+    return multinomial
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+@pytest.mark.parametrize("masked", [False, True])
+def test_nothing_is_drawn_from_logits_that_are_not_finite(monkeypatch, what, masked):
+    """Said in words, and not by the draw's own check on the device; a temperature that takes logits beyond float32 does the same."""
+    monkeypatch.setattr(torch, "multinomial", _checked(torch.multinomial))
+    g = torch.Generator().manual_seed(3)
+    table, prompt = torch.randn(12, 3, 20, generator=g), torch.randint(0, 20, (3, 2), generator=g)
+    kw = dict(allowed=torch.tensor([0b11111111110], dtype=torch.int32)) if masked else {}
+    call = lambda t, temperature: _generate(monkeypatch, t, prompt, 8, temperature=temperature, generator=torch.Generator().manual_seed(7), **kw)
+    assert call(table, 0.7).shape == (3, 10)
+    broken = table.clone()
+    broken[4, 1, 5] = what
+    with pytest.raises(ValueError, match="not finite"):
+        call(broken, 0.7)
+    with pytest.raises(ValueError, match="not finite"):
+        call(table, 1e-42)
+
+
+def test_a_temperature_that_takes_all_logits_below_float32_ends_nothing(monkeypatch):
+    table = -1 - torch.rand(12, 3, 20, generator=torch.Generator().manual_seed(3))
+    with pytest.raises(ValueError, match="not finite"):
+        _generate(monkeypatch, table, torch.zeros(3, 2, dtype=torch.int64), 8, temperature=1e-42, end_id=3)
+
+
+@pytest.mark.parametrize("temperature", [0.0, 0.7])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+def test_a_mask_that_allows_nothing_from_the_first_step_on(monkeypatch, temperature, steps):
+    """Given for one row of three; the other rows' ids do not show it."""
+    table, prompt = torch.randn(12, 3, 20, generator=torch.Generator().manual_seed(3)), torch.ones(3, 2, dtype=torch.int64)
+    mask = torch.full((3, 1), 0xfffff, dtype=torch.int32)
+    call = lambda **kw: _generate(monkeypatch, table, prompt, steps, temperature=temperature, generator=torch.Generator().manual_seed(7), allowed=mask, **kw)
+    free = call()
+    mask[1] = 0
+    got = call(end_id=4)
+    assert got.shape == (3, 2 + steps) and torch.equal(got[::2], free[::2]) and bool((got[1, 2:] == 4).all()) and bool((got[:, :2] == 1).all())
+    if steps:
+        with pytest.raises(ValueError, match="end_id"):
+            call()

@@ -363,7 +363,8 @@ bpt_status bpt_res_norm_bwd(const bpt_res_norm_args* args, const float* stats, c
  *
  * Backward: d_weight[v, :] = scale * sum of d_out[b, t, :] over the places with ids[b, t] = v, in weight_dtype; zeros for ids that stand
  * nowhere and for padding_idx (-1: none; the forward pays no attention to it).  Every row is overwritten.  d_out: [batch, out_rows, D] of out_dtype;
- * rows behind the tokens add nothing, whatever stands there.  `weight` is not looked at.  Sums are taken in fp32 in a fixed order without atomics: bit-reproducible.
+ * rows behind the tokens add nothing, whatever stands there.  `weight` is not looked at.  Sums are taken in fp32 in a fixed order without
+ * atomics: bit-reproducible.
  * Tensors may start at any element; widths that are multiples of 8 on 16-byte boundaries take the shortest kernels.
  * `workspace`: bpt_embed_bwd_workspace_bytes bytes (host query; 0 on invalid arguments), plain scratch without a status
  * block, 16-byte aligned; two calls whose GPU work overlaps need one each.

@@ -33,7 +33,8 @@ constexpr int kEmDigit = 9;                 // bits per sort pass, at most
 constexpr int kEmBins = 1 << kEmDigit;
 constexpr int kEmSortThreads = 1024;
 
-// n / d of n < 2^31 by a multiplication (Granlund and Montgomery, Division by Invariant Integers using Multiplication, 1994): with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1 it is (floor(m n / 2^32) + n) >> s.
+// n / d of n < 2^31 by a multiplication, after Granlund and Montgomery, Division by Invariant Integers using Multiplication (1994): with
+// s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1 it is (floor(m n / 2^32) + n) >> s.
 struct FastDiv {
     unsigned d, m, s;
     FastDiv(unsigned by = 1) : d(by), m(1), s(0) {

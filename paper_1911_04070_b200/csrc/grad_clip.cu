@@ -10,7 +10,8 @@
 // bf16 in 54 tensors: the norm alone 16.4 us, below the limit 17, of which grad_norm is 12.3 (4.1 TB/s; a reduction of 67 MB of PyTorch's takes
 // 24) and the launch behind it the rest; cut in place 31; cut into fp32 41 (150 MB read and written once are 23, the norm's own read
 // comes on top).  1.2 GB in 432 tensors scaled into bf16 608 us (norm 6.2 TB/s, scaling 5.6).  Eight groups of 8 elements on their way per thread
-// instead of four: 25 (below the limit) / 53 (into fp32) / 597 where four took 17.8 / 41 / 608; units dealt out in turn instead of in one range per CTA: 20 / 44 / 595.
+// instead of four: 25 (below the limit) / 53 (into fp32) / 597 where four took 17.8 / 41 / 608; units dealt out in turn instead of in one range
+// per CTA: 20 / 44 / 595.
 //
 // Squares are summed in fp32 over 8 elements and then in fp64, which costs one addition per 16 or 32 bytes; where a sum of 8 squares
 // leaves the range in which fp32 loses nothing, those 8 are squared in fp64: no gradient is too large or too small for its norm.  Where that

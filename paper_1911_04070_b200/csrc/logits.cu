@@ -8,9 +8,9 @@
 // (one sequence, 256 ids, history of 8192: 5.5 us; 32 rows of 32000, histories of 4096: 6.6 us); or, for many pieces, a launch that lists each
 // row's ids by a hash table beside the pass, and one that writes them behind it (256 rows of 128001 in bf16 with bias and mask: the pass
 // 34 us without a history, 3.9 TB/s, where PyTorch's copy_ of the logits takes 28 and its neg 24; 48 us with histories of 2048, of which listing leaves
-// the pass fewer SMs at first and the last launch is the tail.  With the ids found by every piece for itself 95 us).  In place the pass waits for the listing before it
-// writes: with a mask and such histories 53 us against 49 (fp32 77 against 71); 32 rows of 32000 in one launch 10.2 against 8.2, since the ids of
-// a piece are read before it is written.
+// the pass fewer SMs at first and the last launch is the tail.  With the ids found by every piece for itself 95 us).  In place the pass waits
+// for the listing before it writes: with a mask and such histories 53 us against 49 (fp32 77 against 71); 32 rows of 32000 in one launch 10.2
+// against 8.2, since the logits of a piece's ids are read before it is written.
 //
 // Rows may start anywhere (an odd vocabulary, a slice of a larger tensor): a row's elements are taken in groups of 8 that lie on
 // 16-byte boundaries of the logits, whatever their index.

@@ -725,6 +725,7 @@ PYBIND11_MODULE(_bpt_torch, m) {
     m.def("gated_feed_forward", &gated_feed_forward);
     m.def("token_states", &token_states);
     m.def("clip_gradients", &clip_gradients);
-    m.def("share_memory", [](const Tensor& a, const std::optional<Tensor>& b) { return share_memory(a, b.has_value() ? *b : a); }, py::arg("a"), py::arg("b") = py::none());
+    m.def("share_memory", [](const Tensor& a, const std::optional<Tensor>& b) { return share_memory(a, b.has_value() ? *b : a); }, py::arg("a"),
+          py::arg("b") = py::none());
     m.def("adjust_logits", &adjust_logits);
 }

@@ -195,7 +195,8 @@ def _clip(grads, out, norm_type, clip, max_norm, eps):
 def gradient_norm(grads, norm_type=2.0):
     """The 2-norm (norm_type=float("inf"): the largest absolute value) over all elements of a list of tensors, float32 or bfloat16 mixed, as
     a float32 tensor [].  None entries count for nothing; nothing at all gives 0.  Squares are summed in 64 bits where 32 would
-    lose them: right for gradients of any size (infinite where float32 has no such number).  Two launches whatever the number of tensors up to 960; bit-reproducible; can be captured."""
+    lose them: right for gradients of any size (infinite where float32 has no such number).  Two launches whatever the number of tensors up to
+    960; bit-reproducible; can be captured."""
     return _clip(grads, None, norm_type, False, 0.0, 0.0)
 
 
